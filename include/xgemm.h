@@ -558,6 +558,54 @@ int xgemv_trace_workgroup(int64_t M, int64_t K, const float *A, int64_t lda, con
                           const xgemv_config *cfg, int64_t block, xgemm_trace_event *out, int64_t capacity,
                           int64_t *counts);
 
+/*
+ * Operators around a decoding step and a loss.
+ *
+ * All of them are enqueued asynchronously on `stream` (a hipStream_t; NULL:
+ * the default stream), return a status and enqueue nothing when validation
+ * (XGEMM_ERR_INVALID_ARG) or a workspace allocation (XGEMM_ERR_ALLOC) fails.
+ * Matrices are row-major with leading dimensions in elements.  Sums, softmax
+ * statistics and gradients are held in fp32 and rounded once, to the type of
+ * the output.  Every sum has a fixed order: a call gives the same bits each
+ * time.
+ */
+
+/* Type of an output: fp32, or the type of the call's 16-bit inputs. */
+enum xgemm_out {
+    XGEMM_OUT_FP32 = 0,
+    XGEMM_OUT_SAME = 1
+};
+
+/*
+ * Products of a few rows with 4-bit weights and group scales:
+ *
+ *     y[m][n] = sum over k of x[m][k] * s[n][k / group] * (q[n][k] - z[n][k / group])
+ *
+ *   M, N, K      sizes, each >= 0 and < 2^31.  M == 0 or N == 0: no-op.
+ *                K == 0: y = 0.  Meant for M up to 64: the weights are read
+ *                once for every 64 rows.
+ *   x, ldx       M x K values of dtype (XGEMM_BF16 or XGEMM_FP16), ldx >= K
+ *   q, ldq       N rows of ceil(K / 2) bytes, ldq (bytes) >= that: value k is
+ *                the low half of byte k / 2 where k is even, else the high
+ *                half.  What a last byte holds past K does not matter.
+ *   scales, lds  N x ceil(K / group) values of dtype
+ *   zeros, ldz   N x ceil(K / group) bytes, each the value that stands for
+ *                zero; NULL: 8 everywhere
+ *   group        32, 64 or a multiple of 128.  (One scale a row: K rounded up
+ *                to such a number.)
+ *   y, ldy       M x N values of the type that `out` names; must not overlap
+ *                the inputs
+ * Alignment: x, scales and y that of their element; q any.  Uses no workspace.
+ * Accuracy: the products x (16 + q) and x (16 + z) are exact and summed in
+ * fp32, so the error against exact arithmetic on the stored values is some
+ * 2^-24 of sum |x s (16 + q)| times the length of the sums, before the
+ * output's rounding.  A NaN or an infinity in a row of x makes that row of y
+ * NaN.
+ */
+int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const uint8_t *q,
+                    int64_t ldq, const void *scales, int64_t lds, const uint8_t *zeros, int64_t ldz, int64_t group,
+                    void *y, int64_t ldy, int dtype, int out, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *xgemm_strerror(int status);
 

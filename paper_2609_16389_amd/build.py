@@ -4,31 +4,43 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "xgemm.hip")
-DEPS = [SRC, os.path.join(PKG, "csrc", "direct_kernel.hpp"), os.path.join(PKG, "csrc", "gemm_kernel.hpp"), os.path.join(PKG, "csrc", "gemv_kernel.hpp"),
-        os.path.join(PKG, "csrc", "pack_kernel.hpp"), os.path.join(PKG, "csrc", "sk_kernel.hpp"),
-        os.path.join(ROOT, "include", "xgemm.h")]
+SOURCES = [SRC, os.path.join(PKG, "csrc", "decode.hip")]
+DEPS = SOURCES + [os.path.join(PKG, "csrc", f) for f in (
+    "context.hpp", "decode_device.hpp", "direct_kernel.hpp", "gemm_kernel.hpp", "gemv_kernel.hpp", "pack_kernel.hpp",
+    "quant_kernel.hpp", "sk_kernel.hpp")] + [os.path.join(ROOT, "include", "xgemm.h")]
 LIB = os.path.join(PKG, "libxgemm.so")
 FAST_SRC = os.path.join(PKG, "csrc", "fastcall.cpp")
 FAST_LIB = os.path.join(PKG, "_fastcall.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed fp32 vector ops are disabled for all device code.
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-shared",
+LINK_FLAGS = ["--offload-arch=gfx950", "-fPIC", "-shared"]
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include")]
 
 
 def build(verbose: bool = False) -> str:
-    """Compile the library; always rebuilds.  Returns the path of the .so."""
+    """Compile the library, its sources side by side; always rebuilds.
+    Returns the path of the .so."""
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + [SRC, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as work:
+        jobs, objects = [], []
+        for src in SOURCES:
+            objects.append(os.path.join(work, os.path.basename(src) + ".o"))
+            cmd = [HIPCC, "-c"] + FLAGS + [src, "-o", objects[-1]]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((cmd, subprocess.Popen(cmd)))
+        for status, cmd in [(p.wait(), cmd) for cmd, p in jobs]:
+            if status != 0:
+                raise subprocess.CalledProcessError(status, cmd)
+        subprocess.run([HIPCC] + LINK_FLAGS + objects + ["-o", tmp], check=True)
     os.replace(tmp, LIB)
     build_fastcall(verbose)
     return LIB

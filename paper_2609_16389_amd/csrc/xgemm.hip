@@ -14,7 +14,7 @@
 #include <type_traits>
 #include <vector>
 
-#include "xgemm.h"
+#include "context.hpp"
 #include "direct_kernel.hpp"
 #include "gemm_kernel.hpp"
 #include "gemv_kernel.hpp"
@@ -37,31 +37,90 @@ std::mutex g_scratch_mu;
 void *g_scratch_ptr[kMaxDevices];  // device address of `scratch` on each device (null until looked up)
 }  // namespace
 
-struct xgemm_ctx {
-    int device;
-    int cu_count;
-    void *workspace;
-    size_t ws_bytes;
-    // Calls that share the workspace never overlap, whichever streams they
-    // are enqueued on.  While a handle's calls all come on one stream, the
-    // stream's order is enough and nothing is recorded (an event record
-    // between two GEMMs leaves the GPU idle for about 10 us).  The first
-    // call on another stream waits for the device to drain (the previous
-    // stream may no longer exist), and from then on every call records
-    // ws_event on its stream after its last launch, and a call on another
-    // stream makes its stream wait for that event.  The workspace is only
-    // freed (to grow it) once its last user has completed.
-    hipEvent_t ws_event;
-    hipStream_t ws_stream;  // stream of the last call that used the workspace
-    bool ws_used;           // ws_stream is set
-    bool ws_recorded;       // ws_event follows the last use on ws_stream
-    bool ws_multi;          // calls have come on more than one stream
-    size_t ws_limit;        // largest workspace the handle may allocate (0: no limit)
-    bool persistent;        // the selected plans may use the persistent kernel
-    void *scratch;          // this device's `scratch` array (xgemm_run_noalloc)
-    struct PlanCache *plans;  // selections already made (sizes and layout flags only)
-    char last_error[256];
-};
+namespace xgemm_host {
+
+void set_error(xgemm_ctx *h, const char *what, hipError_t e)
+{
+    if (h)
+        snprintf(h->last_error, sizeof(h->last_error), "%s: %s", what, hipGetErrorString(e));
+}
+
+// Make the handle's workspace usable by work enqueued next on stream s with
+// at least `bytes` after its counter prefix (it never shrinks).  Work of
+// earlier calls on other streams that used the workspace is ordered before
+// s's next work (a wait on the handle's event); a buffer being replaced is
+// freed only after that work has completed, and a new one gets its counter
+// prefix zeroed on s.  Every caller enqueues its workspace users and then
+// calls release_workspace on the same stream.
+int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s)
+{
+    hipError_t e;
+    bytes += kWsPrefix;
+    if (h->ws_limit > 0 && bytes > h->ws_limit) {
+        snprintf(h->last_error, sizeof(h->last_error), "workspace of %zu bytes exceeds the handle's limit of %zu",
+                 bytes, h->ws_limit);
+        return XGEMM_ERR_ALLOC;
+    }
+    if (h->ws_used && h->ws_stream != s) {
+        // the last user is on another stream: wait for its event, or (the
+        // first switch of streams, nothing recorded) for the whole device
+        e = h->ws_recorded ? hipStreamWaitEvent(s, h->ws_event, 0) : hipDeviceSynchronize();
+        if (e != hipSuccess) {
+            set_error(h, h->ws_recorded ? "hipStreamWaitEvent" : "hipDeviceSynchronize", e);
+            return XGEMM_ERR_HIP;
+        }
+        h->ws_multi = true;
+    }
+    if (bytes <= h->ws_bytes)
+        return XGEMM_OK;
+    if (h->workspace) {
+        // the last user completes before the buffer goes: its event, or this
+        // stream (the last user was on it, or the device has drained)
+        e = h->ws_recorded ? hipEventSynchronize(h->ws_event) : hipStreamSynchronize(s);
+        if (e != hipSuccess) {
+            set_error(h, "workspace drain", e);
+            return XGEMM_ERR_HIP;
+        }
+        (void)hipFree(h->workspace);
+        h->workspace = nullptr;
+        h->ws_bytes = 0;
+    }
+    e = hipMalloc(&h->workspace, bytes);
+    if (e != hipSuccess) {
+        h->workspace = nullptr;
+        (void)hipGetLastError();
+        set_error(h, "hipMalloc workspace", e);
+        return XGEMM_ERR_ALLOC;
+    }
+    h->ws_bytes = bytes;
+    hipLaunchKernelGGL(xgemm_dev::fill_zero, dim3(1), dim3(256), 0, s, (float *)h->workspace, (int64_t)0, 1,
+                       (int)(kWsPrefix / sizeof(float)));
+    e = hipGetLastError();
+    if (e != hipSuccess) {
+        set_error(h, "workspace prefix clear", e);
+        return XGEMM_ERR_HIP;
+    }
+    return XGEMM_OK;
+}
+
+// Mark the end of the workspace users just enqueued on stream s.
+int release_workspace(xgemm_ctx *h, hipStream_t s)
+{
+    h->ws_stream = s;
+    h->ws_used = true;
+    h->ws_recorded = false;
+    if (!h->ws_multi)
+        return XGEMM_OK;
+    const hipError_t e = hipEventRecord(h->ws_event, s);
+    if (e != hipSuccess) {
+        set_error(h, "hipEventRecord", e);
+        return XGEMM_ERR_HIP;
+    }
+    h->ws_recorded = true;
+    return XGEMM_OK;
+}
+
+}  // namespace xgemm_host
 
 namespace {
 
@@ -141,20 +200,14 @@ bool combines(int tile, int split)
 // fewest K steps in every split that a tile's pipelined kernel takes
 int dma_min_steps(int tile) { return tile == XGEMM_TILE_128x128_K2 ? 4 : 3; }
 
-constexpr int64_t kMaxDim = (int64_t)1 << 31;
+using xgemm_host::kMaxDim;
+using xgemm_host::kWsPrefix;
+using xgemm_host::acquire_workspace;
+using xgemm_host::release_workspace;
+using xgemm_host::set_error;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-void set_error(xgemm_ctx *h, const char *what, hipError_t e)
-{
-    if (h)
-        snprintf(h->last_error, sizeof(h->last_error), "%s: %s", what, hipGetErrorString(e));
-}
-
-// Counter words of the persistent kernel's split tiles: the first bytes of
-// every workspace, zero when the workspace is allocated and zero again after
-// every call that uses them; the other workspace users start after them.
-constexpr size_t kWsPrefix = 4096;
 constexpr int kMaxSkGrid = (int)(kWsPrefix / sizeof(int));
 
 bool valid_tile(int tile)
@@ -1095,83 +1148,8 @@ int make_plan_with(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, 
     return finish();
 }
 
-// Make the handle's workspace usable by work enqueued next on stream s with
-// at least `bytes` after its counter prefix (it never shrinks).  Work of
-// earlier calls on other streams that used the workspace is ordered before
-// s's next work (a wait on the handle's event); a buffer being replaced is
-// freed only after that work has completed, and a new one gets its counter
-// prefix zeroed on s.  Every caller enqueues its workspace users and then
-// calls release_workspace on the same stream.
-int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s)
-{
-    hipError_t e;
-    bytes += kWsPrefix;
-    if (h->ws_limit > 0 && bytes > h->ws_limit) {
-        snprintf(h->last_error, sizeof(h->last_error), "workspace of %zu bytes exceeds the handle's limit of %zu",
-                 bytes, h->ws_limit);
-        return XGEMM_ERR_ALLOC;
-    }
-    if (h->ws_used && h->ws_stream != s) {
-        // the last user is on another stream: wait for its event, or (the
-        // first switch of streams, nothing recorded) for the whole device
-        e = h->ws_recorded ? hipStreamWaitEvent(s, h->ws_event, 0) : hipDeviceSynchronize();
-        if (e != hipSuccess) {
-            set_error(h, h->ws_recorded ? "hipStreamWaitEvent" : "hipDeviceSynchronize", e);
-            return XGEMM_ERR_HIP;
-        }
-        h->ws_multi = true;
-    }
-    if (bytes <= h->ws_bytes)
-        return XGEMM_OK;
-    if (h->workspace) {
-        // the last user completes before the buffer goes: its event, or this
-        // stream (the last user was on it, or the device has drained)
-        e = h->ws_recorded ? hipEventSynchronize(h->ws_event) : hipStreamSynchronize(s);
-        if (e != hipSuccess) {
-            set_error(h, "workspace drain", e);
-            return XGEMM_ERR_HIP;
-        }
-        (void)hipFree(h->workspace);
-        h->workspace = nullptr;
-        h->ws_bytes = 0;
-    }
-    e = hipMalloc(&h->workspace, bytes);
-    if (e != hipSuccess) {
-        h->workspace = nullptr;
-        (void)hipGetLastError();
-        set_error(h, "hipMalloc workspace", e);
-        return XGEMM_ERR_ALLOC;
-    }
-    h->ws_bytes = bytes;
-    hipLaunchKernelGGL(xgemm_dev::fill_zero, dim3(1), dim3(256), 0, s, (float *)h->workspace, (int64_t)0, 1,
-                       (int)(kWsPrefix / sizeof(float)));
-    e = hipGetLastError();
-    if (e != hipSuccess) {
-        set_error(h, "workspace prefix clear", e);
-        return XGEMM_ERR_HIP;
-    }
-    return XGEMM_OK;
-}
-
 // The workspace's data after its counter prefix.
 char *ws_data(void *ws) { return (char *)ws + kWsPrefix; }
-
-// Mark the end of the workspace users just enqueued on stream s.
-int release_workspace(xgemm_ctx *h, hipStream_t s)
-{
-    h->ws_stream = s;
-    h->ws_used = true;
-    h->ws_recorded = false;
-    if (!h->ws_multi)
-        return XGEMM_OK;
-    const hipError_t e = hipEventRecord(h->ws_event, s);
-    if (e != hipSuccess) {
-        set_error(h, "hipEventRecord", e);
-        return XGEMM_ERR_HIP;
-    }
-    h->ws_recorded = true;
-    return XGEMM_OK;
-}
 
 // The copy of `batch` src_rows x src_cols operands (leading dimension ld,
 // batch stride src_stride) into dense rows x cols ones at dst (rows, cols

@@ -24,6 +24,9 @@ _HEADER = os.path.join(os.path.dirname(_PKG), "include", "xgemm.h")
 XGEMM_BF16 = 0
 XGEMM_FP16 = 1
 
+XGEMM_OUT_FP32 = 0
+XGEMM_OUT_SAME = 1
+
 XGEMM_OK = 0
 XGEMM_ERR_INVALID_ARG = 1
 XGEMM_ERR_UNSUPPORTED = 2
@@ -191,6 +194,9 @@ lib.xgemv_select_config.restype = _i32
 lib.xgemv_trace_workgroup.argtypes = [_i64, _i64, _p, _i64, _p, _p, _p, ctypes.POINTER(xgemv_config), _i64, _p,
                                       _i64, _p]
 lib.xgemv_trace_workgroup.restype = _i32
+lib.xgemv_quant_run.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64,
+                                _i32, _i32, _p]
+lib.xgemv_quant_run.restype = _i32
 lib.xgemm_strerror.argtypes = [_i32]
 lib.xgemm_strerror.restype = ctypes.c_char_p
 lib.xgemm_last_error.argtypes = [_handle_t]
@@ -359,6 +365,10 @@ def xgemv_select_config(M, K, cu_count) -> xgemv_config:
     if rc != XGEMM_OK:
         raise XgemmError(rc)
     return out
+
+
+def xgemv_quant_run(h, M, N, K, x, ldx, q, ldq, scales, lds, zeros, ldz, group, y, ldy, dtype, out, stream) -> int:
+    return lib.xgemv_quant_run(h, M, N, K, x, ldx, q, ldq, scales, lds, zeros, ldz, group, y, ldy, dtype, out, stream)
 
 
 def xgemm_strerror(status: int) -> str:
@@ -539,6 +549,63 @@ def gemv(A, x, out=None, config: xgemv_config | None = None, stream=None):
     args = (h, M, K, A.data_ptr() or None, lda, x.data_ptr() or None, out.data_ptr() or None,
             _stream_ptr(stream) or None)
     rc = xgemv_run_config(*args, config) if config is not None else xgemv_run(*args)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _place(stream, *tensors):
+    """The stream of a call on these GPU tensors (None: left out) and its
+    handle."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError("expected tensors on one GPU")
+    s = stream if stream is not None else torch.cuda.current_stream(device)
+    return s, handle(device.index, s)
+
+
+def _out_code(out, dtype) -> int:
+    if out.dtype == torch.float32:
+        return XGEMM_OUT_FP32
+    if out.dtype == dtype:
+        return XGEMM_OUT_SAME
+    raise TypeError("out must be float32 or of the inputs' dtype, got %s" % out.dtype)
+
+
+def gemv_quant(x, q, scales, zeros=None, group=128, out=None, stream=None):
+    """y = x @ W.T for a few rows x and 4-bit weights, through xgemv_quant_run:
+
+        W[n, k] = scales[n, k // group] * (value k of q[n] - zeros[n, k // group])
+
+    x: (M, K) bfloat16/float16 CUDA tensor; q: (N, ceil(K / 2)) uint8, value k
+    in the low half of byte k // 2 where k is even, else in the high half;
+    scales: (N, ceil(K / group)) of x's dtype; zeros: the same shape in uint8,
+    or None (8 everywhere); group: 32, 64 or a multiple of 128.  out: (M, N)
+    float32 (the default) or of x's dtype.  Rows are contiguous, at any
+    distance.
+    """
+    dtype = _dtype_code(x)
+    if x.dim() != 2 or q.dim() != 2:
+        raise ValueError("expected x (M, K) and q (N, ceil(K / 2))")
+    (M, K), N = x.shape, q.shape[0]
+    if group not in (32, 64) and (group < 128 or group % 128):
+        raise ValueError("group must be 32, 64 or a multiple of 128, got %r" % (group,))
+    if q.dtype != torch.uint8 or q.shape[1] != (K + 1) // 2:
+        raise ValueError("q must be a uint8 (N, %d) tensor" % ((K + 1) // 2))
+    if scales.dtype != x.dtype or tuple(scales.shape) != (N, -(-K // group)):
+        raise ValueError("scales must be a (%d, %d) tensor of x's dtype" % (N, -(-K // group)))
+    if zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != scales.shape):
+        raise ValueError("zeros must be a uint8 tensor of the scales' shape")
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.float32, device=x.device)
+    if tuple(out.shape) != (M, N):
+        raise ValueError("out must be an (M, N) tensor")
+    s, h = _place(stream, x, q, scales, zeros, out)
+    rc = xgemv_quant_run(h, M, N, K, x.data_ptr() or None, _ld(x), q.data_ptr() or None, _ld(q),
+                         scales.data_ptr() or None, _ld(scales), zeros.data_ptr() or None if zeros is not None else None,
+                         _ld(zeros) if zeros is not None else 0, group, out.data_ptr() or None, _ld(out), dtype,
+                         _out_code(out, x.dtype), _stream_ptr(s) or None)
     if rc != XGEMM_OK:
         raise XgemmError(rc, xgemm_last_error(h))
     return out
