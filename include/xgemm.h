@@ -606,6 +606,42 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
                     int64_t ldq, const void *scales, int64_t lds, const uint8_t *zeros, int64_t ldz, int64_t group,
                     void *y, int64_t ldy, int dtype, int out, void *stream);
 
+/*
+ * A mixture-of-experts layer for a few tokens, from its router's scores (a
+ * product that xgemm_run makes, fp32) to the weighted sum of its experts:
+ *
+ *     for token t, its `top` choices are the experts of the largest scores (where scores
+ *     are equal, the lower index first), and for choice j, expert e, with score s:
+ *     w = exp(s - m) / D     m: the token's largest score; D: the same summed over its
+ *                            choices (renormalize = 1) or over all experts (0)
+ *     h = silu(up[e][0 .. I-1] x[t]) * (up[e][I .. 2I-1] x[t])      silu(a) = a / (1 + exp(-a))
+ *     y[t] = sum over the choices of w * (down[e] h)
+ *
+ *   T, H, I      tokens, hidden and inner size, each >= 0.  T == 0 or H == 0:
+ *                no-op; I == 0: y = 0.  Meant for few tokens: the weights of
+ *                the chosen experts are read once for every 64 tokens.
+ *   E, top       experts (1 .. XGEMM_EXPERTS_MAX) and choices a token (1 ..
+ *                min(E, XGEMM_EXPERTS_MAX_TOP))
+ *   x, ldx       T x H values of dtype (XGEMM_BF16 or XGEMM_FP16)
+ *   scores, lds  T x E floats
+ *   up           E matrices of 2 I x H values of dtype, the gate's rows first,
+ *                with leading dimension ldu, stride_up apart
+ *   down         E matrices of H x I values, ldd, stride_down apart
+ *   y, ldy       T x H values of the type that `out` names; must not overlap
+ *                the inputs
+ * A score of -inf gives its expert no weight; a token whose chosen scores are
+ * all -inf gets a row of zeros; a NaN among a token's scores (it counts as the
+ * largest) makes its row NaN.  h is kept to 24 bits (with XGEMM_FP16: |h| up
+ * to 2.6e8, resolved to 2^-34).  Uses the handle's workspace: 6 bytes for each
+ * of min(T, 64) * top * (I rounded up to 128), and some KiB.
+ */
+#define XGEMM_EXPERTS_MAX 1024
+#define XGEMM_EXPERTS_MAX_TOP 32
+int xgemm_experts_run(xgemm_handle_t h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x,
+                      int64_t ldx, const float *scores, int64_t lds, const void *up, int64_t ldu, int64_t stride_up,
+                      const void *down, int64_t ldd, int64_t stride_down, void *y, int64_t ldy, int renormalize,
+                      int dtype, int out, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *xgemm_strerror(int status);
 

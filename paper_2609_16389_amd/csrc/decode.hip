@@ -1,6 +1,7 @@
 // Host side of the operators around a decoding step: argument checks, launch
 // selection and launches.  The C ABI is declared in include/xgemm.h.
 #include "context.hpp"
+#include "experts_kernel.hpp"
 #include "quant_kernel.hpp"
 
 #include <algorithm>
@@ -100,9 +101,113 @@ int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int6
     return launch_status(h, "quant launch");
 }
 
+// ---------------------------------------------------------------------------
+// layer of experts
+// ---------------------------------------------------------------------------
+
+using xexperts_dev::ExpertsParams;
+
+template <int DT, int MT>
+void launch_experts(const ExpertsParams &p, hipStream_t s)
+{
+    if (p.slots > 0)
+        hipLaunchKernelGGL((xexperts_dev::route_up<DT, MT>), dim3(cdiv(p.I, 16), p.slots),
+                           dim3(xexperts_dev::kUpThreads), 0, s, p);
+    hipLaunchKernelGGL((xexperts_dev::down_sum<DT, MT>), dim3(cdiv(p.H, 16)), dim3(xexperts_dev::kDownThreads), 0, s, p);
+}
+
+template <int DT>
+void launch_experts(const ExpertsParams &p, hipStream_t s)
+{
+    if (p.T <= 16)
+        launch_experts<DT, 1>(p, s);
+    else if (p.T <= 32)
+        launch_experts<DT, 2>(p, s);
+    else
+        launch_experts<DT, 4>(p, s);
+}
+
+int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x, int64_t ldx,
+                const float *scores, int64_t lds, const void *up, int64_t ldu, int64_t su, const void *down,
+                int64_t ldd, int64_t sd, void *y, int64_t ldy, int renormalize, int dtype, int out, hipStream_t s)
+{
+    using namespace xexperts_dev;
+    if (!h || (dtype != XGEMM_BF16 && dtype != XGEMM_FP16) || (out != XGEMM_OUT_FP32 && out != XGEMM_OUT_SAME) ||
+        (renormalize != 0 && renormalize != 1))
+        return XGEMM_ERR_INVALID_ARG;
+    if (E < 1 || E > XGEMM_EXPERTS_MAX || top < 1 || top > XGEMM_EXPERTS_MAX_TOP || top > E)
+        return XGEMM_ERR_INVALID_ARG;
+    // (2 I rows of up; the inner dimension padded stays below 2^31)
+    if (!dims_ok(T, H, ldx) || !dims_ok(T, E, lds) || !dims_ok(T, H, ldy) || I < 0 || I > kMaxDim / 4 ||
+        !dims_ok(2 * I, H, ldu) || !dims_ok(H, I, ldd) || su < 0 || sd < 0 || H > kMaxDim - 2 * kUnit * kUpWaves)
+        return XGEMM_ERR_INVALID_ARG;
+    if ((double)E * (double)su > 9.0e18 || (double)E * (double)sd > 9.0e18)
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (T == 0 || H == 0)
+        return XGEMM_OK;
+    if (!x || !scores || !y || (I > 0 && (!up || !down)))
+        return XGEMM_ERR_INVALID_ARG;
+    ExpertsParams p;
+    p.scores = scores;
+    p.up = (const uint16_t *)up;
+    p.down = (const uint16_t *)down;
+    p.ldx = ldx;
+    p.lds = lds;
+    p.ldu = ldu;
+    p.su = su;
+    p.ldd = ldd;
+    p.sd = sd;
+    p.ldy = ldy;
+    p.E = (int)E;
+    p.top = (int)top;
+    p.H = (int)H;
+    p.I = (int)I;
+    p.Ip = (int)(cdiv(I, kPad) * kPad);
+    p.renormalize = renormalize && I > 0;
+    p.out16 = out == XGEMM_OUT_SAME;
+    // tokens in chunks of at most kMaxTokens, each in the same workspace
+    const int64_t most = std::min<int64_t>(T, kMaxTokens);
+    const size_t slot_bytes = cdiv(std::min(most * top, E) * sizeof(Slot), 256) * 256;
+    const size_t weight_bytes = cdiv(most * top * sizeof(float), 256) * 256;
+    if ((double)most * (double)top * (double)p.Ip * 6.0 > 9.0e15)
+        return XGEMM_ERR_INVALID_ARG;
+    const size_t h_bytes = (size_t)most * top * p.Ip * 6;
+    const int rc = xgemm_host::acquire_workspace(h, slot_bytes + weight_bytes + h_bytes, s);
+    if (rc != XGEMM_OK)
+        return rc;
+    char *const ws = (char *)h->workspace + xgemm_host::kWsPrefix;
+    p.slot = (Slot *)ws;
+    p.weight = (float *)(ws + slot_bytes);
+    p.h = (uint16_t *)(ws + slot_bytes + weight_bytes);
+    for (int64_t t = 0; t < T; t += kMaxTokens) {
+        p.T = (int)std::min<int64_t>(kMaxTokens, T - t);
+        p.slots = I > 0 ? (int)std::min<int64_t>(p.T * top, E) : 0;   // (without inner columns y is zero)
+        p.x = (const uint16_t *)x + t * ldx;
+        p.scores = scores + t * lds;
+        p.y = (char *)y + t * ldy * (p.out16 ? 2 : 4);
+        if (dtype == XGEMM_BF16)
+            launch_experts<0>(p, s);
+        else
+            launch_experts<1>(p, s);
+    }
+    const int launched = launch_status(h, "experts launch");
+    const int released = xgemm_host::release_workspace(h, s);
+    return launched != XGEMM_OK ? launched : released;
+}
+
 }  // namespace
 
 extern "C" {
+
+int xgemm_experts_run(xgemm_handle_t h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x,
+                      int64_t ldx, const float *scores, int64_t lds, const void *up, int64_t ldu, int64_t stride_up,
+                      const void *down, int64_t ldd, int64_t stride_down, void *y, int64_t ldy, int renormalize,
+                      int dtype, int out, void *stream)
+{
+    return run_experts(h, T, E, top, H, I, x, ldx, scores, lds, up, ldu, stride_up, down, ldd, stride_down, y, ldy,
+                       renormalize, dtype, out, (hipStream_t)stream);
+}
 
 int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const uint8_t *q,
                     int64_t ldq, const void *scales, int64_t lds, const uint8_t *zeros, int64_t ldz, int64_t group,

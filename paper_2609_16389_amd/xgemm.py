@@ -197,6 +197,9 @@ lib.xgemv_trace_workgroup.restype = _i32
 lib.xgemv_quant_run.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64,
                                 _i32, _i32, _p]
 lib.xgemv_quant_run.restype = _i32
+lib.xgemm_experts_run.argtypes = [_handle_t, _i64, _i64, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64,
+                                  _i64, _p, _i64, _i32, _i32, _i32, _p]
+lib.xgemm_experts_run.restype = _i32
 lib.xgemm_strerror.argtypes = [_i32]
 lib.xgemm_strerror.restype = ctypes.c_char_p
 lib.xgemm_last_error.argtypes = [_handle_t]
@@ -369,6 +372,12 @@ def xgemv_select_config(M, K, cu_count) -> xgemv_config:
 
 def xgemv_quant_run(h, M, N, K, x, ldx, q, ldq, scales, lds, zeros, ldz, group, y, ldy, dtype, out, stream) -> int:
     return lib.xgemv_quant_run(h, M, N, K, x, ldx, q, ldq, scales, lds, zeros, ldz, group, y, ldy, dtype, out, stream)
+
+
+def xgemm_experts_run(h, T, E, top, H, I, x, ldx, scores, lds, up, ldu, stride_up, down, ldd, stride_down, y, ldy,
+                      renormalize, dtype, out, stream) -> int:
+    return lib.xgemm_experts_run(h, T, E, top, H, I, x, ldx, scores, lds, up, ldu, stride_up, down, ldd, stride_down,
+                                 y, ldy, renormalize, dtype, out, stream)
 
 
 def xgemm_strerror(status: int) -> str:
@@ -606,6 +615,54 @@ def gemv_quant(x, q, scales, zeros=None, group=128, out=None, stream=None):
                          scales.data_ptr() or None, _ld(scales), zeros.data_ptr() or None if zeros is not None else None,
                          _ld(zeros) if zeros is not None else 0, group, out.data_ptr() or None, _ld(out), dtype,
                          _out_code(out, x.dtype), _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _ld3(t):
+    """Leading dimension and stride of the matrices of a 3-D tensor."""
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("rows must be contiguous (stride(2) == 1)")
+    ld = t.stride(1) if t.shape[1] > 1 else max(t.shape[2], 1)
+    return ld, t.stride(0) if t.shape[0] > 1 else 0
+
+
+def experts(x, scores, up, down, top, renormalize=True, out=None, stream=None):
+    """A mixture-of-experts layer for a few tokens, through xgemm_experts_run.
+
+    Each token's `top` experts of the largest scores (equal ones: the lower
+    index first) are weighted by the softmax of their scores, among themselves
+    or, without ``renormalize``, among all experts:
+
+        out[t] = sum of weight * down[e] @ (silu(up[e, :I] @ x[t]) * (up[e, I:] @ x[t]))
+
+    x: (T, H) and up: (E, 2 I, H), down: (E, H, I) bfloat16/float16 CUDA tensors
+    of one dtype; scores: (T, E) float32, as ``gemm`` leaves them; out: (T, H)
+    float32 or of x's dtype (the default).  Rows are contiguous.
+    """
+    dtype = _dtype_code(x)
+    if up.dtype != x.dtype or down.dtype != x.dtype:
+        raise TypeError("x, up and down must have the same dtype")
+    if scores.dtype != torch.float32:
+        raise TypeError("scores must be float32")
+    if x.dim() != 2 or scores.dim() != 2 or up.dim() != 3 or down.dim() != 3:
+        raise ValueError("expected x (T, H), scores (T, E), up (E, 2 I, H) and down (E, H, I)")
+    (T, H), (E, _, I) = x.shape, down.shape
+    if tuple(scores.shape) != (T, E) or tuple(up.shape) != (E, 2 * I, H) or down.shape[1] != H:
+        raise ValueError("shapes %s, %s, %s and %s do not match" % tuple(tuple(t.shape) for t in (x, scores, up, down)))
+    if not 1 <= top <= E:
+        raise ValueError("top must be between 1 and the number of experts, got %r" % (top,))
+    if out is None:
+        out = torch.empty((T, H), dtype=x.dtype, device=x.device)
+    if tuple(out.shape) != (T, H):
+        raise ValueError("out must be a (T, H) tensor")
+    s, h = _place(stream, x, scores, up, down, out)
+    ldu, su = _ld3(up)
+    ldd, sd = _ld3(down)
+    rc = xgemm_experts_run(h, T, E, top, H, I, x.data_ptr() or None, _ld(x), scores.data_ptr() or None, _ld(scores),
+                           up.data_ptr() or None, ldu, su, down.data_ptr() or None, ldd, sd, out.data_ptr() or None,
+                           _ld(out), int(bool(renormalize)), dtype, _out_code(out, x.dtype), _stream_ptr(s) or None)
     if rc != XGEMM_OK:
         raise XgemmError(rc, xgemm_last_error(h))
     return out

@@ -1,0 +1,261 @@
+"""The layer of experts against the plain form in 64 bits.
+
+Bound: |y - exact| <= ((H + I) / 32 + 128) 2^-24 S + rounding of the output.  S
+holds, for each output, the sum of |w down| times everything that forms h:
+an error of the first products (at most H / 32 / 8 + 8 accumulations of matrix
+products, 32 roundings each counted on their own part, as for the products
+with 4-bit weights) enters through silu's slope, and the second product's
+own sums, its three parts of h (24 bits), the exponentials and the weights
+(some 2^-22) multiply |h|.
+"""
+import numpy as np
+import pytest
+import torch
+
+import decode_ref
+from paper_2609_16389_amd import xgemm as xg
+
+TORCH = {"bf16": torch.bfloat16, "fp16": torch.float16}
+EPS = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+
+
+def make(T, E, H, I, dtype, seed, pad=0, device="cuda"):
+    rng = np.random.default_rng(seed)
+    dt = TORCH[dtype]
+
+    def view(shape, scale, t):
+        a = torch.from_numpy((rng.normal(size=shape) * scale).astype(np.float32)).to(t)
+        ld = shape[-1] + pad
+        sizes = [1]
+        strides = [ld, 1] if len(shape) == 2 else [shape[1] * ld + pad, ld, 1]
+        n = pad + sum((s - 1) * d for s, d in zip(shape, strides) if s) + 1
+        buf = torch.full((max(n, 1),), float("nan"), dtype=t, device=device)
+        v = buf.as_strided(shape, strides, pad)
+        v.copy_(a)
+        return v
+
+    return (view((T, H), 1.0, dt), view((T, E), 1.0, torch.float32), view((E, 2 * I, H), H ** -0.5, dt),
+            view((E, H, I), max(I, 1) ** -0.5, dt))
+
+
+def host(t):
+    return t.cpu().float().numpy()
+
+
+def tolerance(ref, S, H, I, dtype, out):
+    tol = ((H + I) / 32 + 128) * 2.0 ** -24 * S + 2.0 ** -32
+    if out != torch.float32:
+        tol = tol * (1 + EPS[dtype]) + EPS[dtype] * np.abs(ref) + 2.0 ** -24
+    return tol
+
+
+def check(y, args, top, renormalize, dtype, what):
+    x, scores, up, down = (host(t) for t in args)
+    ref, S, _ = decode_ref.experts(x, scores, up, down, top, renormalize)
+    err = np.abs(y.cpu().double().numpy() - ref)
+    tol = tolerance(ref, S, x.shape[1], down.shape[2], dtype, y.dtype)
+    assert np.all(err <= tol), "%s: off by %.3g of the bound" % (what, np.max(err / tol))
+
+
+SHAPES = [(1, 1, 1, 1, 1), (1, 8, 2, 64, 32), (1, 128, 8, 256, 48), (2, 5, 3, 33, 17), (3, 16, 4, 129, 130),
+          (7, 13, 3, 101, 77), (16, 8, 2, 128, 128), (17, 64, 6, 200, 31), (31, 4, 4, 40, 300), (33, 7, 1, 257, 16),
+          (64, 16, 2, 1100, 20), (65, 200, 3, 24, 15), (130, 9, 2, 40, 40), (5, 1024, 32, 8, 24)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%dt%de%dk%dx%d" % s)
+def test_shapes(shape, renormalize, dtype):
+    T, E, top, H, I = shape
+    for pad, out in ((0, torch.float32), (3, TORCH[dtype])):
+        args = make(T, E, H, I, dtype, T + E + H + I, pad)
+        buf = torch.full((T + 1, H + 5), 77.0, dtype=out, device="cuda")
+        y = xg.experts(*args, top, renormalize, out=buf[:T, 2:H + 2])
+        check(y, args, top, renormalize, dtype, "pad %d" % pad)
+        assert torch.all(buf[T] == 77) and torch.all(buf[:, :2] == 77) and torch.all(buf[:, H + 2:] == 77)
+
+
+@pytest.mark.gpu
+def test_default_output_and_determinism():
+    args = make(20, 12, 300, 200, "bf16", 3)
+    y = xg.experts(*args, 3)
+    assert y.dtype == torch.bfloat16
+    for _ in range(3):
+        assert torch.equal(xg.experts(*args, 3), y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 40])
+def test_equal_scores_go_to_the_lower_index(T):
+    args = make(T, 10, 64, 48, "bf16", 4)
+    args[1].zero_()
+    args[1][:, 7] = -0.0                                   # the zeros are alike
+    args[1][1, 3:] = 2.0
+    assert decode_ref.choices(host(args[1]), 3)[1].tolist() == [3, 4, 5]
+    check(xg.experts(*args, 3), args, 3, True, "bf16", "ties")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 50])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_masked_scores(T, renormalize):
+    inf = float("inf")
+    args = make(T, 9, 64, 48, "fp16", 5)
+    args[1][0, 1:] = -inf                                  # one expert left, two wanted
+    args[1][1, :] = -inf                                   # none left: zeros
+    args[1][2, 2:] = torch.finfo(torch.float32).min        # the type's lowest value instead
+    y = xg.experts(*args, 2, renormalize, out=torch.empty((T, 64), device="cuda"))
+    check(y, args, 2, renormalize, "fp16", "masked")
+    assert torch.all(y[1] == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 50])
+def test_a_nan_stays_in_its_row(T):
+    args = make(T, 9, 64, 48, "bf16", 6)
+    clean = xg.experts(*args, 2)
+    args[1][1, 4] = float("nan")
+    args[0][2, 5] = float("nan")
+    y = xg.experts(*args, 2)
+    assert torch.all(torch.isnan(y[1])) and torch.all(torch.isnan(y[2]))
+    keep = [t for t in range(T) if t not in (1, 2)]
+    assert torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.gpu
+def test_unchosen_experts_are_not_read():
+    args = make(4, 6, 64, 48, "bf16", 7)
+    args[1][:, 5] = -50.0
+    y = xg.experts(*args, 2)
+    args[2][5], args[3][5] = float("nan"), float("inf")
+    assert torch.equal(xg.experts(*args, 2), y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [2.0 ** -12, 2.0 ** 9])
+def test_inner_values_of_any_size(scale, dtype):
+    """h from 1e-7 to 1e5 and more, past binary16's range, fp32 out."""
+    args = make(6, 4, 96, 200, dtype, 8)
+    args[0].mul_(scale)
+    y = xg.experts(*args, 2, out=torch.empty((6, 96), device="cuda"))
+    check(y, args, 2, True, dtype, "scale %g" % scale)
+
+
+@pytest.mark.gpu
+def test_tokens_do_not_depend_on_their_company():
+    """The sums over a token's experts run in another order with other company,
+    nothing else changes."""
+    args = make(40, 16, 128, 96, "bf16", 9)
+    out = torch.empty((40, 128), device="cuda")
+    y = xg.experts(*args, 4, out=out)
+    for t in (0, 17, 39):
+        one = xg.experts(args[0][t:t + 1], args[1][t:t + 1], args[2], args[3], 4, out=torch.empty((1, 128), device="cuda"))
+        assert torch.allclose(one[0], y[t], rtol=1e-4, atol=1e-5)
+
+
+@pytest.mark.gpu
+def test_empty():
+    args = make(3, 4, 20, 12, "bf16", 10)
+    assert xg.experts(args[0][:0], args[1][:0], args[2], args[3], 2).shape == (0, 20)
+    out = torch.full((3, 20), float("nan"), device="cuda")
+    up, down = torch.empty((4, 0, 20), device="cuda").bfloat16(), torch.empty((4, 20, 0), device="cuda").bfloat16()
+    assert torch.all(xg.experts(args[0], args[1], up, down, 2, out=out) == 0)
+    up, down = torch.empty((4, 24, 0), device="cuda").bfloat16(), torch.empty((4, 0, 12), device="cuda").bfloat16()
+    assert xg.experts(args[0][:, :0], args[1], up, down, 2).shape == (3, 0)
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Experts more than 2^31 elements apart."""
+    args = make(2, 3, 64, 32, "bf16", 11)
+    far = 1 << 30
+    store = torch.empty((2 * far + 64 * 64,), dtype=torch.bfloat16, device="cuda")
+    up = store.as_strided((3, 64, 64), (far, 64, 1))
+    up.copy_(args[2])
+    down = store.as_strided((3, 64, 32), (far, 32, 1))
+    y = xg.experts(args[0], args[1], up, args[3], 3)
+    assert torch.equal(y, xg.experts(*args, 3))
+    down.copy_(args[3])
+    assert torch.equal(xg.experts(args[0], args[1], args[2], down, 3), y)
+
+
+@pytest.mark.gpu
+def test_two_streams_share_nothing():
+    a, b = make(5, 8, 256, 128, "bf16", 12), make(30, 8, 256, 128, "bf16", 13)
+    ya, yb = xg.experts(*a, 2), xg.experts(*b, 2)
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        got.append((xg.experts(*a, 2, stream=sa), xg.experts(*b, 2, stream=sb)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, ya) and torch.equal(q, yb) for p, q in got)
+
+
+@pytest.mark.gpu
+def test_replayed_from_a_graph():
+    args = make(4, 16, 256, 128, "fp16", 14)
+    out = torch.empty((4, 256), dtype=torch.float16, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        xg.experts(*args, 4, out=out)                      # the stream's handle and workspace
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        xg.experts(*args, 4, out=out)
+    for _ in range(3):
+        args[0].copy_(torch.randn(4, 256, device="cuda"))
+        args[1].copy_(torch.randn(4, 16, device="cuda"))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, xg.experts(*args, 4))
+
+
+def test_refusals_without_a_gpu():
+    x, scores, up, down = make(2, 4, 20, 12, "bf16", 1, device="cpu")
+    with pytest.raises(ValueError):
+        xg.experts(x, scores, up, down, 2)                 # not on a GPU
+    for bad in ((x.float(), scores, up, down, 2), (x, scores.double(), up, down, 2), (x, scores, up.half(), down, 2)):
+        with pytest.raises(TypeError):
+            xg.experts(*bad)
+    for bad in ((x, scores, up, down, 0), (x, scores, up, down, 5), (x, scores[:, 1:], up, down, 2),
+                (x, scores, up[:, 1:], down, 2), (x, scores, up, down[:, 1:], 2), (x[0], scores, up, down, 2),
+                (x, scores, up.transpose(1, 2), down, 2)):
+        with pytest.raises(ValueError):
+            xg.experts(*bad)
+    assert xg.xgemm_experts_run(None, 1, 1, 1, 1, 1, 16, 1, 16, 1, 16, 1, 1, 16, 1, 1, 16, 1, 1, 0, 0, None) == \
+        xg.XGEMM_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_c_call():
+    h = xg.xgemm_create()
+    x, scores, up, down = make(2, 4, 20, 12, "bf16", 1)
+    y = torch.full((2, 20), 7.0, device="cuda")
+    base = dict(T=2, E=4, top=2, H=20, I=12, x=x.data_ptr(), ldx=20, scores=scores.data_ptr(), lds=4, up=up.data_ptr(),
+                ldu=20, su=480, down=down.data_ptr(), ldd=12, sd=240, y=y.data_ptr(), ldy=20, renormalize=1, dtype=0,
+                out=0, stream=None)
+
+    def call(**change):
+        return xg.xgemm_experts_run(h, *{**base, **change}.values())
+
+    bad = [dict(T=-1), dict(H=-1), dict(I=-1), dict(E=0), dict(E=1025), dict(top=0), dict(top=5), dict(x=None),
+           dict(scores=None), dict(up=None), dict(down=None), dict(y=None), dict(ldx=19), dict(lds=3), dict(ldu=19),
+           dict(ldd=11), dict(ldy=19), dict(su=-1), dict(sd=-1), dict(dtype=2), dict(out=2), dict(renormalize=2),
+           dict(T=1 << 31), dict(I=1 << 31), dict(su=1 << 62)]
+    for b in bad:
+        assert call(**b) == xg.XGEMM_ERR_INVALID_ARG, b
+    assert call(E=64, top=33, lds=64) == xg.XGEMM_ERR_INVALID_ARG
+    # a workspace that the handle may not have
+    assert xg.xgemm_set_workspace_limit(h, 5000) == xg.XGEMM_OK
+    assert call() == xg.XGEMM_ERR_ALLOC and "limit" in xg.xgemm_last_error(h)
+    torch.cuda.synchronize()
+    assert torch.all(y == 7)
+    assert xg.xgemm_set_workspace_limit(h, 0) == xg.XGEMM_OK
+    assert call() == xg.XGEMM_OK
+    torch.cuda.synchronize()
+    check(y, (x, scores, up, down), 2, True, "bf16", "C call")
+    assert xg.xgemm_destroy(h) == xg.XGEMM_OK
