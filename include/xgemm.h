@@ -642,6 +642,55 @@ int xgemm_experts_run(xgemm_handle_t h, int64_t T, int64_t E, int64_t top, int64
                       const void *down, int64_t ldd, int64_t stride_down, void *y, int64_t ldy, int renormalize,
                       int dtype, int out, void *stream);
 
+/*
+ * Rows of logits (what xgemm_run leaves, fp32, or 16 bits): for row r with
+ * values x,
+ *
+ *     lse = log sum exp x        logprob = x[target] - lse
+ *     entropy = - sum p log p    p = exp(x - lse)
+ *     the `top` largest values in descending order (where values are equal, the lower index
+ *     first): their indices top_id and log probabilities top_logprob
+ *
+ *   R, V         rows (>= 0; 0: no-op) and values a row (1 .. 2^30)
+ *   logits, ldl  R x V values of dtype: XGEMM_BF16, XGEMM_FP16 or XGEMM_FP32
+ *   targets      R indices; a negative one: logprob is 0; one of V or more:
+ *                NaN.  May be NULL where logprob is.
+ *   top          0 .. min(V, XGEMM_LOGPROB_MAX_TOP)
+ *   logprob, lse, entropy   R floats each; NULL: not wanted
+ *   top_logprob, top_id     R x top, contiguous; not looked at when top is 0
+ * A value of -inf has probability 0 and adds nothing to the entropy.  A row
+ * of nothing but -inf has lse = logprob = top_logprob = -inf and entropy 0.  A
+ * NaN or +inf makes lse, logprob, entropy and top_logprob NaN; a NaN is never
+ * among the largest (places left over have top_id -1).  With few rows (up to
+ * the number of CUs) the handle's workspace holds partial results: at most
+ * 12 + 8 top bytes for each of 64 parts a row.
+ */
+#define XGEMM_FP32 2
+#define XGEMM_LOGPROB_MAX_TOP 32
+int xgemm_logprob_run(xgemm_handle_t h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
+                      int64_t top, float *logprob, float *lse, float *entropy, float *top_logprob, int64_t *top_id,
+                      int dtype, void *stream);
+
+/*
+ * The gradient in the logits, given that of logprob, entropy and lse:
+ *
+ *     dlogits = d_logprob (delta[target] - p) - d_entropy p (log p + entropy) + d_lse p
+ *
+ *   lse, entropy          what xgemm_logprob_run gave (entropy: only with
+ *                         d_entropy)
+ *   d_logprob, d_entropy, d_lse   R floats each; NULL: zero
+ *   targets               as above (only with d_logprob): a negative one takes
+ *                         no part, one of V or more makes the row NaN
+ *   dlogits, ldd          R x V values of dtype; may be logits itself (with
+ *                         the same leading dimension), must not overlap it
+ *                         otherwise
+ * A row whose lse is below -1e37 (nothing in it but -inf or the lowest value of
+ * fp32 or bfloat16: every token masked) gets zeros.  Uses no workspace.
+ */
+int xgemm_logprob_grad(xgemm_handle_t h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
+                       const float *lse, const float *entropy, const float *d_logprob, const float *d_entropy,
+                       const float *d_lse, void *dlogits, int64_t ldd, int dtype, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *xgemm_strerror(int status);
 

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "xgemm.hip")
 SOURCES = [SRC, os.path.join(PKG, "csrc", "decode.hip")]
 DEPS = SOURCES + [os.path.join(PKG, "csrc", f) for f in (
-    "context.hpp", "decode_device.hpp", "direct_kernel.hpp", "experts_kernel.hpp", "gemm_kernel.hpp", "gemv_kernel.hpp", "pack_kernel.hpp",
+    "context.hpp", "decode_device.hpp", "direct_kernel.hpp", "experts_kernel.hpp", "gemm_kernel.hpp", "gemv_kernel.hpp", "logprob_kernel.hpp", "pack_kernel.hpp",
     "quant_kernel.hpp", "sk_kernel.hpp")] + [os.path.join(ROOT, "include", "xgemm.h")]
 LIB = os.path.join(PKG, "libxgemm.so")
 FAST_SRC = os.path.join(PKG, "csrc", "fastcall.cpp")

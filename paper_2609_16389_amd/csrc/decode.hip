@@ -2,9 +2,11 @@
 // selection and launches.  The C ABI is declared in include/xgemm.h.
 #include "context.hpp"
 #include "experts_kernel.hpp"
+#include "logprob_kernel.hpp"
 #include "quant_kernel.hpp"
 
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 using xgemm_host::kMaxDim;
@@ -196,9 +198,146 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     return launched != XGEMM_OK ? launched : released;
 }
 
+// ---------------------------------------------------------------------------
+// log probabilities
+// ---------------------------------------------------------------------------
+
+using xlogprob_dev::GradParams;
+using xlogprob_dev::LogprobParams;
+
+constexpr int64_t kMaxVocab = (int64_t)1 << 30;
+constexpr int64_t kGridRows = 65535;   // rows of workgroups in a grid
+
+bool logits_ok(int64_t R, int64_t V, int64_t ld, int dtype)
+{
+    return (dtype == XGEMM_BF16 || dtype == XGEMM_FP16 || dtype == XGEMM_FP32) && V >= 1 && V <= kMaxVocab &&
+           dims_ok(R, V, ld);
+}
+
+template <int DT>
+void launch_logprob(const LogprobParams &p, int64_t rows, hipStream_t s)
+{
+    const dim3 grid(p.parts, (unsigned)rows), block(xlogprob_dev::kThreads);
+    if (p.top > 0)
+        hipLaunchKernelGGL((xlogprob_dev::logprob_rows<DT, true>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((xlogprob_dev::logprob_rows<DT, false>), grid, block, 0, s, p);
+}
+
+int run_logprob(xgemm_ctx *h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets, int64_t top,
+                float *logprob, float *lse, float *entropy, float *top_logprob, int64_t *top_id, int dtype,
+                hipStream_t s)
+{
+    using namespace xlogprob_dev;
+    if (!h || !logits_ok(R, V, ldl, dtype) || top < 0 || top > XGEMM_LOGPROB_MAX_TOP || top > V)
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (R == 0)
+        return XGEMM_OK;
+    if (!logits || (logprob && !targets) || (top > 0 && (!top_logprob || !top_id)))
+        return XGEMM_ERR_INVALID_ARG;
+    LogprobParams p;
+    p.logits = logits;
+    p.targets = targets;
+    p.logprob = logprob;
+    p.lse = lse;
+    p.entropy = entropy;
+    p.top_logprob = top_logprob;
+    p.top_id = top_id;
+    p.ld = ldl;
+    p.V = (int)V;
+    p.top = (int)top;
+    // few rows are cut into parts of at least half a batch a wave, for two
+    // workgroups a CU
+    constexpr int64_t kPart = kWaves * kBatch / 2;
+    int64_t parts = std::min({2 * (int64_t)h->cu_count / R, cdiv(V, kPart), (int64_t)kMaxParts});
+    parts = std::max<int64_t>(parts, 1);
+    p.part_len = (int)(cdiv(cdiv(V, parts), 64) * 64);
+    p.parts = (int)cdiv(V, p.part_len);
+    p.stat = nullptr;
+    p.best = nullptr;
+    p.count = nullptr;
+    if (p.parts > 1) {
+        const size_t stat_bytes = cdiv(R * p.parts * sizeof(Stats), 256) * 256;
+        const int rc = xgemm_host::acquire_workspace(h, stat_bytes + R * p.parts * top * sizeof(uint64_t), s);
+        if (rc != XGEMM_OK)
+            return rc;
+        char *const ws = (char *)h->workspace + xgemm_host::kWsPrefix;
+        p.count = (int *)h->workspace;   // (parts > 1 only for R up to the number of CUs)
+        p.stat = (Stats *)ws;
+        p.best = (uint64_t *)(ws + stat_bytes);
+    }
+    for (int64_t r = 0; r < R; r += kGridRows) {
+        p.row0 = r;
+        const int64_t rows = std::min(kGridRows, R - r);
+        if (dtype == XGEMM_BF16)
+            launch_logprob<0>(p, rows, s);
+        else if (dtype == XGEMM_FP16)
+            launch_logprob<1>(p, rows, s);
+        else
+            launch_logprob<2>(p, rows, s);
+    }
+    const int launched = launch_status(h, "logprob launch");
+    const int released = p.parts > 1 ? xgemm_host::release_workspace(h, s) : XGEMM_OK;
+    return launched != XGEMM_OK ? launched : released;
+}
+
+int run_logprob_grad(xgemm_ctx *h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
+                     const float *lse, const float *entropy, const float *d_logprob, const float *d_entropy,
+                     const float *d_lse, void *dlogits, int64_t ldd, int dtype, hipStream_t s)
+{
+    using namespace xlogprob_dev;
+    if (!h || !logits_ok(R, V, ldl, dtype) || !logits_ok(R, V, ldd, dtype))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (R == 0)
+        return XGEMM_OK;
+    if (!logits || !dlogits || !lse || (d_logprob && !targets) || (d_entropy && !entropy))
+        return XGEMM_ERR_INVALID_ARG;
+    GradParams p;
+    p.logits = logits;
+    p.targets = targets;
+    p.lse = lse;
+    p.entropy = entropy;
+    p.d_logprob = d_logprob;
+    p.d_entropy = d_entropy;
+    p.d_lse = d_lse;
+    p.out = dlogits;
+    p.ld = ldl;
+    p.ldo = ldd;
+    p.V = (int)V;
+    for (int64_t r = 0; r < R; r += kGridRows) {
+        p.row0 = r;
+        const dim3 grid(cdiv(V, kGradSpan), (unsigned)std::min(kGridRows, R - r)), block(kGradThreads);
+        if (dtype == XGEMM_BF16)
+            hipLaunchKernelGGL(logprob_grad<0>, grid, block, 0, s, p);
+        else if (dtype == XGEMM_FP16)
+            hipLaunchKernelGGL(logprob_grad<1>, grid, block, 0, s, p);
+        else
+            hipLaunchKernelGGL(logprob_grad<2>, grid, block, 0, s, p);
+    }
+    return launch_status(h, "logprob gradient launch");
+}
+
 }  // namespace
 
 extern "C" {
+
+int xgemm_logprob_run(xgemm_handle_t h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
+                      int64_t top, float *logprob, float *lse, float *entropy, float *top_logprob, int64_t *top_id,
+                      int dtype, void *stream)
+{
+    return run_logprob(h, R, V, logits, ldl, targets, top, logprob, lse, entropy, top_logprob, top_id, dtype,
+                       (hipStream_t)stream);
+}
+
+int xgemm_logprob_grad(xgemm_handle_t h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
+                       const float *lse, const float *entropy, const float *d_logprob, const float *d_entropy,
+                       const float *d_lse, void *dlogits, int64_t ldd, int dtype, void *stream)
+{
+    return run_logprob_grad(h, R, V, logits, ldl, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits, ldd,
+                            dtype, (hipStream_t)stream);
+}
 
 int xgemm_experts_run(xgemm_handle_t h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x,
                       int64_t ldx, const float *scores, int64_t lds, const void *up, int64_t ldu, int64_t stride_up,

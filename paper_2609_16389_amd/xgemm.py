@@ -24,6 +24,8 @@ _HEADER = os.path.join(os.path.dirname(_PKG), "include", "xgemm.h")
 XGEMM_BF16 = 0
 XGEMM_FP16 = 1
 
+XGEMM_FP32 = 2  # of logits only
+
 XGEMM_OUT_FP32 = 0
 XGEMM_OUT_SAME = 1
 
@@ -200,6 +202,10 @@ lib.xgemv_quant_run.restype = _i32
 lib.xgemm_experts_run.argtypes = [_handle_t, _i64, _i64, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64,
                                   _i64, _p, _i64, _i32, _i32, _i32, _p]
 lib.xgemm_experts_run.restype = _i32
+lib.xgemm_logprob_run.argtypes = [_handle_t, _i64, _i64, _p, _i64, _p, _i64, _p, _p, _p, _p, _p, _i32, _p]
+lib.xgemm_logprob_run.restype = _i32
+lib.xgemm_logprob_grad.argtypes = [_handle_t, _i64, _i64, _p, _i64, _p, _p, _p, _p, _p, _p, _p, _i64, _i32, _p]
+lib.xgemm_logprob_grad.restype = _i32
 lib.xgemm_strerror.argtypes = [_i32]
 lib.xgemm_strerror.restype = ctypes.c_char_p
 lib.xgemm_last_error.argtypes = [_handle_t]
@@ -378,6 +384,18 @@ def xgemm_experts_run(h, T, E, top, H, I, x, ldx, scores, lds, up, ldu, stride_u
                       renormalize, dtype, out, stream) -> int:
     return lib.xgemm_experts_run(h, T, E, top, H, I, x, ldx, scores, lds, up, ldu, stride_up, down, ldd, stride_down,
                                  y, ldy, renormalize, dtype, out, stream)
+
+
+def xgemm_logprob_run(h, R, V, logits, ldl, targets, top, logprob, lse, entropy, top_logprob, top_id, dtype,
+                      stream) -> int:
+    return lib.xgemm_logprob_run(h, R, V, logits, ldl, targets, top, logprob, lse, entropy, top_logprob, top_id, dtype,
+                                 stream)
+
+
+def xgemm_logprob_grad(h, R, V, logits, ldl, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits, ldd, dtype,
+                       stream) -> int:
+    return lib.xgemm_logprob_grad(h, R, V, logits, ldl, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits,
+                                  ldd, dtype, stream)
 
 
 def xgemm_strerror(status: int) -> str:
@@ -663,6 +681,88 @@ def experts(x, scores, up, down, top, renormalize=True, out=None, stream=None):
     rc = xgemm_experts_run(h, T, E, top, H, I, x.data_ptr() or None, _ld(x), scores.data_ptr() or None, _ld(scores),
                            up.data_ptr() or None, ldu, su, down.data_ptr() or None, ldd, sd, out.data_ptr() or None,
                            _ld(out), int(bool(renormalize)), dtype, _out_code(out, x.dtype), _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _logits_code(t) -> int:
+    if t.dim() != 2:
+        raise ValueError("expected logits (R, V)")
+    return XGEMM_FP32 if t.dtype == torch.float32 else _dtype_code(t)
+
+
+def _vector(name, t, shape, dtype=torch.float32):
+    """The address of a contiguous tensor of this shape and type (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, shape))
+    return t.data_ptr() or None
+
+
+def logprobs(logits, targets=None, top=0, out=None, stream=None):
+    """Log probabilities of rows of logits, through xgemm_logprob_run: a dict of
+
+    * "lse" (R,): log of the sum of the exponentials
+    * "logprob" (R,): log probability of ``targets`` (R,) int64, if given; 0
+      where the target is negative
+    * "entropy" (R,)
+    * "top_logprob", "top_id" (R, top): the ``top`` largest, in descending order
+      (equal ones: the lower index first), if top > 0
+
+    all float32 (top_id: int64).  logits: (R, V) float32, bfloat16 or float16
+    CUDA tensor with contiguous rows.  ``out``: a dict of tensors to write into
+    and return; what it leaves out is not computed.
+    """
+    dtype = _logits_code(logits)
+    R, V = logits.shape
+    if not 0 <= top <= min(V, 32):
+        raise ValueError("top must be between 0 and min(V, 32), got %r" % (top,))
+    if out is None:
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+        out = {"lse": new(R), "entropy": new(R)}
+        if targets is not None:
+            out["logprob"] = new(R)
+        if top:
+            out["top_logprob"], out["top_id"] = new(R, top), new(R, top, dtype=torch.int64)
+    get = out.get
+    if (get("logprob") is not None) and targets is None:
+        raise ValueError("logprob needs targets")
+    if top and (get("top_logprob") is None or get("top_id") is None):
+        raise ValueError("top > 0 needs top_logprob and top_id in out")
+    s, h = _place(stream, logits, targets, *out.values())
+    rc = xgemm_logprob_run(h, R, V, logits.data_ptr() or None, _ld(logits), _vector("targets", targets, (R,), torch.int64),
+                           top, _vector("logprob", get("logprob"), (R,)), _vector("lse", get("lse"), (R,)),
+                           _vector("entropy", get("entropy"), (R,)),
+                           _vector("top_logprob", get("top_logprob"), (R, top)) if top else None,
+                           _vector("top_id", get("top_id"), (R, top), torch.int64) if top else None, dtype,
+                           _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def logprobs_grad(logits, targets, lse, entropy=None, d_logprob=None, d_entropy=None, d_lse=None, out=None, stream=None):
+    """The gradient in the logits of ``logprobs``' results, through
+    xgemm_logprob_grad, given theirs (None: zero); lse and entropy are the
+    forward call's (entropy only with d_entropy, targets only with d_logprob).
+    All (R,) float32, targets int64; out: (R, V) of the logits' dtype, which may
+    be ``logits`` itself."""
+    dtype = _logits_code(logits)
+    R, V = logits.shape
+    if lse is None or (d_logprob is not None and targets is None) or (d_entropy is not None and entropy is None):
+        raise ValueError("lse is needed, targets with d_logprob, and entropy with d_entropy")
+    if out is None:
+        out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
+    if tuple(out.shape) != (R, V) or out.dtype != logits.dtype:
+        raise ValueError("out must be an (R, V) tensor of the logits' dtype")
+    s, h = _place(stream, logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, out)
+    rc = xgemm_logprob_grad(h, R, V, logits.data_ptr() or None, _ld(logits),
+                            _vector("targets", targets, (R,), torch.int64), _vector("lse", lse, (R,)),
+                            _vector("entropy", entropy, (R,)), _vector("d_logprob", d_logprob, (R,)),
+                            _vector("d_entropy", d_entropy, (R,)), _vector("d_lse", d_lse, (R,)),
+                            out.data_ptr() or None, _ld(out), dtype, _stream_ptr(s) or None)
     if rc != XGEMM_OK:
         raise XgemmError(rc, xgemm_last_error(h))
     return out

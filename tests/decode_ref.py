@@ -52,3 +52,56 @@ def experts(x, scores, up, down, top, renormalize):
             # |silu'| <= 1.1 and |silu(g)| <= |g|
             S[t] += abs(w) * (np.abs(down[j]) @ (1.1 * ag * np.abs(u) + np.abs(g) * au + np.abs(h)))
     return y, S, ids
+
+
+def logprobs(x, targets, top):
+    """lse, logprob, entropy, top_logprob, top_id of rows x in 64 bits."""
+    R, V = x.shape
+    x = x.astype(np.float64)
+    bad = np.isnan(x).any(1) | (x == np.inf).any(1)
+    m = np.max(np.where(np.isnan(x), -np.inf, x), axis=1)
+    ref = np.where(np.isfinite(m), m, 0.0)[:, None]
+    with np.errstate(all="ignore"):
+        t = x - ref
+        e = np.exp(t)
+        S = e.sum(1)
+        logS = np.log(S)
+        lse = m + logS
+        empty = m == -np.inf
+        lse[empty] = -np.inf
+        entropy = np.where(empty, 0.0, logS - np.where(e > 0, e * t, 0.0).sum(1) / S)
+        hit = x[np.arange(R), np.clip(targets, 0, V - 1)]
+        logprob = np.where(empty, -np.inf, (hit - m) - logS)
+    lse[bad], entropy[bad], logprob[bad] = np.nan, np.nan, np.nan
+    logprob = np.where(targets < 0, 0.0, np.where(targets >= V, np.nan, logprob))
+    ids, vals = np.full((R, top), -1, dtype=np.int64), np.full((R, top), np.nan)
+    for r in range(R):
+        order = np.lexsort((np.arange(V), -np.where(np.isnan(x[r]), -np.inf, x[r])))
+        order = order[~np.isnan(x[r, order])]
+        n = min(top, len(order))
+        ids[r, :n] = order[:n]
+        if not bad[r]:
+            vals[r, :n] = -np.inf if empty[r] else (x[r, order[:n]] - m[r]) - logS[r]
+    return lse, logprob, entropy, vals, ids
+
+
+def logprobs_grad(x, targets, d_logprob, d_entropy, d_lse):
+    """The gradient in x of sum d_logprob logprob + d_entropy entropy + d_lse lse,
+    and the sum of its terms' absolute values."""
+    R, V = x.shape
+    zero = np.zeros(R)
+    gl, ge, gs = (zero if d is None else d.astype(np.float64) for d in (d_logprob, d_entropy, d_lse))
+    lse, _, entropy, _, _ = logprobs(x, targets, 0)
+    with np.errstate(invalid="ignore"):
+        logp = np.where((lse == -np.inf)[:, None], -np.inf, x.astype(np.float64) - lse[:, None])
+    p = np.exp(logp)
+    logp = np.where(p > 0, logp, 0.0)
+    hot = np.zeros((R, V))
+    on = (targets >= 0) & (targets < V)
+    hot[np.arange(R)[on], targets[on]] = 1.0
+    gl = np.where(targets >= V, np.nan if d_logprob is not None else 0.0, np.where(targets < 0, 0.0, gl))
+    gl, ge, gs = gl[:, None], ge[:, None], gs[:, None]
+    d = gl * (hot - p) - ge * p * (logp + entropy[:, None]) + gs * p
+    S = np.abs(gl) * (hot + p) + np.abs(ge) * p * (np.abs(logp) + np.abs(entropy[:, None])) + np.abs(gs) * p
+    empty = (lse == -np.inf)[:, None]
+    return np.where(empty, 0.0, d), np.where(empty, 0.0, S), logp
