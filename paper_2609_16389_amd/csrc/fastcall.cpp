@@ -26,21 +26,40 @@ typedef int (*batched_fn)(void *, int64_t, int64_t, int64_t, int64_t, const void
                           int64_t, int64_t, float *, int64_t, int64_t, int, void *);
 typedef int (*gemv_fn)(void *, int64_t, int64_t, const float *, int64_t, const float *, float *, void *);
 
+typedef int (*quant_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const uint8_t *, int64_t, const void *,
+                        int64_t, const uint8_t *, int64_t, int64_t, void *, int64_t, int, int, void *);
+typedef int (*experts_fn)(void *, int64_t, int64_t, int64_t, int64_t, int64_t, const void *, int64_t, const float *,
+                          int64_t, const void *, int64_t, int64_t, const void *, int64_t, int64_t, void *, int64_t, int,
+                          int, int, void *);
+typedef int (*logprob_fn)(void *, int64_t, int64_t, const void *, int64_t, const int64_t *, int64_t, float *, float *,
+                          float *, float *, int64_t *, int, void *);
+typedef int (*grad_fn)(void *, int64_t, int64_t, const void *, int64_t, const int64_t *, const float *, const float *,
+                       const float *, const float *, const float *, void *, int64_t, int, void *);
+
 gemm_fn f_run, f_noalloc;
 batched_fn f_batched;
 gemv_fn f_gemv;
+quant_fn f_quant;
+experts_fn f_experts;
+logprob_fn f_logprob;
+grad_fn f_grad;
 PyObject *handles;  // the module's dict: (device index, stream address) -> handle address
 
 PyObject *bind(PyObject *, PyObject *args)
 {
-    unsigned long long run, noalloc, batched, gemv;
+    unsigned long long run, noalloc, batched, gemv, quant, experts, logprob, grad;
     PyObject *d;
-    if (!PyArg_ParseTuple(args, "KKKKO!", &run, &noalloc, &batched, &gemv, &PyDict_Type, &d))
+    if (!PyArg_ParseTuple(args, "KKKKKKKKO!", &run, &noalloc, &batched, &gemv, &quant, &experts, &logprob, &grad,
+                          &PyDict_Type, &d))
         return nullptr;
     f_run = (gemm_fn)run;
     f_noalloc = (gemm_fn)noalloc;
     f_batched = (batched_fn)batched;
     f_gemv = (gemv_fn)gemv;
+    f_quant = (quant_fn)quant;
+    f_experts = (experts_fn)experts;
+    f_logprob = (logprob_fn)logprob;
+    f_grad = (grad_fn)grad;
     Py_INCREF(d);
     Py_XDECREF(handles);
     handles = d;
@@ -176,6 +195,176 @@ PyObject *gemv(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
+// A small whole number.
+bool small(PyObject *o, int64_t *v)
+{
+    if (!PyLong_CheckExact(o))
+        return false;
+    int overflow = 0;
+    *v = PyLong_AsLongLongAndOverflow(o, &overflow);
+    return !overflow;
+}
+
+// What `out` names in the library: fp32 (0), the inputs' type (1), or neither.
+int out_of(const at::Tensor &out, const at::Tensor &in)
+{
+    return out.scalar_type() == at::kFloat ? 0 : out.scalar_type() == in.scalar_type() ? 1 : -1;
+}
+
+PyObject *quant(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    int64_t group;
+    if (n != 6 || !handles || !small(a[4], &group) || (group != 32 && group != 64 && (group < 128 || group % 128)))
+        DECLINE;
+    const bool zeroed = a[3] != Py_None;
+    const at::Tensor *x = plain(a[0]), *q = plain(a[1]), *s = plain(a[2]), *z = zeroed ? plain(a[3]) : nullptr,
+                     *y = plain(a[5]);
+    if (!x || !q || !s || (zeroed && !z) || !y || x->dim() != 2 || q->dim() != 2 || s->dim() != 2 || y->dim() != 2 ||
+        q->device() != x->device() || s->device() != x->device() || y->device() != x->device())
+        Py_RETURN_NONE;
+    const int code = code_of(*x), out = out_of(*y, *x);
+    const int64_t M = x->size(0), K = x->size(1), N = q->size(0), G = K / group + (K % group != 0);
+    const int64_t ldx = leading(*x, 0), ldq = leading(*q, 0), lds = leading(*s, 0), ldy = leading(*y, 0);
+    if (code < 0 || out < 0 || q->scalar_type() != at::kByte || s->scalar_type() != x->scalar_type() ||
+        q->size(1) != (K + 1) / 2 || s->size(0) != N || s->size(1) != G || y->size(0) != M || y->size(1) != N ||
+        ldx < 0 || ldq < 0 || lds < 0 || ldy < 0)
+        Py_RETURN_NONE;
+    int64_t ldz = 0;
+    if (z) {
+        if (z->dim() != 2 || z->device() != x->device() || z->scalar_type() != at::kByte || z->size(0) != N ||
+            z->size(1) != G || (ldz = leading(*z, 0)) < 0)
+            Py_RETURN_NONE;
+    }
+    void *stream, *h;
+    if (!stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x), *ps = data(*s);
+    const uint8_t *pq = (const uint8_t *)data(*q), *pz = z ? (const uint8_t *)data(*z) : nullptr;
+    void *py = data(*y);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_quant(h, M, N, K, px, ldx, pq, ldq, ps, lds, pz, ldz, group, py, ldy, code, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+PyObject *experts(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    int64_t top;
+    if (n != 7 || !handles || !small(a[4], &top) || !PyBool_Check(a[5]))
+        DECLINE;
+    const at::Tensor *x = plain(a[0]), *c = plain(a[1]), *u = plain(a[2]), *d = plain(a[3]), *y = plain(a[6]);
+    if (!x || !c || !u || !d || !y || x->dim() != 2 || c->dim() != 2 || u->dim() != 3 || d->dim() != 3 ||
+        y->dim() != 2 || c->device() != x->device() || u->device() != x->device() || d->device() != x->device() ||
+        y->device() != x->device())
+        Py_RETURN_NONE;
+    const int code = code_of(*x), out = out_of(*y, *x);
+    const int64_t T = x->size(0), H = x->size(1), E = d->size(0), I = d->size(2);
+    const int64_t ldx = leading(*x, 0), lds = leading(*c, 0), ldy = leading(*y, 0);
+    if (code < 0 || out < 0 || code_of(*u) != code || code_of(*d) != code || c->scalar_type() != at::kFloat ||
+        c->size(0) != T || c->size(1) != E || u->size(0) != E || u->size(1) != 2 * I || u->size(2) != H ||
+        d->size(1) != H || y->size(0) != T || y->size(1) != H || top < 1 || top > E || ldx < 0 || lds < 0 || ldy < 0 ||
+        (H > 1 && u->stride(2) != 1) || (I > 1 && d->stride(2) != 1))
+        Py_RETURN_NONE;
+    const int64_t one = 1;
+    const int64_t ldu = 2 * I > 1 ? u->stride(1) : std::max(H, one), ldd = H > 1 ? d->stride(1) : std::max(I, one);
+    const int64_t su = E > 1 ? u->stride(0) : 0, sd = E > 1 ? d->stride(0) : 0;
+    void *stream, *h;
+    if (!stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x), *pu = data(*u), *pd = data(*d);
+    const float *pc = (const float *)data(*c);
+    void *py = data(*y);
+    const int renormalize = a[5] == Py_True;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_experts(h, T, E, top, H, I, px, ldx, pc, lds, pu, ldu, su, pd, ldd, sd, py, ldy, renormalize, code, out,
+                   stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// The address of a contiguous R (x top) tensor of this type on x's device;
+// false where it is something else.  Absent (null or None): a null address.
+bool vector_of(PyObject *o, const at::Tensor &x, int64_t R, int64_t top, at::ScalarType type, void **p)
+{
+    *p = nullptr;
+    if (!o || o == Py_None)
+        return true;
+    const at::Tensor *t = plain(o);
+    if (!t || t->device() != x.device() || t->scalar_type() != type || !t->is_contiguous() ||
+        t->dim() != (top ? 2 : 1) || t->size(0) != R || (top && t->size(1) != top))
+        return false;
+    *p = data(*t);
+    return true;
+}
+
+int logits_code(const at::Tensor &t) { return t.scalar_type() == at::kFloat ? 2 : code_of(t); }
+
+PyObject *logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    int64_t top;
+    if (n != 4 || !handles || !small(a[2], &top) || !PyDict_CheckExact(a[3]))
+        DECLINE;
+    const at::Tensor *x = plain(a[0]);
+    if (!x || x->dim() != 2 || top < 0 || top > 32)
+        Py_RETURN_NONE;
+    const int code = logits_code(*x);
+    const int64_t R = x->size(0), V = x->size(1), ld = leading(*x, 0);
+    PyObject *o[5] = {PyDict_GetItemString(a[3], "logprob"), PyDict_GetItemString(a[3], "lse"),
+                      PyDict_GetItemString(a[3], "entropy"), PyDict_GetItemString(a[3], "top_logprob"),
+                      PyDict_GetItemString(a[3], "top_id")};
+    void *t, *p[5], *stream, *h;
+    int known = 0;
+    for (int i = 0; i < 5; ++i)
+        known += o[i] != nullptr;
+    if (code < 0 || ld < 0 || top > V || PyDict_Size(a[3]) != known || !vector_of(a[1], *x, R, 0, at::kLong, &t))
+        DECLINE;
+    for (int i = 0; i < 3; ++i)
+        if (!vector_of(o[i], *x, R, 0, at::kFloat, &p[i]))
+            DECLINE;
+    // (what is there of the alternatives is left to Python where none are wanted)
+    if ((!top && (o[3] || o[4])) || !vector_of(o[3], *x, R, top, at::kFloat, &p[3]) ||
+        !vector_of(o[4], *x, R, top, at::kLong, &p[4]) || (o[0] && o[0] != Py_None && a[1] == Py_None) ||
+        !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_logprob(h, R, V, px, ld, (const int64_t *)t, top, (float *)p[0], (float *)p[1], (float *)p[2], (float *)p[3],
+                   (int64_t *)p[4], code, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+PyObject *logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 8 || !handles)
+        Py_RETURN_NONE;
+    const at::Tensor *x = plain(a[0]), *y = plain(a[7]);
+    if (!x || !y || x->dim() != 2 || y->dim() != 2 || y->device() != x->device() ||
+        y->scalar_type() != x->scalar_type() || y->size(0) != x->size(0) || y->size(1) != x->size(1))
+        Py_RETURN_NONE;
+    const int code = logits_code(*x);
+    const int64_t R = x->size(0), V = x->size(1), ld = leading(*x, 0), ldo = leading(*y, 0);
+    void *t, *p[5], *stream, *h;
+    if (code < 0 || ld < 0 || ldo < 0 || a[2] == Py_None || !vector_of(a[1], *x, R, 0, at::kLong, &t))
+        DECLINE;
+    for (int i = 0; i < 5; ++i)   // lse, entropy and the three gradients
+        if (!vector_of(a[2 + i], *x, R, 0, at::kFloat, &p[i]))
+            DECLINE;
+    if ((a[4] != Py_None && a[1] == Py_None) || (a[5] != Py_None && a[3] == Py_None) || !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x);
+    void *py = data(*y);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_grad(h, R, V, px, ld, (const int64_t *)t, (const float *)p[0], (const float *)p[1], (const float *)p[2],
+                (const float *)p[3], (const float *)p[4], py, ldo, code, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // xgemm_run / xgemm_run_noalloc on twelve plain integers (addresses may be
 // None); anything else is declined.
 PyObject *twelve(gemm_fn f, PyObject *const *a, Py_ssize_t n)
@@ -223,6 +412,13 @@ PyMethodDef methods[] = {
     {"gemm", (PyCFunction)(void *)guarded<gemm>, METH_FASTCALL, "xgemm_run on (A, B, out): a status, or None."},
     {"bmm", (PyCFunction)(void *)guarded<bmm>, METH_FASTCALL, "The strided batched call on (A, B, out)."},
     {"gemv", (PyCFunction)(void *)guarded<gemv>, METH_FASTCALL, "xgemv_run on (A, x, out)."},
+    {"gemv_quant", (PyCFunction)(void *)guarded<quant>, METH_FASTCALL, "xgemv_quant_run on (x, q, scales, zeros, group, out)."},
+    {"experts", (PyCFunction)(void *)guarded<experts>, METH_FASTCALL,
+     "xgemm_experts_run on (x, scores, up, down, top, renormalize, out)."},
+    {"logprobs", (PyCFunction)(void *)guarded<logprobs>, METH_FASTCALL,
+     "xgemm_logprob_run on (logits, targets, top, dict of outputs)."},
+    {"logprobs_grad", (PyCFunction)(void *)guarded<logprobs_grad>, METH_FASTCALL,
+     "xgemm_logprob_grad on (logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, out)."},
     {"run", (PyCFunction)(void *)guarded<run>, METH_FASTCALL, "xgemm_run on its twelve arguments."},
     {"run_noalloc", (PyCFunction)(void *)guarded<run_noalloc>, METH_FASTCALL, "xgemm_run_noalloc likewise."},
     {nullptr, nullptr, 0, nullptr},

@@ -145,6 +145,7 @@ else:
     class _fastcall:
         """Declines every call."""
         bind = run = run_noalloc = gemm = bmm = gemv = staticmethod(lambda *args: None)
+        gemv_quant = experts = logprobs = logprobs_grad = run
 
 _i64, _i32, _p = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p
 _handle_t = ctypes.c_void_p
@@ -413,7 +414,8 @@ def xgemm_last_error(h) -> str:
 _handles = {}
 
 _fastcall.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
-                 (lib.xgemm_run, lib.xgemm_run_noalloc, lib.xgemm_run_strided_batched, lib.xgemv_run)), _handles)
+                 (lib.xgemm_run, lib.xgemm_run_noalloc, lib.xgemm_run_strided_batched, lib.xgemv_run,
+                  lib.xgemv_quant_run, lib.xgemm_experts_run, lib.xgemm_logprob_run, lib.xgemm_logprob_grad)), _handles)
 
 
 def _checked(rc, device_index, out):
@@ -612,6 +614,10 @@ def gemv_quant(x, q, scales, zeros=None, group=128, out=None, stream=None):
     float32 (the default) or of x's dtype.  Rows are contiguous, at any
     distance.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.gemv_quant(x, q, scales, zeros, group, out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype = _dtype_code(x)
     if x.dim() != 2 or q.dim() != 2:
         raise ValueError("expected x (M, K) and q (N, ceil(K / 2))")
@@ -659,6 +665,10 @@ def experts(x, scores, up, down, top, renormalize=True, out=None, stream=None):
     of one dtype; scores: (T, E) float32, as ``gemm`` leaves them; out: (T, H)
     float32 or of x's dtype (the default).  Rows are contiguous.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.experts(x, scores, up, down, top, renormalize, out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype = _dtype_code(x)
     if up.dtype != x.dtype or down.dtype != x.dtype:
         raise TypeError("x, up and down must have the same dtype")
@@ -715,6 +725,10 @@ def logprobs(logits, targets=None, top=0, out=None, stream=None):
     CUDA tensor with contiguous rows.  ``out``: a dict of tensors to write into
     and return; what it leaves out is not computed.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.logprobs(logits, targets, top, out)
+        if rc is not None:
+            return _checked(rc, logits.device.index, out)
     dtype = _logits_code(logits)
     R, V = logits.shape
     if not 0 <= top <= min(V, 32):
@@ -749,6 +763,10 @@ def logprobs_grad(logits, targets, lse, entropy=None, d_logprob=None, d_entropy=
     forward call's (entropy only with d_entropy, targets only with d_logprob).
     All (R,) float32, targets int64; out: (R, V) of the logits' dtype, which may
     be ``logits`` itself."""
+    if out is not None and stream is None:
+        rc = _fastcall.logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, out)
+        if rc is not None:
+            return _checked(rc, logits.device.index, out)
     dtype = _logits_code(logits)
     R, V = logits.shape
     if lse is None or (d_logprob is not None and targets is None) or (d_entropy is not None and entropy is None):
