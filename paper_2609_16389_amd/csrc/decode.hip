@@ -37,22 +37,40 @@ int launch_status(xgemm_ctx *h, const char *what)
 
 using xquant_dev::QuantParams;
 
-template <int DT, int MT, int NT, bool SMALL>
+template <int DT, int GS>
 void launch_quant(const QuantParams &p, hipStream_t s)
 {
-    hipLaunchKernelGGL((xquant_dev::quant_kernel<DT, MT, NT, SMALL>), dim3(cdiv(p.N, 16 * NT), cdiv(p.M, 16 * MT)),
-                       dim3(xquant_dev::kThreads), 0, s, p);
+    using namespace xquant_dev;
+    auto launch = [&](auto kernel, int r, int wn, int wk) {
+        hipLaunchKernelGGL(kernel, dim3(cdiv(p.N, 16 * wn), cdiv(p.M, r)), dim3(64 * wn * wk), 0, s, p);
+    };
+    // a lane's row of weights starts at most 15 leading dimensions from its tile's first
+    const int64_t tiles = cdiv(p.N, 16);
+    if (p.ldq > (int64_t)1 << 27)
+        launch(quant_kernel<DT, 16, 1, 4, GS, int64_t>, 16, 1, 4);
+    else if (p.M <= 2 && tiles <= 512)
+        launch(quant_kernel<DT, 2, 1, 8, GS, uint32_t>, 2, 1, 8);
+    else if (p.M <= 2)
+        launch(quant_kernel<DT, 2, 1, 4, GS, uint32_t>, 2, 1, 4);
+    else if (p.M <= 16 && tiles <= 512)
+        launch(quant_kernel<DT, 16, 1, 8, GS, uint32_t>, 16, 1, 8);
+    else if (p.M <= 16)
+        launch(quant_kernel<DT, 16, 4, 4, GS, uint32_t>, 16, 4, 4);
+    else if (p.M <= 32)
+        launch(quant_kernel<DT, 32, 4, 2, GS, uint32_t>, 32, 4, 2);
+    else
+        launch(quant_kernel<DT, 64, 4, 2, GS, uint32_t>, 64, 4, 2);
 }
 
-template <int DT, bool SMALL>
+template <int DT>
 void launch_quant(const QuantParams &p, hipStream_t s)
 {
-    if (p.M <= 16)
-        launch_quant<DT, 1, 1, SMALL>(p, s);
-    else if (p.M <= 32)
-        launch_quant<DT, 2, 2, SMALL>(p, s);
+    if (p.group == 32)
+        launch_quant<DT, 32>(p, s);
+    else if (p.group == 64)
+        launch_quant<DT, 64>(p, s);
     else
-        launch_quant<DT, 4, 2, SMALL>(p, s);
+        launch_quant<DT, 128>(p, s);
 }
 
 int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const uint8_t *q, int64_t ldq,
@@ -86,19 +104,18 @@ int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int6
     p.ldy = ldy;
     p.N = (int)N;
     p.K = (int)K;
-    p.group = (int)std::min<int64_t>(group, kMaxDim - 128);
+    p.group = (int)std::min<int64_t>(group, kMaxDim - 128);   // (beyond K every group is the one group)
     p.out16 = out == XGEMM_OUT_SAME;
     // (a grid has at most 65535 rows of workgroups)
-    constexpr int64_t kRows = 65535 * 16;
+    constexpr int64_t kRows = 65535 * 2;
     for (int64_t m = 0; m < M; m += kRows) {
         p.M = (int)std::min(kRows, M - m);
         p.x = (const uint16_t *)x + m * ldx;
         p.y = (char *)y + m * ldy * (p.out16 ? 2 : 4);
-        const bool small = group < 128;
         if (dtype == XGEMM_BF16)
-            small ? launch_quant<0, true>(p, s) : launch_quant<0, false>(p, s);
+            launch_quant<0>(p, s);
         else
-            small ? launch_quant<1, true>(p, s) : launch_quant<1, false>(p, s);
+            launch_quant<1>(p, s);
     }
     return launch_status(h, "quant launch");
 }

@@ -36,6 +36,27 @@ __device__ __forceinline__ T load_any(const void *p)
     return ((const any *)p)->v;
 }
 
+// The same from a place that all lanes share (kept in scalar registers, which
+// the empty asm forces) and a lane's own distance from it.
+template <class T>
+__device__ __forceinline__ T load_at(const void *base, uint32_t off)
+{
+    struct __attribute__((packed, aligned(1))) any {
+        T v;
+    };
+    typedef const __attribute__((address_space(1))) char *gptr;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
+    gptr b = (gptr)((uintptr_t)hi << 32 | lo);
+    asm("" : "+s"(b));
+    return ((const __attribute__((address_space(1))) any *)(b + off))->v;
+}
+template <class T>
+__device__ __forceinline__ T load_at(const void *base, int64_t off)
+{
+    return load_any<T>((const char *)base + off);
+}
+
 template <class T>
 __device__ __forceinline__ void store_any(void *p, T v)
 {
@@ -65,16 +86,35 @@ __device__ __forceinline__ uint16_t from_float(float v)
         return __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-// Eight 16-bit values from k of a row of n (zeros past its end).
-__device__ __forceinline__ u32x4 load8_guarded(const uint16_t *row, int64_t k, int64_t n)
+// `v` moved down by `bytes` (0 .. 16), zeros entering at the top.
+__device__ __forceinline__ u32x4 shift_down(u32x4 v, int bytes)
 {
-    if (k + 8 <= n)
-        return load_any<u32x4>(row + k);
+    uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    if (bytes >= 8) {
+        lo = bytes >= 16 ? 0 : hi;
+        hi = 0;
+    }
+    const int b = 8 * (bytes & 7);
+    lo = lo >> b | (b ? hi << (64 - b) : 0);
+    hi >>= b;
+    u32x4 r = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    return r;
+}
+
+// 16 bytes of a row of `n` (> 0) bytes from byte `at`, zeros past its end: the
+// row's last 16 moved into place, without a branch on the lane.
+__device__ __forceinline__ u32x4 load16_end(const void *row, int64_t at, int64_t n)
+{
+    if (n >= 16) {
+        const int64_t from = min(at, n - 16);
+        return shift_down(load_any<u32x4>((const char *)row + from), (int)min(at - from, (int64_t)16));
+    }
     u32x4 v = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (k + j < n)
-            v[j / 2] |= (uint32_t)row[k + j] << (16 * (j & 1));
+    for (int j = 0; j < 16; ++j) {
+        const uint32_t b = ((const uint8_t *)row)[min(at + j, n - 1)];
+        v[j / 4] |= (at + j < n ? b : 0u) << (8 * (j & 3));
+    }
     return v;
 }
 

@@ -223,7 +223,7 @@ route_up(ExpertsParams p)
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 const int k = k0 + 32 * d + 8 * g;
-                w[d][v] = whole ? load_any<u32x4>(wrow[v] + k) : load8_guarded(wrow[v], k, p.H);
+                w[d][v] = whole ? load_any<u32x4>(wrow[v] + k) : load16_end(wrow[v], 2 * (int64_t)k, 2 * (int64_t)p.H);
             }
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -233,7 +233,7 @@ route_up(ExpertsParams p)
                 if (16 * i < count) {
                     u32x4 a = {0u, 0u, 0u, 0u};
                     if (live[i])
-                        a = whole ? load_any<u32x4>(xrow[i] + k) : load8_guarded(xrow[i], k, p.H);
+                        a = whole ? load_any<u32x4>(xrow[i] + k) : load16_end(xrow[i], 2 * (int64_t)k, 2 * (int64_t)p.H);
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
                         acc[i][v] = mfma16<DT>(a, w[d][v], acc[i][v]);
@@ -350,7 +350,7 @@ down_sum(ExpertsParams p)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 const int k = k0 + 32 * d + 8 * g;
-                w[d] = whole ? load_any<u32x4>(wrow + k) : load8_guarded(wrow, k, p.I);
+                w[d] = whole ? load_any<u32x4>(wrow + k) : load16_end(wrow, 2 * (int64_t)k, 2 * (int64_t)p.I);
             }
 #pragma unroll
             for (int d = 0; d < 4; ++d) {

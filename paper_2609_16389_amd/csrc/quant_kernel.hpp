@@ -27,14 +27,14 @@
 // ascending order.
 #pragma once
 
+#include <utility>
+
 #include "decode_device.hpp"
 
 namespace xquant_dev {
 
 using namespace xdecode_dev;
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / 64;
 constexpr int kUnit = 256;  // k per unit of a wave: two blocks of 128
 
 struct QuantParams {
@@ -48,22 +48,34 @@ struct QuantParams {
     int out16;         // y in the type of x, else fp32
 };
 
-// Two weights of a dword as 16-bit floats 16 + q: values i and i + 4.
-template <int DT, int I>
-__device__ __forceinline__ uint32_t widen2(uint32_t w)
+// The masks of widen8, hidden from the compiler so that it keeps them in
+// registers and masks and inserts in one instruction.
+struct Masks {
+    uint32_t mask, base;
+};
+
+template <int DT>
+__device__ __forceinline__ Masks masks()
 {
-    constexpr int at = DT == 0 ? 3 : 6;  // lowest bit of the mantissa's top four
-    constexpr uint32_t mask = DT == 0 ? 0x00780078u : 0x03c003c0u;
-    constexpr uint32_t base = DT == 0 ? 0x41804180u : 0x4c004c00u;
-    constexpr int up = at - 4 * I;
+    Masks m;
+    asm("v_mov_b32 %0, %1" : "=v"(m.mask) : "i"(DT == 0 ? 0x00780078u : 0x03c003c0u));
+    asm("s_mov_b32 %0, %1" : "=s"(m.base) : "i"(DT == 0 ? 0x41804180u : 0x4c004c00u));
+    return m;
+}
+
+// Two weights of a dword as 16-bit floats 16 + q: values I and I + 4.
+template <int DT, int I>
+__device__ __forceinline__ uint32_t widen2(uint32_t w, Masks m)
+{
+    constexpr int up = (DT == 0 ? 3 : 6) - 4 * I;   // to the mantissa's top four bits
     const uint32_t t = up >= 0 ? w << (up & 31) : w >> (-up & 31);
-    return (t & mask) | base;
+    return (t & m.mask) | m.base;
 }
 
 template <int DT>
-__device__ __forceinline__ u32x4 widen8(uint32_t w)
+__device__ __forceinline__ u32x4 widen8(uint32_t w, Masks m)
 {
-    u32x4 r = {widen2<DT, 0>(w), widen2<DT, 1>(w), widen2<DT, 2>(w), widen2<DT, 3>(w)};
+    u32x4 r = {widen2<DT, 0>(w, m), widen2<DT, 1>(w, m), widen2<DT, 2>(w, m), widen2<DT, 3>(w, m)};
     return r;
 }
 
@@ -86,138 +98,254 @@ __device__ __forceinline__ u32x4 transpose_groups(u32x4 v)
     return r;
 }
 
-// 16 bytes of a row of `n` from byte `at` (zeros past its end).
-__device__ __forceinline__ u32x4 load16_guarded(const uint8_t *row, int64_t at, int64_t n)
-{
-    if (at + 16 <= n)
-        return load_any<u32x4>(row + at);
-    u32x4 v = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (at + j < n)
-            v[j / 4] |= (uint32_t)row[at + j] << (8 * (j & 3));
-    return v;
-}
+// LDS of a workgroup of WN x WK waves for rows R.
+template <int R, int WN, int WK>
+struct QuantLds {
+    static constexpr int MT = (R + 15) / 16;
+    static constexpr int XPART = R < 16 ? 32 * R * 16 : MT * 8192;   // x of one unit of k
+    static constexpr int BUFS = WN == 1 ? 1 : 2;
+    static constexpr int PIECES = R * 32 / (WN * 64);   // 16-byte pieces of it that a thread brings in
+    static constexpr int AHEAD = PIECES <= 2 ? 2 : 1;   // units of x on their way to registers
+    __attribute__((aligned(16))) union {
+        struct {
+            char x[WK][BUFS][XPART];
+            float2 scale[WK * WN][16][16];   // {s, 16 + z} of 16 groups of 16 columns
+            uint8_t wend[16 * WN][128];      // the unit that K ends in
+        };
+        float red[WK][WN][MT][256];
+    };
+};
 
-// Workgroup (blockIdx.x, blockIdx.y): columns from 16 NT blockIdx.x, rows from
-// 16 MT blockIdx.y.  SMALL: groups of 32 or 64, else a multiple of 128.
-template <int DT, int MT, int NT, bool SMALL>
-__global__ void __launch_bounds__(kThreads)
+// The waves of a workgroup: WN take 16 columns each, WK a range of k each.
+// Workgroup (blockIdx.x, blockIdx.y): columns from 16 WN blockIdx.x, rows from
+// R blockIdx.y (R: 2 WN, or a multiple of 16).  GS: groups of 32 or 64, or 128
+// for any multiple of that.  off_t holds the distance of a lane's row of q from
+// its tile's first: 32 bits where leading dimensions allow.
+//
+// Per unit a wave waits for x and then for its weights, while the weights of
+// the next unit and x of the next two are on their way.  Loads return in
+// order, so one that may or may not have been issued would make every wait
+// behind it a wait for all: the loop's loads are unconditional, past the end
+// they repeat the last unit's, and the unit that K ends in comes after it.
+template <int DT, int R, int WN, int WK, int GS, class off_t>
+__global__ void __launch_bounds__(64 * WN * WK, R < 16 || (R == 16 && WN > 1) ? 4 : 2)
 quant_kernel(QuantParams p)
 {
-    __shared__ float red[kWaves * MT * NT * 256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    typedef QuantLds<R, WN, WK> Lds;
+    constexpr int MT = Lds::MT, THREADS = 64 * WN * WK, NP = Lds::PIECES, XA = Lds::AHEAD;
+    constexpr int GROUPS = 128 / GS;            // of a block
+    constexpr int CHUNK = 16 * GS / kUnit;      // units that 16 groups cover
+    __shared__ Lds sh;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave % WN, wk = wave / WN;
     const int c = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
-    const int64_t width = ((int64_t)p.K + 1) / 2;
+    const int m0 = blockIdx.y * R, rows = min(R, p.M - m0);
+    const int nw = blockIdx.x * 16 * WN, n0 = nw + 16 * wn;
 
-    const uint8_t *qrow[NT];
-    const uint16_t *srow[NT];
-    const uint8_t *zrow[NT];
+    // this wave's whole units of k (WK is a power of two)
+    const int units = p.K / kUnit;
+    const int u0 = wk * (units / WK) + min(wk, units % WK), mine = units / WK + (wk < units % WK);
+    const int steps = (units + WK - 1) / WK;    // of the longest range
+
+    // columns past N are read from the last one, never stored
+    const int nb = min(n0, p.N - 1), nl = min(c, p.N - 1 - nb);
+    const uint8_t *const qbase = p.q + (int64_t)nb * p.ldq;
+    const off_t qoff = (off_t)nl * (off_t)p.ldq + 16 * g;
+    u32x4 w[2][2];
+    auto load_w = [&](u32x4 (&to)[2], int t) {
+        const uint8_t *const q = qbase + (int64_t)(u0 + min(t, mine - 1)) * (kUnit / 2);
+        to[0] = load_at<u32x4>(q, qoff);
+        to[1] = load_at<u32x4>(q + 64, qoff);
+    };
+
+    // x: of a unit, thread t of the WN waves of a range brings in pieces t, t +
+    // 64 WN, ...: piece i is 8 k from 8 (i % 32) of row i / 32 (rows past M
+    // repeat the last one)
+    const int xi = wn * 64 + lane;
+    const uint16_t *const xbase = p.x + (int64_t)m0 * p.ldx + 8 * (xi & 31);
+    u32x4 xr[XA][NP];
+    auto load_x = [&](u32x4 (&to)[NP], int t) {
+        const int64_t k = (int64_t)(u0 + min(t, mine - 1)) * kUnit;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int64_t n = min(n0 + 16 * j + c, p.N - 1);
-        qrow[j] = p.q + n * p.ldq;
-        srow[j] = p.s + n * p.lds;
-        zrow[j] = p.z ? p.z + n * p.ldz : nullptr;
-    }
-    const uint16_t *xrow[MT];
-    bool live[MT];
+        for (int q = 0; q < NP; ++q)
+            to[q] = load_any<u32x4>(xbase + min((xi >> 5) + 2 * WN * q, rows - 1) * p.ldx + k);
+    };
+    // where 8 k of a row lie in LDS: piece kc of a block of 128 goes to lane
+    // group kg of product kd; 16 rows are swizzled so that neither the pieces of
+    // a row nor the rows of a piece share a bank
+    auto x_place = [&](int buf, int row, int b, int kc) {
+        const int kd = GS < 128 ? kc >> 2 : kc & 3, kg = GS < 128 ? kc & 3 : kc >> 2;
+        return R < 16 ? sh.x[wk][buf] + (((b * 4 + kd) * 4 + kg) * R + row) * 16
+                      : sh.x[wk][buf] + ((b * 4 + kd) * MT + (row >> 4)) * 1024 + kg * 256 + ((row ^ kc) & 15) * 16;
+    };
+    auto store_x = [&](const u32x4 (&from)[NP], int buf) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int m = m0 + 16 * i + c;
-        live[i] = m < p.M;
-        xrow[i] = p.x + (int64_t)min(m, p.M - 1) * p.ldx;
-    }
+        for (int q = 0; q < NP; ++q)
+            *(u32x4 *)x_place(buf, (xi >> 5) + 2 * WN * q, xi >> 4 & 1, xi & 15) = pair_up(from[q]);
+    };
+
+    // scales and zero points of 16 groups (of GS k) from group q0 on: lane
+    // group g brings in four of column c
+    const uint16_t *const sbase = p.s + (int64_t)(nb + nl) * p.lds;
+    const uint8_t *const zbase = p.z ? p.z + (int64_t)(nb + nl) * p.ldz : nullptr;
+    const int groups = (p.K - 1) / p.group + 1;
+    uint64_t sr;
+    uint32_t zr;
+    auto load_scales = [&](int q0) {
+        zr = 0x08080808u;
+        if (p.group == GS && groups >= 4) {
+            // (at the end of a row its last four, moved down: what lies past it
+            // meets x of zero or no product at all)
+            const int q = q0 + 4 * g, at = min(q, groups - 4), past = min(q - at, 3);
+            sr = load_any<uint64_t>(sbase + at) >> (16 * past);
+            if (p.z)
+                zr = load_any<uint32_t>(zbase + at) >> (8 * past);
+        } else {
+            sr = 0;
+            uint32_t z = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = min((int)((uint32_t)(q0 + 4 * g + e) * GS / (uint32_t)p.group), groups - 1);
+                sr |= (uint64_t)sbase[at] << (16 * e);
+                if (p.z)
+                    z |= (uint32_t)zbase[at] << (8 * e);
+            }
+            if (p.z)
+                zr = z;
+        }
+    };
+    auto store_scales = [&] {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            sh.scale[wave][4 * g + e][c] = float2{to_float<DT>((uint16_t)(sr >> (16 * e))),
+                                                  16.0f + (float)(zr >> (8 * e) & 255u)};
+    };
+
+    const Masks widen = masks<DT>();
     const uint32_t one = DT == 0 ? 0x3f803f80u : 0x3c003c00u;
     const u32x4 ones = {one, one, one, one};
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-
-    f32x4 acc[MT][NT];
+    f32x4 acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-            acc[i][j] = zero;
+        acc[i] = zero;
 
-    for (int64_t k0 = (int64_t)wave * kUnit; k0 < p.K; k0 += kWaves * kUnit) {
-        const bool whole = k0 + kUnit <= p.K;
-        u32x4 w[2][NT];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int64_t at = k0 / 2 + 64 * b + 16 * g;
-                w[b][j] = whole ? load_any<u32x4>(qrow[j] + at) : load16_guarded(qrow[j], at, width);
-                if (SMALL)
-                    w[b][j] = transpose_groups(w[b][j]);
-            }
+    // one unit: the products of every group, scaled into the outputs
+    auto compute = [&](const u32x4 (&from)[2], int buf, int q0) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int64_t kb = k0 + 128 * b;
-            f32x4 P[MT][NT], S[MT];
+            const u32x4 v = GS < 128 ? transpose_groups(from[b]) : from[b];
+            f32x4 P[MT], S[MT];
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const int64_t k = SMALL ? kb + 32 * d + 8 * g : kb + 32 * g + 8 * d;
-                const bool first = SMALL ? p.group == 32 || d % 2 == 0 : d == 0;
-                const bool last = SMALL ? p.group == 32 || d % 2 == 1 : d == 3;
-                u32x4 a[MT];
+                const bool first = d % (GS / 32) == 0, last = d % (GS / 32) == GS / 32 - 1;
+                const u32x4 f = widen8<DT>(v[d], widen);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    u32x4 v = {0u, 0u, 0u, 0u};
-                    if (live[i])
-                        v = whole ? load_any<u32x4>(xrow[i] + k) : load8_guarded(xrow[i], k, p.K);
-                    a[i] = pair_up(v);
-                    S[i] = mfma16<DT>(a[i], ones, first ? zero : S[i]);
+                    const u32x4 a = *(const u32x4 *)x_place(buf, R < 16 ? min(c, R - 1) : 16 * i + c, b,
+                                                            GS < 128 ? 4 * d + g : 4 * g + d);
+                    S[i] = mfma16<DT>(a, ones, first ? zero : S[i]);
+                    P[i] = mfma16<DT>(a, f, first ? zero : P[i]);
                 }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const u32x4 f = widen8<DT>(w[b][j][d]);
+                if (last) {
+                    const float2 sc = sh.scale[wave][q0 + b * GROUPS + d / (GS / 32)][c];
 #pragma unroll
                     for (int i = 0; i < MT; ++i)
-                        P[i][j] = mfma16<DT>(a[i], f, first ? zero : P[i][j]);
-                }
-                // the group's first k, which may lie past K
-                const int64_t kg = SMALL ? kb + 32 * (p.group == 32 ? d : d & 2) : kb;
-                if (last && kg < p.K) {
-                    const int64_t gi = kg / p.group;
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        const float s = to_float<DT>(srow[j][gi]);
-                        const float off = 16.0f + (p.z ? (float)zrow[j][gi] : 8.0f);
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                acc[i][j][r] = fmaf(s, fmaf(-off, S[i][r], P[i][j][r]), acc[i][j][r]);
-                    }
+                        for (int r = 0; r < 4; ++r)
+                            acc[i][r] = fmaf(sc.x, fmaf(-sc.y, S[i][r], P[i][r]), acc[i][r]);
                 }
             }
         }
-    }
+    };
+    auto sync = [&] {
+        __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
 
-    // the waves' blocks, added in ascending order
+    if (mine > 0) {
+        load_scales(u0 * (kUnit / GS));
+#pragma unroll
+        for (int a = 0; a < XA; ++a)
+            load_x(xr[a], a);
+        load_w(w[0], 0);
+        load_w(w[1], 1);
+        auto step = [&]<int B>(int t) {
+            const int buf = WN == 1 ? 0 : B;
+            if (B == 0 && t % CHUNK == 0) {
+                store_scales();
+                load_scales((u0 + min(t + CHUNK, mine - 1) / CHUNK * CHUNK) * (kUnit / GS));
+            }
+            store_x(xr[B % XA], buf);
+            load_x(xr[B % XA], t + XA);
+            if (WN > 1)
+                sync();
+            compute(w[B], buf, t % CHUNK * (kUnit / GS));
+            load_w(w[B], t + 2);
+        };
+        for (int t = 0;;) {
+            step.template operator()<0>(t);
+            if (++t == mine)
+                break;
+            step.template operator()<1>(t);
+            if (++t == mine)
+                break;
+        }
+    }
+    if (WN > 1 && mine < steps)
+        sync();   // (ranges differ by one unit)
+    if (p.K % kUnit) {
+        // the unit that K ends in: padded with zeros on its way through LDS, and
+        // taken by the last range's waves
+        const int kend = units * kUnit, bytes = (p.K - kend + 1) / 2;
+        if (WN > 1)
+            sync();
+        for (int o = tid; o < 16 * WN * 128; o += THREADS) {
+            const int n = min(nw + (o >> 7), p.N - 1), b = o & 127;
+            sh.wend[o >> 7][b] = b < bytes ? p.q[(int64_t)n * p.ldq + kend / 2 + b] : 0;
+        }
+        if (wk == WK - 1) {
+            for (int o = xi; o < R * kUnit; o += WN * 64) {
+                const int row = o / kUnit, k = o % kUnit, e = k & 7;
+                const uint16_t v = kend + k < p.K ? p.x[(int64_t)(m0 + min(row, rows - 1)) * p.ldx + kend + k] : 0;
+                ((uint16_t *)x_place(0, row, k >> 7, k >> 3 & 15))[(e & 3) * 2 + (e >> 2)] = v;
+            }
+            load_scales(units * (kUnit / GS));
+            store_scales();
+        }
+        sync();
+        if (wk == WK - 1) {
+            w[0][0] = *(const u32x4 *)(sh.wend[16 * wn + c] + 16 * g);
+            w[0][1] = *(const u32x4 *)(sh.wend[16 * wn + c] + 64 + 16 * g);
+            compute(w[0], 0, 0);
+        }
+    }
+    sync();   // (x and the scales are done with)
+
+    // the ranges' sums, added in ascending order
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                red[((wave * MT * NT + i * NT + j) * 4 + r) * 64 + lane] = acc[i][j][r];
-    __syncthreads();
-    for (int o = tid; o < MT * NT * 256; o += kThreads) {
-        const int tile = o >> 8, r = o >> 6 & 3, l = o & 63;
-        const int m = m0 + 16 * (tile / NT) + 4 * (l >> 4) + r, n = n0 + 16 * (tile % NT) + (l & 15);
-        if (m >= p.M || n >= p.N)
+        for (int r = 0; r < 4; ++r)
+            sh.red[wk][wn][i][64 * r + lane] = acc[i][r];
+    sync();
+    for (int o = tid; o < WN * MT * 256; o += THREADS) {
+        const int j = o / (MT * 256), i = (o >> 8) % MT, r = o >> 6 & 3, l = o & 63;
+        const int row = 16 * i + 4 * (l >> 4) + r, n = nw + 16 * j + (l & 15);
+        if (row >= rows || n >= p.N)
             continue;
-        float v = red[o];
+        float v = sh.red[0][j][i][o & 255];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            v += red[w * MT * NT * 256 + o];
+        for (int w = 1; w < WK; ++w)
+            v += sh.red[w][j][i][o & 255];
+        const int64_t at = (int64_t)(m0 + row) * p.ldy + n;
         if (p.out16)
-            ((uint16_t *)p.y)[(int64_t)m * p.ldy + n] = from_float<DT>(v);
+            ((uint16_t *)p.y)[at] = from_float<DT>(v);
         else
-            ((float *)p.y)[(int64_t)m * p.ldy + n] = v;
+            ((float *)p.y)[at] = v;
     }
 }
 
