@@ -110,12 +110,15 @@ __device__ __forceinline__ u32x4 load16_end(const void *row, int64_t at, int64_t
         return shift_down(load_any<u32x4>((const char *)row + from), (int)min(at - from, (int64_t)16));
     }
     u32x4 v = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const uint32_t b = ((const uint8_t *)row)[min(at + j, n - 1)];
-        v[j / 4] |= (at + j < n ? b : 0u) << (8 * (j & 3));
+#pragma unroll 1
+    for (int j = 0; j < (int)n; ++j) {   // a row shorter than that, from its last byte down
+        const uint32_t b = ((const uint8_t *)row)[n - 1 - j];
+        v[3] = v[3] << 8 | v[2] >> 24;
+        v[2] = v[2] << 8 | v[1] >> 24;
+        v[1] = v[1] << 8 | v[0] >> 24;
+        v[0] = v[0] << 8 | b;
     }
-    return v;
+    return shift_down(v, (int)min(at, (int64_t)16));
 }
 
 }  // namespace xdecode_dev

@@ -110,10 +110,13 @@ struct QuantLds {
         struct {
             char x[WK][BUFS][XPART];
             float2 scale[WK * WN][16][16];   // {s, 16 + z} of 16 groups of 16 columns
-            uint8_t wend[16 * WN][128];      // the unit that K ends in
         };
         float red[WK][WN][MT][256];
     };
+    // the weights of the unit that K ends in, in the place of x of the first
+    // ranges; the last range's holds x of that unit
+    static_assert((WK - 1) * BUFS * XPART >= 16 * WN * 128, "room for the last unit's weights");
+    __device__ __forceinline__ uint8_t *wend() { return (uint8_t *)x; }
 };
 
 // The waves of a workgroup: WN take 16 columns each, WK a range of k each.
@@ -174,15 +177,15 @@ quant_kernel(QuantParams p)
     // where 8 k of a row lie in LDS: piece kc of a block of 128 goes to lane
     // group kg of product kd; 16 rows are swizzled so that neither the pieces of
     // a row nor the rows of a piece share a bank
-    auto x_place = [&](int buf, int row, int b, int kc) {
+    auto x_place = [&](int row, int b, int kc) {
         const int kd = GS < 128 ? kc >> 2 : kc & 3, kg = GS < 128 ? kc & 3 : kc >> 2;
-        return R < 16 ? sh.x[wk][buf] + (((b * 4 + kd) * 4 + kg) * R + row) * 16
-                      : sh.x[wk][buf] + ((b * 4 + kd) * MT + (row >> 4)) * 1024 + kg * 256 + ((row ^ kc) & 15) * 16;
+        return R < 16 ? (((b * 4 + kd) * 4 + kg) * R + row) * 16
+                      : ((b * 4 + kd) * MT + (row >> 4)) * 1024 + kg * 256 + ((row ^ kc) & 15) * 16;
     };
     auto store_x = [&](const u32x4 (&from)[NP], int buf) {
 #pragma unroll
         for (int q = 0; q < NP; ++q)
-            *(u32x4 *)x_place(buf, (xi >> 5) + 2 * WN * q, xi >> 4 & 1, xi & 15) = pair_up(from[q]);
+            *(u32x4 *)(sh.x[wk][buf] + x_place((xi >> 5) + 2 * WN * q, xi >> 4 & 1, xi & 15)) = pair_up(from[q]);
     };
 
     // scales and zero points of 16 groups (of GS k) from group q0 on: lane
@@ -243,8 +246,8 @@ quant_kernel(QuantParams p)
                 const u32x4 f = widen8<DT>(v[d], widen);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const u32x4 a = *(const u32x4 *)x_place(buf, R < 16 ? min(c, R - 1) : 16 * i + c, b,
-                                                            GS < 128 ? 4 * d + g : 4 * g + d);
+                    const u32x4 a = *(const u32x4 *)(sh.x[wk][buf] + x_place(R < 16 ? min(c, R - 1) : 16 * i + c, b,
+                                                                             GS < 128 ? 4 * d + g : 4 * g + d));
                     S[i] = mfma16<DT>(a, ones, first ? zero : S[i]);
                     P[i] = mfma16<DT>(a, f, first ? zero : P[i]);
                 }
@@ -300,26 +303,27 @@ quant_kernel(QuantParams p)
     if (p.K % kUnit) {
         // the unit that K ends in: padded with zeros on its way through LDS, and
         // taken by the last range's waves
-        const int kend = units * kUnit, bytes = (p.K - kend + 1) / 2;
-        if (WN > 1)
-            sync();
-        for (int o = tid; o < 16 * WN * 128; o += THREADS) {
-            const int n = min(nw + (o >> 7), p.N - 1), b = o & 127;
-            sh.wend[o >> 7][b] = b < bytes ? p.q[(int64_t)n * p.ldq + kend / 2 + b] : 0;
+        const int kend = units * kUnit;
+        sync();   // (x is done with)
+        char *const to = sh.x[WK - 1][0];
+        for (int o = tid; o < 16 * WN * 8; o += THREADS)
+            *(u32x4 *)(sh.wend() + 16 * o) =
+                load16_end(p.q + (int64_t)min(nw + (o >> 3), p.N - 1) * p.ldq, kend / 2 + 16 * (o & 7),
+                           ((int64_t)p.K + 1) / 2);
+        for (int o = tid; o < R * 32; o += THREADS) {
+            const int row = o >> 5;
+            const u32x4 v = load16_end(p.x + (int64_t)(m0 + min(row, rows - 1)) * p.ldx,
+                                       2 * ((int64_t)kend + 8 * (o & 31)), 2 * (int64_t)p.K);
+            *(u32x4 *)(to + x_place(row, o >> 4 & 1, o & 15)) = pair_up(v);
         }
         if (wk == WK - 1) {
-            for (int o = xi; o < R * kUnit; o += WN * 64) {
-                const int row = o / kUnit, k = o % kUnit, e = k & 7;
-                const uint16_t v = kend + k < p.K ? p.x[(int64_t)(m0 + min(row, rows - 1)) * p.ldx + kend + k] : 0;
-                ((uint16_t *)x_place(0, row, k >> 7, k >> 3 & 15))[(e & 3) * 2 + (e >> 2)] = v;
-            }
             load_scales(units * (kUnit / GS));
             store_scales();
         }
         sync();
         if (wk == WK - 1) {
-            w[0][0] = *(const u32x4 *)(sh.wend[16 * wn + c] + 16 * g);
-            w[0][1] = *(const u32x4 *)(sh.wend[16 * wn + c] + 64 + 16 * g);
+            w[0][0] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 128 + 16 * g);
+            w[0][1] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 128 + 64 + 16 * g);
             compute(w[0], 0, 0);
         }
     }
