@@ -631,9 +631,11 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
  *                the inputs
  * A score of -inf gives its expert no weight; a token whose chosen scores are
  * all -inf gets a row of zeros; a NaN among a token's scores (it counts as the
- * largest) makes its row NaN.  h is kept to 24 bits (with XGEMM_FP16: |h| up
- * to 2.6e8, resolved to 2^-34).  Uses the handle's workspace: 6 bytes for each
- * of min(T, 64) * top * (I rounded up to 128), and some KiB.
+ * largest) makes its row NaN.  h is kept to 24 bits for an output in fp32, to 16
+ * or more for one in 16 bits (with XGEMM_FP16: |h| up to 2.6e8, resolved to
+ * 2^-34 and 2^-23).  Uses the handle's workspace: 6 bytes (4 for a 16-bit output)
+ * for each of min(T, 64) * top * (I rounded up to 64), 128 bytes for each of
+ * min(T, 64) * H and of the experts in use, and some KiB.
  */
 #define XGEMM_EXPERTS_MAX 1024
 #define XGEMM_EXPERTS_MAX_TOP 32

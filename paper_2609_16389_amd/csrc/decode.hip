@@ -126,24 +126,51 @@ int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int6
 
 using xexperts_dev::ExpertsParams;
 
-template <int DT, int MT>
+template <int DT, int R, int PL, int WN, int WK>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
+    using namespace xexperts_dev;
     if (p.slots > 0)
-        hipLaunchKernelGGL((xexperts_dev::route_up<DT, MT>), dim3(cdiv(p.I, 16), p.slots),
-                           dim3(xexperts_dev::kUpThreads), 0, s, p);
-    hipLaunchKernelGGL((xexperts_dev::down_sum<DT, MT>), dim3(cdiv(p.H, 16)), dim3(xexperts_dev::kDownThreads), 0, s, p);
+        hipLaunchKernelGGL((route_up<DT, R, PL>), dim3(cdiv(p.I, 16), p.slots), dim3(kUpThreads), 0, s, p);
+    const dim3 grid(cdiv(p.H, 16 * WN), p.parts), block(64 * WN * WK);
+    if (p.I % 8 == 0)
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, false>), grid, block, 0, s, p);
+    else if constexpr (PL == 3)   // (see experts_h_parts)
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, true>), grid, block, 0, s, p);
 }
 
-template <int DT>
+// 16-bit parts that h is kept in: two suffice for a 16-bit output (ragged rows
+// are built with three only)
+int experts_h_parts(bool out16, int64_t I) { return out16 && I % 8 == 0 ? 2 : 3; }
+
+// Columns of y a workgroup of the second launch takes.
+int experts_columns(int64_t T) { return T <= 2 ? 16 : 64; }
+
+// Parts that the second launch cuts the slots' inner dimensions into: four
+// workgroups a CU (one where their waves take ranges of their own), parts of at
+// least four units (16 for eight waves), and counters for the workgroups of a
+// part.
+int experts_parts(int64_t T, int64_t H, int64_t slots, int64_t Ip, int cu_count)
+{
+    using namespace xexperts_dev;
+    const int64_t blocks = cdiv(H, experts_columns(T)), units = slots * (Ip / kDownUnit);
+    if (blocks > (int64_t)(xgemm_host::kWsPrefix / sizeof(int)))
+        return 1;
+    const int64_t want = T <= 2 ? cdiv((int64_t)cu_count, blocks) : cdiv(4 * (int64_t)cu_count, blocks);
+    return (int)std::max<int64_t>(1, std::min({want, units / (T <= 2 ? 16 : 4), (int64_t)kMaxParts}));
+}
+
+template <int DT, int PL>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
-    if (p.T <= 16)
-        launch_experts<DT, 1>(p, s);
+    if (p.T <= 2)
+        launch_experts<DT, 2, PL, 1, 8>(p, s);
+    else if (p.T <= 16)
+        launch_experts<DT, 16, PL, 4, 1>(p, s);
     else if (p.T <= 32)
-        launch_experts<DT, 2>(p, s);
+        launch_experts<DT, 32, PL, 4, 1>(p, s);
     else
-        launch_experts<DT, 4>(p, s);
+        launch_experts<DT, 64, PL, 4, 1>(p, s);
 }
 
 int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x, int64_t ldx,
@@ -158,7 +185,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
         return XGEMM_ERR_INVALID_ARG;
     // (2 I rows of up; the inner dimension padded stays below 2^31)
     if (!dims_ok(T, H, ldx) || !dims_ok(T, E, lds) || !dims_ok(T, H, ldy) || I < 0 || I > kMaxDim / 4 ||
-        !dims_ok(2 * I, H, ldu) || !dims_ok(H, I, ldd) || su < 0 || sd < 0 || H > kMaxDim - 2 * kUnit * kUpWaves)
+        !dims_ok(2 * I, H, ldu) || !dims_ok(H, I, ldd) || su < 0 || sd < 0 || H > kMaxDim - 2 * kUpUnit * kUpWaves)
         return XGEMM_ERR_INVALID_ARG;
     if ((double)E * (double)su > 9.0e18 || (double)E * (double)sd > 9.0e18)
         return XGEMM_ERR_INVALID_ARG;
@@ -185,30 +212,44 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     p.Ip = (int)(cdiv(I, kPad) * kPad);
     p.renormalize = renormalize && I > 0;
     p.out16 = out == XGEMM_OUT_SAME;
+    const int PL = experts_h_parts(p.out16, I);
     // tokens in chunks of at most kMaxTokens, each in the same workspace
-    const int64_t most = std::min<int64_t>(T, kMaxTokens);
-    const size_t slot_bytes = cdiv(std::min(most * top, E) * sizeof(Slot), 256) * 256;
-    const size_t weight_bytes = cdiv(most * top * sizeof(float), 256) * 256;
+    const int64_t most = std::min<int64_t>(T, kMaxTokens), most_slots = std::min(most * top, E);
     if ((double)most * (double)top * (double)p.Ip * 6.0 > 9.0e15)
         return XGEMM_ERR_INVALID_ARG;
-    const size_t h_bytes = (size_t)most * top * p.Ip * 6;
-    const int rc = xgemm_host::acquire_workspace(h, slot_bytes + weight_bytes + h_bytes, s);
+    size_t bytes = 0;
+    auto take = [&](size_t n) {
+        const size_t at = bytes;
+        bytes += cdiv(n, 256) * 256;
+        return at;
+    };
+    const size_t at_expert = take(most_slots * sizeof(int)), at_count = take(most_slots * sizeof(int));
+    const size_t at_pair = take(most_slots * kMaxTokens * sizeof(uint16_t));
+    const size_t at_weight = take(most * top * sizeof(float));
+    const size_t at_h = take((size_t)most * top * p.Ip * 2 * PL);
+    const size_t at_part = take((size_t)kMaxParts * most * H * sizeof(float));
+    const int rc = xgemm_host::acquire_workspace(h, bytes, s);
     if (rc != XGEMM_OK)
         return rc;
     char *const ws = (char *)h->workspace + xgemm_host::kWsPrefix;
-    p.slot = (Slot *)ws;
-    p.weight = (float *)(ws + slot_bytes);
-    p.h = (uint16_t *)(ws + slot_bytes + weight_bytes);
+    p.expert = (int *)(ws + at_expert);
+    p.count = (int *)(ws + at_count);
+    p.pair = (uint16_t *)(ws + at_pair);
+    p.weight = (float *)(ws + at_weight);
+    p.h = (uint16_t *)(ws + at_h);
+    p.part = (float *)(ws + at_part);
+    p.done = (int *)h->workspace;
     for (int64_t t = 0; t < T; t += kMaxTokens) {
         p.T = (int)std::min<int64_t>(kMaxTokens, T - t);
         p.slots = I > 0 ? (int)std::min<int64_t>(p.T * top, E) : 0;   // (without inner columns y is zero)
+        p.parts = experts_parts(p.T, H, p.slots, p.Ip, h->cu_count);
         p.x = (const uint16_t *)x + t * ldx;
         p.scores = scores + t * lds;
         p.y = (char *)y + t * ldy * (p.out16 ? 2 : 4);
         if (dtype == XGEMM_BF16)
-            launch_experts<0>(p, s);
+            PL == 2 ? launch_experts<0, 2>(p, s) : launch_experts<0, 3>(p, s);
         else
-            launch_experts<1>(p, s);
+            PL == 2 ? launch_experts<1, 2>(p, s) : launch_experts<1, 3>(p, s);
     }
     const int launched = launch_status(h, "experts launch");
     const int released = xgemm_host::release_workspace(h, s);

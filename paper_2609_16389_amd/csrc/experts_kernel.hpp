@@ -20,18 +20,30 @@
 // then forms 16 gate and 16 up columns for the slot's tokens, the waves
 // splitting the hidden dimension, and writes h.  The first workgroup of a
 // slot also writes the slot's tokens and weights.
-// Second launch (down_sum): one workgroup for 16 columns of y.  Its waves
-// share the slots' inner dimensions evenly and keep sums of their own for
-// every token in LDS, which are added in the order of the waves: no atomics,
-// one order of summation.
+// Second launch (down_sum): the slots' inner dimensions, one after the other in
+// units of 64, are cut into even ranges; a range forms its part of 16 columns
+// of y a wave, for every token, in LDS.  With one or two tokens the waves of a
+// workgroup take a range each, else they take the same range and 16 columns
+// each, sharing h through LDS (each workgroup reads all of h, which with 16
+// columns would be more than the weights).  The ranges' sums are added in
+// ascending order, by whichever workgroup is the last to finish: no float
+// atomics, one order of summation.
+//
+// In both, a wave brings its rows of x or h in through LDS, the pieces of a
+// unit arranged so that the matrix operand is one conflict-free 16-byte read,
+// and keeps two units of weights on their way.  The loops' loads are
+// unconditional (past the end they repeat the last unit's): loads return in
+// order, and one that may not have been issued turns the waits behind it into
+// waits for all.
 //
 // The second product needs h on the matrix units, which take 16 bits.  Rounded
 // to 16 bits h would lose more than the rounding of y does, so it is written as
-// three 16-bit parts that together hold its 24 bits, and multiplied as three
-// products (the matrix units are idle most of the time).
+// 16-bit parts, and multiplied as that many products (the matrix units are
+// idle most of the time): three, which together hold its 24 bits, for a y in
+// fp32, two (16 bits of h or more) for a y that is rounded to 16 bits itself.
 //   bfloat16: h = a + b + c, each part the rounding of what the ones before leave.
 //   binary16, whose range is short: h = 2^12 (a + 2^-11 (b + 2^-11 c)).  This
-//   holds |h| up to 2.6e8 and resolves 2^-34.
+//   holds |h| up to 2.6e8 and resolves 2^-34 (2^-23 with two parts).
 #pragma once
 
 #include "decode_device.hpp"
@@ -42,17 +54,12 @@ using namespace xdecode_dev;
 
 constexpr int kMaxTokens = 64;    // tokens of a launch
 constexpr int kMaxExperts = 1024;
-constexpr int kUpThreads = 512, kUpWaves = kUpThreads / 64;
-constexpr int kDownThreads = 1024, kDownWaves = kDownThreads / 64;
-constexpr int kUnit = 128;        // k per unit of a wave
-constexpr int kPad = 128;         // inner columns of h are padded to this
-
-// A chosen expert and the (token, choice) pairs that chose it.
-struct Slot {
-    int expert;  // -1: empty
-    int count;
-    uint16_t pair[kMaxTokens];  // token * top + choice
-};
+constexpr int kMaxTop = 32;
+constexpr int kUpWaves = 8, kUpThreads = 64 * kUpWaves;
+constexpr int kUpUnit = 128;      // k per unit of a wave in the first product
+constexpr int kDownUnit = 64;     // and in the second
+constexpr int kPad = kDownUnit;   // inner columns of h are padded to this
+constexpr int kMaxParts = 32;     // ranges of the second product that workgroups take
 
 struct ExpertsParams {
     const uint16_t *x;
@@ -63,10 +70,31 @@ struct ExpertsParams {
     int T, E, top, H, I, Ip;                  // Ip: I rounded up to kPad
     int slots;
     int renormalize, out16;
-    Slot *slot;       // [slots]
+    int parts;
+    int *expert;      // [slots]: the slot's expert, -1: empty
+    int *count;       // [slots]: its tokens
+    uint16_t *pair;   // [slots][kMaxTokens]: token * top + choice
     float *weight;    // [T * top]: exp(score - largest), over the whole softmax's sum without renormalize
-    uint16_t *h;      // [3][T * top][Ip]
+    uint16_t *h;      // [parts of h][T * top][Ip]
+    float *part;      // [parts][T][H], where parts > 1
+    int *done;        // [workgroups of a range], zero between launches
 };
+
+// Where 8 k of a row (piece kc of the row's unit, 8 kc .. + 7) lie in LDS, for
+// R rows: lane group kc % 4 of product kc / 4.  16 rows are swizzled so that
+// neither the pieces of a row nor the rows of a piece share a bank.
+template <int R>
+__device__ __forceinline__ int place(int row, int kc)
+{
+    constexpr int MT = (R + 15) / 16;
+    return R < 16 ? (kc * R + row) * 16
+                  : ((kc >> 2) * MT + (row >> 4)) * 1024 + (kc & 3) * 256 + ((row ^ kc) & 15) * 16;
+}
+template <int R>
+constexpr int unit_bytes(int unit)
+{
+    return R < 16 ? unit * R * 2 : (R + 15) / 16 * 16 * unit * 2;
+}
 
 // A score as a whole number in the same order: NaN above all, the two zeros
 // alike.
@@ -78,14 +106,14 @@ __device__ __forceinline__ uint32_t order_of(float v)
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
-// The three parts of h (see above).
-template <int DT>
-__device__ __forceinline__ void split3(float v, uint16_t (&part)[3])
+// The parts of h (see above).
+template <int DT, int PL>
+__device__ __forceinline__ void split_parts(float v, uint16_t (&part)[PL])
 {
     constexpr float down = DT == 0 ? 1.0f : 0x1p-12f, step = DT == 0 ? 1.0f : 0x1p11f;
     float r = v * down;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < PL; ++i) {
         part[i] = from_float<DT>(r);
         const float got = to_float<DT>(part[i]);
         r = (r - got) * step;
@@ -100,54 +128,79 @@ __device__ __forceinline__ float score_exp(float v, float largest)
     return v == -__builtin_inff() ? 0.0f : expf(v - largest);
 }
 
-template <int DT, int MT>
-__global__ void __launch_bounds__(kUpThreads)
+__device__ __forceinline__ void sync_lds()
+{
+    __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// R: rows of a slot that the launch provides for (2, or a multiple of 16); PL:
+// parts of h.
+template <int DT, int R, int PL>
+__global__ void __launch_bounds__(kUpThreads, R <= 16 ? 4 : 2)
 route_up(ExpertsParams p)
 {
-    __shared__ union {
+    constexpr int MTS = (R + 15) / 16;
+    __shared__ __attribute__((aligned(16))) union {
         uint32_t key[kMaxExperts];
-        float red[kUpWaves * MT * 512];
+        char x[kUpWaves][unit_bytes<R>(kUpUnit)];
+        float red[kUpWaves * MTS * 512];
     } sh;
     __shared__ int sh_expert, sh_count, sh_first;
     __shared__ uint8_t sh_rank[kMaxTokens];
     __shared__ uint16_t sh_pair[kMaxTokens];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int slot = blockIdx.y, i0 = 16 * blockIdx.x;
 
-    // the slot's expert
+    // the slot's expert: the one of rank j among its token's scores
     const bool by_choice = p.slots < p.E;
+    const int t0 = by_choice ? slot / p.top : 0;
     if (by_choice) {
-        const int t = slot / p.top, j = slot - t * p.top;
+        const int j = slot - t0 * p.top;
+        const float *const row = p.scores + t0 * p.lds;
         for (int e = tid; e < p.E; e += kUpThreads)
-            sh.key[e] = order_of(p.scores[t * p.lds + e]);
+            sh.key[e] = order_of(row[e]);
         __syncthreads();
-        for (int e = tid; e < p.E; e += kUpThreads) {
-            const uint32_t mine = sh.key[e];
+        int per = 32;   // lanes an expert
+        while (per > 1 && kUpThreads / per < p.E)
+            per /= 2;
+        for (int e0 = 0; e0 < p.E; e0 += kUpThreads / per) {
+            const int e = e0 + tid / per;
+            const uint32_t mine = sh.key[min(e, p.E - 1)];
             int rank = 0;
-            for (int o = 0; o < p.E; ++o)
+            for (int o = tid & (per - 1); o < p.E; o += per)
                 rank += sh.key[o] > mine || (sh.key[o] == mine && o < e);
-            if (rank == j)
+            for (int d = per / 2; d >= 1; d /= 2)
+                rank += __shfl_xor(rank, d, 64);
+            if (rank == j && e < p.E)
                 sh_expert = e;
         }
         __syncthreads();
     }
-    const int expert = by_choice ? sh_expert : slot;
+    const int expert = __builtin_amdgcn_readfirstlane(by_choice ? sh_expert : slot);
 
-    // its rank among each token's scores: `per` lanes a token
-    int per = 64;
-    while (per > 8 && kUpThreads / per < p.T)
-        per /= 2;
-    const int tok = tid / per, sub = tid & (per - 1);
-    {
-        const float *row = p.scores + (int64_t)min(tok, p.T - 1) * p.lds;
+    // its rank among each token's scores: `per` lanes a token.  (One token's
+    // slots hold that token.)
+    const bool one = p.T == 1 && by_choice;
+    if (!one || blockIdx.x == 0) {
+        int per = 64;
+        while (per > 8 && kUpThreads / per < p.T)
+            per /= 2;
+        const int tok = tid / per, sub = tid & (per - 1);
+        const float *const row = p.scores + (int64_t)min(tok, p.T - 1) * p.lds;
         const float own = row[expert];
         const uint32_t mine = order_of(own);
         int rank = 0;
         float largest = -__builtin_inff();
+#pragma unroll 4
         for (int o = sub; o < p.E; o += per) {
-            const uint32_t k = order_of(row[o]);
+            const float v = row[o];
+            const uint32_t k = order_of(v);
             rank += k > mine || (k == mine && o < expert);
-            largest = fmaxf(largest, row[o]);
+            largest = fmaxf(largest, v);
         }
         for (int d = per / 2; d >= 1; d /= 2) {
             rank += __shfl_xor(rank, d, 64);
@@ -169,6 +222,8 @@ route_up(ExpertsParams p)
             if (chosen && sub == 0)
                 p.weight[tok * p.top + rank] = w;
         }
+    } else if (tid == 0) {
+        sh_rank[0] = (uint8_t)slot;
     }
     __syncthreads();
     if (wave == 0) {
@@ -182,16 +237,15 @@ route_up(ExpertsParams p)
         }
     }
     __syncthreads();
-    const int count = sh_count;
-    const bool empty = count == 0 || (by_choice && sh_first != slot / p.top);
+    const int count = __builtin_amdgcn_readfirstlane(sh_count);
+    const bool empty = count == 0 || (by_choice && sh_first != t0);
     if (blockIdx.x == 0) {
-        Slot *const s = p.slot + slot;
         if (tid == 0) {
-            s->expert = empty ? -1 : expert;
-            s->count = count;
+            p.expert[slot] = empty ? -1 : expert;
+            p.count[slot] = count;
         }
         if (tid < count)
-            s->pair[tid] = sh_pair[tid];
+            p.pair[slot * kMaxTokens + tid] = sh_pair[tid];
     }
     if (empty)
         return;
@@ -200,174 +254,303 @@ route_up(ExpertsParams p)
     const uint16_t *wrow[2];
 #pragma unroll
     for (int v = 0; v < 2; ++v)
-        wrow[v] = p.up + (int64_t)expert * p.su + (int64_t)(v * p.I + min(i0 + c, p.I - 1)) * p.ldu;
-    const uint16_t *xrow[MT];
-    bool live[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        live[i] = 16 * i + c < count;
-        xrow[i] = p.x + (int64_t)(live[i] ? sh_pair[16 * i + c] / p.top : 0) * p.ldx;
-    }
-    f32x4 acc[MT][2];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-            acc[i][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        wrow[v] = p.up + (int64_t)expert * p.su + (int64_t)(v * p.I + min(i0 + c, p.I - 1)) * p.ldu + 8 * g;
+    const int64_t plane = (int64_t)p.T * p.top * p.Ip;
 
-    for (int k0 = wave * kUnit; k0 < p.H; k0 += kUpWaves * kUnit) {
-        const bool whole = k0 + kUnit <= p.H;
-        u32x4 w[4][2];
+    // the products for up to RB rows
+    auto body = [&]<int RB>() {
+        constexpr int MT = (RB + 15) / 16, NP = RB * 16 > 64 ? RB * 16 / 64 : 1;
+        char *const xs = sh.x[wave];
+        const uint16_t *xrow[NP];
+        int xdst[NP];
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int q = 0; q < NP; ++q) {
+            const int row = (lane >> 4) + 4 * q, kc = lane & 15;
+            const int r = min(row, RB - 1);
+            xrow[q] = p.x + (int64_t)(sh_pair[min(r, count - 1)] / p.top) * p.ldx + 8 * kc;
+            xdst[q] = place<RB>(r, kc);
+        }
+        f32x4 acc[MT][2];
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int k = k0 + 32 * d + 8 * g;
-                w[d][v] = whole ? load_any<u32x4>(wrow[v] + k) : load16_end(wrow[v], 2 * (int64_t)k, 2 * (int64_t)p.H);
-            }
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            const int k = k0 + 32 * d + 8 * g;
+            for (int v = 0; v < 2; ++v)
+                acc[i][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        u32x4 w[2][4][2], xr[NP];
+        auto store_x = [&] {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-                if (16 * i < count) {
-                    u32x4 a = {0u, 0u, 0u, 0u};
-                    if (live[i])
-                        a = whole ? load_any<u32x4>(xrow[i] + k) : load16_end(xrow[i], 2 * (int64_t)k, 2 * (int64_t)p.H);
+            for (int q = 0; q < NP; ++q)
+                *(u32x4 *)(xs + xdst[q]) = xr[q];
+        };
+        auto compute = [&](const u32x4 (&from)[4][2]) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const u32x4 a = *(const u32x4 *)(xs + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
-                        acc[i][v] = mfma16<DT>(a, w[d][v], acc[i][v]);
+                        acc[i][v] = mfma16<DT>(a, from[d][v], acc[i][v]);
                 }
+        };
+        // this wave's whole units
+        const int units = p.H / kUpUnit;
+        const int u0 = wave * (units / kUpWaves) + min(wave, units % kUpWaves);
+        const int mine = units / kUpWaves + (wave < units % kUpWaves);
+        auto load_x = [&](int t) {
+            const int k = (u0 + min(t, mine - 1)) * kUpUnit;
+#pragma unroll
+            for (int q = 0; q < NP; ++q)
+                xr[q] = load_any<u32x4>(xrow[q] + k);
+        };
+        auto load_w = [&](u32x4 (&to)[4][2], int t) {
+            const int k = (u0 + min(t, mine - 1)) * kUpUnit;
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    to[d][v] = load_any<u32x4>(wrow[v] + k + 32 * d);
+        };
+        if (mine > 0) {
+            load_x(0);
+            load_w(w[0], 0);
+            load_w(w[1], 1);
+            auto step = [&]<int B>(int t) {
+                store_x();
+                load_x(t + 1);
+                compute(w[B]);
+                load_w(w[B], t + 2);
+            };
+            for (int t = 0;;) {
+                step.template operator()<0>(t);
+                if (++t == mine)
+                    break;
+                step.template operator()<1>(t);
+                if (++t == mine)
+                    break;
+            }
         }
-    }
+        // what is left of the rows, by the last wave (x is zero past H)
+        if (units * kUpUnit < p.H && wave == kUpWaves - 1) {
+            const int64_t k = (int64_t)units * kUpUnit;
+#pragma unroll
+            for (int q = 0; q < NP; ++q)
+                xr[q] = load16_end(xrow[q] - 8 * (lane & 15), 2 * (k + 8 * (lane & 15)), 2 * (int64_t)p.H);
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    w[0][d][v] = load16_end(wrow[v] - 8 * g, 2 * (k + 32 * d + 8 * g), 2 * (int64_t)p.H);
+            store_x();
+            compute(w[0]);
+        }
+        sync_lds();   // (x is done with)
 
-    // the waves' blocks, added in ascending order
+        // the waves' blocks, added in ascending order
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int v = 0; v < 2; ++v)
+            for (int v = 0; v < 2; ++v)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                sh.red[((wave * MT + i) * 2 + v) * 256 + 64 * r + lane] = acc[i][v][r];
-    __syncthreads();
-    const int64_t plane = (int64_t)p.T * p.top * p.Ip;
-    for (int o = tid; o < MT * 256; o += kUpThreads) {
-        const int i = o >> 8, r = o >> 6 & 3, l = o & 63;
-        const int m = 16 * i + 4 * (l >> 4) + r, col = i0 + (l & 15);
-        if (m >= count)
-            continue;
-        float sum[2];
+                for (int r = 0; r < 4; ++r)
+                    sh.red[((wave * MT + i) * 2 + v) * 256 + 64 * r + lane] = acc[i][v][r];
+        sync_lds();
+        for (int o = tid; o < MT * 256; o += kUpThreads) {
+            const int i = o >> 8, r = o >> 6 & 3, l = o & 63;
+            const int m = 16 * i + 4 * (l >> 4) + r, col = i0 + (l & 15);
+            if (m >= count)
+                continue;
+            float sum[2];
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            sum[v] = sh.red[(i * 2 + v) * 256 + (o & 255)];
+            for (int v = 0; v < 2; ++v) {
+                sum[v] = sh.red[(i * 2 + v) * 256 + (o & 255)];
 #pragma unroll
-            for (int w = 1; w < kUpWaves; ++w)
-                sum[v] += sh.red[((w * MT + i) * 2 + v) * 256 + (o & 255)];
+                for (int w = 1; w < kUpWaves; ++w)
+                    sum[v] += sh.red[((w * MT + i) * 2 + v) * 256 + (o & 255)];
+            }
+            uint16_t part[PL] = {};
+            if (col < p.I)
+                split_parts<DT>(sum[0] / (1.0f + expf(-sum[0])) * sum[1], part);
+            uint16_t *const at = p.h + (int64_t)sh_pair[m] * p.Ip + col;
+#pragma unroll
+            for (int q = 0; q < PL; ++q)
+                at[q * plane] = part[q];
+            // the last workgroup also clears the padding past its columns
+            if (blockIdx.x == gridDim.x - 1)
+                for (int past = 16; col + past < p.Ip; past += 16)
+#pragma unroll
+                    for (int q = 0; q < PL; ++q)
+                        at[q * plane + past] = 0;
         }
-        uint16_t part[3] = {0, 0, 0};
-        if (col < p.I)
-            split3<DT>(sum[0] / (1.0f + expf(-sum[0])) * sum[1], part);
-        uint16_t *const at = p.h + (int64_t)sh_pair[m] * p.Ip + col;
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-            at[q * plane] = part[q];
-        // the last workgroup also clears the padding past its columns
-        if (blockIdx.x == gridDim.x - 1)
-            for (int past = 16; col + past < p.Ip; past += 16)
-#pragma unroll
-                for (int q = 0; q < 3; ++q)
-                    at[q * plane + past] = 0;
+    };
+    if constexpr (R <= 16) {
+        body.template operator()<R>();
+    } else {
+        if (count <= 16)
+            body.template operator()<16>();
+        else if (R == 32 || count <= 32)
+            body.template operator()<32>();
+        else
+            body.template operator()<R>();
     }
 }
 
-template <int DT, int MT>
-__global__ void __launch_bounds__(kDownThreads)
+// R, PL: as above.  WN waves take 16 columns each of the same range, or (WN ==
+// 1) WK waves a range each.  RAGGED: I is no multiple of 8, so that pieces of
+// rows end inside; otherwise a piece past I is the row's last one again (h is
+// zero there).
+template <int DT, int R, int PL, int WN, int WK, bool RAGGED>
+__global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : R == 32 ? 2 : 1)
 down_sum(ExpertsParams p)
 {
-    constexpr int kSums = DT == 0 ? 1 : 3;   // products of the parts that are kept apart
-    __shared__ float acc_all[kDownWaves * MT * 256];
-    __shared__ float sh_total[16 * MT];
-    __shared__ uint16_t sh_active[kMaxExperts];
-    __shared__ int sh_wave[kDownWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n0 = 16 * blockIdx.x;
+    static_assert(WN == 1 || WK == 1, "a barrier is the whole workgroup's");
+    constexpr int WAVES = WN * WK, THREADS = 64 * WAVES, TOKENS = R;
+    constexpr int SUMS = DT == 0 ? 1 : PL;   // products of the parts that are kept apart
+    constexpr int BUFS = WN == 1 ? 1 : 2;
+    constexpr int HB = unit_bytes<R>(kDownUnit);
+    __shared__ __attribute__((aligned(16))) char sh_h[WK][BUFS][PL][HB];
+    __shared__ float acc_all[WAVES][TOKENS * 16];
+    __shared__ float sh_weight[TOKENS * kMaxTop];
+    __shared__ uint16_t sh_slot[kMaxExperts];           // the slots in use, in ascending order:
+    __shared__ uint16_t sh_start[kMaxExperts + 1];      //   where their pairs start,
+    __shared__ uint16_t sh_pairs[TOKENS * kMaxTop];     //   and the pairs
+    __shared__ int sh_used, sh_last;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave % WN, wk = wave / WN;
+    const int nw = 16 * WN * blockIdx.x, n0 = nw + 16 * wn;
     const int c = lane & 15, g = lane >> 4;
+    float *const mine = acc_all[wave];
+    for (int o = lane; o < TOKENS * 16; o += 64)
+        mine[o] = 0.0f;
 
-    for (int o = tid; o < kDownWaves * MT * 256; o += kDownThreads)
-        acc_all[o] = 0.0f;
-    // what a token's weights are divided by
-    if (tid < p.T) {
+    // the slots in use and where their pairs go, by the first wave
+    if (wave == 0) {
+        int used = 0, pairs = 0;
+        for (int s0 = 0; s0 < p.slots; s0 += 64) {
+            const int s = s0 + lane;
+            const bool on = s < p.slots && p.expert[s] >= 0;
+            const int count = on ? p.count[s] : 0;
+            const uint64_t mask = __ballot(on);
+            int before = count;
+            for (int d = 1; d < 64; d *= 2) {
+                const int v = __shfl_up(before, d, 64);
+                before += lane >= d ? v : 0;
+            }
+            if (on) {
+                const int at = used + __popcll(mask & ((1ull << lane) - 1));
+                sh_slot[at] = (uint16_t)s;
+                sh_start[at] = (uint16_t)(pairs + before - count);
+            }
+            used += __popcll(mask);
+            pairs += __shfl(before, 63, 64);
+        }
+        if (lane == 0) {
+            sh_start[used] = (uint16_t)pairs;
+            sh_used = used;
+        }
+    }
+    // the weights, divided by their sum
+    for (int o = tid; o < p.T * p.top; o += THREADS) {
         float total = 1.0f;
         if (p.renormalize) {
             total = 0.0f;
             for (int j = 0; j < p.top; ++j)
-                total += p.weight[tid * p.top + j];
+                total += p.weight[o / p.top * p.top + j];
         }
-        sh_total[tid] = total;
+        sh_weight[o] = total == 0.0f ? 0.0f : p.weight[o] / total;
     }
-    // the slots in use, in ascending order
-    const bool used = tid < p.slots && p.slot[tid].expert >= 0;
-    const uint64_t mask = __ballot(used);
-    if (lane == 0)
-        sh_wave[wave] = __popcll(mask);
-    __syncthreads();
-    int before = 0, active = 0;
-    for (int w = 0; w < kDownWaves; ++w) {
-        before += w < wave ? sh_wave[w] : 0;
-        active += sh_wave[w];
+    sync_lds();
+    const int used = __builtin_amdgcn_readfirstlane(sh_used);
+    for (int a = wave; a < used; a += WAVES) {
+        const int start = sh_start[a], count = sh_start[a + 1] - start;
+        if (lane < count)
+            sh_pairs[start + lane] = p.pair[sh_slot[a] * kMaxTokens + lane];
     }
-    if (used)
-        sh_active[before + __popcll(mask & ((1ull << lane) - 1))] = (uint16_t)tid;
-    __syncthreads();
+    sync_lds();
 
-    const int chunks = p.Ip / kUnit;
-    const int64_t units = (int64_t)active * chunks;
-    const int64_t u_end = units * (wave + 1) / kDownWaves;
-    int64_t u = units * wave / kDownWaves;
-    float *const mine = acc_all + wave * MT * 256;
+    const int chunks = p.Ip / kDownUnit;
+    const int64_t units = (int64_t)used * chunks;
+    const int ranges = p.parts * WK, range = blockIdx.y * WK + wk;
+    int64_t u = units * range / ranges;
+    const int64_t u_end = units * (range + 1) / ranges;
     const int64_t plane = (int64_t)p.T * p.top * p.Ip;
-    while (u < u_end) {
-        const Slot *const s = p.slot + sh_active[u / chunks];
-        const int count = s->count;
-        const uint16_t *const wrow = p.down + (int64_t)s->expert * p.sd + (int64_t)min(n0 + c, p.H - 1) * p.ldd;
-        const uint16_t *hrow[MT];
-        bool live[MT];
-        f32x4 acc[MT][kSums];
+
+    // `len` units of slot `a` from its unit `first`, for up to RB rows
+    auto segment = [&]<int RB>(int a, int first, int len) {
+        constexpr int MT = (RB + 15) / 16, PIECES = RB * 8 * PL;
+        constexpr int NP = (PIECES + 64 * WN - 1) / (64 * WN);
+        const int start = sh_start[a], count = sh_start[a + 1] - start;
+        const int expert = p.expert[sh_slot[a]];
+        const uint16_t *const wrow =
+            p.down + (int64_t)expert * p.sd + (int64_t)min(n0 + c, p.H - 1) * p.ldd;
+        const uint16_t *hrow[NP];
+        int hdst[NP];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            live[i] = 16 * i + c < count;
-            hrow[i] = p.h + (int64_t)(live[i] ? s->pair[16 * i + c] : 0) * p.Ip;
-#pragma unroll
-            for (int q = 0; q < kSums; ++q)
-                acc[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < NP; ++q) {
+            const int piece = min(wn * 64 + lane + q * 64 * WN, PIECES - 1);
+            const int kc = piece & 7, row = (piece >> 3) % RB, pl = (piece >> 3) / RB;
+            hrow[q] = p.h + pl * plane + (int64_t)sh_pairs[start + min(row, count - 1)] * p.Ip + 8 * kc;
+            hdst[q] = pl * HB + place<RB>(row, kc);
         }
-        const int first = (int)(u % chunks);
-        const int last = (int)min((int64_t)chunks, first + (u_end - u));
-        for (int ch = first; ch < last; ++ch) {
-            const int k0 = ch * kUnit;
-            const bool whole = k0 + kUnit <= p.I;
-            u32x4 w[4];
+        f32x4 acc[MT][SUMS];
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const int k = k0 + 32 * d + 8 * g;
-                w[d] = whole ? load_any<u32x4>(wrow + k) : load16_end(wrow, 2 * (int64_t)k, 2 * (int64_t)p.I);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < SUMS; ++q)
+                acc[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        u32x4 w[2][2], hr[NP];
+        auto load_h = [&](int t) {
+            const int k = (first + min(t, len - 1)) * kDownUnit;
+#pragma unroll
+            for (int q = 0; q < NP; ++q)
+                hr[q] = *(const u32x4 *)(hrow[q] + k);
+        };
+        auto load_w = [&](u32x4 (&to)[2], int t) {
+            const int k = (first + min(t, len - 1)) * kDownUnit;
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                const int at = k + 32 * d + 8 * g;
+                if constexpr (RAGGED)
+                    to[d] = load16_end(wrow, 2 * (int64_t)at, 2 * (int64_t)p.I);
+                else
+                    to[d] = load_any<u32x4>(wrow + min(at, p.I - 8));
             }
+        };
+        load_h(0);
+        load_w(w[0], 0);
+        load_w(w[1], 1);
+        auto step = [&]<int B>(int t) {
+            char *const hs = sh_h[wk][BUFS == 1 ? 0 : B][0];
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const int k = k0 + 32 * d + 8 * g;
+            for (int q = 0; q < NP; ++q)
+                *(u32x4 *)(hs + hdst[q]) = hr[q];
+            load_h(t + 1);
+            if (WN > 1)
+                sync_lds();
+#pragma unroll
+            for (int d = 0; d < 2; ++d)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
-                    if (16 * i < count)
 #pragma unroll
-                        for (int q = 0; q < 3; ++q) {
-                            u32x4 a = {0u, 0u, 0u, 0u};
-                            if (live[i])
-                                a = *(const u32x4 *)(hrow[i] + q * plane + k);
-                            constexpr int one = kSums - 1;
-                            acc[i][q & (one ? 3 : 0)] = mfma16<DT>(a, w[d], acc[i][q & (one ? 3 : 0)]);
-                        }
-            }
+                    for (int q = 0; q < PL; ++q) {
+                        const u32x4 a =
+                            *(const u32x4 *)(hs + q * HB + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
+                        f32x4 &sum = acc[i][SUMS == 1 ? 0 : q];
+                        sum = mfma16<DT>(a, w[B][d], sum);
+                    }
+            load_w(w[B], t + 2);
+        };
+        for (int t = 0;;) {
+            step.template operator()<0>(t);
+            if (++t == len)
+                break;
+            step.template operator()<1>(t);
+            if (++t == len)
+                break;
         }
+        if (WN > 1)
+            sync_lds();   // (the next segment starts with the first buffer again)
         // the tokens' weighted sums
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -375,26 +558,82 @@ down_sum(ExpertsParams p)
             for (int r = 0; r < 4; ++r) {
                 const int m = 16 * i + 4 * g + r;
                 if (m < count) {
-                    const int pair = s->pair[m], t = pair / p.top;
-                    const float total = sh_total[t];
-                    const float weight = total == 0.0f ? 0.0f : p.weight[pair] / total;
+                    const int pair = sh_pairs[start + m], t = pair / p.top;
                     float v = acc[i][0][r];
-                    if constexpr (kSums == 3)
+                    if constexpr (SUMS == 2)
+                        v = 0x1p12f * (v + 0x1p-11f * acc[i][1][r]);
+                    if constexpr (SUMS == 3)
                         v = 0x1p12f * (v + 0x1p-11f * (acc[i][1][r] + 0x1p-11f * acc[i][2][r]));
-                    mine[t * 16 + c] += weight * v;
+                    mine[t * 16 + c] += sh_weight[pair] * v;
                 }
             }
-        u += last - first;
+    };
+    while (u < u_end) {
+        const int a = __builtin_amdgcn_readfirstlane((int)(u / chunks));
+        const int first = __builtin_amdgcn_readfirstlane((int)(u % chunks));
+        const int len = (int)min((int64_t)(chunks - first), u_end - u);
+        if constexpr (R <= 16) {
+            segment.template operator()<R>(a, first, len);
+        } else {
+            const int count = sh_start[a + 1] - sh_start[a];
+            if (count <= 16)
+                segment.template operator()<16>(a, first, len);
+            else if (R == 32 || count <= 32)
+                segment.template operator()<32>(a, first, len);
+            else
+                segment.template operator()<R>(a, first, len);
+        }
+        u += len;
     }
-    __syncthreads();
-    for (int o = tid; o < p.T * 16; o += kDownThreads) {
-        const int t = o >> 4, n = n0 + (o & 15);
+    sync_lds();
+
+    // the workgroup's sums: of its ranges (WK) or of its columns (WN)
+    const int cols = 16 * WN;
+    auto own = [&](int o) {   // value o of T x cols
+        const int t = o / cols, n = o % cols;
+        if (WN > 1)
+            return acc_all[n >> 4][t * 16 + (n & 15)];
+        float v = acc_all[0][o];
+#pragma unroll
+        for (int w = 1; w < WK; ++w)
+            v += acc_all[w][o];
+        return v;
+    };
+    const bool shared = p.parts > 1;
+    if (shared) {
+        // publish them with device-scope stores; once every wave's have
+        // completed, count in.  Nobody waits: the last one adds.
+        for (int o = tid; o < p.T * cols; o += THREADS) {
+            const int t = o / cols, n = nw + o % cols;
+            if (n < p.H)
+                __hip_atomic_store(p.part + ((int64_t)blockIdx.y * p.T + t) * p.H + n, own(o), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        sync_lds();
+        if (tid == 0) {
+            const int before = __hip_atomic_fetch_add(p.done + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sh_last = before == p.parts - 1;
+            if (sh_last)
+                __hip_atomic_store(p.done + blockIdx.x, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        sync_lds();
+        if (!sh_last)
+            return;
+    }
+    for (int o = tid; o < p.T * cols; o += THREADS) {
+        const int t = o / cols, n = nw + o % cols;
         if (n >= p.H)
             continue;
-        float v = acc_all[o];
-#pragma unroll
-        for (int w = 1; w < kDownWaves; ++w)
-            v += acc_all[w * MT * 256 + o];
+        float v = 0.0f;
+        if (shared) {
+#pragma unroll 8
+            for (int q = 0; q < p.parts; ++q)
+                v += __hip_atomic_load(p.part + ((int64_t)q * p.T + t) * p.H + n, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+        } else {
+            v = own(o);
+        }
         if (p.out16)
             ((uint16_t *)p.y)[(int64_t)t * p.ldy + n] = from_float<DT>(v);
         else
