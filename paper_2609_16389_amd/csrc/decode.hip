@@ -131,7 +131,8 @@ void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
     using namespace xexperts_dev;
     if (p.slots > 0)
-        hipLaunchKernelGGL((route_up<DT, R, PL>), dim3(cdiv(p.I, 16), p.slots), dim3(kUpThreads), 0, s, p);
+        hipLaunchKernelGGL((route_up<DT, R, PL, R <= 16 ? 1 : 4, R <= 16 ? 8 : 1>),
+                           dim3(cdiv(p.I, R <= 16 ? 16 : 64), p.slots), dim3(R <= 16 ? 512 : 256), 0, s, p);
     const dim3 grid(cdiv(p.H, 16 * WN), p.parts), block(64 * WN * WK);
     if (p.I % 8 == 0)
         hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, false>), grid, block, 0, s, p);
@@ -185,7 +186,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
         return XGEMM_ERR_INVALID_ARG;
     // (2 I rows of up; the inner dimension padded stays below 2^31)
     if (!dims_ok(T, H, ldx) || !dims_ok(T, E, lds) || !dims_ok(T, H, ldy) || I < 0 || I > kMaxDim / 4 ||
-        !dims_ok(2 * I, H, ldu) || !dims_ok(H, I, ldd) || su < 0 || sd < 0 || H > kMaxDim - 2 * kUpUnit * kUpWaves)
+        !dims_ok(2 * I, H, ldu) || !dims_ok(H, I, ldd) || su < 0 || sd < 0 || H > kMaxDim - 16 * kUpUnit)
         return XGEMM_ERR_INVALID_ARG;
     if ((double)E * (double)su > 9.0e18 || (double)E * (double)sd > 9.0e18)
         return XGEMM_ERR_INVALID_ARG;

@@ -14,12 +14,13 @@
 // token s / top, left empty when an earlier token has chosen that expert too;
 // with many, slot s is expert s, left empty when nobody has.
 //
-// First launch (route_up): one workgroup a slot and 16 of the inner columns.
-// It works out its slot from the scores by itself (a comparison of every
-// score with the expert's own, per token, which costs less than a launch),
-// then forms 16 gate and 16 up columns for the slot's tokens, the waves
-// splitting the hidden dimension, and writes h.  The first workgroup of a
-// slot also writes the slot's tokens and weights.
+// First launch (route_up): one workgroup a slot and 16 or 64 of the inner
+// columns.  It works out its slot from the scores by itself (a comparison of
+// every score with the expert's own, per token, which costs less than a
+// launch), then forms its gate and up columns for the slot's tokens, 16 of
+// each a wave, and writes h.  With up to 16 tokens its waves split the hidden
+// dimension, with more they take columns and share x through LDS.  The first
+// workgroup of a slot also writes the slot's tokens and weights.
 // Second launch (down_sum): the slots' inner dimensions, one after the other in
 // units of 64, are cut into even ranges; a range forms its part of 16 columns
 // of y a wave, for every token, in LDS.  With one or two tokens the waves of a
@@ -55,7 +56,6 @@ using namespace xdecode_dev;
 constexpr int kMaxTokens = 64;    // tokens of a launch
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxTop = 32;
-constexpr int kUpWaves = 8, kUpThreads = 64 * kUpWaves;
 constexpr int kUpUnit = 128;      // k per unit of a wave in the first product
 constexpr int kDownUnit = 64;     // and in the second
 constexpr int kPad = kDownUnit;   // inner columns of h are padded to this
@@ -137,23 +137,26 @@ __device__ __forceinline__ void sync_lds()
 }
 
 // R: rows of a slot that the launch provides for (2, or a multiple of 16); PL:
-// parts of h.
-template <int DT, int R, int PL>
-__global__ void __launch_bounds__(kUpThreads, R <= 16 ? 4 : 2)
+// parts of h; WN waves take 16 columns each, or (WN == 1) WK waves a range of k
+// each.
+template <int DT, int R, int PL, int WN, int WK>
+__global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : 3)
 route_up(ExpertsParams p)
 {
-    constexpr int MTS = (R + 15) / 16;
+    static_assert(WN == 1 || WK == 1, "a barrier is the whole workgroup's");
+    constexpr int MTS = (R + 15) / 16, THREADS = 64 * WN * WK, BUFS = WN == 1 ? 1 : 2;
     __shared__ __attribute__((aligned(16))) union {
         uint32_t key[kMaxExperts];
-        char x[kUpWaves][unit_bytes<R>(kUpUnit)];
-        float red[kUpWaves * MTS * 512];
+        char x[WK][BUFS][unit_bytes<R>(kUpUnit)];
+        float red[WK > 1 ? WK * MTS * 512 : 1];
     } sh;
     __shared__ int sh_expert, sh_count, sh_first;
     __shared__ uint8_t sh_rank[kMaxTokens];
     __shared__ uint16_t sh_pair[kMaxTokens];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int slot = blockIdx.y, i0 = 16 * blockIdx.x;
+    const int wn = wave % WN, wk = wave / WN;
+    const int slot = blockIdx.y, i0 = 16 * (WN * blockIdx.x + wn);
 
     // the slot's expert: the one of rank j among its token's scores
     const bool by_choice = p.slots < p.E;
@@ -161,13 +164,13 @@ route_up(ExpertsParams p)
     if (by_choice) {
         const int j = slot - t0 * p.top;
         const float *const row = p.scores + t0 * p.lds;
-        for (int e = tid; e < p.E; e += kUpThreads)
+        for (int e = tid; e < p.E; e += THREADS)
             sh.key[e] = order_of(row[e]);
         __syncthreads();
         int per = 32;   // lanes an expert
-        while (per > 1 && kUpThreads / per < p.E)
+        while (per > 1 && THREADS / per < p.E)
             per /= 2;
-        for (int e0 = 0; e0 < p.E; e0 += kUpThreads / per) {
+        for (int e0 = 0; e0 < p.E; e0 += THREADS / per) {
             const int e = e0 + tid / per;
             const uint32_t mine = sh.key[min(e, p.E - 1)];
             int rank = 0;
@@ -182,12 +185,11 @@ route_up(ExpertsParams p)
     }
     const int expert = __builtin_amdgcn_readfirstlane(by_choice ? sh_expert : slot);
 
-    // its rank among each token's scores: `per` lanes a token.  (One token's
-    // slots hold that token.)
-    const bool one = p.T == 1 && by_choice;
-    if (!one || blockIdx.x == 0) {
+    // its rank among each token's scores, `per` lanes a token, and, for the
+    // first workgroup of a slot, its weight
+    auto ranks = [&](bool weigh) {
         int per = 64;
-        while (per > 8 && kUpThreads / per < p.T)
+        while (per > THREADS / kMaxTokens && THREADS / per < p.T)
             per /= 2;
         const int tok = tid / per, sub = tid & (per - 1);
         const float *const row = p.scores + (int64_t)min(tok, p.T - 1) * p.lds;
@@ -209,7 +211,7 @@ route_up(ExpertsParams p)
         const bool chosen = rank < p.top && tok < p.T;
         if (tok < kMaxTokens && sub == 0)
             sh_rank[tok] = chosen ? (uint8_t)rank : 255;
-        if (blockIdx.x == 0) {
+        if (weigh) {
             float w = score_exp(own, largest);
             if (!p.renormalize) {
                 float all = 0.0f;
@@ -222,33 +224,47 @@ route_up(ExpertsParams p)
             if (chosen && sub == 0)
                 p.weight[tok * p.top + rank] = w;
         }
-    } else if (tid == 0) {
-        sh_rank[0] = (uint8_t)slot;
-    }
-    __syncthreads();
-    if (wave == 0) {
-        const int rank = lane < p.T ? sh_rank[lane] : 255;
-        const uint64_t mask = __ballot(rank != 255);
-        if (rank != 255)
-            sh_pair[__popcll(mask & ((1ull << lane) - 1))] = (uint16_t)(lane * p.top + rank);
-        if (lane == 0) {
-            sh_count = __popcll(mask);
-            sh_first = mask ? __builtin_ctzll(mask) : -1;
-        }
-    }
-    __syncthreads();
-    const int count = __builtin_amdgcn_readfirstlane(sh_count);
-    const bool empty = count == 0 || (by_choice && sh_first != t0);
-    if (blockIdx.x == 0) {
+    };
+    // (one token's slots hold that token: its weights can wait)
+    const bool one = p.T == 1 && by_choice;
+    int count = 1;
+    if (one) {
         if (tid == 0) {
-            p.expert[slot] = empty ? -1 : expert;
-            p.count[slot] = count;
+            sh_pair[0] = (uint16_t)slot;
+            if (blockIdx.x == 0) {
+                p.expert[slot] = expert;
+                p.count[slot] = 1;
+                p.pair[slot * kMaxTokens] = (uint16_t)slot;
+            }
         }
-        if (tid < count)
-            p.pair[slot * kMaxTokens + tid] = sh_pair[tid];
+        __syncthreads();
+    } else {
+        ranks(blockIdx.x == 0);
+        __syncthreads();
+        if (wave == 0) {
+            const int rank = lane < p.T ? sh_rank[lane] : 255;
+            const uint64_t mask = __ballot(rank != 255);
+            if (rank != 255)
+                sh_pair[__popcll(mask & ((1ull << lane) - 1))] = (uint16_t)(lane * p.top + rank);
+            if (lane == 0) {
+                sh_count = __popcll(mask);
+                sh_first = mask ? __builtin_ctzll(mask) : -1;
+            }
+        }
+        __syncthreads();
+        count = __builtin_amdgcn_readfirstlane(sh_count);
+        const bool empty = count == 0 || (by_choice && sh_first != t0);
+        if (blockIdx.x == 0) {
+            if (tid == 0) {
+                p.expert[slot] = empty ? -1 : expert;
+                p.count[slot] = count;
+            }
+            if (tid < count)
+                p.pair[slot * kMaxTokens + tid] = sh_pair[tid];
+        }
+        if (empty)
+            return;
     }
-    if (empty)
-        return;
 
     const int c = lane & 15, g = lane >> 4;
     const uint16_t *wrow[2];
@@ -259,13 +275,12 @@ route_up(ExpertsParams p)
 
     // the products for up to RB rows
     auto body = [&]<int RB>() {
-        constexpr int MT = (RB + 15) / 16, NP = RB * 16 > 64 ? RB * 16 / 64 : 1;
-        char *const xs = sh.x[wave];
+        constexpr int MT = (RB + 15) / 16, NP = RB * 16 > 64 * WN ? RB * 16 / (64 * WN) : 1;
         const uint16_t *xrow[NP];
         int xdst[NP];
 #pragma unroll
         for (int q = 0; q < NP; ++q) {
-            const int row = (lane >> 4) + 4 * q, kc = lane & 15;
+            const int row = (wn * 64 + lane) / 16 + 4 * WN * q, kc = lane & 15;
             const int r = min(row, RB - 1);
             xrow[q] = p.x + (int64_t)(sh_pair[min(r, count - 1)] / p.top) * p.ldx + 8 * kc;
             xdst[q] = place<RB>(r, kc);
@@ -277,12 +292,13 @@ route_up(ExpertsParams p)
             for (int v = 0; v < 2; ++v)
                 acc[i][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         u32x4 w[2][4][2], xr[NP];
-        auto store_x = [&] {
+        auto store_x = [&](int buf) {
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                *(u32x4 *)(xs + xdst[q]) = xr[q];
+                *(u32x4 *)(sh.x[wk][buf] + xdst[q]) = xr[q];
         };
-        auto compute = [&](const u32x4 (&from)[4][2]) {
+        auto compute = [&](const u32x4 (&from)[4][2], int buf) {
+            const char *const xs = sh.x[wk][buf];
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -295,8 +311,7 @@ route_up(ExpertsParams p)
         };
         // this wave's whole units
         const int units = p.H / kUpUnit;
-        const int u0 = wave * (units / kUpWaves) + min(wave, units % kUpWaves);
-        const int mine = units / kUpWaves + (wave < units % kUpWaves);
+        const int u0 = wk * (units / WK) + min(wk, units % WK), mine = units / WK + (wk < units % WK);
         auto load_x = [&](int t) {
             const int k = (u0 + min(t, mine - 1)) * kUpUnit;
 #pragma unroll
@@ -316,9 +331,12 @@ route_up(ExpertsParams p)
             load_w(w[0], 0);
             load_w(w[1], 1);
             auto step = [&]<int B>(int t) {
-                store_x();
+                constexpr int buf = BUFS == 1 ? 0 : B;
+                store_x(buf);
                 load_x(t + 1);
-                compute(w[B]);
+                if (WN > 1)
+                    sync_lds();
+                compute(w[B], buf);
                 load_w(w[B], t + 2);
             };
             for (int t = 0;;) {
@@ -330,8 +348,8 @@ route_up(ExpertsParams p)
                     break;
             }
         }
-        // what is left of the rows, by the last wave (x is zero past H)
-        if (units * kUpUnit < p.H && wave == kUpWaves - 1) {
+        // what is left of the rows, by the last range (x is zero past H)
+        if (units * kUpUnit < p.H && wk == WK - 1) {
             const int64_t k = (int64_t)units * kUpUnit;
 #pragma unroll
             for (int q = 0; q < NP; ++q)
@@ -341,11 +359,33 @@ route_up(ExpertsParams p)
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
                     w[0][d][v] = load16_end(wrow[v] - 8 * g, 2 * (k + 32 * d + 8 * g), 2 * (int64_t)p.H);
-            store_x();
-            compute(w[0]);
+            if (WN > 1)
+                sync_lds();   // (the first buffer may still be read)
+            store_x(0);
+            if (WN > 1)
+                sync_lds();
+            compute(w[0], 0);
         }
+        // h of row m (of the slot) and column col from its two sums
+        auto finish = [&](int m, int col, float gate, float lift) {
+            uint16_t part[PL] = {};
+            if (col < p.I)
+                split_parts<DT>(gate / (1.0f + expf(-gate)) * lift, part);
+            uint16_t *const at = p.h + (int64_t)sh_pair[m] * p.Ip + col;
+#pragma unroll
+            for (int q = 0; q < PL; ++q)
+                at[q * plane] = part[q];
+        };
+        if constexpr (WK == 1) {
+            // (columns up to the padded size: 64 a workgroup)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * i + 4 * g + r < count)
+                        finish(16 * i + 4 * g + r, i0 + c, acc[i][0][r], acc[i][1][r]);
+        } else {
         sync_lds();   // (x is done with)
-
         // the waves' blocks, added in ascending order
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -355,7 +395,7 @@ route_up(ExpertsParams p)
                 for (int r = 0; r < 4; ++r)
                     sh.red[((wave * MT + i) * 2 + v) * 256 + 64 * r + lane] = acc[i][v][r];
         sync_lds();
-        for (int o = tid; o < MT * 256; o += kUpThreads) {
+        for (int o = tid; o < MT * 256; o += THREADS) {
             const int i = o >> 8, r = o >> 6 & 3, l = o & 63;
             const int m = 16 * i + 4 * (l >> 4) + r, col = i0 + (l & 15);
             if (m >= count)
@@ -365,34 +405,31 @@ route_up(ExpertsParams p)
             for (int v = 0; v < 2; ++v) {
                 sum[v] = sh.red[(i * 2 + v) * 256 + (o & 255)];
 #pragma unroll
-                for (int w = 1; w < kUpWaves; ++w)
+                for (int w = 1; w < WK; ++w)
                     sum[v] += sh.red[((w * MT + i) * 2 + v) * 256 + (o & 255)];
             }
-            uint16_t part[PL] = {};
-            if (col < p.I)
-                split_parts<DT>(sum[0] / (1.0f + expf(-sum[0])) * sum[1], part);
-            uint16_t *const at = p.h + (int64_t)sh_pair[m] * p.Ip + col;
-#pragma unroll
-            for (int q = 0; q < PL; ++q)
-                at[q * plane] = part[q];
+            finish(m, col, sum[0], sum[1]);
             // the last workgroup also clears the padding past its columns
             if (blockIdx.x == gridDim.x - 1)
-                for (int past = 16; col + past < p.Ip; past += 16)
-#pragma unroll
-                    for (int q = 0; q < PL; ++q)
-                        at[q * plane + past] = 0;
+                for (int past = col + 16; past < p.Ip; past += 16)
+                    finish(m, past, 0.0f, 0.0f);
+        }
         }
     };
-    if constexpr (R <= 16) {
+    if constexpr (R < 16) {
         body.template operator()<R>();
     } else {
-        if (count <= 16)
+        if (count <= 4)
+            body.template operator()<4>();
+        else if (R == 16 || count <= 16)
             body.template operator()<16>();
-        else if (R == 32 || count <= 32)
-            body.template operator()<32>();
+        else if (R == 32 || (R > 32 && count <= 32))
+            body.template operator()<R < 32 ? R : 32>();
         else
             body.template operator()<R>();
     }
+    if (one && blockIdx.x == 0)
+        ranks(true);
 }
 
 // R, PL: as above.  WN waves take 16 columns each of the same range, or (WN ==
@@ -411,7 +448,8 @@ down_sum(ExpertsParams p)
     __shared__ __attribute__((aligned(16))) char sh_h[WK][BUFS][PL][HB];
     __shared__ float acc_all[WAVES][TOKENS * 16];
     __shared__ float sh_weight[TOKENS * kMaxTop];
-    __shared__ uint16_t sh_slot[kMaxExperts];           // the slots in use, in ascending order:
+    __shared__ uint16_t sh_slot[kMaxExperts];           // the slots in use, in ascending order,
+    __shared__ uint16_t sh_expert[kMaxExperts];         //   their experts,
     __shared__ uint16_t sh_start[kMaxExperts + 1];      //   where their pairs start,
     __shared__ uint16_t sh_pairs[TOKENS * kMaxTop];     //   and the pairs
     __shared__ int sh_used, sh_last;
@@ -428,9 +466,10 @@ down_sum(ExpertsParams p)
     if (wave == 0) {
         int used = 0, pairs = 0;
         for (int s0 = 0; s0 < p.slots; s0 += 64) {
-            const int s = s0 + lane;
-            const bool on = s < p.slots && p.expert[s] >= 0;
-            const int count = on ? p.count[s] : 0;
+            const int s = s0 + lane, at = min(s, p.slots - 1);
+            const int expert = p.expert[at], listed = p.count[at];
+            const bool on = s < p.slots && expert >= 0;
+            const int count = on ? listed : 0;
             const uint64_t mask = __ballot(on);
             int before = count;
             for (int d = 1; d < 64; d *= 2) {
@@ -440,6 +479,7 @@ down_sum(ExpertsParams p)
             if (on) {
                 const int at = used + __popcll(mask & ((1ull << lane) - 1));
                 sh_slot[at] = (uint16_t)s;
+                sh_expert[at] = (uint16_t)expert;
                 sh_start[at] = (uint16_t)(pairs + before - count);
             }
             used += __popcll(mask);
@@ -464,8 +504,8 @@ down_sum(ExpertsParams p)
     const int used = __builtin_amdgcn_readfirstlane(sh_used);
     for (int a = wave; a < used; a += WAVES) {
         const int start = sh_start[a], count = sh_start[a + 1] - start;
-        if (lane < count)
-            sh_pairs[start + lane] = p.pair[sh_slot[a] * kMaxTokens + lane];
+        if (lane < count)   // (one token's slots are its choices)
+            sh_pairs[start + lane] = p.T == 1 && p.slots < p.E ? sh_slot[a] : p.pair[sh_slot[a] * kMaxTokens + lane];
     }
     sync_lds();
 
@@ -481,7 +521,7 @@ down_sum(ExpertsParams p)
         constexpr int MT = (RB + 15) / 16, PIECES = RB * 8 * PL;
         constexpr int NP = (PIECES + 64 * WN - 1) / (64 * WN);
         const int start = sh_start[a], count = sh_start[a + 1] - start;
-        const int expert = p.expert[sh_slot[a]];
+        const int expert = __builtin_amdgcn_readfirstlane(sh_expert[a]);
         const uint16_t *const wrow =
             p.down + (int64_t)expert * p.sd + (int64_t)min(n0 + c, p.H - 1) * p.ldd;
         const uint16_t *hrow[NP];
@@ -572,14 +612,16 @@ down_sum(ExpertsParams p)
         const int a = __builtin_amdgcn_readfirstlane((int)(u / chunks));
         const int first = __builtin_amdgcn_readfirstlane((int)(u % chunks));
         const int len = (int)min((int64_t)(chunks - first), u_end - u);
-        if constexpr (R <= 16) {
+        if constexpr (R < 16) {
             segment.template operator()<R>(a, first, len);
         } else {
-            const int count = sh_start[a + 1] - sh_start[a];
-            if (count <= 16)
+            const int count = __builtin_amdgcn_readfirstlane(sh_start[a + 1] - sh_start[a]);
+            if (count <= 4)
+                segment.template operator()<4>(a, first, len);
+            else if (R == 16 || count <= 16)
                 segment.template operator()<16>(a, first, len);
-            else if (R == 32 || count <= 32)
-                segment.template operator()<32>(a, first, len);
+            else if (R == 32 || (R > 32 && count <= 32))
+                segment.template operator()<R < 32 ? R : 32>(a, first, len);
             else
                 segment.template operator()<R>(a, first, len);
         }
