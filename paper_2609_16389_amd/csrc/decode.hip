@@ -126,52 +126,73 @@ int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int6
 
 using xexperts_dev::ExpertsParams;
 
-template <int DT, int R, int PL, int WN, int WK>
+// R: tokens the launch provides for; UN x UK and WN x WK: waves over columns
+// and over k in the two launches.
+template <int DT, int R, int PL, int UN, int UK, int WN, int WK>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
     using namespace xexperts_dev;
     if (p.slots > 0)
-        hipLaunchKernelGGL((route_up<DT, R, PL, R <= 16 ? 1 : 4, R <= 16 ? 8 : 1>),
-                           dim3(cdiv(p.I, R <= 16 ? 16 : 64), p.slots), dim3(R <= 16 ? 512 : 256), 0, s, p);
+        hipLaunchKernelGGL((route_up<DT, R, PL, UN, UK>), dim3(cdiv(p.I, 16 * UN), p.slots), dim3(64 * UN * UK), 0, s,
+                           p);
     const dim3 grid(cdiv(p.H, 16 * WN), p.parts), block(64 * WN * WK);
     if (p.I % 8 == 0)
-        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, false>), grid, block, 0, s, p);
-    else if constexpr (PL == 3)   // (see experts_h_parts)
-        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, true>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 0>), grid, block, 0, s, p);
+    else if constexpr (PL == 3) {   // (see experts_h_parts)
+        if (p.I > 8)
+            hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 1>), grid, block, 0, s, p);
+        else if constexpr (R == 64)
+            hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 2>), grid, block, 0, s, p);
+    }
 }
 
 // 16-bit parts that h is kept in: two suffice for a 16-bit output (ragged rows
 // are built with three only)
 int experts_h_parts(bool out16, int64_t I) { return out16 && I % 8 == 0 ? 2 : 3; }
 
-// Columns of y a workgroup of the second launch takes.
-int experts_columns(int64_t T) { return T <= 2 ? 16 : 64; }
+// Whether the waves of a workgroup of the second launch take ranges of their
+// own (16 columns, all the tokens' h) or columns of the same range (64).
+// (16 tokens, 6 of 64 experts of 2048 x 1408: 219 us with ranges of their own
+// against 212; 7 tokens, 3 of 13 of 1000 x 776: 25 against 31.)
+bool experts_own_ranges(int64_t T, int64_t top, int64_t I)
+{
+    return I >= 8 && (T <= 2 || (T <= 16 && T * top <= 32));
+}
 
-// Parts that the second launch cuts the slots' inner dimensions into: four
-// workgroups a CU (one where their waves take ranges of their own), parts of at
-// least four units (16 for eight waves), and counters for the workgroups of a
-// part.
-int experts_parts(int64_t T, int64_t H, int64_t slots, int64_t Ip, int cu_count)
+// Parts that the second launch cuts the slots' inner dimensions into, of at
+// least four units a wave, with a counter for the workgroups of each: four
+// workgroups a CU; with waves on ranges of their own only where the columns
+// give few workgroups.
+int experts_parts(int64_t T, int64_t top, int64_t H, int64_t I, int64_t slots, int64_t Ip, int cu_count)
 {
     using namespace xexperts_dev;
-    const int64_t blocks = cdiv(H, experts_columns(T)), units = slots * (Ip / kDownUnit);
+    const bool own = experts_own_ranges(T, top, I);
+    const int waves = T <= 2 ? 16 : 8;
+    const int64_t blocks = cdiv(H, own ? 16 : 64), units = slots * (Ip / kDownUnit);
     if (blocks > (int64_t)(xgemm_host::kWsPrefix / sizeof(int)))
         return 1;
-    const int64_t want = T <= 2 ? cdiv((int64_t)cu_count, blocks) : cdiv(4 * (int64_t)cu_count, blocks);
-    return (int)std::max<int64_t>(1, std::min({want, units / (T <= 2 ? 16 : 4), (int64_t)kMaxParts}));
+    const int64_t want = !own ? cdiv(4 * (int64_t)cu_count, blocks)
+                       : T > 2 ? cdiv((int64_t)cu_count, blocks)
+                               : blocks * 4 < cu_count ? cdiv((int64_t)cu_count / 2, blocks) : 1;
+    return (int)std::max<int64_t>(1, std::min({want, units / (own ? 4 * waves : 4), (int64_t)kMaxParts}));
 }
 
 template <int DT, int PL>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
-    if (p.T <= 2)
-        launch_experts<DT, 2, PL, 1, 8>(p, s);
+    // (the few inner columns below 8 are built for 64 tokens only)
+    if (p.I < 8)
+        launch_experts<DT, 64, PL, 4, 1, 4, 1>(p, s);
+    else if (p.T <= 2)
+        launch_experts<DT, 2, PL, 1, 8, 1, 16>(p, s);
+    else if (experts_own_ranges(p.T, p.top, p.I))
+        launch_experts<DT, 16, PL, 1, 4, 1, 8>(p, s);
     else if (p.T <= 16)
-        launch_experts<DT, 16, PL, 4, 1>(p, s);
+        launch_experts<DT, 16, PL, 1, 4, 4, 1>(p, s);
     else if (p.T <= 32)
-        launch_experts<DT, 32, PL, 4, 1>(p, s);
+        launch_experts<DT, 32, PL, 4, 1, 4, 1>(p, s);
     else
-        launch_experts<DT, 64, PL, 4, 1>(p, s);
+        launch_experts<DT, 64, PL, 4, 1, 4, 1>(p, s);
 }
 
 int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int64_t I, const void *x, int64_t ldx,
@@ -243,7 +264,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     for (int64_t t = 0; t < T; t += kMaxTokens) {
         p.T = (int)std::min<int64_t>(kMaxTokens, T - t);
         p.slots = I > 0 ? (int)std::min<int64_t>(p.T * top, E) : 0;   // (without inner columns y is zero)
-        p.parts = experts_parts(p.T, H, p.slots, p.Ip, h->cu_count);
+        p.parts = experts_parts(p.T, top, H, I, p.slots, p.Ip, h->cu_count);
         p.x = (const uint16_t *)x + t * ldx;
         p.scores = scores + t * lds;
         p.y = (char *)y + t * ldy * (p.out16 ? 2 : 4);

@@ -56,8 +56,10 @@ using namespace xdecode_dev;
 constexpr int kMaxTokens = 64;    // tokens of a launch
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxTop = 32;
-constexpr int kUpUnit = 128;      // k per unit of a wave in the first product
-constexpr int kDownUnit = 64;     // and in the second
+// k per unit of a wave.  (128 in the first product: 16 tokens, 6 of 64 experts
+// of 2048 x 1408 212 us against 190: the registers of two units then leave two
+// workgroups a CU.)
+constexpr int kUpUnit = 64, kDownUnit = 64;
 constexpr int kPad = kDownUnit;   // inner columns of h are padded to this
 constexpr int kMaxParts = 32;     // ranges of the second product that workgroups take
 
@@ -275,12 +277,13 @@ route_up(ExpertsParams p)
 
     // the products for up to RB rows
     auto body = [&]<int RB>() {
-        constexpr int MT = (RB + 15) / 16, NP = RB * 16 > 64 * WN ? RB * 16 / (64 * WN) : 1;
+        constexpr int MT = (RB + 15) / 16, D = kUpUnit / 32, PR = kUpUnit / 8;   // pieces of 8 k of a row
+        constexpr int NP = RB * PR > 64 * WN ? RB * PR / (64 * WN) : 1;
         const uint16_t *xrow[NP];
         int xdst[NP];
 #pragma unroll
         for (int q = 0; q < NP; ++q) {
-            const int row = (wn * 64 + lane) / 16 + 4 * WN * q, kc = lane & 15;
+            const int row = (wn * 64 + lane) / PR + 64 / PR * WN * q, kc = lane % PR;
             const int r = min(row, RB - 1);
             xrow[q] = p.x + (int64_t)(sh_pair[min(r, count - 1)] / p.top) * p.ldx + 8 * kc;
             xdst[q] = place<RB>(r, kc);
@@ -291,16 +294,16 @@ route_up(ExpertsParams p)
 #pragma unroll
             for (int v = 0; v < 2; ++v)
                 acc[i][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        u32x4 w[2][4][2], xr[NP];
+        u32x4 w[2][D][2], xr[NP];
         auto store_x = [&](int buf) {
 #pragma unroll
             for (int q = 0; q < NP; ++q)
                 *(u32x4 *)(sh.x[wk][buf] + xdst[q]) = xr[q];
         };
-        auto compute = [&](const u32x4 (&from)[4][2], int buf) {
+        auto compute = [&](const u32x4 (&from)[D][2], int buf) {
             const char *const xs = sh.x[wk][buf];
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < D; ++d)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     const u32x4 a = *(const u32x4 *)(xs + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
@@ -318,12 +321,12 @@ route_up(ExpertsParams p)
             for (int q = 0; q < NP; ++q)
                 xr[q] = load_any<u32x4>(xrow[q] + k);
         };
-        auto load_w = [&](u32x4 (&to)[4][2], int t) {
+        auto load_w = [&](u32x4 (&to)[D][2], int t) {
             const int k = (u0 + min(t, mine - 1)) * kUpUnit;
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+                for (int d = 0; d < D; ++d)
                     to[d][v] = load_any<u32x4>(wrow[v] + k + 32 * d);
         };
         if (mine > 0) {
@@ -353,11 +356,11 @@ route_up(ExpertsParams p)
             const int64_t k = (int64_t)units * kUpUnit;
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                xr[q] = load16_end(xrow[q] - 8 * (lane & 15), 2 * (k + 8 * (lane & 15)), 2 * (int64_t)p.H);
+                xr[q] = load16_end(xrow[q] - 8 * (lane % PR), 2 * (k + 8 * (lane % PR)), 2 * (int64_t)p.H);
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+                for (int d = 0; d < D; ++d)
                     w[0][d][v] = load16_end(wrow[v] - 8 * g, 2 * (k + 32 * d + 8 * g), 2 * (int64_t)p.H);
             if (WN > 1)
                 sync_lds();   // (the first buffer may still be read)
@@ -433,10 +436,10 @@ route_up(ExpertsParams p)
 }
 
 // R, PL: as above.  WN waves take 16 columns each of the same range, or (WN ==
-// 1) WK waves a range each.  RAGGED: I is no multiple of 8, so that pieces of
-// rows end inside; otherwise a piece past I is the row's last one again (h is
-// zero there).
-template <int DT, int R, int PL, int WN, int WK, bool RAGGED>
+// 1) WK waves a range each.  END: 0 for I a multiple of 8, where a piece of a row
+// past I is the row's last one again (h is zero there); 1: a piece that ends
+// inside is the row's last 8, moved into place; 2: for I below 8.
+template <int DT, int R, int PL, int WN, int WK, int END>
 __global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : R == 32 ? 2 : 1)
 down_sum(ExpertsParams p)
 {
@@ -551,7 +554,7 @@ down_sum(ExpertsParams p)
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
                 const int at = k + 32 * d + 8 * g;
-                if constexpr (RAGGED)
+                if constexpr (END == 2)
                     to[d] = load16_end(wrow, 2 * (int64_t)at, 2 * (int64_t)p.I);
                 else
                     to[d] = load_any<u32x4>(wrow + min(at, p.I - 8));
@@ -568,6 +571,12 @@ down_sum(ExpertsParams p)
             load_h(t + 1);
             if (WN > 1)
                 sync_lds();
+            if (END == 1 && first + t == chunks - 1)
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const int at = (chunks - 1) * kDownUnit + 32 * d + 8 * g;
+                    w[B][d] = shift_down(w[B][d], 2 * min(max(at - (p.I - 8), 0), 8));
+                }
 #pragma unroll
             for (int d = 0; d < 2; ++d)
 #pragma unroll
