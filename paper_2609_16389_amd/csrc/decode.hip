@@ -327,12 +327,12 @@ int run_logprob(xgemm_ctx *h, int64_t R, int64_t V, const void *logits, int64_t 
     p.ld = ldl;
     p.V = (int)V;
     p.top = (int)top;
-    // few rows are cut into parts of at least half a batch a wave, for two
-    // workgroups a CU
-    constexpr int64_t kPart = kWaves * kBatch / 2;
+    // few rows are cut into parts of at least a batch a wave, for two workgroups
+    // a CU
+    constexpr int64_t kPart = kWaves * kBatch;
     int64_t parts = std::min({2 * (int64_t)h->cu_count / R, cdiv(V, kPart), (int64_t)kMaxParts});
     parts = std::max<int64_t>(parts, 1);
-    p.part_len = (int)(cdiv(cdiv(V, parts), 64) * 64);
+    p.part_len = (int)(cdiv(cdiv(V, parts), kBatch) * kBatch);   // (only the last part ends inside a batch)
     p.parts = (int)cdiv(V, p.part_len);
     p.stat = nullptr;
     p.best = nullptr;

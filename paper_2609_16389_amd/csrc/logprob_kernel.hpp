@@ -5,20 +5,30 @@
 //     lse = m + log S    logprob = (x[target] - m) - log S    entropy = log S - U / S
 //
 // One pass over the row: every lane keeps m, S and U of its own values and
-// rescales S and U when m grows:  with d = m_old - m_new,
+// rescales S and U when m grows: with d = m_old - m_new,
 //     U' = exp(d) (U + d S)    S' = exp(d) S.
 // The same rule joins lanes, waves and, where few rows would leave CUs idle,
 // the parts of a row that several workgroups take (the last one to finish
-// joins them, in the order of the parts, whichever it is).
+// joins them, in the order of the parts, whichever it is).  (exp is 2^(t log2 e)
+// of the difference t: folding the factor into one fused multiply-add, 2^(x log2
+// e - r), saves an instruction of eleven a value, but a row of one certain
+// token then no longer has an entropy of exactly 0, and the lowest values of
+// fp32 and bfloat16, which masks are made of, overflow.)
 //
 // The alternatives come from the same pass.  A wave sets aside values that may
-// be among the row's n largest: at least n values are as large as the least
-// over the waves of the ceil(n / 8)-th largest of a wave's lane maxima so far,
-// so nothing below that bound is kept; the bound is renewed after 1, 2, 4, ...
-// batches.  What is kept lies in a buffer of 128 a wave, cut back to the n
+// be among the row's n largest: with w waves that have whole batches, at least
+// n values are as large as the least over them of the ceil(n / w)-th largest of
+// a wave's lane maxima so far, so nothing below that bound is kept; the bound is
+// renewed after 1, 2, 4, ... batches.  What is kept lies in a buffer of 128 a wave, cut back to the n
 // largest when it would run over.  Values are ordered by (value, lower index
 // first) as one 64-bit number, so the result does not depend on who found
 // what first.
+//
+// What bounds it: some ten instructions a value (a 2^x counts for four) beside
+// its two or four bytes, and with few rows the chain of latencies from the
+// first load to the last join.  What a call executes once is kept short (code
+// that is not in the instruction cache yet costs more to fetch than to run),
+// so the paths that are seldom taken are loops and not unrolled.
 #pragma once
 
 #include "decode_device.hpp"
@@ -33,7 +43,7 @@ constexpr int kBatch = 64 * kLane;         // values of a wave in a batch
 constexpr int kBuffer = 128;
 constexpr int kMaxTop = 32;
 constexpr int kMaxParts = 64;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -1e30f;          // stands in for -inf where it meets a zero factor
 
 struct Stats {
@@ -54,25 +64,50 @@ struct LogprobParams {
     int *count;       // [rows], zero between launches
 };
 
-// exp(d) for d <= 0 (-inf and the NaN of equal infinities: 0).
-__device__ __forceinline__ float shrink(float d) { return __builtin_amdgcn_exp2f(fmaxf(d, kLowest) * kLog2e); }
-
-__device__ __forceinline__ Stats join(Stats a, Stats b)
+// The largest of the wave's values, and their sum, in all lanes.  Each step
+// takes the value of another lane within a row of 16, then of the rows before
+// (lanes without one: `none`, which changes nothing).
+template <class F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, uint32_t none, F &&f)
 {
-    Stats r;
-    r.m = fmaxf(a.m, b.m);
-    const float da = fmaxf(a.m - r.m, kLowest), db = fmaxf(b.m - r.m, kLowest);
-    const float fa = shrink(da), fb = shrink(db);
-    r.S = a.S * fa + b.S * fb;
-    r.U = fa * fmaf(a.S, da, a.U) + fb * fmaf(b.S, db, b.U);
-    return r;
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x111, 0xf, 0xf, false));  // row_shr 1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x112, 0xf, 0xf, false));  // row_shr 2
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x114, 0xf, 0xf, false));  // row_shr 4
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x118, 0xf, 0xf, false));  // row_shr 8
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x142, 0xa, 0xf, false));  // row_bcast 15
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x143, 0xc, 0xf, false));  // row_bcast 31
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    return wave_reduce(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    const float none = -__builtin_inff();
+    return __builtin_bit_cast(float, wave_reduce(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, none),
+                                                 [](uint32_t a, uint32_t b) {
+                                                     return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+                                                 }));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    return __builtin_bit_cast(float, wave_reduce(__builtin_bit_cast(uint32_t, v), 0u, [](uint32_t a, uint32_t b) {
+                                  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+                              }));
 }
 
+// s with its maximum raised to m (the exponential of -inf and of the NaN of
+// equal infinities: 0).
+__device__ __forceinline__ Stats raise(Stats s, float m)
+{
+    const float d = fmaxf(s.m - m, kLowest), f = __builtin_amdgcn_exp2f(d * kLog2e);
+    return Stats{m, s.S * f, f * fmaf(s.S, d, s.U)};
+}
 __device__ __forceinline__ Stats join_wave(Stats s)
 {
-    for (int d = 1; d < 64; d *= 2)
-        s = join(s, Stats{__shfl_xor(s.m, d, 64), __shfl_xor(s.S, d, 64), __shfl_xor(s.U, d, 64)});
-    return s;
+    s = raise(s, wave_max(s.m));
+    return Stats{s.m, wave_sum(s.S), wave_sum(s.U)};
 }
 
 // A value as a whole number in the same order, the two zeros alike.
@@ -85,8 +120,8 @@ __device__ __forceinline__ float value_of(uint32_t k)
 {
     return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-constexpr uint32_t kOrderNegInf = 0x007fffffu;  // order_of(-inf)
 
+// (never 0: an index is below 2^31)
 __device__ __forceinline__ uint64_t entry_of(uint32_t key, int index)
 {
     return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)index);
@@ -119,186 +154,214 @@ __device__ __forceinline__ int cut_back(uint64_t *buf, int count, int n, int lan
     return min(count, n);
 }
 
-// The waves' buffers to the workgroup's n largest entries in descending
-// order (all threads take part).
-__device__ __forceinline__ int gather(uint64_t (*buf)[kBuffer], int *counts, uint64_t *out, int count, int n, int tid)
+// VEC values of a row from index v as they are in memory.
+template <int DT>
+__device__ __forceinline__ u32x4 load_raw(const void *row, int64_t v)
 {
-    const int lane = tid & 63, wave = tid >> 6;
-    count = cut_back(buf[wave], count, n, lane);
-    if (lane == 0)
-        counts[wave] = count;
-    __syncthreads();
-    int total = 0;
-    for (int w = 0; w < kWaves; ++w)
-        total += counts[w];
-    const int w0 = tid / kMaxTop, i0 = tid % kMaxTop;
-    if (w0 < kWaves && i0 < counts[w0]) {
-        const uint64_t mine = buf[w0][i0];
-        int rank = 0;
-        for (int w = 0; w < kWaves; ++w)
-            for (int i = 0; i < counts[w]; ++i)
-                rank += buf[w][i] > mine;
-        if (rank < n)
-            out[rank] = mine;
-    }
-    __syncthreads();
-    return min(total, n);
+    return load_any<u32x4>((const char *)row + v * (DT == 2 ? 4 : 2));
 }
-
-// VEC values of a row from index v (those at or past `end`: -inf).
 template <int DT, int VEC>
-__device__ __forceinline__ void load_values(const void *row, int v, int end, float (&x)[VEC])
+__device__ __forceinline__ void convert(u32x4 t, float *x)
 {
-    if constexpr (DT == 2) {
-        const float *const q = (const float *)row + v;
-        if (v + VEC <= end) {
-            const f32x4 t = load_any<f32x4>(q);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                x[e] = t[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                x[e] = v + e < end ? q[e] : -__builtin_inff();
-        }
-    } else {
-        const uint16_t *const q = (const uint16_t *)row + v;
-        if (v + VEC <= end) {
-            const u32x4 t = load_any<u32x4>(q);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                x[e] = to_float<DT>((uint16_t)(t[e / 2] >> (16 * (e & 1))));
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                x[e] = v + e < end ? to_float<DT>(q[e]) : -__builtin_inff();
-        }
-    }
+    for (int e = 0; e < VEC; ++e)
+        if constexpr (DT == 2)
+            x[e] = __builtin_bit_cast(f32x4, t)[e];
+        else if constexpr (DT == 0)
+            x[e] = __builtin_bit_cast(float, e & 1 ? t[e / 2] & 0xffff0000u : t[e / 2] << 16);
+        else
+            x[e] = to_float<DT>((uint16_t)(t[e / 2] >> (16 * (e & 1))));
+}
+template <int DT>
+__device__ __forceinline__ float load_value(const void *row, int64_t v)
+{
+    if constexpr (DT == 2)
+        return ((const float *)row)[v];
+    else
+        return to_float<DT>(((const uint16_t *)row)[v]);
 }
 
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 logprob_rows(LogprobParams p)
 {
     constexpr int VEC = DT == 2 ? 4 : 8, UN = kLane / VEC;
     __shared__ uint64_t buf[TOP ? kWaves : 1][kBuffer];
+    __shared__ uint64_t list[TOP ? kMaxParts * kMaxTop : 1];   // candidates of all waves, or of all parts
     __shared__ uint64_t best[kMaxTop];
-    __shared__ int counts[kWaves];
     __shared__ uint32_t bounds[kWaves];
     __shared__ Stats stats[kWaves];
-    __shared__ int sh_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int sh_listed, sh_last;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = p.row0 + blockIdx.y;
     const int part = blockIdx.x;
     const void *const x = (const char *)p.logits + row * p.ld * (DT == 2 ? 4 : 2);
     const int v0 = part * p.part_len, v1 = min(p.V, v0 + p.part_len);
-    const int n = p.top, every = (n + kWaves - 1) / kWaves;
+    const int n = p.top;
+
+    // whole batches, and what is left after them, value by value.  (They start
+    // with the row wherever it lies, so that a result does not depend on its
+    // address.)
+    const int batches = (v1 - v0) / kBatch, rest = v0 + batches * kBatch;
+    const int bounding = max(min(batches, kWaves), 1);   // waves that set a bound (without whole batches: the first)
+    const int every = (n + bounding - 1) / bounding;
+    const int mine = batches > wave ? (batches - 1 - wave) / kWaves + 1 : 0;
 
     Stats s = {-__builtin_inff(), 0.0f, 0.0f};
     float lane_max = -__builtin_inff();
     uint64_t cut = 0;      // nothing at or below it is among this wave's n largest
     int kept = 0;
+    if (tid == 0)
+        sh_listed = 0;
 
-    auto stat_batch = [&](const float (&v)[UN][VEC]) {
-        float most = v[0][0];
+    auto stat_batch = [&](const float (&v)[kLane]) {
+        float most = v[0];
 #pragma unroll
         for (int i = 1; i < kLane; ++i)
-            most = fmaxf(most, v[i / VEC][i % VEC]);
-        const float m = fmaxf(s.m, most);
-        const float d = fmaxf(s.m - m, kLowest), f = shrink(d);
-        s.U = f * fmaf(s.S, d, s.U);
-        s.S *= f;
-        s.m = m;
-        const float ref = m == -__builtin_inff() ? 0.0f : m;
+            most = fmaxf(most, v[i]);
+        s = raise(s, fmaxf(s.m, most));
+        const float ref = s.m == -__builtin_inff() ? 0.0f : s.m;
 #pragma unroll
         for (int i = 0; i < kLane; ++i) {
-            const float t = v[i / VEC][i % VEC] - ref;
-            const float e = __builtin_amdgcn_exp2f(t * kLog2e);
+            const float t = v[i] - ref, e = __builtin_amdgcn_exp2f(t * kLog2e);
             s.S += e;
             s.U = fmaf(e, fmaxf(t, kLowest), s.U);
         }
         lane_max = fmaxf(lane_max, most);
+        return most;
     };
     // this wave's bound: the `every`-th largest of its lanes' maxima
-    auto renew = [&] {
-        uint32_t mine = order_of(lane_max), most = 0;
+    auto renew = [&](bool bounds_any) {
+        if (!bounds_any) {
+            if (lane == 0)
+                *(volatile uint32_t *)&bounds[wave] = 0xffffffffu;
+            return;
+        }
+        uint32_t left = order_of(lane_max), most = 0;
+#pragma unroll 1
         for (int i = 0; i < every; ++i) {
-            most = mine;
-            for (int d = 1; d < 64; d *= 2)
-                most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
-            const uint64_t who = __ballot(mine == most);
+            most = wave_max(left);
+            const uint64_t who = __ballot(left == most);
             if (lane == __builtin_ctzll(who))
-                mine = 0;
+                left = 0;
         }
         if (lane == 0)
             *(volatile uint32_t *)&bounds[wave] = most;
     };
-    auto keep_batch = [&](const float (&v)[UN][VEC], int at) {
-        uint32_t bound = 0xffffffffu;
+    auto least_bound = [&] {
+        uint32_t bound = *(volatile uint32_t *)&bounds[0];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 1; w < kWaves; ++w)
             bound = min(bound, *(volatile uint32_t *)&bounds[w]);
-        bound = max(bound, (uint32_t)(cut >> 32));
+        return bound;
+    };
+    // index(i): place of this lane's value i, or -1
+    auto keep_batch = [&](const float (&v)[kLane], float most, auto index) {
+        uint32_t bound = max(least_bound(), (uint32_t)(cut >> 32));
+        if (!__any(order_of(most) >= bound))
+            return;
+        uint32_t todo = 0;
 #pragma unroll
-        for (int u = 0; u < UN; ++u) {
-            float most = v[u][0];
+        for (int i = 0; i < kLane; ++i)
+            todo |= order_of(v[i]) >= bound && v[i] == v[i] ? 1u << i : 0u;
+#pragma unroll 1
+        while (__any(todo != 0)) {
+            const int i = todo ? __builtin_ctz(todo) : 0;
+            float mine = v[0];
 #pragma unroll
-            for (int e = 1; e < VEC; ++e)
-                most = fmaxf(most, v[u][e]);
-            if (!__any(order_of(most) >= bound || bound <= kOrderNegInf))
-                continue;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const int index = at + 64 * VEC * u + VEC * lane + e;
-                const uint32_t key = order_of(v[u][e]);
-                const uint64_t entry = entry_of(key, index);
-                bool on = index < v1 && v[u][e] == v[u][e] && key >= bound && entry > cut;
-                uint64_t who = __ballot(on);
-                if (who == 0)
-                    continue;
-                if (kept + __popcll(who) > kBuffer) {
-                    kept = cut_back(buf[wave], kept, n, lane);
-                    if (kept == n) {
-                        cut = buf[wave][n - 1];
-                        bound = max(bound, (uint32_t)(cut >> 32));
-                        on = on && entry > cut;
-                        who = __ballot(on);
-                    }
-                }
-                if (on)
-                    buf[wave][kept + __popcll(who & ((1ull << lane) - 1))] = entry;
-                kept += __popcll(who);
+            for (int j = 1; j < kLane; ++j)
+                mine = i == j ? v[j] : mine;
+            const int at = index(i);
+            const uint64_t entry = entry_of(order_of(mine), at);
+            bool on = todo != 0 && at >= 0 && entry > cut;
+            todo &= todo - 1;
+            uint64_t who = __ballot(on);
+            if (kept + __popcll(who) > kBuffer) {
+                kept = __builtin_amdgcn_readfirstlane(cut_back(buf[wave], kept, n, lane));
+                if (kept == n)
+                    cut = buf[wave][n - 1];
+                on = on && entry > cut;
+                who = __ballot(on);
             }
+            if (on)
+                buf[wave][kept + __popcll(who & ((1ull << lane) - 1))] = entry;
+            kept += __popcll(who);
         }
     };
-    auto load_batch = [&](float (&v)[UN][VEC], int at) {
-#pragma unroll
-        for (int u = 0; u < UN; ++u)
-            load_values<DT, VEC>(x, at + 64 * VEC * u + VEC * lane, v1, v[u]);
+    // place a wave's candidates (on) in the list
+    auto add_to_list = [&](bool on, uint64_t entry) {
+        const uint64_t who = __ballot(on);
+        int base = 0;
+        if (lane == 0 && who)
+            base = atomicAdd(&sh_listed, __popcll(who));
+        base = __builtin_amdgcn_readfirstlane(base);
+        if (on)
+            list[base + __popcll(who & ((1ull << lane) - 1))] = entry;
+    };
+    // the n largest of the list, in descending order
+    auto rank_list = [&] {
+        const int listed = sh_listed;
+        for (int t = tid; t < listed; t += kThreads) {
+            const uint64_t entry = list[t];
+            int rank = 0;
+#pragma unroll 4
+            for (int i = 0; i < listed; ++i)
+                rank += list[i] > entry;
+            if (rank < n)
+                best[rank] = entry;
+        }
+        __syncthreads();
+        return min(listed, n);
     };
 
-    {
-        // the first batch sets the bounds that its own values are held to
-        float v[UN][VEC];
-        const int at = v0 + wave * kBatch;
-        load_batch(v, at);
-        stat_batch(v);
+    // the wave's whole batches, the next one on its way; the first sets the
+    // bounds that its own values are held to
+    u32x4 raw[UN];
+    auto load_batch = [&](int j) {
+        const int64_t at = v0 + (int64_t)(wave + kWaves * min(j, mine - 1)) * kBatch;
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+            raw[u] = load_raw<DT>(x, at + 64 * VEC * u + VEC * lane);
+    };
+    if (mine > 0)
+        load_batch(0);
+#pragma unroll 1
+    for (int j = 0; j < max(mine, 1); ++j) {
+        float v[kLane];
+        float most = -__builtin_inff();
+        if (mine > 0) {
+#pragma unroll
+            for (int u = 0; u < UN; ++u)
+                convert<DT, VEC>(raw[u], v + VEC * u);
+            load_batch(j + 1);
+            most = stat_batch(v);
+        }
         if constexpr (TOP) {
-            renew();
-            __syncthreads();
-            keep_batch(v, at);
+            if ((j & (j + 1)) == 0)
+                renew(mine > 0);
+            if (j == 0)
+                __syncthreads();
+            if (mine > 0) {
+                const int at = v0 + (wave + kWaves * j) * kBatch + VEC * lane;
+                keep_batch(v, most, [&](int i) { return at + 64 * VEC * (i / VEC) + i % VEC; });
+            }
         }
     }
-    int done = 1;
-    for (int at = v0 + (wave + kWaves) * kBatch; at < v1; at += kWaves * kBatch) {
-        float v[UN][VEC];
-        load_batch(v, at);
-        stat_batch(v);
+    if (wave == batches % kWaves && rest < v1) {
+        const auto index = [&](int i) { return rest + lane + 64 * i < v1 ? rest + lane + 64 * i : -1; };
+        float v[kLane];
+#pragma unroll
+        for (int i = 0; i < kLane; ++i)
+            v[i] = load_value<DT>(x, max(index(i), v0));
+#pragma unroll
+        for (int i = 0; i < kLane; ++i)
+            v[i] = index(i) >= 0 ? v[i] : -__builtin_inff();
+        const float most = stat_batch(v);
         if constexpr (TOP) {
-            ++done;
-            if ((done & (done - 1)) == 0)
-                renew();
-            keep_batch(v, at);
+            if (batches == 0)
+                renew(true);
+            keep_batch(v, most, index);
         }
     }
 
@@ -306,14 +369,24 @@ logprob_rows(LogprobParams p)
     if (lane == 0)
         stats[wave] = s;
     int found = 0;
-    if constexpr (TOP)
-        found = gather(buf, counts, best, kept, n, tid);
-    else
+    if constexpr (TOP) {
+        renew(wave < bounding);
         __syncthreads();
-    s = stats[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w)
-        s = join(s, stats[w]);
+        const uint32_t bound = least_bound();
+        wave_sync();
+        for (int i = lane; i < kBuffer; i += 64) {
+            const uint64_t entry = i < kept ? buf[wave][i] : 0;
+            add_to_list(i < kept && (uint32_t)(entry >> 32) >= bound, entry);
+        }
+        __syncthreads();
+        found = rank_list();
+    } else {
+        __syncthreads();
+    }
+    {
+        Stats q = lane < kWaves ? stats[lane] : Stats{-__builtin_inff(), 0.0f, 0.0f};
+        s = join_wave(q);
+    }
 
     if (p.parts > 1) {
         // publish this part with device-scope stores; once they have
@@ -335,6 +408,7 @@ logprob_rows(LogprobParams p)
                 sh_last = before == p.parts - 1;
                 if (sh_last)
                     __hip_atomic_store(p.count + r, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                sh_listed = 0;
             }
         }
         __syncthreads();
@@ -342,28 +416,29 @@ logprob_rows(LogprobParams p)
             return;
         asm volatile("" ::: "memory");
         Stats q = {-__builtin_inff(), 0.0f, 0.0f};
+        uint64_t least = 0;
         if (lane < p.parts) {
             Stats *const from = p.stat + r * p.parts + lane;
             q.m = __hip_atomic_load(&from->m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             q.S = __hip_atomic_load(&from->S, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             q.U = __hip_atomic_load(&from->U, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (TOP)
+                least = __hip_atomic_load(p.best + (r * p.parts + lane) * n + n - 1, __ATOMIC_RELAXED,
+                                          __HIP_MEMORY_SCOPE_AGENT);
         }
         s = join_wave(q);
         if constexpr (TOP) {
-            kept = 0;
+            // (a part's n-th is below the row's n-th or it)
+            const uint32_t bound = wave_max((uint32_t)(least >> 32));
             for (int q0 = wave; q0 < p.parts; q0 += kWaves) {
                 uint64_t e = 0;
                 if (lane < n)
                     e = __hip_atomic_load(p.best + (r * p.parts + q0) * n + lane, __ATOMIC_RELAXED,
                                           __HIP_MEMORY_SCOPE_AGENT);
-                const uint64_t who = __ballot(e != 0);   // an entry is never 0: its index is below 2^31
-                if (kept + __popcll(who) > kBuffer)
-                    kept = cut_back(buf[wave], kept, n, lane);
-                if (e != 0)
-                    buf[wave][kept + __popcll(who & ((1ull << lane) - 1))] = e;
-                kept += __popcll(who);
+                add_to_list(e != 0 && (uint32_t)(e >> 32) >= bound, e);
             }
-            found = gather(buf, counts, best, kept, n, tid);
+            __syncthreads();
+            found = rank_list();
         }
     }
 
@@ -371,6 +446,7 @@ logprob_rows(LogprobParams p)
         return;
     const float log_S = logf(s.S);
     const bool empty = s.m == -__builtin_inff() && s.S == 0.0f;   // every logit is -inf
+    auto log_of = [&](float v) { return empty ? -__builtin_inff() : (v - s.m) - log_S; };
     if (lane == 0) {
         if (p.lse)
             p.lse[row] = empty ? -__builtin_inff() : s.m + log_S;
@@ -378,25 +454,14 @@ logprob_rows(LogprobParams p)
             p.entropy[row] = empty ? 0.0f : log_S - s.U / s.S;
         if (p.logprob) {
             const int64_t t = p.targets[row];
-            float v = 0.0f;
-            if (t >= p.V)
-                v = __builtin_nanf("");
-            else if (t >= 0) {
-                float xt;
-                if constexpr (DT == 2)
-                    xt = ((const float *)x)[t];
-                else
-                    xt = to_float<DT>(((const uint16_t *)x)[t]);
-                v = empty ? -__builtin_inff() : (xt - s.m) - log_S;
-            }
-            p.logprob[row] = v;
+            p.logprob[row] = t < 0 ? 0.0f : t >= p.V ? __builtin_nanf("") : log_of(load_value<DT>(x, t));
         }
     }
     if (TOP && lane < n) {
         const bool is = lane < found;
         const uint64_t e = is ? best[lane] : 0;
         p.top_id[row * n + lane] = is ? (int64_t)(0xffffffffu - (uint32_t)e) : -1;
-        p.top_logprob[row * n + lane] = !is ? __builtin_nanf("") : empty ? -__builtin_inff() : (value_of((uint32_t)(e >> 32)) - s.m) - log_S;
+        p.top_logprob[row * n + lane] = is ? log_of(value_of((uint32_t)(e >> 32))) : __builtin_nanf("");
     }
 }
 
@@ -437,8 +502,16 @@ logprob_grad(GradParams p)
 
     float v[UN][VEC];
 #pragma unroll
-    for (int u = 0; u < UN; ++u)
-        load_values<DT, VEC>(x, v0 + (u * kGradThreads + (int)threadIdx.x) * VEC, p.V, v[u]);
+    for (int u = 0; u < UN; ++u) {
+        const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
+        if (at + VEC <= p.V) {
+            convert<DT, VEC>(load_raw<DT>(x, at), v[u]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                v[u][e] = at + e < p.V ? load_value<DT>(x, at + e) : 0.0f;
+        }
+    }
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
         const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
