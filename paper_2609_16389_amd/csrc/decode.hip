@@ -37,6 +37,20 @@ int launch_status(xgemm_ctx *h, const char *what)
 
 using xquant_dev::QuantParams;
 
+// Waves of a workgroup: 8 ranges of K for 16 columns, of which two workgroups
+// run on a CU, up to 512 workgroups; beyond that 4 ranges (one or two rows), or
+// 4 ranges of 4 x 16 columns, which share x (16 rows of 4096 k: 6400 columns
+// 9.1 us / 10.4 with 4 x 16, 9216 11.6 / 9.9).  Past 16 rows a workgroup of all
+// rows widens each weight once, but takes long over it: it is used where there
+// are 192 of them, blocks of 16 rows elsewhere.  Microseconds of N x K, for M
+// rows: 32 or 64 rows a workgroup / 16 rows, 4 x 16 columns / 16 rows, 16
+// columns:
+//     2560 x 1280    M 32:  8.6 /  7.2 /  5.4   M 64: 10.8 /  7.4 /   7.8
+//     2560 x 5120    M 32: 19.8 / 15.8 / 11.4   M 64: 21.9 / 12.0 /  13.7
+//     4096 x 4096    M 32: 12.7 / 10.2 /  9.1   M 64: 18.0 / 10.7 /  14.9
+//     7680 x 7680    M 32: 21.9 / 16.4 / 23.3   M 64: 32.7 / 31.2 /  42.2
+//     14336 x 4096   M 32: 14.8 / 20.7 / 24.9   M 64: 21.9 / 39.4 /  45.2
+//     16384 x 16384  M 32: 56.0 / 68.7 / 96.7   M 64: 84.1 /  121 /   172
 template <int DT, int GS>
 void launch_quant(const QuantParams &p, hipStream_t s)
 {
@@ -44,22 +58,22 @@ void launch_quant(const QuantParams &p, hipStream_t s)
     auto launch = [&](auto kernel, int r, int wn, int wk) {
         hipLaunchKernelGGL(kernel, dim3(cdiv(p.N, 16 * wn), cdiv(p.M, r)), dim3(64 * wn * wk), 0, s, p);
     };
+    const int64_t tiles = cdiv(p.N, 16), shared = cdiv(tiles, 4);
     // a lane's row of weights starts at most 15 leading dimensions from its tile's first
-    const int64_t tiles = cdiv(p.N, 16);
     if (p.ldq > (int64_t)1 << 27)
-        launch(quant_kernel<DT, 16, 1, 4, GS, int64_t>, 16, 1, 4);
+        launch(quant_kernel<DT, 16, 1, 4, 2, GS, int64_t>, 16, 1, 4);
     else if (p.M <= 2 && tiles <= 512)
-        launch(quant_kernel<DT, 2, 1, 8, GS, uint32_t>, 2, 1, 8);
+        launch(quant_kernel<DT, 2, 1, 8, 2, GS, uint32_t>, 2, 1, 8);
     else if (p.M <= 2)
-        launch(quant_kernel<DT, 2, 1, 4, GS, uint32_t>, 2, 1, 4);
-    else if (p.M <= 16 && tiles <= 512)
-        launch(quant_kernel<DT, 16, 1, 8, GS, uint32_t>, 16, 1, 8);
-    else if (p.M <= 16)
-        launch(quant_kernel<DT, 16, 4, 4, GS, uint32_t>, 16, 4, 4);
-    else if (p.M <= 32)
-        launch(quant_kernel<DT, 32, 4, 2, GS, uint32_t>, 32, 4, 2);
+        launch(quant_kernel<DT, 2, 1, 4, 2, GS, uint32_t>, 2, 1, 4);
+    else if (p.M > 32 && shared * cdiv(p.M, 64) >= 192)
+        launch(quant_kernel<DT, 64, 4, 4, 1, GS, uint32_t>, 64, 4, 4);
+    else if (p.M > 16 && shared * cdiv(p.M, 32) >= 192)
+        launch(quant_kernel<DT, 32, 4, 4, 2, GS, uint32_t>, 32, 4, 4);
+    else if (tiles * cdiv(p.M, 16) > 512)
+        launch(quant_kernel<DT, 16, 4, 4, 2, GS, uint32_t>, 16, 4, 4);
     else
-        launch(quant_kernel<DT, 64, 4, 2, GS, uint32_t>, 64, 4, 2);
+        launch(quant_kernel<DT, 16, 1, 8, 2, GS, uint32_t>, 16, 1, 8);
 }
 
 template <int DT>
@@ -171,7 +185,7 @@ int experts_parts(int64_t T, int64_t top, int64_t H, int64_t I, int64_t slots, i
     const int64_t blocks = cdiv(H, own ? 16 : 64), units = slots * (Ip / kDownUnit);
     if (blocks > (int64_t)(xgemm_host::kWsPrefix / sizeof(int)))
         return 1;
-    const int64_t want = !own ? cdiv(4 * (int64_t)cu_count, blocks)
+    const int64_t want = !own ? cdiv(2 * (int64_t)cu_count, blocks)
                        : T > 2 ? cdiv((int64_t)cu_count, blocks)
                                : blocks * 4 < cu_count ? cdiv((int64_t)cu_count / 2, blocks) : 1;
     return (int)std::max<int64_t>(1, std::min({want, units / (own ? 4 * waves : 4), (int64_t)kMaxParts}));
@@ -249,7 +263,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     const size_t at_pair = take(most_slots * kMaxTokens * sizeof(uint16_t));
     const size_t at_weight = take(most * top * sizeof(float));
     const size_t at_h = take((size_t)most * top * p.Ip * 2 * PL);
-    const size_t at_part = take((size_t)kMaxParts * most * H * sizeof(float));
+    const size_t at_part = take((size_t)kMaxParts * most * cdiv(H, 64) * 64 * sizeof(float));
     const int rc = xgemm_host::acquire_workspace(h, bytes, s);
     if (rc != XGEMM_OK)
         return rc;

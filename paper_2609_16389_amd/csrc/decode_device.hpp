@@ -121,4 +121,21 @@ __device__ __forceinline__ u32x4 load16_end(const void *row, int64_t at, int64_t
     return shift_down(v, (int)min(at, (int64_t)16));
 }
 
+// Partial sums between workgroups: 16 bytes at a distance of at most 2^32 from
+// `base`, at device scope (sc1).  Such a store, once complete, is visible to
+// such loads from every XCD.
+constexpr int kDeviceScope = 1 << 4;
+__device__ __forceinline__ void store4_device(void *base, uint32_t off, f32x4 v)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(
+        __builtin_bit_cast(u32x4, v), __builtin_amdgcn_make_buffer_rsrc(base, (short)0, (int)0xffffffff, 0x00020000), off,
+        0, kDeviceScope);
+}
+__device__ __forceinline__ f32x4 load4_device(void *base, uint32_t off)
+{
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                         __builtin_amdgcn_make_buffer_rsrc(base, (short)0, (int)0xffffffff, 0x00020000),
+                                         off, 0, kDeviceScope));
+}
+
 }  // namespace xdecode_dev

@@ -78,7 +78,7 @@ struct ExpertsParams {
     uint16_t *pair;   // [slots][kMaxTokens]: token * top + choice
     float *weight;    // [T * top]: exp(score - largest), over the whole softmax's sum without renormalize
     uint16_t *h;      // [parts of h][T * top][Ip]
-    float *part;      // [parts][T][H], where parts > 1
+    float *part;      // [parts][T][H rounded up to whole workgroups], where parts > 1
     int *done;        // [workgroups of a range], zero between launches
 };
 
@@ -449,7 +449,7 @@ down_sum(ExpertsParams p)
     constexpr int BUFS = WN == 1 ? 1 : 2;
     constexpr int HB = unit_bytes<R>(kDownUnit);
     __shared__ __attribute__((aligned(16))) char sh_h[WK][BUFS][PL][HB];
-    __shared__ float acc_all[WAVES][TOKENS * 16];
+    __shared__ __attribute__((aligned(16))) float acc_all[WAVES][TOKENS * 16];
     __shared__ float sh_weight[TOKENS * kMaxTop];
     __shared__ uint16_t sh_slot[kMaxExperts];           // the slots in use, in ascending order,
     __shared__ uint16_t sh_expert[kMaxExperts];         //   their experts,
@@ -638,28 +638,26 @@ down_sum(ExpertsParams p)
     }
     sync_lds();
 
-    // the workgroup's sums: of its ranges (WK) or of its columns (WN)
-    const int cols = 16 * WN;
-    auto own = [&](int o) {   // value o of T x cols
-        const int t = o / cols, n = o % cols;
-        if (WN > 1)
-            return acc_all[n >> 4][t * 16 + (n & 15)];
-        float v = acc_all[0][o];
+    // the workgroup's sums, four columns of a token at a time: of its ranges
+    // (WK) or of its columns (WN)
+    constexpr int G = 4 * WN;
+    const int values = p.T * G;
+    auto own = [&](int o) {
+        const int t = o / G, n = o % G * 4;
+        f32x4 v = *(const f32x4 *)&acc_all[n >> 4][t * 16 + (n & 15)];
 #pragma unroll
         for (int w = 1; w < WK; ++w)
-            v += acc_all[w][o];
+            v += *(const f32x4 *)&acc_all[w][t * 16 + n];
         return v;
     };
     const bool shared = p.parts > 1;
+    const uint32_t hp = (uint32_t)gridDim.x * 16 * WN;   // columns of a row of partial sums
+    auto place_of = [&](int q, int o) { return (((uint32_t)(q * p.T + o / G)) * hp + nw + o % G * 4) * 4u; };
     if (shared) {
         // publish them with device-scope stores; once every wave's have
         // completed, count in.  Nobody waits: the last one adds.
-        for (int o = tid; o < p.T * cols; o += THREADS) {
-            const int t = o / cols, n = nw + o % cols;
-            if (n < p.H)
-                __hip_atomic_store(p.part + ((int64_t)blockIdx.y * p.T + t) * p.H + n, own(o), __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-        }
+        for (int o = tid; o < values; o += THREADS)
+            store4_device(p.part, place_of(blockIdx.y, o), own(o));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         sync_lds();
         if (tid == 0) {
@@ -672,23 +670,31 @@ down_sum(ExpertsParams p)
         if (!sh_last)
             return;
     }
-    for (int o = tid; o < p.T * cols; o += THREADS) {
-        const int t = o / cols, n = nw + o % cols;
-        if (n >= p.H)
-            continue;
-        float v = 0.0f;
+    for (int o = tid; o < values; o += THREADS) {
+        const int t = o / G, n = nw + o % G * 4;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (shared) {
-#pragma unroll 8
-            for (int q = 0; q < p.parts; ++q)
-                v += __hip_atomic_load(p.part + ((int64_t)q * p.T + t) * p.H + n, __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
+            for (int q0 = 0; q0 < p.parts; q0 += 8) {
+                f32x4 x[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    x[q] = load4_device(p.part, place_of(min(q0 + q, p.parts - 1), o));
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q0 + q < p.parts)
+                        v += x[q];
+            }
         } else {
             v = own(o);
         }
-        if (p.out16)
-            ((uint16_t *)p.y)[(int64_t)t * p.ldy + n] = from_float<DT>(v);
-        else
-            ((float *)p.y)[(int64_t)t * p.ldy + n] = v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.H) {
+                if (p.out16)
+                    ((uint16_t *)p.y)[(int64_t)t * p.ldy + n + e] = from_float<DT>(v[e]);
+                else
+                    ((float *)p.y)[(int64_t)t * p.ldy + n + e] = v[e];
+            }
     }
 }
 

@@ -14,10 +14,11 @@
 // of 4, which costs two bits of fp32; 128 + q would cost five.)
 //
 // Layout: the weights are the matrix units' second operand, lane l holding
-// column n = l % 16, so that a lane needs one scale a group.  A wave takes
-// every kWaves-th unit of 256 k: per column 128 bytes, one cache line, in two
-// 16-byte loads a lane.  Lane group g (l / 16) holds k 32 g .. + 31 of a block
-// of 128; any assignment of k to lanes is valid as long as x is loaded alike.
+// column n = l % 16, so that a lane needs one scale a group.  A wave takes a
+// range of K in units of one or two blocks of 128 k: per column and unit of two
+// blocks 128 bytes, one cache line, in two 16-byte loads a lane.  Lane group g
+// (l / 16) holds k 32 g .. + 31 of a block; any assignment of k to lanes is
+// valid as long as x is loaded alike.
 // Groups smaller than 128 need each product inside one group: there the four
 // dwords are transposed between the lane groups (four lane swaps), so that
 // dword i holds k 32 i + 8 g .. + 7.
@@ -25,6 +26,13 @@
 // to match, once for all columns.
 // The waves of a workgroup split K and add their blocks through LDS in
 // ascending order.
+//
+// What bounds it: with one row the bytes of q and a launch's latency (bfloat16,
+// groups of 128: 1 x 4096 x 4096 4.2 us in a stream of calls, 1 x 14336 x 4096
+// with groups of 64 and zero points 9.7 us or 3.4 TB/s); with many rows the
+// vector instructions that widen the weights and apply the scales (64 x 16384 x
+// 16384, groups of 128: 78 us, 1.8 TB/s of weights and 440 TFLOP/s; groups of
+// 32 with zero points: 112 us).
 #pragma once
 
 #include <utility>
@@ -35,7 +43,6 @@ namespace xquant_dev {
 
 using namespace xdecode_dev;
 
-constexpr int kUnit = 256;  // k per unit of a wave: two blocks of 128
 
 struct QuantParams {
     const uint16_t *x;
@@ -98,13 +105,13 @@ __device__ __forceinline__ u32x4 transpose_groups(u32x4 v)
     return r;
 }
 
-// LDS of a workgroup of WN x WK waves for rows R.
-template <int R, int WN, int WK>
+// LDS of a workgroup of WN x WK waves for rows R and units of BL blocks.
+template <int R, int WN, int WK, int BL>
 struct QuantLds {
     static constexpr int MT = (R + 15) / 16;
-    static constexpr int XPART = R < 16 ? 32 * R * 16 : MT * 8192;   // x of one unit of k
+    static constexpr int XPART = BL * (R < 16 ? 16 * R * 16 : MT * 4096);   // x of one unit of k
     static constexpr int BUFS = WN == 1 ? 1 : 2;
-    static constexpr int PIECES = R * 32 / (WN * 64);   // 16-byte pieces of it that a thread brings in
+    static constexpr int PIECES = R * 16 * BL / (WN * 64);   // 16-byte pieces of it that a thread brings in
     static constexpr int AHEAD = PIECES <= 2 ? 2 : 1;   // units of x on their way to registers
     __attribute__((aligned(16))) union {
         struct {
@@ -115,11 +122,12 @@ struct QuantLds {
     };
     // the weights of the unit that K ends in, in the place of x of the first
     // ranges; the last range's holds x of that unit
-    static_assert((WK - 1) * BUFS * XPART >= 16 * WN * 128, "room for the last unit's weights");
+    static_assert((WK - 1) * BUFS * XPART >= 16 * WN * 64 * BL, "room for the last unit's weights");
     __device__ __forceinline__ uint8_t *wend() { return (uint8_t *)x; }
 };
 
-// The waves of a workgroup: WN take 16 columns each, WK a range of k each.
+// The waves of a workgroup: WN take 16 columns each, WK a range of k each, in
+// units of BL blocks of 128.
 // Workgroup (blockIdx.x, blockIdx.y): columns from 16 WN blockIdx.x, rows from
 // R blockIdx.y (R: 2 WN, or a multiple of 16).  GS: groups of 32 or 64, or 128
 // for any multiple of that.  off_t holds the distance of a lane's row of q from
@@ -130,11 +138,12 @@ struct QuantLds {
 // order, so one that may or may not have been issued would make every wait
 // behind it a wait for all: the loop's loads are unconditional, past the end
 // they repeat the last unit's, and the unit that K ends in comes after it.
-template <int DT, int R, int WN, int WK, int GS, class off_t>
-__global__ void __launch_bounds__(64 * WN * WK, R < 16 || (R == 16 && WN > 1) ? 4 : 2)
+template <int DT, int R, int WN, int WK, int BL, int GS, class off_t>
+__global__ void __launch_bounds__(64 * WN * WK, R < 16 || WN > 1 ? 4 : 2)
 quant_kernel(QuantParams p)
 {
-    typedef QuantLds<R, WN, WK> Lds;
+    typedef QuantLds<R, WN, WK, BL> Lds;
+    constexpr int kUnit = 128 * BL;
     constexpr int MT = Lds::MT, THREADS = 64 * WN * WK, NP = Lds::PIECES, XA = Lds::AHEAD;
     constexpr int GROUPS = 128 / GS;            // of a block
     constexpr int CHUNK = 16 * GS / kUnit;      // units that 16 groups cover
@@ -155,24 +164,26 @@ quant_kernel(QuantParams p)
     const int nb = min(n0, p.N - 1), nl = min(c, p.N - 1 - nb);
     const uint8_t *const qbase = p.q + (int64_t)nb * p.ldq;
     const off_t qoff = (off_t)nl * (off_t)p.ldq + 16 * g;
-    u32x4 w[2][2];
-    auto load_w = [&](u32x4 (&to)[2], int t) {
+    u32x4 w[2][BL];
+    auto load_w = [&](u32x4 (&to)[BL], int t) {
         const uint8_t *const q = qbase + (int64_t)(u0 + min(t, mine - 1)) * (kUnit / 2);
-        to[0] = load_at<u32x4>(q, qoff);
-        to[1] = load_at<u32x4>(q + 64, qoff);
+#pragma unroll
+        for (int b = 0; b < BL; ++b)
+            to[b] = load_at<u32x4>(q + 64 * b, qoff);
     };
 
     // x: of a unit, thread t of the WN waves of a range brings in pieces t, t +
-    // 64 WN, ...: piece i is 8 k from 8 (i % 32) of row i / 32 (rows past M
+    // 64 WN, ...: piece i is 8 k from 8 (i % PR) of row i / PR (rows past M
     // repeat the last one)
+    constexpr int PR = 16 * BL;
     const int xi = wn * 64 + lane;
-    const uint16_t *const xbase = p.x + (int64_t)m0 * p.ldx + 8 * (xi & 31);
+    const uint16_t *const xbase = p.x + (int64_t)m0 * p.ldx + 8 * (xi % PR);
     u32x4 xr[XA][NP];
     auto load_x = [&](u32x4 (&to)[NP], int t) {
         const int64_t k = (int64_t)(u0 + min(t, mine - 1)) * kUnit;
 #pragma unroll
         for (int q = 0; q < NP; ++q)
-            to[q] = load_any<u32x4>(xbase + min((xi >> 5) + 2 * WN * q, rows - 1) * p.ldx + k);
+            to[q] = load_any<u32x4>(xbase + min(xi / PR + 64 / PR * WN * q, rows - 1) * p.ldx + k);
     };
     // where 8 k of a row lie in LDS: piece kc of a block of 128 goes to lane
     // group kg of product kd; 16 rows are swizzled so that neither the pieces of
@@ -185,7 +196,7 @@ quant_kernel(QuantParams p)
     auto store_x = [&](const u32x4 (&from)[NP], int buf) {
 #pragma unroll
         for (int q = 0; q < NP; ++q)
-            *(u32x4 *)(sh.x[wk][buf] + x_place((xi >> 5) + 2 * WN * q, xi >> 4 & 1, xi & 15)) = pair_up(from[q]);
+            *(u32x4 *)(sh.x[wk][buf] + x_place(xi / PR + 64 / PR * WN * q, xi % PR >> 4, xi & 15)) = pair_up(from[q]);
     };
 
     // scales and zero points of 16 groups (of GS k) from group q0 on: lane
@@ -234,33 +245,45 @@ quant_kernel(QuantParams p)
     for (int i = 0; i < MT; ++i)
         acc[i] = zero;
 
-    // one unit: the products of every group, scaled into the outputs
-    auto compute = [&](const u32x4 (&from)[2], int buf, int q0) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
+    // one unit: the products of every group, scaled into the outputs.  (Loops
+    // over constants that the compiler is not asked to unroll but given
+    // unrolled, so that no array of registers is ever indexed.)
+    auto compute = [&](const u32x4 (&from)[BL], int buf, int q0) {
+        auto block = [&]<int b>() {
             const u32x4 v = GS < 128 ? transpose_groups(from[b]) : from[b];
             f32x4 P[MT], S[MT];
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const bool first = d % (GS / 32) == 0, last = d % (GS / 32) == GS / 32 - 1;
+            auto piece = [&]<int d>() {
+                constexpr bool first = d % (GS / 32) == 0, last = d % (GS / 32) == GS / 32 - 1;
                 const u32x4 f = widen8<DT>(v[d], widen);
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
+                auto tile = [&]<int i>() {
                     const u32x4 a = *(const u32x4 *)(sh.x[wk][buf] + x_place(R < 16 ? min(c, R - 1) : 16 * i + c, b,
                                                                              GS < 128 ? 4 * d + g : 4 * g + d));
                     S[i] = mfma16<DT>(a, ones, first ? zero : S[i]);
                     P[i] = mfma16<DT>(a, f, first ? zero : P[i]);
-                }
-                if (last) {
+                };
+                [&]<int... I>(std::integer_sequence<int, I...>) {
+                    (tile.template operator()<I>(), ...);
+                }(std::make_integer_sequence<int, MT>{});
+                if constexpr (last) {
                     const float2 sc = sh.scale[wave][q0 + b * GROUPS + d / (GS / 32)][c];
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
+                    auto flush = [&]<int i>() {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             acc[i][r] = fmaf(sc.x, fmaf(-sc.y, S[i][r], P[i][r]), acc[i][r]);
+                    };
+                    [&]<int... I>(std::integer_sequence<int, I...>) {
+                        (flush.template operator()<I>(), ...);
+                    }(std::make_integer_sequence<int, MT>{});
                 }
-            }
-        }
+            };
+            piece.template operator()<0>();
+            piece.template operator()<1>();
+            piece.template operator()<2>();
+            piece.template operator()<3>();
+        };
+        block.template operator()<0>();
+        if constexpr (BL == 2)
+            block.template operator()<1>();
     };
     auto sync = [&] {
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
@@ -306,15 +329,15 @@ quant_kernel(QuantParams p)
         const int kend = units * kUnit;
         sync();   // (x is done with)
         char *const to = sh.x[WK - 1][0];
-        for (int o = tid; o < 16 * WN * 8; o += THREADS)
+        for (int o = tid; o < 16 * WN * 4 * BL; o += THREADS)
             *(u32x4 *)(sh.wend() + 16 * o) =
-                load16_end(p.q + (int64_t)min(nw + (o >> 3), p.N - 1) * p.ldq, kend / 2 + 16 * (o & 7),
+                load16_end(p.q + (int64_t)min(nw + o / (4 * BL), p.N - 1) * p.ldq, kend / 2 + 16 * (o % (4 * BL)),
                            ((int64_t)p.K + 1) / 2);
-        for (int o = tid; o < R * 32; o += THREADS) {
-            const int row = o >> 5;
+        for (int o = tid; o < R * PR; o += THREADS) {
+            const int row = o / PR;
             const u32x4 v = load16_end(p.x + (int64_t)(m0 + min(row, rows - 1)) * p.ldx,
-                                       2 * ((int64_t)kend + 8 * (o & 31)), 2 * (int64_t)p.K);
-            *(u32x4 *)(to + x_place(row, o >> 4 & 1, o & 15)) = pair_up(v);
+                                       2 * ((int64_t)kend + 8 * (o % PR)), 2 * (int64_t)p.K);
+            *(u32x4 *)(to + x_place(row, o % PR >> 4, o & 15)) = pair_up(v);
         }
         if (wk == WK - 1) {
             load_scales(units * (kUnit / GS));
@@ -322,8 +345,9 @@ quant_kernel(QuantParams p)
         }
         sync();
         if (wk == WK - 1) {
-            w[0][0] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 128 + 16 * g);
-            w[0][1] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 128 + 64 + 16 * g);
+#pragma unroll
+            for (int b = 0; b < BL; ++b)
+                w[0][b] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 64 * BL + 64 * b + 16 * g);
             compute(w[0], 0, 0);
         }
     }
