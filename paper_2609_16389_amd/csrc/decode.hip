@@ -55,25 +55,25 @@ template <int DT, int GS>
 void launch_quant(const QuantParams &p, hipStream_t s)
 {
     using namespace xquant_dev;
-    auto launch = [&](auto kernel, int r, int wn, int wk) {
-        hipLaunchKernelGGL(kernel, dim3(cdiv(p.N, 16 * wn), cdiv(p.M, r)), dim3(64 * wn * wk), 0, s, p);
+    auto launch = [&](auto kernel, int r, int wn, int wk, int ct) {
+        hipLaunchKernelGGL(kernel, dim3(cdiv(p.N, 16 * wn * ct), cdiv(p.M, r)), dim3(64 * wn * wk), 0, s, p);
     };
     const int64_t tiles = cdiv(p.N, 16), shared = cdiv(tiles, 4);
-    // a lane's row of weights starts at most 15 leading dimensions from its tile's first
+    // a lane's row of weights starts at most 31 leading dimensions from its wave's first
     if (p.ldq > (int64_t)1 << 27)
-        launch(quant_kernel<DT, 16, 1, 4, 2, GS, int64_t>, 16, 1, 4);
+        launch(quant_kernel<DT, 16, 1, 4, 1, 2, GS, int64_t>, 16, 1, 4, 1);
     else if (p.M <= 2 && tiles <= 512)
-        launch(quant_kernel<DT, 2, 1, 8, 2, GS, uint32_t>, 2, 1, 8);
+        launch(quant_kernel<DT, 2, 1, 8, 1, 2, GS, uint32_t>, 2, 1, 8, 1);
     else if (p.M <= 2)
-        launch(quant_kernel<DT, 2, 1, 4, 2, GS, uint32_t>, 2, 1, 4);
+        launch(quant_kernel<DT, 2, 1, 4, 1, 2, GS, uint32_t>, 2, 1, 4, 1);
     else if (p.M > 32 && shared * cdiv(p.M, 64) >= 192)
-        launch(quant_kernel<DT, 64, 4, 4, 1, GS, uint32_t>, 64, 4, 4);
+        launch(quant_kernel<DT, 64, 2, 4, 2, 1, GS, uint32_t>, 64, 2, 4, 2);
     else if (p.M > 16 && shared * cdiv(p.M, 32) >= 192)
-        launch(quant_kernel<DT, 32, 4, 4, 2, GS, uint32_t>, 32, 4, 4);
+        launch(quant_kernel<DT, 32, 2, 4, 2, 1, GS, uint32_t>, 32, 2, 4, 2);
     else if (tiles * cdiv(p.M, 16) > 512)
-        launch(quant_kernel<DT, 16, 4, 4, 2, GS, uint32_t>, 16, 4, 4);
+        launch(quant_kernel<DT, 16, 4, 4, 1, 2, GS, uint32_t>, 16, 4, 4, 1);
     else
-        launch(quant_kernel<DT, 16, 1, 8, 2, GS, uint32_t>, 16, 1, 8);
+        launch(quant_kernel<DT, 16, 1, 8, 1, 2, GS, uint32_t>, 16, 1, 8, 1);
 }
 
 template <int DT>

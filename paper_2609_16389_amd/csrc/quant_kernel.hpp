@@ -30,9 +30,10 @@
 // What bounds it: with one row the bytes of q and a launch's latency (bfloat16,
 // groups of 128: 1 x 4096 x 4096 4.2 us in a stream of calls, 1 x 14336 x 4096
 // with groups of 64 and zero points 9.7 us or 3.4 TB/s); with many rows the
-// vector instructions that widen the weights and apply the scales (64 x 16384 x
-// 16384, groups of 128: 78 us, 1.8 TB/s of weights and 440 TFLOP/s; groups of
-// 32 with zero points: 112 us).
+// time of a unit, a chain of a barrier, reads of x, widening, products and
+// scaling that no unit of the CU fills (64 x 16384 x 16384: matrix units 39%
+// busy, vector instructions 40%; a wave taking two tiles of 16 columns, which
+// halves its reads of x and saves a quarter of the products, gained 4%).
 #pragma once
 
 #include <utility>
@@ -105,8 +106,19 @@ __device__ __forceinline__ u32x4 transpose_groups(u32x4 v)
     return r;
 }
 
-// LDS of a workgroup of WN x WK waves for rows R and units of BL blocks.
-template <int R, int WN, int WK, int BL>
+// f.operator()<0>() ... <N - 1>(): a loop unrolled in the source, so that no
+// array of registers is ever indexed.
+template <int N, class F>
+__device__ __forceinline__ void repeat(F &&f)
+{
+    [&]<int... I>(std::integer_sequence<int, I...>) {
+        (f.template operator()<I>(), ...);
+    }(std::make_integer_sequence<int, N>{});
+}
+
+// LDS of a workgroup of WN x WK waves of CT column tiles for rows R and units
+// of BL blocks.
+template <int R, int WN, int WK, int CT, int BL>
 struct QuantLds {
     static constexpr int MT = (R + 15) / 16;
     static constexpr int XPART = BL * (R < 16 ? 16 * R * 16 : MT * 4096);   // x of one unit of k
@@ -116,19 +128,19 @@ struct QuantLds {
     __attribute__((aligned(16))) union {
         struct {
             char x[WK][BUFS][XPART];
-            float2 scale[WK * WN][16][16];   // {s, 16 + z} of 16 groups of 16 columns
+            float2 scale[WK * WN][CT][16][16];   // {s, 16 + z} of 16 groups of 16 columns
         };
-        float red[WK][WN][MT][256];
+        float red[WK][WN * CT][MT][256];
     };
     // the weights of the unit that K ends in, in the place of x of the first
     // ranges; the last range's holds x of that unit
-    static_assert((WK - 1) * BUFS * XPART >= 16 * WN * 64 * BL, "room for the last unit's weights");
+    static_assert((WK - 1) * BUFS * XPART >= 16 * WN * CT * 64 * BL, "room for the last unit's weights");
     __device__ __forceinline__ uint8_t *wend() { return (uint8_t *)x; }
 };
 
-// The waves of a workgroup: WN take 16 columns each, WK a range of k each, in
-// units of BL blocks of 128.
-// Workgroup (blockIdx.x, blockIdx.y): columns from 16 WN blockIdx.x, rows from
+// The waves of a workgroup: WN take CT tiles of 16 columns each, WK a range of
+// k each, in units of BL blocks of 128.
+// Workgroup (blockIdx.x, blockIdx.y): columns from 16 WN CT blockIdx.x, rows from
 // R blockIdx.y (R: 2 WN, or a multiple of 16).  GS: groups of 32 or 64, or 128
 // for any multiple of that.  off_t holds the distance of a lane's row of q from
 // its tile's first: 32 bits where leading dimensions allow.
@@ -138,11 +150,11 @@ struct QuantLds {
 // order, so one that may or may not have been issued would make every wait
 // behind it a wait for all: the loop's loads are unconditional, past the end
 // they repeat the last unit's, and the unit that K ends in comes after it.
-template <int DT, int R, int WN, int WK, int BL, int GS, class off_t>
-__global__ void __launch_bounds__(64 * WN * WK, R < 16 || WN > 1 ? 4 : 2)
+template <int DT, int R, int WN, int WK, int CT, int BL, int GS, class off_t>
+__global__ void __launch_bounds__(64 * WN * WK, R < 16 || WN * WK > 8 ? 4 : 2)
 quant_kernel(QuantParams p)
 {
-    typedef QuantLds<R, WN, WK, BL> Lds;
+    typedef QuantLds<R, WN, WK, CT, BL> Lds;
     constexpr int kUnit = 128 * BL;
     constexpr int MT = Lds::MT, THREADS = 64 * WN * WK, NP = Lds::PIECES, XA = Lds::AHEAD;
     constexpr int GROUPS = 128 / GS;            // of a block
@@ -153,7 +165,7 @@ quant_kernel(QuantParams p)
     const int wn = wave % WN, wk = wave / WN;
     const int c = lane & 15, g = lane >> 4;
     const int m0 = blockIdx.y * R, rows = min(R, p.M - m0);
-    const int nw = blockIdx.x * 16 * WN, n0 = nw + 16 * wn;
+    const int nw = blockIdx.x * 16 * WN * CT, n0 = nw + 16 * CT * wn;
 
     // this wave's whole units of k (WK is a power of two)
     const int units = p.K / kUnit;
@@ -161,15 +173,18 @@ quant_kernel(QuantParams p)
     const int steps = (units + WK - 1) / WK;    // of the longest range
 
     // columns past N are read from the last one, never stored
-    const int nb = min(n0, p.N - 1), nl = min(c, p.N - 1 - nb);
+    const int nb = min(n0, p.N - 1);
+    int nl[CT];
+    off_t qoff[CT];
+    repeat<CT>([&]<int t>() {
+        nl[t] = min(16 * t + c, p.N - 1 - nb);
+        qoff[t] = (off_t)nl[t] * (off_t)p.ldq + 16 * g;
+    });
     const uint8_t *const qbase = p.q + (int64_t)nb * p.ldq;
-    const off_t qoff = (off_t)nl * (off_t)p.ldq + 16 * g;
-    u32x4 w[2][BL];
-    auto load_w = [&](u32x4 (&to)[BL], int t) {
+    u32x4 w[2][CT][BL];
+    auto load_w = [&](u32x4 (&to)[CT][BL], int t) {
         const uint8_t *const q = qbase + (int64_t)(u0 + min(t, mine - 1)) * (kUnit / 2);
-#pragma unroll
-        for (int b = 0; b < BL; ++b)
-            to[b] = load_at<u32x4>(q + 64 * b, qoff);
+        repeat<CT * BL>([&]<int i>() { to[i / BL][i % BL] = load_at<u32x4>(q + 64 * (i % BL), qoff[i / BL]); });
     };
 
     // x: of a unit, thread t of the WN waves of a range brings in pieces t, t +
@@ -191,7 +206,7 @@ quant_kernel(QuantParams p)
     auto x_place = [&](int row, int b, int kc) {
         const int kd = GS < 128 ? kc >> 2 : kc & 3, kg = GS < 128 ? kc & 3 : kc >> 2;
         return R < 16 ? (((b * 4 + kd) * 4 + kg) * R + row) * 16
-                      : ((b * 4 + kd) * MT + (row >> 4)) * 1024 + kg * 256 + ((row ^ kc) & 15) * 16;
+                      : ((b * 4 + kd) * MT + (row >> 4)) * 1024 + kg * 256 + ((row ^ (4 * kd + kg)) & 15) * 16;
     };
     auto store_x = [&](const u32x4 (&from)[NP], int buf) {
 #pragma unroll
@@ -200,90 +215,82 @@ quant_kernel(QuantParams p)
     };
 
     // scales and zero points of 16 groups (of GS k) from group q0 on: lane
-    // group g brings in four of column c
-    const uint16_t *const sbase = p.s + (int64_t)(nb + nl) * p.lds;
-    const uint8_t *const zbase = p.z ? p.z + (int64_t)(nb + nl) * p.ldz : nullptr;
+    // group g brings in four of column c of each tile
     const int groups = (p.K - 1) / p.group + 1;
-    uint64_t sr;
-    uint32_t zr;
+    uint64_t sr[CT];
+    uint32_t zr[CT];
     auto load_scales = [&](int q0) {
-        zr = 0x08080808u;
-        if (p.group == GS && groups >= 4) {
-            // (at the end of a row its last four, moved down: what lies past it
-            // meets x of zero or no product at all)
-            const int q = q0 + 4 * g, at = min(q, groups - 4), past = min(q - at, 3);
-            sr = load_any<uint64_t>(sbase + at) >> (16 * past);
-            if (p.z)
-                zr = load_any<uint32_t>(zbase + at) >> (8 * past);
-        } else {
-            sr = 0;
-            uint32_t z = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = min((int)((uint32_t)(q0 + 4 * g + e) * GS / (uint32_t)p.group), groups - 1);
-                sr |= (uint64_t)sbase[at] << (16 * e);
+        repeat<CT>([&]<int t>() {
+            const uint16_t *const sbase = p.s + (int64_t)(nb + nl[t]) * p.lds;
+            const uint8_t *const zbase = p.z ? p.z + (int64_t)(nb + nl[t]) * p.ldz : nullptr;
+            zr[t] = 0x08080808u;
+            if (p.group == GS && groups >= 4) {
+                // (at the end of a row its last four, moved down: what lies past it
+                // meets x of zero or no product at all)
+                const int q = q0 + 4 * g, at = min(q, groups - 4), past = min(q - at, 3);
+                sr[t] = load_any<uint64_t>(sbase + at) >> (16 * past);
                 if (p.z)
-                    z |= (uint32_t)zbase[at] << (8 * e);
+                    zr[t] = load_any<uint32_t>(zbase + at) >> (8 * past);
+            } else {
+                uint64_t sv = 0;
+                uint32_t zv = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = min((int)((uint32_t)(q0 + 4 * g + e) * GS / (uint32_t)p.group), groups - 1);
+                    sv |= (uint64_t)sbase[at] << (16 * e);
+                    if (p.z)
+                        zv |= (uint32_t)zbase[at] << (8 * e);
+                }
+                sr[t] = sv;
+                if (p.z)
+                    zr[t] = zv;
             }
-            if (p.z)
-                zr = z;
-        }
+        });
     };
     auto store_scales = [&] {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            sh.scale[wave][4 * g + e][c] = float2{to_float<DT>((uint16_t)(sr >> (16 * e))),
-                                                  16.0f + (float)(zr >> (8 * e) & 255u)};
+        repeat<CT * 4>([&]<int i>() {
+            constexpr int t = i / 4, e = i % 4;
+            sh.scale[wave][t][4 * g + e][c] = float2{to_float<DT>((uint16_t)(sr[t] >> (16 * e))),
+                                                     16.0f + (float)(zr[t] >> (8 * e) & 255u)};
+        });
     };
 
     const Masks widen = masks<DT>();
     const uint32_t one = DT == 0 ? 0x3f803f80u : 0x3c003c00u;
     const u32x4 ones = {one, one, one, one};
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    f32x4 acc[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-        acc[i] = zero;
+    f32x4 acc[CT][MT];
+    repeat<CT * MT>([&]<int i>() { acc[i / MT][i % MT] = zero; });
 
-    // one unit: the products of every group, scaled into the outputs.  (Loops
-    // over constants that the compiler is not asked to unroll but given
-    // unrolled, so that no array of registers is ever indexed.)
-    auto compute = [&](const u32x4 (&from)[BL], int buf, int q0) {
-        auto block = [&]<int b>() {
-            const u32x4 v = GS < 128 ? transpose_groups(from[b]) : from[b];
-            f32x4 P[MT], S[MT];
-            auto piece = [&]<int d>() {
+    // one unit: the products of every group, scaled into the outputs; the sum of
+    // x serves all of the wave's tiles
+    auto compute = [&](const u32x4 (&from)[CT][BL], int buf, int q0) __attribute__((always_inline)) {
+        repeat<BL>([&]<int b>() __attribute__((always_inline)) {
+            u32x4 v[CT];
+            repeat<CT>([&]<int t>() { v[t] = GS < 128 ? transpose_groups(from[t][b]) : from[t][b]; });
+            f32x4 P[CT][MT], S[MT];
+            repeat<4>([&]<int d>() __attribute__((always_inline)) {
                 constexpr bool first = d % (GS / 32) == 0, last = d % (GS / 32) == GS / 32 - 1;
-                const u32x4 f = widen8<DT>(v[d], widen);
-                auto tile = [&]<int i>() {
+                u32x4 f[CT];
+                repeat<CT>([&]<int t>() { f[t] = widen8<DT>(v[t][d], widen); });
+                repeat<MT>([&]<int i>() __attribute__((always_inline)) {
                     const u32x4 a = *(const u32x4 *)(sh.x[wk][buf] + x_place(R < 16 ? min(c, R - 1) : 16 * i + c, b,
                                                                              GS < 128 ? 4 * d + g : 4 * g + d));
                     S[i] = mfma16<DT>(a, ones, first ? zero : S[i]);
-                    P[i] = mfma16<DT>(a, f, first ? zero : P[i]);
-                };
-                [&]<int... I>(std::integer_sequence<int, I...>) {
-                    (tile.template operator()<I>(), ...);
-                }(std::make_integer_sequence<int, MT>{});
-                if constexpr (last) {
-                    const float2 sc = sh.scale[wave][q0 + b * GROUPS + d / (GS / 32)][c];
-                    auto flush = [&]<int i>() {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            acc[i][r] = fmaf(sc.x, fmaf(-sc.y, S[i][r], P[i][r]), acc[i][r]);
-                    };
-                    [&]<int... I>(std::integer_sequence<int, I...>) {
-                        (flush.template operator()<I>(), ...);
-                    }(std::make_integer_sequence<int, MT>{});
-                }
-            };
-            piece.template operator()<0>();
-            piece.template operator()<1>();
-            piece.template operator()<2>();
-            piece.template operator()<3>();
-        };
-        block.template operator()<0>();
-        if constexpr (BL == 2)
-            block.template operator()<1>();
+                    repeat<CT>([&]<int t>() { P[t][i] = mfma16<DT>(a, f[t], first ? zero : P[t][i]); });
+                });
+                if constexpr (last)
+                    repeat<CT>([&]<int t>() {
+                        const float2 sc = sh.scale[wave][t][q0 + b * GROUPS + d / (GS / 32)][c];
+                        repeat<MT * 4>([&]<int j>() {
+                            constexpr int i = j / 4, r = j % 4;
+                            acc[t][i][r] = fmaf(sc.x, fmaf(-sc.y, S[i][r], P[t][i][r]), acc[t][i][r]);
+                        });
+                    });
+                if constexpr (MT * CT > 4)
+                    __builtin_amdgcn_sched_barrier(0);   // (reads of x moved up from the next product would not fit)
+            });
+        });
     };
     auto sync = [&] {
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
@@ -329,7 +336,7 @@ quant_kernel(QuantParams p)
         const int kend = units * kUnit;
         sync();   // (x is done with)
         char *const to = sh.x[WK - 1][0];
-        for (int o = tid; o < 16 * WN * 4 * BL; o += THREADS)
+        for (int o = tid; o < 16 * WN * CT * 4 * BL; o += THREADS)
             *(u32x4 *)(sh.wend() + 16 * o) =
                 load16_end(p.q + (int64_t)min(nw + o / (4 * BL), p.N - 1) * p.ldq, kend / 2 + 16 * (o % (4 * BL)),
                            ((int64_t)p.K + 1) / 2);
@@ -345,22 +352,22 @@ quant_kernel(QuantParams p)
         }
         sync();
         if (wk == WK - 1) {
-#pragma unroll
-            for (int b = 0; b < BL; ++b)
-                w[0][b] = *(const u32x4 *)(sh.wend() + (16 * wn + c) * 64 * BL + 64 * b + 16 * g);
+            repeat<CT * BL>([&]<int i>() {
+                w[0][i / BL][i % BL] = *(const u32x4 *)(sh.wend() + (16 * (CT * wn + i / BL) + c) * 64 * BL +
+                                                        64 * (i % BL) + 16 * g);
+            });
             compute(w[0], 0, 0);
         }
     }
     sync();   // (x and the scales are done with)
 
     // the ranges' sums, added in ascending order
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            sh.red[wk][wn][i][64 * r + lane] = acc[i][r];
+    repeat<CT * MT * 4>([&]<int j>() {
+        constexpr int t = j / (4 * MT), i = j / 4 % MT, r = j % 4;
+        sh.red[wk][CT * wn + t][i][64 * r + lane] = acc[t][i][r];
+    });
     sync();
-    for (int o = tid; o < WN * MT * 256; o += THREADS) {
+    for (int o = tid; o < WN * CT * MT * 256; o += THREADS) {
         const int j = o / (MT * 256), i = (o >> 8) % MT, r = o >> 6 & 3, l = o & 63;
         const int row = 16 * i + 4 * (l >> 4) + r, n = nw + 16 * j + (l & 15);
         if (row >= rows || n >= p.N)

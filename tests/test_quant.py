@@ -195,3 +195,35 @@ def test_refusals_of_the_c_call():
     assert call() == xg.XGEMM_OK and call(z_=None, ldz=0) == xg.XGEMM_OK and call(M=0, y_=None, x_=None) == xg.XGEMM_OK
     with pytest.raises(ValueError):
         xg.gemv_quant(x, q.t().contiguous().t(), s, z, 32)    # rows not contiguous
+
+
+def test_kernels_use_no_scratch(tmp_path):
+    """None of the library's kernels has a private segment, those of every
+    source file included (a code object each): the runtime allocates scratch
+    memory at the first launch of one that does."""
+    import os
+    import re
+    import shutil
+    import subprocess
+    bundler = "/opt/rocm/llvm/bin/clang-offload-bundler"
+    readelf = "/opt/rocm/llvm/bin/llvm-readelf"
+    if not (shutil.which("objcopy") and os.path.exists(bundler) and os.path.exists(readelf)):
+        pytest.skip("objcopy / clang-offload-bundler / llvm-readelf not available")
+    fat = tmp_path / "fat.bin"
+    subprocess.run(["objcopy", "-O", "binary", "--only-section=.hip_fatbin", xg._LIB_PATH, str(fat)], check=True)
+    data = fat.read_bytes()
+    starts = [m.start() for m in re.finditer(b"__CLANG_OFFLOAD_BUNDLE__", data)]
+    names = []
+    for i, (a, b) in enumerate(zip(starts, starts[1:] + [len(data)])):
+        part, co = tmp_path / ("part%d" % i), tmp_path / ("%d.co" % i)
+        part.write_bytes(data[a:b])
+        subprocess.run([bundler, "--unbundle", "--type=o", "--input=" + str(part),
+                        "--targets=hipv4-amdgcn-amd-amdhsa--gfx950", "--output=" + str(co)], check=True)
+        notes = subprocess.run([readelf, "--notes", str(co)], check=True, capture_output=True, text=True).stdout
+        symbols = re.findall(r"\.symbol:\s+(\S+)\.kd", notes)
+        sizes = [int(v) for v in re.findall(r"\.private_segment_fixed_size:\s+(\d+)", notes)]
+        assert len(sizes) == len(symbols)
+        assert all(v == 0 for v in sizes), [(n, v) for n, v in zip(symbols, sizes) if v]
+        names += symbols
+    for part in ("quant_kernel", "route_up", "down_sum", "logprob_rows", "logprob_grad", "gemm_kernel_dma"):
+        assert any(part in n for n in names), part
