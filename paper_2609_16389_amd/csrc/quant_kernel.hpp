@@ -31,8 +31,8 @@
 // groups of 128: 1 x 4096 x 4096 4.2 us in a stream of calls, 1 x 14336 x 4096
 // with groups of 64 and zero points 9.7 us or 3.4 TB/s); with many rows the
 // time of a unit, a chain of a barrier, reads of x, widening, products and
-// scaling that no unit of the CU fills (64 x 16384 x 16384: matrix units 39%
-// busy, vector instructions 40%; a wave taking two tiles of 16 columns, which
+// scaling that no unit of the CU fills (64 x 16384 x 16384 75 us: matrix units 27%
+// busy, vector instructions 36%; a wave taking two tiles of 16 columns, which
 // halves its reads of x and saves a quarter of the products, gained 4%).
 #pragma once
 

@@ -227,3 +227,27 @@ def test_kernels_use_no_scratch(tmp_path):
         names += symbols
     for part in ("quant_kernel", "route_up", "down_sum", "logprob_rows", "logprob_grad", "gemm_kernel_dma"):
         assert any(part in n for n in names), part
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True), (256, False)])
+@pytest.mark.parametrize("shape", [(2, 8300, 300), (3, 8300, 257), (16, 8209, 700), (30, 12290, 640), (17, 12305, 129),
+                                   (64, 12289, 1100), (40, 12301, 96), (100, 6200, 515)], ids=lambda s: "%dx%dx%d" % s)
+def test_many_columns(shape, group, zeros):
+    """The kernels that share rows between waves over columns."""
+    M, N, K = shape
+    for dtype, pad in (("bf16", 0), ("fp16", 3)):
+        x, q, s, z = make(M, N, K, dtype, group, zeros, M + 2 * N + 3 * K, pad)
+        check(xg.gemv_quant(x, q, s, z, group), x, q, s, z, group, K, dtype, "pad %d" % pad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 20])
+def test_rows_far_apart(M):
+    """Rows of weights at distances past 27 and past 32 bits."""
+    x, q, s, z = make(M, 3, 700, "bf16", 64, True, 8)
+    for ld in (2 ** 27 + 8, 2 ** 31 + 24):
+        far = torch.empty(2 * ld + 350, dtype=torch.uint8, device="cuda").as_strided((3, 350), (ld, 1))
+        far.copy_(q)
+        check(xg.gemv_quant(x, far, s, z, 64), x, q, s, z, 64, 700, "bf16", "ld %d" % ld)
+        del far
