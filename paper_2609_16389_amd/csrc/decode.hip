@@ -37,54 +37,62 @@ int launch_status(xgemm_ctx *h, const char *what)
 
 using xquant_dev::QuantParams;
 
-// Waves of a workgroup: 8 ranges of K for 16 columns, of which two workgroups
-// run on a CU, up to 512 workgroups; beyond that 4 ranges (one or two rows), or
-// 4 ranges of 4 x 16 columns, which share x (16 rows of 4096 k: 6400 columns
-// 9.1 us / 10.4 with 4 x 16, 9216 11.6 / 9.9).  Past 16 rows a workgroup of all
-// rows widens each weight once, but takes long over it: it is used where there
-// are 192 of them, blocks of 16 rows elsewhere.  Microseconds of N x K, for M
-// rows: 32 or 64 rows a workgroup / 16 rows, 4 x 16 columns / 16 rows, 16
-// columns:
+// Waves of a workgroup: 8 ranges of K for 16 columns, or 4 ranges of 64 columns,
+// which share x.  One or two rows: 8 ranges up to 512 tiles of 16 columns, 4
+// beyond.  More rows: the least of (rounds of workgroups that the CUs take) x
+// (time of one, in ns a k), with 16 rows a workgroup 1.7 for 16 columns, of which
+// two run on a CU, and 2.5 for 64 columns, 3.2 with 32 rows, 5.0 with 64.  A
+// workgroup of more rows widens each weight for all of them, but where columns
+// leave CUs idle blocks of 16 rows are faster.  Microseconds of N x K, for M
+// rows: 32 or 64 rows a workgroup / 16 rows, 64 columns / 16 rows, 16 columns:
+//     9216 x 4096    M 16:           9.9 / 11.6
+//     6400 x 4096    M 16:          10.4 /  9.1
 //     2560 x 1280    M 32:  8.6 /  7.2 /  5.4   M 64: 10.8 /  7.4 /   7.8
 //     2560 x 5120    M 32: 19.8 / 15.8 / 11.4   M 64: 21.9 / 12.0 /  13.7
 //     4096 x 4096    M 32: 12.7 / 10.2 /  9.1   M 64: 18.0 / 10.7 /  14.9
 //     7680 x 7680    M 32: 21.9 / 16.4 / 23.3   M 64: 32.7 / 31.2 /  42.2
 //     14336 x 4096   M 32: 14.8 / 20.7 / 24.9   M 64: 21.9 / 39.4 /  45.2
 //     16384 x 16384  M 32: 56.0 / 68.7 / 96.7   M 64: 84.1 /  121 /   172
+enum QuantKernel { kFewColumns, kRows16, kRows32, kRows64 };
+QuantKernel quant_choice(int64_t M, int64_t N, int cu_count)
+{
+    const int64_t tiles = cdiv(N, 16), shared = cdiv(N, 64), cus = std::max(cu_count, 1);
+    const double cost[] = {1.7 * (double)cdiv(tiles * cdiv(M, 16), 2 * cus), 2.5 * (double)cdiv(shared * cdiv(M, 16), cus),
+                           3.2 * (double)cdiv(shared * cdiv(M, 32), cus), 5.0 * (double)cdiv(shared * cdiv(M, 64), cus)};
+    return (QuantKernel)(std::min_element(cost, cost + 4) - cost);
+}
+
 template <int DT, int GS>
-void launch_quant(const QuantParams &p, hipStream_t s)
+void launch_quant(const QuantParams &p, int cu_count, hipStream_t s)
 {
     using namespace xquant_dev;
     auto launch = [&](auto kernel, int r, int wn, int wk, int ct) {
         hipLaunchKernelGGL(kernel, dim3(cdiv(p.N, 16 * wn * ct), cdiv(p.M, r)), dim3(64 * wn * wk), 0, s, p);
     };
-    const int64_t tiles = cdiv(p.N, 16), shared = cdiv(tiles, 4);
     // a lane's row of weights starts at most 31 leading dimensions from its wave's first
     if (p.ldq > (int64_t)1 << 27)
-        launch(quant_kernel<DT, 16, 1, 4, 1, 2, GS, int64_t>, 16, 1, 4, 1);
-    else if (p.M <= 2 && tiles <= 512)
-        launch(quant_kernel<DT, 2, 1, 8, 1, 2, GS, uint32_t>, 2, 1, 8, 1);
-    else if (p.M <= 2)
-        launch(quant_kernel<DT, 2, 1, 4, 1, 2, GS, uint32_t>, 2, 1, 4, 1);
-    else if (p.M > 32 && shared * cdiv(p.M, 64) >= 192)
-        launch(quant_kernel<DT, 64, 2, 4, 2, 1, GS, uint32_t>, 64, 2, 4, 2);
-    else if (p.M > 16 && shared * cdiv(p.M, 32) >= 192)
-        launch(quant_kernel<DT, 32, 2, 4, 2, 1, GS, uint32_t>, 32, 2, 4, 2);
-    else if (tiles * cdiv(p.M, 16) > 512)
-        launch(quant_kernel<DT, 16, 4, 4, 1, 2, GS, uint32_t>, 16, 4, 4, 1);
-    else
-        launch(quant_kernel<DT, 16, 1, 8, 1, 2, GS, uint32_t>, 16, 1, 8, 1);
+        return launch(quant_kernel<DT, 16, 1, 4, 1, 2, GS, int64_t>, 16, 1, 4, 1);
+    if (p.M <= 2 && p.N <= 16 * 512)
+        return launch(quant_kernel<DT, 2, 1, 8, 1, 2, GS, uint32_t>, 2, 1, 8, 1);
+    if (p.M <= 2)
+        return launch(quant_kernel<DT, 2, 1, 4, 1, 2, GS, uint32_t>, 2, 1, 4, 1);
+    switch (quant_choice(p.M, p.N, cu_count)) {
+    case kFewColumns: return launch(quant_kernel<DT, 16, 1, 8, 1, 2, GS, uint32_t>, 16, 1, 8, 1);
+    case kRows16: return launch(quant_kernel<DT, 16, 4, 4, 1, 2, GS, uint32_t>, 16, 4, 4, 1);
+    case kRows32: return launch(quant_kernel<DT, 32, 2, 4, 2, 1, GS, uint32_t>, 32, 2, 4, 2);
+    case kRows64: return launch(quant_kernel<DT, 64, 2, 4, 2, 1, GS, uint32_t>, 64, 2, 4, 2);
+    }
 }
 
 template <int DT>
-void launch_quant(const QuantParams &p, hipStream_t s)
+void launch_quant(const QuantParams &p, int cu_count, hipStream_t s)
 {
     if (p.group == 32)
-        launch_quant<DT, 32>(p, s);
+        launch_quant<DT, 32>(p, cu_count, s);
     else if (p.group == 64)
-        launch_quant<DT, 64>(p, s);
+        launch_quant<DT, 64>(p, cu_count, s);
     else
-        launch_quant<DT, 128>(p, s);
+        launch_quant<DT, 128>(p, cu_count, s);
 }
 
 int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const uint8_t *q, int64_t ldq,
@@ -127,9 +135,9 @@ int run_quant(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int6
         p.x = (const uint16_t *)x + m * ldx;
         p.y = (char *)y + m * ldy * (p.out16 ? 2 : 4);
         if (dtype == XGEMM_BF16)
-            launch_quant<0>(p, s);
+            launch_quant<0>(p, h->cu_count, s);
         else
-            launch_quant<1>(p, s);
+            launch_quant<1>(p, h->cu_count, s);
     }
     return launch_status(h, "quant launch");
 }
