@@ -154,14 +154,17 @@ template <int DT, int R, int PL, int UN, int UK, int WN, int WK>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
     using namespace xexperts_dev;
-    if (p.slots > 0)
-        hipLaunchKernelGGL((route_up<DT, R, PL, UN, UK>), dim3(cdiv(p.I, 16 * UN), p.slots), dim3(64 * UN * UK), 0, s,
-                           p);
+    const bool odd = ((int64_t)((uintptr_t)p.up >> 1) | p.ldu | p.su) & 1;   // rows of up at 2 mod 4
+    const dim3 up_grid(cdiv(p.I, 16 * UN), p.slots), up_block(64 * UN * UK);
+    if (p.slots > 0 && odd)
+        hipLaunchKernelGGL((route_up<DT, R, PL, UN, UK, true>), up_grid, up_block, 0, s, p);
+    else if (p.slots > 0)
+        hipLaunchKernelGGL((route_up<DT, R, PL, UN, UK, false>), up_grid, up_block, 0, s, p);
     const dim3 grid(cdiv(p.H, 16 * WN), p.parts), block(64 * WN * WK);
     if (p.I % 8 == 0)
         hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 0>), grid, block, 0, s, p);
     else if constexpr (PL == 3) {   // (see experts_h_parts)
-        if (p.I > 8)
+        if (p.I > 16)
             hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 1>), grid, block, 0, s, p);
         else if constexpr (R == 64)
             hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 2>), grid, block, 0, s, p);
@@ -178,7 +181,7 @@ int experts_h_parts(bool out16, int64_t I) { return out16 && I % 8 == 0 ? 2 : 3;
 // against 212; 7 tokens, 3 of 13 of 1000 x 776: 25 against 31.)
 bool experts_own_ranges(int64_t T, int64_t top, int64_t I)
 {
-    return I >= 8 && (T <= 2 || (T <= 16 && T * top <= 32));
+    return I >= 16 && (T <= 2 || (T <= 16 && T * top <= 32));
 }
 
 // Parts that the second launch cuts the slots' inner dimensions into, of at
@@ -202,8 +205,8 @@ int experts_parts(int64_t T, int64_t top, int64_t H, int64_t I, int64_t slots, i
 template <int DT, int PL>
 void launch_experts(const ExpertsParams &p, hipStream_t s)
 {
-    // (the few inner columns below 8 are built for 64 tokens only)
-    if (p.I < 8)
+    // (few inner columns are built for 64 tokens only)
+    if (p.I < 16)
         launch_experts<DT, 64, PL, 4, 1, 4, 1>(p, s);
     else if (p.T <= 2)
         launch_experts<DT, 2, PL, 1, 8, 1, 16>(p, s);

@@ -53,6 +53,8 @@
 // as the reading: 8 of 128 of 2048 x 768 17 us for 50 MB and 12 us for 25 MB.
 #pragma once
 
+#include <type_traits>
+
 #include "decode_device.hpp"
 
 namespace xexperts_dev {
@@ -136,6 +138,52 @@ __device__ __forceinline__ float score_exp(float v, float largest)
     return v == -__builtin_inff() ? 0.0f : expf(v - largest);
 }
 
+// 16 values of a row, kept as they were loaded: at an address that is 2 mod 4 the
+// 16-byte loads begin a value earlier, in the same four bytes, and `end` is the
+// last value.  (16-byte loads at 2 mod 4 take more than twice as long as at 0 mod
+// 4.  25 tokens, 1 of 8 experts of 1855 x 3961: 175 us with them, 124 so; 7 tokens,
+// 3 of 13 of 1001 x 777 36 and 28.)
+struct Odd16 {
+    u32x4 v[2];
+    uint32_t end;
+    __device__ __forceinline__ void load(const uint16_t *p)
+    {
+        const uint16_t *const from = p - ((uintptr_t)p >> 1 & 1);
+        v[0] = load_any<u32x4>(from);
+        v[1] = load_any<u32x4>(from + 8);
+        end = p[15];
+    }
+    // moved into place, for an address that is `mis` (0 or 2) mod 4
+    __device__ __forceinline__ void align(uint32_t mis)
+    {
+        const uint32_t d[9] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3], end};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i >> 2][i & 3] = __builtin_amdgcn_alignbyte(d[i + 1], d[i], mis);
+    }
+    // moved down by n (0 .. 16) values, zeros entering at the top
+    __device__ __forceinline__ void drop(int n)
+    {
+        uint32_t d[17] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+#pragma unroll
+        for (int by = 8; by >= 1; by /= 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                d[i] = n >> 1 & by ? d[i + by] : d[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i >> 2][i & 3] = __builtin_amdgcn_alignbyte(d[i + 1], d[i], 2 * (n & 1));
+    }
+};
+
+// The piece of a row (8 k) that product d takes from lane group g, as d 4 + g:
+// with Odd16 a lane group holds 16 k in a row.
+template <bool ODD>
+__device__ __forceinline__ int piece_at(int kc)
+{
+    return ODD ? (kc & 1) * 4 + (kc >> 1) : kc;
+}
+
 __device__ __forceinline__ void sync_lds()
 {
     __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
@@ -146,8 +194,8 @@ __device__ __forceinline__ void sync_lds()
 
 // R: rows of a slot that the launch provides for (2, or a multiple of 16); PL:
 // parts of h; WN waves take 16 columns each, or (WN == 1) WK waves a range of k
-// each.
-template <int DT, int R, int PL, int WN, int WK>
+// each.  ODD: rows of weights may begin at addresses that are 2 mod 4.
+template <int DT, int R, int PL, int WN, int WK, bool ODD>
 __global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : 3)
 route_up(ExpertsParams p)
 {
@@ -278,7 +326,7 @@ route_up(ExpertsParams p)
     const uint16_t *wrow[2];
 #pragma unroll
     for (int v = 0; v < 2; ++v)
-        wrow[v] = p.up + (int64_t)expert * p.su + (int64_t)(v * p.I + min(i0 + c, p.I - 1)) * p.ldu + 8 * g;
+        wrow[v] = p.up + (int64_t)expert * p.su + (int64_t)(v * p.I + min(i0 + c, p.I - 1)) * p.ldu + (ODD ? 16 : 8) * g;
     const int64_t plane = (int64_t)p.T * p.top * p.Ip;
 
     // the products for up to RB rows
@@ -292,7 +340,7 @@ route_up(ExpertsParams p)
             const int row = (wn * 64 + lane) / PR + 64 / PR * WN * q, kc = lane % PR;
             const int r = min(row, RB - 1);
             xrow[q] = p.x + (int64_t)(sh_pair[min(r, count - 1)] / p.top) * p.ldx + 8 * kc;
-            xdst[q] = place<RB>(r, kc);
+            xdst[q] = place<RB>(r, piece_at<ODD>(kc));
         }
         f32x4 acc[MT][2];
 #pragma unroll
@@ -300,14 +348,23 @@ route_up(ExpertsParams p)
 #pragma unroll
             for (int v = 0; v < 2; ++v)
                 acc[i][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        u32x4 w[2][D][2], xr[NP];
+        static_assert(D == 2, "pieces of a unit that a lane holds");
+        struct Pieces {
+            u32x4 v[2];
+        };
+        std::conditional_t<ODD, Odd16, Pieces> w[2][2];
+        u32x4 xr[NP];
         auto store_x = [&](int buf) {
 #pragma unroll
             for (int q = 0; q < NP; ++q)
                 *(u32x4 *)(sh.x[wk][buf] + xdst[q]) = xr[q];
         };
-        auto compute = [&](const u32x4 (&from)[D][2], int buf) {
+        auto compute = [&](auto (&from)[2], int buf, bool loaded = true) __attribute__((always_inline)) {
             const char *const xs = sh.x[wk][buf];
+            if constexpr (ODD)
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+                    from[v].align(loaded ? (uint32_t)(uintptr_t)wrow[v] & 2u : 0u);
 #pragma unroll
             for (int d = 0; d < D; ++d)
 #pragma unroll
@@ -315,7 +372,7 @@ route_up(ExpertsParams p)
                     const u32x4 a = *(const u32x4 *)(xs + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
-                        acc[i][v] = mfma16<DT>(a, from[d][v], acc[i][v]);
+                        acc[i][v] = mfma16<DT>(a, from[v].v[d], acc[i][v]);
                 }
         };
         // this wave's whole units
@@ -327,13 +384,16 @@ route_up(ExpertsParams p)
             for (int q = 0; q < NP; ++q)
                 xr[q] = load_any<u32x4>(xrow[q] + k);
         };
-        auto load_w = [&](u32x4 (&to)[D][2], int t) {
+        auto load_w = [&](auto (&to)[2], int t) {
             const int k = (u0 + min(t, mine - 1)) * kUpUnit;
 #pragma unroll
             for (int v = 0; v < 2; ++v)
+                if constexpr (ODD)
+                    to[v].load(wrow[v] + k);
+                else
 #pragma unroll
-                for (int d = 0; d < D; ++d)
-                    to[d][v] = load_any<u32x4>(wrow[v] + k + 32 * d);
+                    for (int d = 0; d < D; ++d)
+                        to[v].v[d] = load_any<u32x4>(wrow[v] + k + 32 * d);
         };
         if (mine > 0) {
             load_x(0);
@@ -366,14 +426,16 @@ route_up(ExpertsParams p)
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
-                for (int d = 0; d < D; ++d)
-                    w[0][d][v] = load16_end(wrow[v] - 8 * g, 2 * (k + 32 * d + 8 * g), 2 * (int64_t)p.H);
+                for (int d = 0; d < D; ++d) {
+                    const int at = ODD ? 16 * g : 8 * g, step = ODD ? 8 * d : 32 * d;
+                    w[0][v].v[d] = load16_end(wrow[v] - at, 2 * (k + at + step), 2 * (int64_t)p.H);
+                }
             if (WN > 1)
                 sync_lds();   // (the first buffer may still be read)
             store_x(0);
             if (WN > 1)
                 sync_lds();
-            compute(w[0], 0);
+            compute(w[0], 0, false);
         }
         // h of row m (of the slot) and column col from its two sums
         auto finish = [&](int m, int col, float gate, float lift) {
@@ -443,8 +505,9 @@ route_up(ExpertsParams p)
 
 // R, PL: as above.  WN waves take 16 columns each of the same range, or (WN ==
 // 1) WK waves a range each.  END: 0 for I a multiple of 8, where a piece of a row
-// past I is the row's last one again (h is zero there); 1: a piece that ends
-// inside is the row's last 8, moved into place; 2: for I below 8.
+// past I is the row's last one again (h is zero there); 1: rows of any alignment
+// and a last unit that ends inside, whose lanes load the row's last 16 and move
+// them into place; 2: for I below 16.
 template <int DT, int R, int PL, int WN, int WK, int END>
 __global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : R == 32 ? 2 : 1)
 down_sum(ExpertsParams p)
@@ -540,7 +603,7 @@ down_sum(ExpertsParams p)
             const int piece = min(wn * 64 + lane + q * 64 * WN, PIECES - 1);
             const int kc = piece & 7, row = (piece >> 3) % RB, pl = (piece >> 3) / RB;
             hrow[q] = p.h + pl * plane + (int64_t)sh_pairs[start + min(row, count - 1)] * p.Ip + 8 * kc;
-            hdst[q] = pl * HB + place<RB>(row, kc);
+            hdst[q] = pl * HB + place<RB>(row, piece_at<END == 1>(kc));
         }
         f32x4 acc[MT][SUMS];
 #pragma unroll
@@ -548,23 +611,30 @@ down_sum(ExpertsParams p)
 #pragma unroll
             for (int q = 0; q < SUMS; ++q)
                 acc[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        u32x4 w[2][2], hr[NP];
+        struct Pieces {
+            u32x4 v[2];
+        };
+        std::conditional_t<END == 1, Odd16, Pieces> w[2];
+        u32x4 hr[NP];
         auto load_h = [&](int t) {
             const int k = (first + min(t, len - 1)) * kDownUnit;
 #pragma unroll
             for (int q = 0; q < NP; ++q)
                 hr[q] = *(const u32x4 *)(hrow[q] + k);
         };
-        auto load_w = [&](u32x4 (&to)[2], int t) {
+        auto load_w = [&](auto &to, int t) {
             const int k = (first + min(t, len - 1)) * kDownUnit;
+            if constexpr (END == 1)
+                to.load(wrow + min(k + 16 * g, p.I - 16));
+            else
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-                const int at = k + 32 * d + 8 * g;
-                if constexpr (END == 2)
-                    to[d] = load16_end(wrow, 2 * (int64_t)at, 2 * (int64_t)p.I);
-                else
-                    to[d] = load_any<u32x4>(wrow + min(at, p.I - 8));
-            }
+                for (int d = 0; d < 2; ++d) {
+                    const int at = k + 32 * d + 8 * g;
+                    if constexpr (END == 2)
+                        to.v[d] = load16_end(wrow, 2 * (int64_t)at, 2 * (int64_t)p.I);
+                    else
+                        to.v[d] = load_any<u32x4>(wrow + min(at, p.I - 8));
+                }
         };
         load_h(0);
         load_w(w[0], 0);
@@ -577,12 +647,12 @@ down_sum(ExpertsParams p)
             load_h(t + 1);
             if (WN > 1)
                 sync_lds();
-            if (END == 1 && first + t == chunks - 1)
-#pragma unroll
-                for (int d = 0; d < 2; ++d) {
-                    const int at = (chunks - 1) * kDownUnit + 32 * d + 8 * g;
-                    w[B][d] = shift_down(w[B][d], 2 * min(max(at - (p.I - 8), 0), 8));
-                }
+            if constexpr (END == 1) {
+                const int at = (first + t) * kDownUnit + 16 * g, from = min(at, p.I - 16);
+                w[B].align((uint32_t)(uintptr_t)(wrow + from) & 2u);
+                if (first + t == chunks - 1)
+                    w[B].drop(min(at - from, 16));
+            }
 #pragma unroll
             for (int d = 0; d < 2; ++d)
 #pragma unroll
@@ -592,7 +662,7 @@ down_sum(ExpertsParams p)
                         const u32x4 a =
                             *(const u32x4 *)(hs + q * HB + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
                         f32x4 &sum = acc[i][SUMS == 1 ? 0 : q];
-                        sum = mfma16<DT>(a, w[B][d], sum);
+                        sum = mfma16<DT>(a, w[B].v[d], sum);
                     }
             load_w(w[B], t + 2);
         };
