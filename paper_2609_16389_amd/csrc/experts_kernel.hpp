@@ -689,7 +689,9 @@ down_sum(ExpertsParams p)
                         v = 0x1p12f * (v + 0x1p-11f * acc[i][1][r]);
                     if constexpr (SUMS == 3)
                         v = 0x1p12f * (v + 0x1p-11f * (acc[i][1][r] + 0x1p-11f * acc[i][2][r]));
-                    mine[t * 16 + c] += sh_weight[pair] * v;
+                    // (no weight: nothing of what came out, were it infinite or NaN)
+                    const float weight = sh_weight[pair];
+                    mine[t * 16 + c] += weight == 0.0f ? 0.0f : weight * v;
                 }
             }
     };

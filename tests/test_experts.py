@@ -111,6 +111,27 @@ def test_masked_scores(T, renormalize):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 3, 12, 50])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_without_weight_nothing_counts(T, renormalize):
+    """A choice whose score is -inf adds nothing, whatever its expert or the
+    token hold."""
+    inf = float("inf")
+    args = make(T, 9, 64, 48, "bf16", 15)
+    args[1][:, 2:] = -inf                                  # two experts left, three wanted:
+    clean = xg.experts(*args, 3, renormalize)              # the third is expert 2
+    args[3][2] = float("nan")
+    args[2][2] = inf
+    assert torch.equal(xg.experts(*args, 3, renormalize), clean)
+    args[0][T // 2] = float("nan")                         # a padded token
+    args[1][T // 2] = -inf
+    y = xg.experts(*args, 3, renormalize)
+    assert torch.all(y[T // 2] == 0)
+    keep = [t for t in range(T) if t != T // 2]
+    assert torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [3, 50])
 def test_a_nan_stays_in_its_row(T):
     args = make(T, 9, 64, 48, "bf16", 6)
