@@ -630,7 +630,7 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
  *   y, ldy       T x H values of the type that `out` names; must not overlap
  *                the inputs
  * A score of -inf gives its expert no weight; a token whose chosen scores are
- * all -inf gets a row of zeros; a NaN among a token's scores (it counts as the
+ * all -inf gets a row of zeros, whatever x holds; a NaN among a token's scores (it counts as the
  * largest) makes its row NaN.  h is kept to 24 bits for an output in fp32, to 16
  * or more for one in 16 bits (with XGEMM_FP16: |h| up to 2.6e8, resolved to
  * 2^-34 and 2^-23).  Uses the handle's workspace: 6 bytes (4 for a 16-bit output)

@@ -150,6 +150,12 @@ struct QuantLds {
 // order, so one that may or may not have been issued would make every wait
 // behind it a wait for all: the loop's loads are unconditional, past the end
 // they repeat the last unit's, and the unit that K ends in comes after it.
+//
+// With WN == 1 a wave alone writes and reads its x, and always its scales: its
+// LDS accesses complete in order, and the compiler keeps those of one array at
+// places it cannot tell apart in order, so there is no barrier between them.
+// (A fence at wavefront scope there moves the loads too: 5 x 4097 x 2047 8.3 us
+// without, 11.1 with.)
 template <int DT, int R, int WN, int WK, int CT, int BL, int GS, class off_t>
 __global__ void __launch_bounds__(64 * WN * WK, R < 16 || WN * WK > 8 ? 4 : 2)
 quant_kernel(QuantParams p)
