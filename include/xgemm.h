@@ -109,15 +109,17 @@ typedef struct xgemm_config {
 int xgemm_create(xgemm_handle_t *out);
 
 /*
- * Release a handle, its workspace and its event.  NULL is accepted (no-op).
+ * Release a handle, its workspaces and its event.  NULL is accepted (no-op).
  * Work that uses the handle's workspace must have completed (synchronize
- * the streams it was enqueued on first).
+ * the streams it was enqueued on first), and a graph that recorded such work
+ * must not be launched any more.
  */
 int xgemm_destroy(xgemm_handle_t h);
 
 /*
  * Cap the device memory the handle's workspace may hold at `bytes` (0, the
- * default: no cap).  A later call that needs a larger workspace returns
+ * default: no cap; the workspaces of recorded calls, below, each keep the same
+ * cap).  A later call that needs a larger workspace returns
  * XGEMM_ERR_ALLOC and enqueues nothing, as when hipMalloc fails; a
  * workspace already larger than the cap is kept.  A call that fits the cap
  * runs as it would without one; where its launch (xgemm_launch_config) does
@@ -166,7 +168,18 @@ int xgemm_set_persistent(xgemm_handle_t h, int enable);
  * finish its work (hipDeviceSynchronize, so not inside a graph capture);
  * from then on each such call records an event on its stream and the next
  * one on another stream makes its stream wait for it.  A buffer being grown
- * is freed only after its last user has completed.  Calls on different
+ * is freed only after its last user has completed.
+ *   Calls that a stream capture records into a graph have a workspace of
+ * their own, which replays use and other calls do not.  It is kept until the
+ * handle is destroyed, and grown for a later capture by adding a larger one.
+ * Most captures forbid hipMalloc, so it is the buffer of the handle's earlier
+ * calls that is handed over to the first recorded one: make the call once
+ * before the capture, with the same handle (a recorded call that finds
+ * none large enough and cannot allocate returns XGEMM_ERR_ALLOC).  What is
+ * left to the program: work that the handle's calls enqueued before the
+ * capture has completed when the graph is launched, and launches of graphs
+ * that recorded calls of one handle do not overlap in time.
+ *   Calls on different
  * streams run concurrently only with one handle per stream.  A handle must not be used by two host threads at
  * once.  The configuration comes from the problem shape, the operands' layout
  * and the device's CU count (xgemm_select_band: one plan, or a body and a band
@@ -567,7 +580,8 @@ int xgemv_trace_workgroup(int64_t M, int64_t K, const float *A, int64_t lda, con
  * Matrices are row-major with leading dimensions in elements.  Sums, softmax
  * statistics and gradients are held in fp32 and rounded once, to the type of
  * the output.  Every sum has a fixed order: a call gives the same bits each
- * time.
+ * time.  They may be captured into a graph, under the rules for recorded calls
+ * at xgemm_run where they use the workspace.
  */
 
 /* Type of an output: fp32, or the type of the call's 16-bit inputs. */

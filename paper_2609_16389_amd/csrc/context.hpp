@@ -6,14 +6,30 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <vector>
+
 #include "xgemm.h"
+
+struct Workspace {
+    void *p;
+    size_t bytes;
+};
 
 struct xgemm_ctx {
     int device;
     int cu_count;
+    // The workspace of the call being enqueued: that of calls which run at
+    // once, or that of calls which a stream capture records.  A recorded call
+    // keeps its workspace's address for every replay, so that buffer is never
+    // freed before the handle is (one that a larger call replaces is kept in
+    // ws_old), and calls that run at once have a buffer of their own, whatever
+    // stream a graph is replayed on.
     void *workspace;
-    size_t ws_bytes;
-    // Calls that share the workspace never overlap, whichever streams they
+    Workspace ws_direct, ws_record;
+    std::vector<void *> ws_old;
+    bool recording;         // `workspace` is ws_record's
+    bool record_clears;     // ws_record was allocated within a capture: each recorded call clears its counters
+    // Direct calls that share the workspace never overlap, whichever streams they
     // are enqueued on.  While a handle's calls all come on one stream, the
     // stream's order is enough and nothing is recorded (an event record
     // between two GEMMs leaves the GPU idle for about 10 us).  The first
@@ -21,7 +37,8 @@ struct xgemm_ctx {
     // stream may no longer exist), and from then on every call records
     // ws_event on its stream after its last launch, and a call on another
     // stream makes its stream wait for that event.  The workspace is only
-    // freed (to grow it) once its last user has completed.
+    // freed (to grow it) once its last user has completed.  Recorded calls take
+    // no part in this: their graphs' replays are ordered by the program.
     hipEvent_t ws_event;
     hipStream_t ws_stream;  // stream of the last call that used the workspace
     bool ws_used;           // ws_stream is set
@@ -46,8 +63,9 @@ constexpr int64_t kMaxDim = (int64_t)1 << 31;
 
 __attribute__((visibility("hidden"))) void set_error(xgemm_ctx *h, const char *what, hipError_t e);
 
-// Make `bytes` of workspace after the counter prefix available to work
-// enqueued on stream s, and mark the end of the users just enqueued.
+// Make `bytes` of workspace after the counter prefix available at h->workspace
+// to work enqueued (or recorded) on stream s, and mark the end of the users
+// just enqueued.
 __attribute__((visibility("hidden"))) int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s);
 __attribute__((visibility("hidden"))) int release_workspace(xgemm_ctx *h, hipStream_t s);
 

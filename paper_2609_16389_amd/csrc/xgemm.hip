@@ -45,13 +45,84 @@ void set_error(xgemm_ctx *h, const char *what, hipError_t e)
         snprintf(h->last_error, sizeof(h->last_error), "%s: %s", what, hipGetErrorString(e));
 }
 
-// Make the handle's workspace usable by work enqueued next on stream s with
-// at least `bytes` after its counter prefix (it never shrinks).  Work of
-// earlier calls on other streams that used the workspace is ordered before
-// s's next work (a wait on the handle's event); a buffer being replaced is
-// freed only after that work has completed, and a new one gets its counter
-// prefix zeroed on s.  Every caller enqueues its workspace users and then
-// calls release_workspace on the same stream.
+// Whether a capture records what is enqueued on s (never the null stream).
+static bool recorded(hipStream_t s)
+{
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (s == nullptr)
+        return false;
+    if (hipStreamIsCapturing(s, &status) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    return status == hipStreamCaptureStatusActive;
+}
+
+static int allocate_workspace(xgemm_ctx *h, Workspace *ws, size_t bytes)
+{
+    const hipError_t e = hipMalloc(&ws->p, bytes);
+    if (e != hipSuccess) {
+        ws->p = nullptr;
+        (void)hipGetLastError();
+        set_error(h, "hipMalloc workspace", e);
+        return XGEMM_ERR_ALLOC;
+    }
+    ws->bytes = bytes;
+    return XGEMM_OK;
+}
+
+// A workspace's counter prefix zeroed on s.
+static int clear_prefix(xgemm_ctx *h, void *ws, hipStream_t s)
+{
+    hipLaunchKernelGGL(xgemm_dev::fill_zero, dim3(1), dim3(256), 0, s, (float *)ws, (int64_t)0, 1,
+                       (int)(kWsPrefix / sizeof(float)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {
+        set_error(h, "workspace prefix clear", e);
+        return XGEMM_ERR_HIP;
+    }
+    return XGEMM_OK;
+}
+
+// The workspace of a call that a capture on s records.  Nothing is waited for
+// and nothing freed.  A buffer of direct calls that is large enough is handed
+// over (the next direct call allocates another), since most captures forbid
+// hipMalloc; one allocated all the same has its counters cleared by the graph.
+static int acquire_recorded(xgemm_ctx *h, size_t bytes, hipStream_t s)
+{
+    if (bytes > h->ws_record.bytes) {
+        if (h->ws_old.size() == h->ws_old.capacity())
+            try {
+                h->ws_old.reserve(2 * h->ws_old.size() + 4);
+            } catch (...) {
+                return XGEMM_ERR_ALLOC;
+            }
+        Workspace next = h->ws_direct;
+        const bool clears = bytes > next.bytes;
+        if (clears) {
+            const int rc = allocate_workspace(h, &next, bytes);
+            if (rc != XGEMM_OK)
+                return rc;
+        } else {
+            h->ws_direct = Workspace{nullptr, 0};
+        }
+        if (h->ws_record.p)
+            h->ws_old.push_back(h->ws_record.p);
+        h->ws_record = next;
+        h->record_clears = clears;
+    }
+    h->workspace = h->ws_record.p;
+    h->recording = true;
+    return h->record_clears ? clear_prefix(h, h->workspace, s) : XGEMM_OK;
+}
+
+// Make a workspace usable by work enqueued next on stream s with at least
+// `bytes` after its counter prefix (it never shrinks).  Work of earlier calls
+// on other streams that used the handle's workspace is ordered before s's next
+// work (a wait on the handle's event); a buffer being replaced is freed only
+// after that work has completed, and a new one gets its counter prefix zeroed
+// on s.  Every caller enqueues its workspace users and then calls
+// release_workspace on the same stream.
 int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s)
 {
     hipError_t e;
@@ -61,6 +132,9 @@ int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s)
                  bytes, h->ws_limit);
         return XGEMM_ERR_ALLOC;
     }
+    if (recorded(s))
+        return acquire_recorded(h, bytes, s);
+    h->recording = false;
     if (h->ws_used && h->ws_stream != s) {
         // the last user is on another stream: wait for its event, or (the
         // first switch of streams, nothing recorded) for the whole device
@@ -71,41 +145,36 @@ int acquire_workspace(xgemm_ctx *h, size_t bytes, hipStream_t s)
         }
         h->ws_multi = true;
     }
-    if (bytes <= h->ws_bytes)
-        return XGEMM_OK;
-    if (h->workspace) {
-        // the last user completes before the buffer goes: its event, or this
-        // stream (the last user was on it, or the device has drained)
-        e = h->ws_recorded ? hipEventSynchronize(h->ws_event) : hipStreamSynchronize(s);
-        if (e != hipSuccess) {
-            set_error(h, "workspace drain", e);
-            return XGEMM_ERR_HIP;
+    if (bytes > h->ws_direct.bytes) {
+        if (h->ws_direct.p) {
+            // the last user completes before the buffer goes: its event, or this
+            // stream (the last user was on it, or the device has drained)
+            e = h->ws_recorded ? hipEventSynchronize(h->ws_event) : hipStreamSynchronize(s);
+            if (e != hipSuccess) {
+                set_error(h, "workspace drain", e);
+                return XGEMM_ERR_HIP;
+            }
+            (void)hipFree(h->ws_direct.p);
+            h->ws_direct = Workspace{nullptr, 0};
         }
-        (void)hipFree(h->workspace);
-        h->workspace = nullptr;
-        h->ws_bytes = 0;
+        int rc = allocate_workspace(h, &h->ws_direct, bytes);
+        if (rc != XGEMM_OK)
+            return rc;
+        if ((rc = clear_prefix(h, h->ws_direct.p, s)) != XGEMM_OK) {
+            (void)hipFree(h->ws_direct.p);
+            h->ws_direct = Workspace{nullptr, 0};
+            return rc;
+        }
     }
-    e = hipMalloc(&h->workspace, bytes);
-    if (e != hipSuccess) {
-        h->workspace = nullptr;
-        (void)hipGetLastError();
-        set_error(h, "hipMalloc workspace", e);
-        return XGEMM_ERR_ALLOC;
-    }
-    h->ws_bytes = bytes;
-    hipLaunchKernelGGL(xgemm_dev::fill_zero, dim3(1), dim3(256), 0, s, (float *)h->workspace, (int64_t)0, 1,
-                       (int)(kWsPrefix / sizeof(float)));
-    e = hipGetLastError();
-    if (e != hipSuccess) {
-        set_error(h, "workspace prefix clear", e);
-        return XGEMM_ERR_HIP;
-    }
+    h->workspace = h->ws_direct.p;
     return XGEMM_OK;
 }
 
 // Mark the end of the workspace users just enqueued on stream s.
 int release_workspace(xgemm_ctx *h, hipStream_t s)
 {
+    if (h->recording)
+        return XGEMM_OK;
     h->ws_stream = s;
     h->ws_used = true;
     h->ws_recorded = false;
@@ -2026,7 +2095,8 @@ int xgemm_create(xgemm_handle_t *out)
     h->device = dev;
     h->cu_count = prop.multiProcessorCount;
     h->workspace = nullptr;
-    h->ws_bytes = 0;
+    h->ws_direct = h->ws_record = Workspace{nullptr, 0};
+    h->recording = h->record_clears = false;
     h->ws_stream = nullptr;
     h->ws_used = false;
     h->ws_recorded = false;
@@ -2075,10 +2145,16 @@ int xgemm_destroy(xgemm_handle_t h)
     if (!h)
         return XGEMM_OK;
     int rc = XGEMM_OK;
-    if (h->workspace && hipFree(h->workspace) != hipSuccess) {
-        (void)hipGetLastError();
-        rc = XGEMM_ERR_HIP;
-    }
+    auto release = [&rc](void *p) {
+        if (p && hipFree(p) != hipSuccess) {
+            (void)hipGetLastError();
+            rc = XGEMM_ERR_HIP;
+        }
+    };
+    release(h->ws_direct.p);
+    release(h->ws_record.p);
+    for (void *p : h->ws_old)
+        release(p);
     if (hipEventDestroy(h->ws_event) != hipSuccess) {
         (void)hipGetLastError();
         rc = XGEMM_ERR_HIP;
