@@ -645,9 +645,10 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
  *                the inputs
  * A score of -inf gives its expert no weight; a token whose chosen scores are
  * all -inf gets a row of zeros, whatever x holds; a NaN among a token's scores (it counts as the
- * largest) makes its row NaN.  h is kept to 24 bits for an output in fp32, to 16
- * or more for one in 16 bits (with XGEMM_FP16: |h| up to 2.6e8, resolved to
- * 2^-34 and 2^-23).  Uses the handle's workspace: 6 bytes (4 for a 16-bit output)
+ * largest) makes its row NaN.  h is kept to fp32's 24 bits, for an output in
+ * binary16 to 23 (with XGEMM_FP16 an h below 2^-25 of the largest of the same 64
+ * inner columns has fewer: it is resolved to 2^-39 of that).  Uses the
+ * handle's workspace: 6 bytes (4 for an output in binary16, and 1/16 with XGEMM_FP16)
  * for each of min(T, 64) * top * (I rounded up to 64), 128 bytes for each of
  * min(T, 64) * H and of the experts in use, and some KiB.
  */

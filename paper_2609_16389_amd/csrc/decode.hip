@@ -161,19 +161,14 @@ void launch_experts(const ExpertsParams &p, hipStream_t s)
     else if (p.slots > 0)
         hipLaunchKernelGGL((route_up<DT, R, PL, UN, UK, false>), up_grid, up_block, 0, s, p);
     const dim3 grid(cdiv(p.H, 16 * WN), p.parts), block(64 * WN * WK);
+    const int lds = down_sum_lds(p.T * p.top, p.slots);
     if (p.I % 8 == 0)
-        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 0>), grid, block, 0, s, p);
-    else if constexpr (PL == 3) {   // (see experts_h_parts)
-        if (p.I > 16)
-            hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 1>), grid, block, 0, s, p);
-        else if constexpr (R == 64)
-            hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 2>), grid, block, 0, s, p);
-    }
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 0>), grid, block, lds, s, p);
+    else if (p.I > 16)
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 1>), grid, block, lds, s, p);
+    else if constexpr (R == 64)
+        hipLaunchKernelGGL((down_sum<DT, R, PL, WN, WK, 2>), grid, block, lds, s, p);
 }
-
-// 16-bit parts that h is kept in: two suffice for a 16-bit output (ragged rows
-// are built with three only)
-int experts_h_parts(bool out16, int64_t I) { return out16 && I % 8 == 0 ? 2 : 3; }
 
 // Whether the waves of a workgroup of the second launch take ranges of their
 // own (16 columns, all the tokens' h) or columns of the same range (64).
@@ -259,7 +254,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     p.Ip = (int)(cdiv(I, kPad) * kPad);
     p.renormalize = renormalize && I > 0;
     p.out16 = out == XGEMM_OUT_SAME;
-    const int PL = experts_h_parts(p.out16, I);
+    const int parts_of_h = dtype == XGEMM_FP16 && p.out16 ? 2 : 3;
     // tokens in chunks of at most kMaxTokens, each in the same workspace
     const int64_t most = std::min<int64_t>(T, kMaxTokens), most_slots = std::min(most * top, E);
     if ((double)most * (double)top * (double)p.Ip * 6.0 > 9.0e15)
@@ -273,7 +268,8 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     const size_t at_expert = take(most_slots * sizeof(int)), at_count = take(most_slots * sizeof(int));
     const size_t at_pair = take(most_slots * kMaxTokens * sizeof(uint16_t));
     const size_t at_weight = take(most * top * sizeof(float));
-    const size_t at_h = take((size_t)most * top * p.Ip * 2 * PL);
+    const size_t at_h = take((size_t)most * top * p.Ip * 2 * parts_of_h);
+    const size_t at_scale = take((size_t)most * top * (p.Ip / 16));
     const size_t at_part = take((size_t)kMaxParts * most * cdiv(H, 64) * 64 * sizeof(float));
     const int rc = xgemm_host::acquire_workspace(h, bytes, s);
     if (rc != XGEMM_OK)
@@ -284,6 +280,7 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     p.pair = (uint16_t *)(ws + at_pair);
     p.weight = (float *)(ws + at_weight);
     p.h = (uint16_t *)(ws + at_h);
+    p.scale = (int8_t *)(ws + at_scale);
     p.part = (float *)(ws + at_part);
     p.done = (int *)h->workspace;
     for (int64_t t = 0; t < T; t += kMaxTokens) {
@@ -294,9 +291,9 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
         p.scores = scores + t * lds;
         p.y = (char *)y + t * ldy * (p.out16 ? 2 : 4);
         if (dtype == XGEMM_BF16)
-            PL == 2 ? launch_experts<0, 2>(p, s) : launch_experts<0, 3>(p, s);
+            launch_experts<0, 3>(p, s);
         else
-            PL == 2 ? launch_experts<1, 2>(p, s) : launch_experts<1, 3>(p, s);
+            parts_of_h == 2 ? launch_experts<1, 2>(p, s) : launch_experts<1, 3>(p, s);
     }
     const int launched = launch_status(h, "experts launch");
     const int released = xgemm_host::release_workspace(h, s);

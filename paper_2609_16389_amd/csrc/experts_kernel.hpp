@@ -40,11 +40,16 @@
 // The second product needs h on the matrix units, which take 16 bits.  Rounded
 // to 16 bits h would lose more than the rounding of y does, so it is written as
 // 16-bit parts, and multiplied as that many products (the matrix units are
-// idle most of the time): three, which together hold its 24 bits, for a y in
-// fp32, two (16 bits of h or more) for a y that is rounded to 16 bits itself.
+// idle most of the time): three, which hold its 24 bits, or for binary16 with a
+// y of 16 bits two, which hold 23 (its y has 11; with three of them 64 tokens, 2
+// of 8 experts of 4096 x 14336 take 590 us instead of 561).
 //   bfloat16: h = a + b + c, each part the rounding of what the ones before leave.
-//   binary16, whose range is short: h = 2^12 (a + 2^-11 (b + 2^-11 c)).  This
-//   holds |h| up to 2.6e8 and resolves 2^-34 (2^-23 with two parts).
+//   binary16, whose range is short: h = 2^e (a + 2^-11 (b + 2^-11 c)), with e such
+//   that the largest h of a token's 16 columns has an a between 2^14 and 2^15.
+//   The second launch brings the four e of a unit to their largest, E, as it
+//   puts the parts in LDS, and multiplies the unit's sums by 2^E.  So h may have
+//   any size that fp32 holds.  Brought to E, the least that a resolves is 2^-39
+//   of the largest of the 64 columns, and h keeps its bits down to 2^-25 of that.
 //
 // Measured, first and second launch: 64 tokens, 2 of 8 experts of 4096 x 14336
 // (hidden x inner, every expert read) 359 us at 5.2 TB/s and 193 us at 4.9 TB/s;
@@ -86,6 +91,7 @@ struct ExpertsParams {
     uint16_t *pair;   // [slots][kMaxTokens]: token * top + choice
     float *weight;    // [T * top]: exp(score - largest), over the whole softmax's sum without renormalize
     uint16_t *h;      // [parts of h][T * top][Ip]
+    int8_t *scale;    // [T * top][Ip / 16]: e of 16 columns of h (binary16)
     float *part;      // [parts][T][H rounded up to whole workgroups], where parts > 1
     int *done;        // [workgroups of a range], zero between launches
 };
@@ -116,12 +122,12 @@ __device__ __forceinline__ uint32_t order_of(float v)
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
-// The parts of h (see above).
+// The parts of h (see above), of binary16 once it is divided by 2^e.
 template <int DT, int PL>
 __device__ __forceinline__ void split_parts(float v, uint16_t (&part)[PL])
 {
-    constexpr float down = DT == 0 ? 1.0f : 0x1p-12f, step = DT == 0 ? 1.0f : 0x1p11f;
-    float r = v * down;
+    constexpr float step = DT == 0 ? 1.0f : 0x1p11f;
+    float r = v;
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
         part[i] = from_float<DT>(r);
@@ -130,6 +136,39 @@ __device__ __forceinline__ void split_parts(float v, uint16_t (&part)[PL])
         if (!(__builtin_fabsf(got) < __builtin_inff()))   // nothing is left of what has overflowed
             r = 0.0f;
     }
+}
+
+// 2^n, n from -126 to 127.
+__device__ __forceinline__ float power2(int n) { return __builtin_bit_cast(float, (127 + n) << 23); }
+
+// e of the 16 lanes' values (a row of lanes), -112 .. 114.  (An infinity or a
+// NaN among them leaves nothing of the others, nor do they count.)
+__device__ __forceinline__ int row_exponent(float v)
+{
+    int m = __builtin_bit_cast(int, v) & 0x7fffffff;
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x128, 0xf, 0xf, false));   // row_ror 8
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x124, 0xf, 0xf, false));   // row_ror 4
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x122, 0xf, 0xf, false));   // row_ror 2
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x121, 0xf, 0xf, false));   // row_ror 1
+    return max((m >> 23) - 141, -112);
+}
+
+// Eight binary16 values times 2^-d, d >= 0.
+__device__ __forceinline__ u32x4 scale_down(u32x4 v, int d)
+{
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    auto times = [&](int n) {
+        const _Float16 f = (_Float16)power2(-n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t two = v[i];
+            v[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, two) * f16x2{f, f});
+        }
+    };
+    times(min(d, 24));   // 2^-24 is the least that binary16 holds
+    if (d > 24)
+        times(min(d - 24, 100));
+    return v;
 }
 
 // exp of a score against the largest; a score of -inf has no weight.
@@ -437,12 +476,20 @@ route_up(ExpertsParams p)
                 sync_lds();
             compute(w[0], 0, false);
         }
-        // h of row m (of the slot) and column col from its two sums
+        // h of row m (of the slot) and column col from its two sums, the 16
+        // columns of a block side by side
         auto finish = [&](int m, int col, float gate, float lift) {
-            uint16_t part[PL] = {};
-            if (col < p.I)
-                split_parts<DT>(gate / (1.0f + expf(-gate)) * lift, part);
-            uint16_t *const at = p.h + (int64_t)sh_pair[m] * p.Ip + col;
+            uint16_t part[PL];
+            const int64_t pair = sh_pair[m];
+            float v = col < p.I ? gate / (1.0f + expf(-gate)) * lift : 0.0f;
+            if constexpr (DT == 1) {
+                const int e = row_exponent(v);
+                if (c == 0)
+                    p.scale[pair * (p.Ip / 16) + (col >> 4)] = (int8_t)e;
+                v *= power2(-e);
+            }
+            split_parts<DT, PL>(v, part);
+            uint16_t *const at = p.h + pair * p.Ip + col;
 #pragma unroll
             for (int q = 0; q < PL; ++q)
                 at[q * plane] = part[q];
@@ -508,23 +555,30 @@ route_up(ExpertsParams p)
 // past I is the row's last one again (h is zero there); 1: rows of any alignment
 // and a last unit that ends inside, whose lanes load the row's last 16 and move
 // them into place; 2: for I below 16.
+//
+// LDS beyond the declared arrays: down_sum_lds(pairs, slots) bytes.  (Sized by
+// the call and not by its limits: 64 tokens and three parts then leave room for
+// two workgroups a CU.  2 of 8 experts of 4096 x 14336 590 us, with one 652.)
+__host__ __device__ constexpr int down_sum_lds(int pairs, int slots) { return 6 * pairs + 6 * slots + 2; }
+
 template <int DT, int R, int PL, int WN, int WK, int END>
 __global__ void __launch_bounds__(64 * WN * WK, R <= 16 ? 4 : R == 32 ? 2 : 1)
 down_sum(ExpertsParams p)
 {
     static_assert(WN == 1 || WK == 1, "a barrier is the whole workgroup's");
     constexpr int WAVES = WN * WK, THREADS = 64 * WAVES, TOKENS = R;
-    constexpr int SUMS = DT == 0 ? 1 : PL;   // products of the parts that are kept apart
     constexpr int BUFS = WN == 1 ? 1 : 2;
     constexpr int HB = unit_bytes<R>(kDownUnit);
     __shared__ __attribute__((aligned(16))) char sh_h[WK][BUFS][PL][HB];
+    __shared__ __attribute__((aligned(16))) float sh_scale[DT == 1 ? WK : 1][BUFS][DT == 1 ? (R + 15) / 16 * 16 : 4];
     __shared__ __attribute__((aligned(16))) float acc_all[WAVES][TOKENS * 16];
-    __shared__ float sh_weight[TOKENS * kMaxTop];
-    __shared__ uint16_t sh_slot[kMaxExperts];           // the slots in use, in ascending order,
-    __shared__ uint16_t sh_expert[kMaxExperts];         //   their experts,
-    __shared__ uint16_t sh_start[kMaxExperts + 1];      //   where their pairs start,
-    __shared__ uint16_t sh_pairs[TOKENS * kMaxTop];     //   and the pairs
     __shared__ int sh_used, sh_last;
+    extern __shared__ __attribute__((aligned(16))) char sh_more[];
+    float *const sh_weight = (float *)sh_more;                     // [T * top]
+    uint16_t *const sh_pairs = (uint16_t *)(sh_weight + p.T * p.top);   // the pairs,
+    uint16_t *const sh_slot = sh_pairs + p.T * p.top;              // the slots in use, in ascending order,
+    uint16_t *const sh_expert = sh_slot + p.slots;                 //   their experts,
+    uint16_t *const sh_start = sh_expert + p.slots;                //   where their pairs start
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wn = wave % WN, wk = wave / WN;
@@ -592,35 +646,46 @@ down_sum(ExpertsParams p)
     auto segment = [&]<int RB>(int a, int first, int len) {
         constexpr int MT = (RB + 15) / 16, PIECES = RB * 8 * PL;
         constexpr int NP = (PIECES + 64 * WN - 1) / (64 * WN);
+        // (a thread's pieces of one row, or each its own, part included)
+        constexpr int NE = NP % PL ? NP : NP / PL;
+        static_assert(NE == NP || RB * 8 == NE * 64 * WN, "a thread's pieces of a part");
         const int start = sh_start[a], count = sh_start[a + 1] - start;
         const int expert = __builtin_amdgcn_readfirstlane(sh_expert[a]);
         const uint16_t *const wrow =
             p.down + (int64_t)expert * p.sd + (int64_t)min(n0 + c, p.H - 1) * p.ldd;
-        const uint16_t *hrow[NP];
-        int hdst[NP];
+        const uint16_t *hrow[NE];
+        const int8_t *erow[NE];
+        int hdst[NE];
+        auto piece_of = [&](int q) { return min(wn * 64 + lane + q * 64 * WN, PIECES - 1); };
 #pragma unroll
-        for (int q = 0; q < NP; ++q) {
-            const int piece = min(wn * 64 + lane + q * 64 * WN, PIECES - 1);
+        for (int q = 0; q < NE; ++q) {
+            const int piece = piece_of(q);
             const int kc = piece & 7, row = (piece >> 3) % RB, pl = (piece >> 3) / RB;
-            hrow[q] = p.h + pl * plane + (int64_t)sh_pairs[start + min(row, count - 1)] * p.Ip + 8 * kc;
+            const int64_t pair = sh_pairs[start + min(row, count - 1)];
+            hrow[q] = p.h + pl * plane + pair * p.Ip + 8 * kc;
+            erow[q] = p.scale + pair * (p.Ip / 16);
             hdst[q] = pl * HB + place<RB>(row, piece_at<END == 1>(kc));
         }
-        f32x4 acc[MT][SUMS];
+        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 acc[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int q = 0; q < SUMS; ++q)
-                acc[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            acc[i] = zero;
         struct Pieces {
             u32x4 v[2];
         };
         std::conditional_t<END == 1, Odd16, Pieces> w[2];
         u32x4 hr[NP];
+        uint32_t er[NE];   // e of the unit's four blocks
         auto load_h = [&](int t) {
             const int k = (first + min(t, len - 1)) * kDownUnit;
+            if constexpr (DT == 1)
+#pragma unroll
+                for (int q = 0; q < NE; ++q)
+                    er[q] = *(const uint32_t *)(erow[q] + k / 16);
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                hr[q] = *(const u32x4 *)(hrow[q] + k);
+                hr[q] = *(const u32x4 *)(hrow[q % NE] + q / NE * plane + k);
         };
         auto load_w = [&](auto &to, int t) {
             const int k = (first + min(t, len - 1)) * kDownUnit;
@@ -640,10 +705,27 @@ down_sum(ExpertsParams p)
         load_w(w[0], 0);
         load_w(w[1], 1);
         auto step = [&]<int B>(int t) {
-            char *const hs = sh_h[wk][BUFS == 1 ? 0 : B][0];
+            constexpr int buf = BUFS == 1 ? 0 : B;
+            char *const hs = sh_h[wk][buf][0];
+            if constexpr (DT == 1)
+#pragma unroll
+                for (int q = 0; q < NE; ++q) {
+                    const int piece = piece_of(q);
+                    const int E = max(max((int)(int8_t)er[q], (int)(int8_t)(er[q] >> 8)),
+                                      max((int)(int8_t)(er[q] >> 16), (int)er[q] >> 24));
+                    const int d = E - (int)(int8_t)(er[q] >> (4 * (piece & 6)));
+#pragma unroll
+                    for (int i = q; i < NP; i += NE)
+                        hr[i] = scale_down(hr[i], d);
+                    // (every lane writes its row's: one that did not would be
+                    // taken to read what it read before)
+                    sh_scale[wk][buf][(piece >> 3) % RB] = power2(E);
+                }
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                *(u32x4 *)(hs + hdst[q]) = hr[q];
+                *(u32x4 *)(hs + q / NE * HB + hdst[q % NE]) = hr[q];
+            if constexpr (DT == 1 && END == 1)
+                __builtin_amdgcn_sched_barrier(0);   // (weights moved into place before this would not fit)
             load_h(t + 1);
             if (WN > 1)
                 sync_lds();
@@ -653,17 +735,40 @@ down_sum(ExpertsParams p)
                 if (first + t == chunks - 1)
                     w[B].drop(min(at - from, 16));
             }
+            f32x4 part[MT][DT == 1 ? PL : 1];   // the parts' sums over this unit
+            // (16 rows or fewer, columns of one range: all of h is read before the
+            // first product, or each would wait for its own read.  16 tokens, 6 of
+            // 64 of 2048 x 1408: 172 us, 181 without.)
+            u32x4 ha[2][MT][PL];
 #pragma unroll
-            for (int d = 0; d < 2; ++d)
+            for (int o = 0; o < 2 * MT * PL; ++o) {
+                const int d = o / (MT * PL), i = o / PL % MT, q = o % PL;
+                ha[d][i][q] =
+                    *(const u32x4 *)(hs + q * HB + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
+            }
+            if constexpr (MT == 1 && WN > 1)
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+            for (int o = 0; o < 2 * MT * PL; ++o) {
+                const int d = o / (MT * PL), i = o / PL % MT, q = o % PL;
+                if constexpr (DT == 1)
+                    part[i][q] = mfma16<DT>(ha[d][i][q], w[B].v[d], d == 0 ? zero : part[i][q]);
+                else
+                    acc[i] = mfma16<DT>(ha[d][i][q], w[B].v[d], acc[i]);
+            }
+            if constexpr (DT == 1)
 #pragma unroll
-                    for (int q = 0; q < PL; ++q) {
-                        const u32x4 a =
-                            *(const u32x4 *)(hs + q * HB + place<RB>(RB < 16 ? min(c, RB - 1) : 16 * i + c, 4 * d + g));
-                        f32x4 &sum = acc[i][SUMS == 1 ? 0 : q];
-                        sum = mfma16<DT>(a, w[B].v[d], sum);
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 scale = *(const f32x4 *)&sh_scale[wk][buf][16 * i + 4 * g];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float sum = part[i][PL - 1][r];
+#pragma unroll
+                        for (int q = PL - 2; q >= 0; --q)
+                            sum = fmaf(0x1p-11f, sum, part[i][q][r]);
+                        acc[i][r] = fmaf(scale[r], sum, acc[i][r]);
                     }
+                }
             load_w(w[B], t + 2);
         };
         for (int t = 0;;) {
@@ -684,11 +789,7 @@ down_sum(ExpertsParams p)
                 const int m = 16 * i + 4 * g + r;
                 if (m < count) {
                     const int pair = sh_pairs[start + m], t = pair / p.top;
-                    float v = acc[i][0][r];
-                    if constexpr (SUMS == 2)
-                        v = 0x1p12f * (v + 0x1p-11f * acc[i][1][r]);
-                    if constexpr (SUMS == 3)
-                        v = 0x1p12f * (v + 0x1p-11f * (acc[i][1][r] + 0x1p-11f * acc[i][2][r]));
+                    const float v = acc[i][r];
                     // (no weight: nothing of what came out, were it infinite or NaN)
                     const float weight = sh_weight[pair];
                     mine[t * 16 + c] += weight == 0.0f ? 0.0f : weight * v;
