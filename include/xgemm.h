@@ -702,7 +702,11 @@ int xgemm_logprob_run(xgemm_handle_t h, int64_t R, int64_t V, const void *logits
  *                         the same leading dimension), must not overlap it
  *                         otherwise
  * A row whose lse is below -1e37 (nothing in it but -inf or the lowest value of
- * fp32 or bfloat16: every token masked) gets zeros.  Uses no workspace.
+ * fp32 or bfloat16: every token masked) gets zeros.  p = exp(x - lse) holds lse's
+ * own rounding, a relative |lse| 2^-24, as long as |lse| is below 256 (fp32) or
+ * 1024 (16 bits); beyond, the call sums the row again and p is right whatever the
+ * size of lse (a row of nothing but -1e9: 1 / V), in about twice the time for many
+ * rows.  Uses no workspace.
  */
 int xgemm_logprob_grad(xgemm_handle_t h, int64_t R, int64_t V, const void *logits, int64_t ldl, const int64_t *targets,
                        const float *lse, const float *entropy, const float *d_logprob, const float *d_entropy,

@@ -408,9 +408,13 @@ int run_logprob_grad(xgemm_ctx *h, int64_t R, int64_t V, const void *logits, int
     p.ld = ldl;
     p.ldo = ldd;
     p.V = (int)V;
+    // (a workgroup that sums its row takes up to 8 spans, as many as leave 4
+    // workgroups a CU: one row of 131072 fp32 12 us, in one workgroup 35)
+    const int64_t spans = cdiv(V, kGradSpan), shared = R * spans / (4 * std::max(h->cu_count, 1));
+    p.group = (int)(dlogits == logits ? spans : std::min<int64_t>(std::max<int64_t>(shared, 1), 8));
     for (int64_t r = 0; r < R; r += kGridRows) {
         p.row0 = r;
-        const dim3 grid(cdiv(V, kGradSpan), (unsigned)std::min(kGridRows, R - r)), block(kGradThreads);
+        const dim3 grid(spans, (unsigned)std::min(kGridRows, R - r)), block(kGradThreads);
         if (dtype == XGEMM_BF16)
             hipLaunchKernelGGL(logprob_grad<0>, grid, block, 0, s, p);
         else if (dtype == XGEMM_FP16)

@@ -477,21 +477,37 @@ struct GradParams {
     int64_t ld, ldo;  // elements
     int64_t row0;
     int V;
+    int group;        // spans that one workgroup takes where it sums a row itself
 };
 
 // dx = d_logprob (delta - p) - d_entropy p (log p + entropy) + d_lse p, with
 // log p = x - lse: a read and a write of every logit, the bytes of which bound
 // it (2048 rows of 131072 bfloat16: 172 us, 6.2 TB/s read and written).  A
-// workgroup takes kGradSpan values of one row.
+// workgroup takes a span of kGradSpan values of one row.
+//
+// A large lse is held too coarsely for this: p is off by a relative |lse| 2^-24,
+// and a row of nothing but -1e9 has lse = x and a p of 1.  From coarse_lse() on
+// a workgroup forms Z = sum of exp(x - lse) over its row, which is 1 but for the
+// rounding of lse, and takes log Z off log p.  (Below, the rounding leaves at
+// most 2^-17 in p for fp32 and 2^-15, an eighth of binary16's, for 16 bits.)  One
+// workgroup then takes `group` spans, so that a row is read group times less
+// often; into the logits themselves one takes the whole row, or it would read what
+// others have written.  2048 rows of 131072 bfloat16 at -3000: 335 us, with one span
+// a workgroup 1408, a whole row 345.  A Z that rounding does not explain is not this row's sum (a row that is
+// part of a longer one), and is left alone.
 constexpr int kGradThreads = 256, kGradSpan = kGradThreads * 8 * 2;
+template <int DT>
+constexpr float coarse_lse()
+{
+    return DT == 2 ? 256.0f : 1024.0f;
+}
 
 template <int DT>
-__global__ void __launch_bounds__(kGradThreads)
+__global__ void __launch_bounds__(kGradThreads, 8)
 logprob_grad(GradParams p)
 {
     constexpr int VEC = DT == 2 ? 4 : 8, UN = kGradSpan / (kGradThreads * VEC);
     const int64_t row = p.row0 + blockIdx.y;
-    const int v0 = blockIdx.x * kGradSpan;
     const int bytes = DT == 2 ? 4 : 2;
     const void *const x = (const char *)p.logits + row * p.ld * bytes;
     char *const y = (char *)p.out + row * p.ldo * bytes;
@@ -504,52 +520,105 @@ logprob_grad(GradParams p)
     const float c2 = p.d_entropy ? p.d_entropy[row] : 0.0f;
     const float c1 = gl - (p.d_lse ? p.d_lse[row] : 0.0f) + (p.d_entropy ? c2 * p.entropy[row] : 0.0f);
 
-    float v[UN][VEC];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-        const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
+    // VEC values from index `at`
+    auto load = [&](int at, float (&v)[VEC], float past) {
         if (at + VEC <= p.V) {
-            convert<DT, VEC>(load_raw<DT>(x, at), v[u]);
+            convert<DT, VEC>(load_raw<DT>(x, at), v);
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                v[u][e] = at + e < p.V ? load_value<DT>(x, at + e) : 0.0f;
+                v[e] = at + e < p.V ? load_value<DT>(x, at + e) : past;
         }
-    }
+    };
+    // one span; off: log Z, where FINE
+    auto span = [&]<bool FINE>(int v0, float off) __attribute__((always_inline)) {
+        float v[UN][VEC];
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-        const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
+        for (int u = 0; u < UN; ++u)
+            load(v0 + (u * kGradThreads + (int)threadIdx.x) * VEC, v[u], 0.0f);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float t = v[u][e] - lse;
-            const float q = __builtin_amdgcn_exp2f(t * kLog2e);
-            float d = -q * fmaf(c2, fmaxf(t, kLowest), c1);
-            if (at + e == target)
-                d += gl;
-            v[u][e] = empty ? 0.0f : d;
-        }
-        if (at + VEC <= p.V) {
-            if constexpr (DT == 2) {
-                f32x4 o = {v[u][0], v[u][1], v[u][2], v[u][3]};
-                store_any<f32x4>(y + (int64_t)at * 4, o);
-            } else {
-                u32x4 o;
+        for (int u = 0; u < UN; ++u) {
+            const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[e] = from_float<DT>(v[u][2 * e]) | (uint32_t)from_float<DT>(v[u][2 * e + 1]) << 16;
-                store_any<u32x4>(y + (int64_t)at * 2, o);
+            for (int e = 0; e < VEC; ++e) {
+                const float t = FINE ? (v[u][e] - lse) - off : v[u][e] - lse;
+                const float q = __builtin_amdgcn_exp2f(t * kLog2e);
+                float d = -q * fmaf(c2, fmaxf(t, kLowest), c1);
+                if (at + e == target)
+                    d += gl;
+                v[u][e] = empty ? 0.0f : d;
             }
-        } else {
+            if (at + VEC <= p.V) {
+                if constexpr (DT == 2) {
+                    f32x4 o = {v[u][0], v[u][1], v[u][2], v[u][3]};
+                    store_any<f32x4>(y + (int64_t)at * 4, o);
+                } else {
+                    u32x4 o;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (at + e < p.V) {
-                    if constexpr (DT == 2)
-                        ((float *)y)[at + e] = v[u][e];
-                    else
-                        ((uint16_t *)y)[at + e] = from_float<DT>(v[u][e]);
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = from_float<DT>(v[u][2 * e]) | (uint32_t)from_float<DT>(v[u][2 * e + 1]) << 16;
+                    store_any<u32x4>(y + (int64_t)at * 2, o);
                 }
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (at + e < p.V) {
+                        if constexpr (DT == 2)
+                            ((float *)y)[at + e] = v[u][e];
+                        else
+                            ((uint16_t *)y)[at + e] = from_float<DT>(v[u][e]);
+                    }
+            }
+        }
+    };
+
+    const float size = __builtin_fabsf(lse);
+    if (empty || !(size >= coarse_lse<DT>() && size < __builtin_inff())) {
+        span.template operator()<false>(blockIdx.x * kGradSpan, 0.0f);
+        return;
+    }
+    // (the workgroup of a group that does the work differs from row to row:
+    // workgroups go to the XCDs in turn)
+    const int first = blockIdx.x - blockIdx.x % p.group, spans = min(p.group, (int)gridDim.x - first);
+    if ((int)blockIdx.x - first != (int)(row % spans))
+        return;
+    float Z = 0.0f;
+    auto add = [&](const float (&v)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            Z += __builtin_amdgcn_exp2f((v[e] - lse) * kLog2e);
+    };
+    constexpr int kLoads = 4, kPass = kGradThreads * VEC;
+    int64_t at = threadIdx.x * VEC;
+    for (; at + (kLoads - 1) * kPass + VEC <= p.V; at += kLoads * kPass) {
+        u32x4 raw[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+            raw[u] = load_raw<DT>(x, at + u * kPass);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            float v[VEC];
+            convert<DT, VEC>(raw[u], v);
+            add(v);
         }
     }
+    for (; at < p.V; at += kPass) {
+        float v[VEC];
+        load((int)at, v, -__builtin_inff());
+        add(v);
+    }
+    __shared__ float sums[kGradThreads / 64];
+    Z = wave_sum(Z);
+    if ((threadIdx.x & 63) == 0)
+        sums[threadIdx.x >> 6] = Z;
+    __syncthreads();
+    Z = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    float off = logf(Z);
+    if (!(__builtin_fabsf(off) <= size * 0x1p-23f))
+        off = 0.0f;
+#pragma unroll 1
+    for (int i = first; i < first + spans; ++i)
+        span.template operator()<true>(i * kGradSpan, off);
 }
 
 }  // namespace xlogprob_dev
