@@ -614,7 +614,9 @@ enum xgemm_out {
  * fp32, so the error against exact arithmetic on the stored values is some
  * 2^-24 of sum |x s (16 + q)| times the length of the sums, before the
  * output's rounding.  A NaN or an infinity in a row of x makes that row of y
- * NaN.
+ * NaN (an infinity too, whose products would be infinite by the formula).  With
+ * XGEMM_BF16 x and y may be as large as their types, but below 2^-110 they may
+ * count as zero.
  */
 int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const uint8_t *q,
                     int64_t ldq, const void *scales, int64_t lds, const uint8_t *zeros, int64_t ldz, int64_t group,

@@ -12,6 +12,9 @@
 // in fp32, and the group adds s (P - (16 + z) S) to the output.  (16 and not a
 // larger power of two: the part that cancels is 24 on average against |q - 8|
 // of 4, which costs two bits of fp32; 128 + q would cost five.)
+// bfloat16 reaches as far as fp32, so that 128 products x (16 + q), or x 271 with
+// the largest z, would leave fp32's range for an x of 1e35: there the weights,
+// and the ones, are held times 2^-16, and the output is multiplied by 2^16.
 //
 // Layout: the weights are the matrix units' second operand, lane l holding
 // column n = l % 16, so that a lane needs one scale a group.  A wave takes a
@@ -67,11 +70,12 @@ __device__ __forceinline__ Masks masks()
 {
     Masks m;
     asm("v_mov_b32 %0, %1" : "=v"(m.mask) : "i"(DT == 0 ? 0x00780078u : 0x03c003c0u));
-    asm("s_mov_b32 %0, %1" : "=s"(m.base) : "i"(DT == 0 ? 0x41804180u : 0x4c004c00u));
+    asm("s_mov_b32 %0, %1" : "=s"(m.base) : "i"(DT == 0 ? 0x39803980u : 0x4c004c00u));
     return m;
 }
 
-// Two weights of a dword as 16-bit floats 16 + q: values I and I + 4.
+// Two weights of a dword as 16-bit floats 16 + q (bfloat16: times 2^-16): values
+// I and I + 4.
 template <int DT, int I>
 __device__ __forceinline__ uint32_t widen2(uint32_t w, Masks m)
 {
@@ -262,7 +266,7 @@ quant_kernel(QuantParams p)
     };
 
     const Masks widen = masks<DT>();
-    const uint32_t one = DT == 0 ? 0x3f803f80u : 0x3c003c00u;
+    const uint32_t one = DT == 0 ? 0x37803780u : 0x3c003c00u;   // (bfloat16: 2^-16)
     const u32x4 ones = {one, one, one, one};
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     f32x4 acc[CT][MT];
@@ -382,6 +386,8 @@ quant_kernel(QuantParams p)
 #pragma unroll
         for (int w = 1; w < WK; ++w)
             v += sh.red[w][j][i][o & 255];
+        if (DT == 0)
+            v *= 0x1p16f;
         const int64_t at = (int64_t)(m0 + row) * p.ldy + n;
         if (p.out16)
             ((uint16_t *)p.y)[at] = from_float<DT>(v);
