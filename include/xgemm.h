@@ -651,8 +651,10 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
  * binary16 to 23 (with XGEMM_FP16 an h below 2^-25 of the largest of the same 64
  * inner columns has fewer: it is resolved to 2^-39 of that).  Uses the
  * handle's workspace: 6 bytes (4 for an output in binary16, and 1/16 with XGEMM_FP16)
- * for each of min(T, 64) * top * (I rounded up to 64), 128 bytes for each of
- * min(T, 64) * H and of the experts in use, and some KiB.
+ * for each of min(T, 64) * top * (I rounded up to 64), up to 128 bytes for each
+ * of min(T, 64) * H (4 for each of the parts, up to 32, that the experts' inner
+ * columns are cut into, none for one) and 128 for each of the experts in use,
+ * and some KiB.
  */
 #define XGEMM_EXPERTS_MAX 1024
 #define XGEMM_EXPERTS_MAX_TOP 32

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 using xgemm_host::kMaxDim;
 
@@ -269,8 +270,17 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     const size_t at_pair = take(most_slots * kMaxTokens * sizeof(uint16_t));
     const size_t at_weight = take(most * top * sizeof(float));
     const size_t at_h = take((size_t)most * top * p.Ip * 2 * parts_of_h);
-    const size_t at_scale = take((size_t)most * top * (p.Ip / 16));
-    const size_t at_part = take((size_t)kMaxParts * most * cdiv(H, 64) * 64 * sizeof(float));
+    const size_t at_scale = take(dtype == XGEMM_FP16 ? (size_t)most * top * (p.Ip / 16) : 0);
+    // partial sums of the chunk that has the most of them: a full one or the last
+    auto chunk = [&](int64_t tokens) {
+        const int64_t slots = I > 0 ? std::min(tokens * top, E) : 0;   // (without inner columns y is zero)
+        return std::pair<int64_t, int64_t>(slots, experts_parts(tokens, top, H, I, slots, p.Ip, h->cu_count));
+    };
+    size_t sums = 0;
+    for (const int64_t tokens : {most, (T - 1) % kMaxTokens + 1})
+        if (const int64_t parts = chunk(tokens).second; parts > 1)
+            sums = std::max(sums, (size_t)(parts * tokens * cdiv(H, 64) * 64) * sizeof(float));
+    const size_t at_part = take(sums);
     const int rc = xgemm_host::acquire_workspace(h, bytes, s);
     if (rc != XGEMM_OK)
         return rc;
@@ -285,8 +295,9 @@ int run_experts(xgemm_ctx *h, int64_t T, int64_t E, int64_t top, int64_t H, int6
     p.done = (int *)h->workspace;
     for (int64_t t = 0; t < T; t += kMaxTokens) {
         p.T = (int)std::min<int64_t>(kMaxTokens, T - t);
-        p.slots = I > 0 ? (int)std::min<int64_t>(p.T * top, E) : 0;   // (without inner columns y is zero)
-        p.parts = experts_parts(p.T, top, H, I, p.slots, p.Ip, h->cu_count);
+        const auto [slots, parts] = chunk(p.T);
+        p.slots = (int)slots;
+        p.parts = (int)parts;
         p.x = (const uint16_t *)x + t * ldx;
         p.scores = scores + t * lds;
         p.y = (char *)y + t * ldy * (p.out16 ? 2 : 4);
