@@ -234,11 +234,16 @@ logprob_rows(LogprobParams p)
         lane_max = fmaxf(lane_max, most);
         return most;
     };
+    // (waves renew their bounds while others read them, which changes what is set
+    // aside on the way but not the result: atomics, in no order)
+    auto set_bound = [&](uint32_t v) {
+        if (lane == 0)
+            __hip_atomic_store(&bounds[wave], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
     // this wave's bound: the `every`-th largest of its lanes' maxima
     auto renew = [&](bool bounds_any) {
         if (!bounds_any) {
-            if (lane == 0)
-                *(volatile uint32_t *)&bounds[wave] = 0xffffffffu;
+            set_bound(0xffffffffu);
             return;
         }
         uint32_t left = order_of(lane_max), most = 0;
@@ -249,14 +254,13 @@ logprob_rows(LogprobParams p)
             if (lane == __builtin_ctzll(who))
                 left = 0;
         }
-        if (lane == 0)
-            *(volatile uint32_t *)&bounds[wave] = most;
+        set_bound(most);
     };
     auto least_bound = [&] {
-        uint32_t bound = *(volatile uint32_t *)&bounds[0];
+        uint32_t bound = 0xffffffffu;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            bound = min(bound, *(volatile uint32_t *)&bounds[w]);
+        for (int w = 0; w < kWaves; ++w)
+            bound = min(bound, __hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         return bound;
     };
     // index(i): place of this lane's value i, or -1
