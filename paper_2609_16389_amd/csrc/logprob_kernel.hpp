@@ -534,12 +534,14 @@ logprob_grad(GradParams p)
                 v[e] = at + e < p.V ? load_value<DT>(x, at + e) : past;
         }
     };
-    // one span; off: log Z, where FINE
-    auto span = [&]<bool FINE>(int v0, float off) __attribute__((always_inline)) {
-        float v[UN][VEC];
+    // one span, in two steps; off: log Z, where FINE
+    float v[UN][VEC];
+    auto fetch = [&](int v0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < UN; ++u)
             load(v0 + (u * kGradThreads + (int)threadIdx.x) * VEC, v[u], 0.0f);
+    };
+    auto finish = [&]<bool FINE>(int v0, float off) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int at = v0 + (u * kGradThreads + (int)threadIdx.x) * VEC;
@@ -576,9 +578,10 @@ logprob_grad(GradParams p)
         }
     };
 
+    fetch(blockIdx.x * kGradSpan);   // (before anything waits for lse)
     const float size = __builtin_fabsf(lse);
     if (empty || !(size >= coarse_lse<DT>() && size < __builtin_inff())) {
-        span.template operator()<false>(blockIdx.x * kGradSpan, 0.0f);
+        finish.template operator()<false>(blockIdx.x * kGradSpan, 0.0f);
         return;
     }
     // (the workgroup of a group that does the work differs from row to row:
@@ -621,8 +624,10 @@ logprob_grad(GradParams p)
     if (!(__builtin_fabsf(off) <= size * 0x1p-23f))
         off = 0.0f;
 #pragma unroll 1
-    for (int i = first; i < first + spans; ++i)
-        span.template operator()<true>(i * kGradSpan, off);
+    for (int i = first; i < first + spans; ++i) {
+        fetch(i * kGradSpan);
+        finish.template operator()<true>(i * kGradSpan, off);
+    }
 }
 
 }  // namespace xlogprob_dev
