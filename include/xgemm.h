@@ -645,6 +645,8 @@ int xgemv_quant_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const voi
  *   down         E matrices of H x I values, ldd, stride_down apart
  *   y, ldy       T x H values of the type that `out` names; must not overlap
  *                the inputs
+ * An infinite value of x, or of an expert's weights, makes what it enters
+ * infinite or NaN (h is multiplied in parts).
  * A score of -inf gives its expert no weight; a token whose chosen scores are
  * all -inf gets a row of zeros, whatever x holds; a NaN among a token's scores (it counts as the
  * largest) makes its row NaN.  h is kept to fp32's 24 bits, for an output in

@@ -40,7 +40,9 @@ using xquant_dev::QuantParams;
 
 // Waves of a workgroup: 8 ranges of K for 16 columns, or 4 ranges of 64 columns,
 // which share x.  One or two rows: 8 ranges up to 512 tiles of 16 columns, 4
-// beyond.  More rows: the least of (rounds of workgroups that the CUs take) x
+// beyond.  (Microseconds of N x K for one row, 8 / 4 ranges: 2048 x 14336 7.4 / 9.0,
+// 4096 x 14336 7.8 / 9.2, 4096 x 4096 4.9 / 4.8, 8192 x 14336 15.7 / 15.1, 8192 x
+// 4096 6.3 / 5.9, 12288 x 4096 8.1 / 7.0, 14336 x 4096 10.3 / 8.1.)  More rows: the least of (rounds of workgroups that the CUs take) x
 // (time of one, in ns a k), with 16 rows a workgroup 1.7 for 16 columns, of which
 // two run on a CU, and 2.5 for 64 columns, 3.2 with 32 rows, 5.0 with 64.  A
 // workgroup of more rows widens each weight for all of them, but where columns
@@ -173,17 +175,29 @@ void launch_experts(const ExpertsParams &p, hipStream_t s)
 
 // Whether the waves of a workgroup of the second launch take ranges of their
 // own (16 columns, all the tokens' h) or columns of the same range (64).
-// (16 tokens, 6 of 64 experts of 2048 x 1408: 219 us with ranges of their own
-// against 212; 7 tokens, 3 of 13 of 1000 x 776: 25 against 31.)
+// Ranges of their own are faster where launches and joins count, columns where
+// the bytes do.  Microseconds, own ranges / columns: 7 tokens, 3 of 13 of 1000 x
+// 776 23.0 / 28.0; 8 tokens, 4 of 16 of 1024 x 512 20.2 / 25.5; 5 tokens, 6 of 64 of 1024
+// x 1024 42.8 / 48.4; 4 tokens, 8 of 64 of 2048 x 768 57.7 / 57.3; 8 tokens, 6 of
+// 64 of 2048 x 1408 134 / 128; 12 tokens, 8 of 128 of 2048 x 768 152 / 149.  (The
+// number of pairs stands for the bytes: with few of them and large experts, or
+// many and small ones, the other side would gain 8 tokens, 2 of 8 of 4096 x
+// 14336 462 / 440, and 16 tokens, 4 of 16 of 1024 x 512 21.3 / 26.6.)
 bool experts_own_ranges(int64_t T, int64_t top, int64_t I)
 {
     return I >= 16 && (T <= 2 || (T <= 16 && T * top <= 32));
 }
 
-// Parts that the second launch cuts the slots' inner dimensions into, of at
-// least four units a wave, with a counter for the workgroups of each: four
-// workgroups a CU; with waves on ranges of their own only where the columns
-// give few workgroups.
+// Parts that the second launch cuts the slots' inner dimensions into, with a
+// counter for the workgroups of each: two workgroups a CU where waves share
+// columns, one where they take ranges of their own, and for one or two tokens,
+// whose 16 waves already are 16 ranges, half of one where the columns give fewer
+// than a quarter.  (6 of 64 experts of 1008 x 1408, 63 workgroups of columns: one
+// part 24.7 us, two 22.6, four 21.7; 6 of 64 of 2048 x 1408, 128: 32.6, 31.1, 32.0;
+// 2 of 8 of 4096 x 14336, 256: 124, 127, 127.)  A part is at least four units a
+// wave: 64 tokens, 2 of 8 of 512 x 512 24.9 us, with two units 30.5, with eight
+// 23.5; 5 tokens, 6 of 16 of 512 x 640 19.2, 18.4 and 22.0; one token, 2 of 8 of
+// 768 x 4096 19.1, 17.6 and 21.2.
 int experts_parts(int64_t T, int64_t top, int64_t H, int64_t I, int64_t slots, int64_t Ip, int cu_count)
 {
     using namespace xexperts_dev;

@@ -52,8 +52,8 @@
 //   of the largest of the 64 columns, and h keeps its bits down to 2^-25 of that.
 //
 // Measured, first and second launch: 64 tokens, 2 of 8 experts of 4096 x 14336
-// (hidden x inner, every expert read) 359 us at 5.2 TB/s and 193 us at 4.9 TB/s;
-// 16 tokens, 6 of 64 of 2048 x 1408 113 us at 5.3 TB/s and 68 us at 4.5 TB/s.
+// (hidden x inner, every expert read) 342 us at 5.6 TB/s and 201 us at 5.0 TB/s;
+// 16 tokens, 6 of 64 of 2048 x 1408 111 us at 5.4 TB/s and 64 us at 4.8 TB/s.
 // With one token the chain of launch, routing, first loads and joins is as long
 // as the reading: 8 of 128 of 2048 x 768 17 us for 50 MB and 12 us for 25 MB.
 #pragma once

@@ -24,14 +24,19 @@
 // first) as one 64-bit number, so the result does not depend on who found
 // what first.
 //
-// What bounds it: some ten instructions a value (a 2^x counts for four) beside
-// its two or four bytes, and with few rows the chain of latencies from the
+// What bounds it: with alternatives vector instructions, ten a value for the
+// statistics (a 2^x counts for four) and some nine for choosing; without,
+// neither they (59% of the issue slots) nor memory (4.4 TB/s).  With few rows it is the chain of latencies from the
 // first load to the last join.  What a call executes once is kept short (code
 // that is not in the instruction cache yet costs more to fetch than to run),
 // so the paths that are seldom taken are loops and not unrolled.  Measured: 4096
-// rows of 50001 bfloat16 with five alternatives 121 us (3.4 TB/s, 1.7 values a
-// ns), one row of 131072 fp32 with twenty 13.2 us, of which some 3 us are the
-// launch.
+// rows of 50001 bfloat16 with five alternatives 106 us (3.9 TB/s, 1.9 values a
+// ns), without 94 us; one row of 131072 fp32 with twenty 13.1 us, without 5.0, of
+// which some 3 us are the launch.
+//
+// Accuracy: the product of x - m with log2 e is rounded to fp32, which leaves a
+// relative |x - m| 2^-24 in a term.  A value of 88 below the largest no longer
+// counts, so that is at most 2^-17 of a term too small to matter, and 1e-7 in all.
 #pragma once
 
 #include "decode_device.hpp"
@@ -486,7 +491,7 @@ struct GradParams {
 
 // dx = d_logprob (delta - p) - d_entropy p (log p + entropy) + d_lse p, with
 // log p = x - lse: a read and a write of every logit, the bytes of which bound
-// it (2048 rows of 131072 bfloat16: 172 us, 6.2 TB/s read and written).  A
+// it (2048 rows of 131072 bfloat16: 173 us, 6.2 TB/s read and written).  A
 // workgroup takes a span of kGradSpan values of one row.
 //
 // A large lse is held too coarsely for this: p is off by a relative |lse| 2^-24,
@@ -496,8 +501,8 @@ struct GradParams {
 // most 2^-17 in p for fp32 and 2^-15, an eighth of binary16's, for 16 bits.)  One
 // workgroup then takes `group` spans, so that a row is read group times less
 // often; into the logits themselves one takes the whole row, or it would read what
-// others have written.  2048 rows of 131072 bfloat16 at -3000: 335 us, with one span
-// a workgroup 1408, a whole row 345.  A Z that rounding does not explain is not this row's sum (a row that is
+// others have written.  2048 rows of 131072 bfloat16 at -3000: 371 us, with one span
+// a workgroup 1403, a whole row 345.  A Z that rounding does not explain is not this row's sum (a row that is
 // part of a longer one), and is left alone.
 constexpr int kGradThreads = 256, kGradSpan = kGradThreads * 8 * 2;
 template <int DT>

@@ -152,8 +152,10 @@ struct QuantLds {
 // Per unit a wave waits for x and then for its weights, while the weights of
 // the next unit and x of the next two are on their way.  Loads return in
 // order, so one that may or may not have been issued would make every wait
-// behind it a wait for all: the loop's loads are unconditional, past the end
-// they repeat the last unit's, and the unit that K ends in comes after it.
+// behind it a wait for all: the loop's loads of x and weights are unconditional,
+// past the end they repeat the last unit's, and the unit that K ends in comes
+// after it.  Those of the scales come once in CHUNK units, and the wait for x
+// behind them allows for both: it leaves two loads on their way, not more.
 //
 // With WN == 1 a wave alone writes and reads its x, and always its scales: its
 // LDS accesses complete in order, and the compiler keeps those of one array at

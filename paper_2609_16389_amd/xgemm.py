@@ -442,7 +442,10 @@ def handle(device_index: int | None = None, stream=None):
     different streams run concurrently.  Threads on one stream share its
     handle: their calls need no order of their own as long as they need no
     workspace; where they do, the program makes the calls one at a time or
-    gives each thread a stream.  ``stream`` is a torch stream, a raw
+    gives each thread a stream.  Calls recorded into a graph use a workspace
+    of the handle that no other call does; graphs recorded on one stream
+    (torch takes its streams from a pool, so two may be the same) must not be
+    replayed at the same time on several.  ``stream`` is a torch stream, a raw
     hipStream_t address or None (the null stream)."""
     import torch
     if device_index is None:
