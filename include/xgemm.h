@@ -718,6 +718,147 @@ int xgemm_logprob_grad(xgemm_handle_t h, int64_t R, int64_t V, const void *logit
                        const float *lse, const float *entropy, const float *d_logprob, const float *d_entropy,
                        const float *d_lse, void *dlogits, int64_t ldd, int dtype, void *stream);
 
+/*
+ * Products whose ends are fused: layers whose products go on to something that
+ * need not pass through memory.  As above they are enqueued on `stream`, enqueue
+ * nothing when validation or a workspace allocation fails, sum in fp32 (8-bit
+ * products: exactly, in 32-bit integers) in a fixed order, may be captured under
+ * the rules for recorded calls at xgemm_run, and none of their outputs may
+ * overlap an input.  Sides (H, N, V, 2 I) are at most XGEMM_FUSED_MAX_SIDE, rows
+ * (M, T) 2^30.
+ *
+ * Alignment: matrices that go into a product (x, w, up, head) are read in place
+ * where they begin on 16 bytes and rows and their distance are multiples of 16
+ * bytes; others are copied into the handle's workspace first, at every call.
+ * Everything else may have any alignment that its type has.
+ */
+#define XGEMM_FUSED_MAX_SIDE (1 << 22)
+
+/*
+ * Rows of 8-bit integers, with a scale each, from rows of R x K values:
+ *
+ *     scales[r] = max over k of |x[r][k]| * (1 / 127) (in fp32), at least 2^-126
+ *     q[r][k] = x[r][k] / scales[r] (in fp32) rounded to the nearest whole number, ties to
+ *               even; -127 .. 127
+ *
+ *   x, ldx     R x K values of dtype: XGEMM_BF16, XGEMM_FP16 or XGEMM_FP32
+ *   q, ldq     R x K bytes;  scales: R floats
+ * A row that holds a NaN or an infinity has a NaN for its scale, and zeros.  The
+ * weights of xgemm_scaled_run are made the same way, a row for each channel.
+ * Uses no workspace.
+ */
+#define XGEMM_INT8 3
+int xgemm_scaled_rows(xgemm_handle_t h, int64_t R, int64_t K, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
+                      float *scales, int dtype, void *stream);
+
+/*
+ * Products in 8-bit integers with a scale for each token and each channel:
+ *
+ *     y[m][n] = (sum over k of x[m][k] w[n][k]) * x_scales[m] * w_scales[n]
+ *
+ *   M, N, K        sizes; M == 0 or N == 0: no-op; K at most XGEMM_SCALED_MAX_K,
+ *                  where no sum passes 32 bits
+ *   x, ldx         M x K values of x_dtype: XGEMM_INT8, with x_scales (M
+ *                  floats), or XGEMM_BF16, XGEMM_FP16 or XGEMM_FP32, which become
+ *                  8-bit rows on the way as by xgemm_scaled_rows (x_scales NULL)
+ *   w, ldw         N x K bytes;  w_scales: N floats
+ *   y, ldy         M x N values of y_dtype: XGEMM_FP32, XGEMM_BF16 or XGEMM_FP16
+ * The sum is exact, rounded to fp32 once, and so is each product with a scale, in
+ * the order written.  Uses the workspace for x where it is quantised, for copies,
+ * and for partial sums where there are few tiles.
+ */
+#define XGEMM_SCALED_MAX_K 131071
+int xgemm_scaled_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const float *x_scales,
+                     const int8_t *w, int64_t ldw, const float *w_scales, void *y, int64_t ldy, int x_dtype, int y_dtype,
+                     void *stream);
+
+/*
+ * A gated feed-forward block up to its inner values, in one product:
+ *
+ *     gate = x[m] . up[i]    lift = x[m] . up[I + i]    y[m][i] = act(gate) * lift
+ *
+ *   x, ldx     M x H values of dtype (XGEMM_BF16 or XGEMM_FP16)
+ *   up, ldu    2 I x H values of dtype, the gate's rows first
+ *   y, ldy     M x I values of the type that `out` names.  H == 0: zeros.
+ *   pre, ldp   M x 2 I values of dtype: gate and lift, for the gradient; NULL:
+ *              not wanted
+ *   act        XGEMM_ACT_SILU: a / (1 + exp(-a)); XGEMM_ACT_GELU: a (1 + erf(a /
+ *              sqrt(2))) / 2; XGEMM_ACT_GELU_TANH: a (1 + tanh(sqrt(2 / pi) (a +
+ *              0.044715 a^3))) / 2
+ * y is computed from gate and lift in fp32, before their rounding to pre.
+ */
+enum xgemm_act {
+    XGEMM_ACT_SILU = 0,
+    XGEMM_ACT_GELU = 1,
+    XGEMM_ACT_GELU_TANH = 2
+};
+int xgemm_gated_run(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up,
+                    int64_t ldu, void *y, int64_t ldy, void *pre, int64_t ldp, int act, int dtype, int out, void *stream);
+
+/*
+ * Its gradient, given that of y and what the forward call left in pre:
+ *
+ *     d_gate = d_y * lift * act'(gate)    d_lift = d_y * act(gate)
+ *     d_x = [d_gate d_lift] up            d_up = [d_gate d_lift]^T x
+ *
+ *   d_y, ldd       M x I values of dtype
+ *   d_x, d_up      M x H and 2 I x H values of the type that `out` names, both;
+ *                  NULL: not wanted (x is read for d_up only, up for d_x only)
+ * d_gate and d_lift are rounded to dtype between the products (with XGEMM_FP16
+ * times a power of two, so that their size does not matter): whatever `out` is,
+ * d_x and d_up have an error of half a step of dtype in each term.  (Up to 128 rows
+ * they are kept in two parts, and the error is that of fp32.)  Uses 4 I bytes of
+ * workspace for each row, 8 I up to 128 rows.
+ */
+int xgemm_gated_grad(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up,
+                     int64_t ldu, const void *pre, int64_t ldp, const void *d_y, int64_t ldd, void *d_x, int64_t ld_dx,
+                     void *d_up, int64_t ld_dup, int act, int dtype, int out, void *stream);
+
+/*
+ * Log probabilities of given tokens from hidden states and the head's weights,
+ * without keeping the logits x[t] . head[v]:
+ *
+ *     lse[t] = log sum over v of exp(x[t] . head[v])    logprob[t] = x[t] . head[targets[t]] - lse[t]
+ *
+ *   x, ldx        T x H values of dtype (XGEMM_BF16 or XGEMM_FP16)
+ *   head, ldw     V x H values of dtype, V >= 1
+ *   targets       T indices; a negative one: logprob is 0; one of V or more:
+ *                 NaN.  May be NULL where logprob is.
+ *   logprob, lse  T floats each; NULL: not wanted
+ * Logits are fp32 sums.  A row with a logit of NaN or +inf has lse and logprob
+ * NaN; one of nothing but -inf has -inf.  Uses the workspace: 8 bytes for each 128
+ * or 256 logits of at most 16384 rows.
+ */
+int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
+                   int64_t ldw, const int64_t *targets, float *logprob, float *lse, int dtype, void *stream);
+
+/*
+ * Their gradient, given that of logprob and lse:
+ *
+ *     d = d_logprob (delta[target] - p) + d_lse p    p = exp(x . head - lse)
+ *     d_x = d head    d_head = d^T x
+ *
+ *   lse                what xgemm_head_run gave
+ *   targets            as above (only with d_logprob): a negative one takes no
+ *                      part in d_logprob, one of V or more makes d's row NaN
+ *   d_logprob, d_lse   T floats each; NULL: zero
+ *   d_x, d_head        T x H and V x H values of the type that `out` names,
+ *                      both; NULL: not wanted
+ * The logits are computed again in pieces of the vocabulary.  d is rounded to
+ * dtype between the products, relative to the largest |d_logprob| + |d_lse|, whose
+ * size does not matter: whatever `out` is, d_x and d_head have an error of half a
+ * step of dtype in each term.  (Up to 128 rows d is kept in two parts, with twice the
+ * bits.)  p holds lse's own
+ * rounding, a relative |lse| 2^-24.  A row whose lse is -inf, or whose d_logprob (or
+ * target's part in it) and d_lse are zero, has d = 0.  Uses the
+ * workspace: some 256 MB for d (2 bytes a logit; 4096 bytes a row if that is
+ * more), and 4 bytes for each value of d_x where it is not fp32 and there are several
+ * pieces.
+ */
+int xgemm_head_grad(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
+                    int64_t ldw, const int64_t *targets, const float *lse, const float *d_logprob, const float *d_lse,
+                    void *d_x, int64_t ld_dx, void *d_head, int64_t ld_dw, int dtype, int out, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *xgemm_strerror(int status);
 

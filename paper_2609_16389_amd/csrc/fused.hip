@@ -1,0 +1,630 @@
+// Host side of the products whose ends are fused: argument checks, layouts,
+// launch selection and launches.  The C ABI is declared in include/xgemm.h.
+#include "context.hpp"
+#include "fused_ends.hpp"
+#include "fused_tile.hpp"
+
+#include <algorithm>
+
+using xgemm_host::kMaxDim;
+using namespace xfused_dev;
+
+namespace {
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t up_to(int64_t a, int64_t b) { return cdiv(a, b) * b; }
+
+// Inner sizes, columns and vocabularies: a wave's rows of an operand lie within
+// the 2^31 bytes that its loads address.
+constexpr int64_t kMaxSide = (int64_t)1 << 22;
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxStep = (int64_t)1 << 26;   // bytes between rows read in place
+constexpr int64_t kRowsLaunch = 65536;           // rows of a result in one launch
+
+bool matrix_ok(int64_t rows, int64_t cols, int64_t ld)
+{
+    return rows >= 0 && cols >= 0 && rows < kMaxDim && cols < kMaxDim && ld >= cols && (double)rows * (double)ld <= 9.0e18;
+}
+
+bool sixteen(int dtype) { return dtype == XGEMM_BF16 || dtype == XGEMM_FP16; }
+
+int launch_status(xgemm_ctx *h, const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess)
+        return XGEMM_OK;
+    xgemm_host::set_error(h, what, e);
+    return XGEMM_ERR_HIP;
+}
+
+// Places in the workspace, 256 bytes apart.
+struct Space {
+    size_t bytes = 0;
+    size_t take(size_t n)
+    {
+        const size_t at = bytes;
+        bytes += (size_t)cdiv((int64_t)n, 256) * 256;
+        return at;
+    }
+};
+
+// An operand as the tiles read it: in place, or as a copy whose rows are whole
+// 16-byte chunks.
+struct Matrix {
+    const char *p;
+    int64_t rows, cols, ld;   // bytes
+    bool copied;
+    int times;                // the copy holds the rows so many times, one after another
+    size_t at;                // of the copy
+
+    Matrix(const void *data, int64_t r, int64_t c, int64_t leading, int size, Space &ws, int n = 1)
+        : p((const char *)data), rows(r), cols(c * size), ld(r > 1 ? leading * size : up_to(c * size, 16)), times(n), at(0)
+    {
+        copied = rows > 0 && cols > 0 && (((uintptr_t)p | ld | cols) % 16 != 0 || ld > kMaxStep || times > 1);
+        if (copied)
+            at = ws.take((size_t)(rows * times) * up_to(cols, 16));
+    }
+    void place(char *ws, hipStream_t s)
+    {
+        if (!copied)
+            return;
+        const int64_t chunks = cdiv(cols, 16), some = std::max<int64_t>(1, ((int64_t)1 << 30) / chunks);
+        for (int k = 0; k < times; ++k)
+            for (int64_t r = 0; r < rows; r += some) {
+                const int64_t n = std::min(some, rows - r);
+                hipLaunchKernelGGL(copy_rows, dim3(cdiv(n * chunks, 256)), dim3(256), 0, s, p + r * ld, ld, cols, n,
+                                   ws + at + (k * rows + r) * chunks * 16, chunks);
+            }
+        p = ws + at;
+        ld = chunks * 16;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+
+// How a product is cut: tiles of 256 or 128, and ranges of k whose sums are
+// joined by a second launch.
+struct Cut {
+    bool large;
+    int split, chunk;   // steps of a range
+    int64_t ld;         // of the parts
+    int halves = 1;     // 2: the rows come twice, as two parts of their values, and are joined too
+};
+
+// Rows up to which slopes are kept in two parts (fused_ends.hpp).
+constexpr int64_t kTwoParts = 128;
+
+Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool may_split, int cu_count)
+{
+    const int64_t cols = gated ? 2 * N : N, cus = std::max(cu_count, 1);
+    M = std::min(M, kRowsLaunch);
+    Cut c;
+    c.large = cdiv(M, 256) * cdiv(cols, 256) * 2 >= cus;
+    c.split = 1;
+    const int64_t tiles = c.large ? cdiv(M, 256) * cdiv(cols, 256) : cdiv(M, 128) * cdiv(cols, 128);
+    if (may_split && tiles < cus)
+        c.split = (int)std::max<int64_t>(1, std::min<int64_t>({2 * cus / std::max<int64_t>(tiles, 1), steps / 4, 32}));
+    c.chunk = (int)std::max<int64_t>(cdiv(steps, c.split), 1);
+    c.split = (int)std::max<int64_t>(cdiv(steps, c.chunk), 1);
+    c.ld = gated ? 2 * up_to(N, 4) : up_to(N, 4);
+    return c;
+}
+
+size_t part_bytes(const Cut &c, int64_t M)
+{
+    return c.split * c.halves > 1 ? (size_t)c.split * (size_t)std::min(M, kRowsLaunch) * c.ld * 4 : 0;
+}
+
+template <int TYPE, int LA, int LB, class End>
+void launch_tiles(TileParams p, const typename End::Params &e, bool large, hipStream_t s)
+{
+    const int b = large ? 256 : 128;
+    p.tiles_m = (int)cdiv(p.M, b);
+    p.tiles_n = (int)cdiv(p.N, End::kGated ? b / 2 : b);
+    p.group_m = 8;
+    p.grid = p.tiles_m * p.tiles_n * p.split;
+    if (large)
+        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 256, 256, 2, 4, End>), dim3(p.grid), dim3(512), 0, s, p, e);
+    else
+        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 128, 128, 2, 2, End>), dim3(p.grid), dim3(256), 0, s, p, e);
+}
+
+// One product of rows [.., .. + p.M) of the result, its sums' parts in `part`.
+template <int TYPE, int LA, int LB, class End>
+void launch_product(TileParams p, const typename End::Params &e, const Cut &c, char *part, hipStream_t s)
+{
+    p.split = c.split;
+    p.chunk = c.chunk;
+    if constexpr (End::kJoins) {
+        if (c.split * c.halves > 1) {
+            typedef PartEnd<TYPE, End::kGated> Part;
+            launch_tiles<TYPE, LA, LB, Part>(p, typename Part::Params{part, (int)c.ld}, c.large, s);
+            // (the second half's rows follow the first's: a part of their own)
+            const int64_t quads = cdiv(p.N, 4), M = p.M / c.halves;
+            hipLaunchKernelGGL(join_parts<End>, dim3(cdiv(M * quads, 256)), dim3(256), 0, s, part, c.split * c.halves,
+                               (int)M, p.N, (int)c.ld, quads, e);
+            return;
+        }
+    }
+    launch_tiles<TYPE, LA, LB, End>(p, e, c.large, s);
+}
+
+TileParams tile_params(const Matrix &A, const Matrix &B, int64_t M, int64_t N, int64_t K)
+{
+    TileParams p{};
+    p.A = A.p;
+    p.B = p.B2 = B.p;
+    p.lda = A.ld;
+    p.ldb = B.ld;
+    p.M = (int)M;
+    p.N = (int)N;
+    p.K = (int)K;
+    return p;
+}
+
+// out = a product of 16-bit operands (rows of A and out in launches of
+// kRowsLaunch).
+template <int LA, int LB>
+void product(int dtype, TileParams p, StoreEnd::Params e, const Cut &c, char *part, hipStream_t s)
+{
+    const int64_t M = p.M;
+    const char *const A = p.A;
+    void *const out = e.out;
+    const float *const add = e.add;
+    for (int64_t m = 0; m < M; m += kRowsLaunch) {
+        p.M = (int)std::min(kRowsLaunch, M - m);
+        p.A = A + m * (LA == kAlong ? p.lda : 2);
+        e.out = (char *)out + m * e.ld * (e.kind == kFp32 ? 4 : 2);
+        e.add = add ? add + m * e.ld_add : nullptr;
+        if (dtype == XGEMM_BF16)
+            launch_product<kBf16, LA, LB, StoreEnd>(p, e, c, part, s);
+        else
+            launch_product<kFp16, LA, LB, StoreEnd>(p, e, c, part, s);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit products
+// ---------------------------------------------------------------------------
+
+bool real(int dtype) { return sixteen(dtype) || dtype == XGEMM_FP32; }
+
+void launch_scale_rows(int dtype, int64_t R, int64_t K, const void *x, int64_t ldx, int8_t *q, int64_t ldq, int64_t padded,
+                       float *scales, hipStream_t s)
+{
+    constexpr int64_t some = (int64_t)1 << 22;
+    for (int64_t r = 0; r < R; r += some) {
+        const dim3 grid(std::min(some, R - r)), block(256);
+        const char *const from = (const char *)x + r * ldx * (dtype == XGEMM_FP32 ? 4 : 2);
+        if (dtype == XGEMM_BF16)
+            hipLaunchKernelGGL(scale_rows<kBf16>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+        else if (dtype == XGEMM_FP16)
+            hipLaunchKernelGGL(scale_rows<kFp16>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+        else
+            hipLaunchKernelGGL(scale_rows<kFp32>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+    }
+}
+
+int run_scaled_rows(xgemm_ctx *h, int64_t R, int64_t K, const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scales,
+                    int dtype, hipStream_t s)
+{
+    if (!h || !real(dtype) || !matrix_ok(R, K, ldx) || !matrix_ok(R, K, ldq))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (R == 0)
+        return XGEMM_OK;
+    if (!scales || (K > 0 && (!x || !q)))
+        return XGEMM_ERR_INVALID_ARG;
+    launch_scale_rows(dtype, R, K, x, ldx, q, ldq, K, scales, s);
+    return launch_status(h, "scaled rows launch");
+}
+
+int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const float *x_scales,
+               const int8_t *w, int64_t ldw, const float *w_scales, void *y, int64_t ldy, int x_dtype, int y_dtype,
+               hipStream_t s)
+{
+    if (!h || (x_dtype != XGEMM_INT8 && !real(x_dtype)) || !real(y_dtype))
+        return XGEMM_ERR_INVALID_ARG;
+    if (!matrix_ok(M, K, ldx) || !matrix_ok(N, K, ldw) || !matrix_ok(M, N, ldy) || M > kMaxRows || N > kMaxSide ||
+        K > XGEMM_SCALED_MAX_K)
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (M == 0 || N == 0)
+        return XGEMM_OK;
+    const bool whole = x_dtype == XGEMM_INT8;
+    if (!y || !w_scales || (K > 0 && (!x || !w)) || whole != (x_scales != nullptr))
+        return XGEMM_ERR_INVALID_ARG;
+    Space ws;
+    const int64_t padded = up_to(K, 16);
+    const size_t at_q = ws.take(whole ? 0 : (size_t)M * padded), at_scales = ws.take(whole ? 0 : (size_t)M * 4);
+    Matrix A(whole ? x : nullptr, whole ? M : 0, K, ldx, 1, ws), B(w, N, K, ldw, 1, ws);
+    const Cut c = cut_of(M, N, cdiv(padded, 128), false, true, h->cu_count);
+    const size_t at_part = ws.take(part_bytes(c, M));
+    if (ws.bytes > 0) {
+        const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+        if (rc != XGEMM_OK)
+            return rc;
+    }
+    char *const base = ws.bytes > 0 ? (char *)h->workspace + xgemm_host::kWsPrefix : nullptr;
+    A.place(base, s);
+    B.place(base, s);
+    if (!whole) {
+        A.p = base + at_q;
+        A.ld = padded;
+        launch_scale_rows(x_dtype, M, K, x, ldx, (int8_t *)A.p, padded, padded, (float *)(base + at_scales), s);
+        x_scales = (const float *)(base + at_scales);
+    }
+    TileParams p = tile_params(A, B, M, N, padded);
+    const int kind = y_dtype == XGEMM_FP32 ? kFp32 : y_dtype == XGEMM_FP16 ? kFp16 : kBf16;
+    for (int64_t m = 0; m < M; m += kRowsLaunch) {
+        p.M = (int)std::min(kRowsLaunch, M - m);
+        p.A = A.p + m * A.ld;
+        const ScaledEnd::Params e{x_scales + m, w_scales, (char *)y + m * ldy * (kind == kFp32 ? 4 : 2), ldy, kind};
+        launch_product<kInt8, kAlong, kAlong, ScaledEnd>(p, e, c, base + at_part, s);
+    }
+    const int launched = launch_status(h, "scaled product launch");
+    const int released = ws.bytes > 0 ? xgemm_host::release_workspace(h, s) : XGEMM_OK;
+    return launched != XGEMM_OK ? launched : released;
+}
+
+// ---------------------------------------------------------------------------
+// gated feed-forward block
+// ---------------------------------------------------------------------------
+
+bool act_ok(int act) { return act == XGEMM_ACT_SILU || act == XGEMM_ACT_GELU || act == XGEMM_ACT_GELU_TANH; }
+
+template <int DT>
+void launch_gated(TileParams p, int64_t M, void *out, int64_t ld, int kind, int act, uint16_t *pre, int64_t ldp,
+                  const Cut &c, char *part, hipStream_t s)
+{
+    const char *const A = p.A;
+    for (int64_t m = 0; m < M; m += kRowsLaunch) {
+        p.M = (int)std::min(kRowsLaunch, M - m);
+        p.A = A + m * p.lda;
+        const typename GatedEnd<DT>::Params e{(char *)out + m * ld * (kind == kFp32 ? 4 : 2), ld, kind, act,
+                                              pre ? pre + m * ldp : nullptr, ldp};
+        launch_product<DT, kAlong, kAlong, GatedEnd<DT>>(p, e, c, part, s);
+    }
+}
+
+int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up, int64_t ldu,
+              void *y, int64_t ldy, void *pre, int64_t ldp, int act, int dtype, int out, hipStream_t s)
+{
+    if (!h || !sixteen(dtype) || (out != XGEMM_OUT_FP32 && out != XGEMM_OUT_SAME) || !act_ok(act))
+        return XGEMM_ERR_INVALID_ARG;
+    if (H < 0 || I < 0 || M > kMaxRows || H > kMaxSide || I > kMaxSide / 2 || !matrix_ok(M, H, ldx) ||
+        !matrix_ok(2 * I, H, ldu) || !matrix_ok(M, I, ldy) || (pre && !matrix_ok(M, 2 * I, ldp)))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (M == 0 || I == 0)
+        return XGEMM_OK;
+    if (!y || (H > 0 && (!x || !up)))
+        return XGEMM_ERR_INVALID_ARG;
+    Space ws;
+    Matrix A(x, M, H, ldx, 2, ws), B(up, 2 * I, H, ldu, 2, ws);
+    const int64_t K = up_to(H, 8);
+    const Cut c = cut_of(M, I, cdiv(K, 64), true, true, h->cu_count);
+    const size_t at_part = ws.take(part_bytes(c, M));
+    if (ws.bytes > 0) {
+        const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+        if (rc != XGEMM_OK)
+            return rc;
+    }
+    char *const base = ws.bytes > 0 ? (char *)h->workspace + xgemm_host::kWsPrefix : nullptr;
+    A.place(base, s);
+    B.place(base, s);
+    TileParams p = tile_params(A, B, M, I, K);
+    p.B2 = B.p + I * B.ld;
+    const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
+    if (dtype == XGEMM_BF16)
+        launch_gated<kBf16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, base + at_part, s);
+    else
+        launch_gated<kFp16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, base + at_part, s);
+    const int launched = launch_status(h, "gated launch");
+    const int released = ws.bytes > 0 ? xgemm_host::release_workspace(h, s) : XGEMM_OK;
+    return launched != XGEMM_OK ? launched : released;
+}
+
+int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up, int64_t ldu,
+                   const void *pre, int64_t ldp, const void *d_y, int64_t ldd, void *d_x, int64_t ld_dx, void *d_up,
+                   int64_t ld_dup, int act, int dtype, int out, hipStream_t s)
+{
+    if (!h || !sixteen(dtype) || (out != XGEMM_OUT_FP32 && out != XGEMM_OUT_SAME) || !act_ok(act))
+        return XGEMM_ERR_INVALID_ARG;
+    if (H < 0 || I < 0 || M > kMaxRows || H > kMaxSide || I > kMaxSide / 2 || (d_up && !matrix_ok(M, H, ldx)) ||
+        (d_x && !matrix_ok(2 * I, H, ldu)) || !matrix_ok(M, 2 * I, ldp) || !matrix_ok(M, I, ldd) ||
+        (d_x && !matrix_ok(M, H, ld_dx)) || (d_up && !matrix_ok(2 * I, H, ld_dup)))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    // (d_x is M x H, d_up 2 I x H: empty products are zeros)
+    const bool want_x = d_x && M > 0 && H > 0, want_up = d_up && I > 0 && H > 0;
+    if (!want_x && !want_up)
+        return XGEMM_OK;
+    const bool some = M > 0 && I > 0;
+    if (some && (!pre || !d_y || (want_x && !up) || (want_up && !x)))
+        return XGEMM_ERR_INVALID_ARG;
+    const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
+    Space ws;
+    const size_t at_word = ws.take(8);
+    const int64_t ld = up_to(2 * I, 8);
+    const int halves = M <= kTwoParts ? 2 : 1;
+    const int64_t rows = M * halves;   // of slopes
+    const size_t at_d = ws.take((size_t)rows * ld * 2);
+    Matrix X(x, want_up && some ? M : 0, H, ldx, 2, ws, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2, ws);
+    Cut cx = cut_of(rows, H, cdiv(ld, 64), false, true, h->cu_count);
+    cx.halves = halves;
+    const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, h->cu_count);
+    const size_t at_part = ws.take(std::max(want_x ? part_bytes(cx, rows) : 0, want_up ? part_bytes(cw, 2 * I) : 0));
+    const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+    if (rc != XGEMM_OK)
+        return rc;
+    char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
+    X.place(base, s);
+    W.place(base, s);
+    uint32_t *const word = (uint32_t *)(base + at_word);   // bits of the largest slope, inverse of its power of two
+    GatedSlopeParams g;
+    g.ldp = ldp;
+    g.ldd = ldd;
+    g.ld = ld;
+    g.rest = halves > 1 ? M * ld : 0;
+    g.I = (int)I;
+    g.act = act;
+    g.chunks = (int)cdiv(I, 8);
+    g.most = word;
+    g.inverse = (float *)(word + 1);
+    auto slopes = [&](auto kernel) {
+        const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 30) / g.chunks);
+        for (int64_t m = 0; m < M; m += rows) {
+            g.M = (int)std::min(rows, M - m);
+            g.pre = (const uint16_t *)pre + m * ldp;
+            g.d = (const uint16_t *)d_y + m * ldd;
+            g.out = (uint16_t *)(base + at_d) + m * ld;
+            hipLaunchKernelGGL(kernel, dim3(cdiv((int64_t)g.M * g.chunks, 256)), dim3(256), 0, s, g);
+        }
+    };
+    if (some && dtype == XGEMM_BF16) {
+        slopes(gated_slope<kBf16, false>);
+    } else if (some) {
+        hipLaunchKernelGGL(set_words, dim3(1), dim3(64), 0, s, word, 2);
+        slopes(gated_slope<kFp16, true>);
+        slopes(gated_slope<kFp16, false>);
+    }
+    const float *const scale = some && dtype == XGEMM_FP16 ? g.inverse : nullptr;
+    TileParams p{};
+    p.A = base + at_d;
+    p.lda = ld * 2;
+    if (want_x) {
+        p.B = p.B2 = W.p;
+        p.ldb = W.ld;
+        p.M = (int)rows;
+        p.N = (int)H;
+        p.K = some ? (int)(2 * I) : 0;
+        product<kAlong, kAcross>(dtype, p, StoreEnd::Params{d_x, ld_dx, kind, scale, nullptr, 0}, cx, base + at_part, s);
+    }
+    if (want_up) {
+        p.B = p.B2 = X.p;
+        p.ldb = X.ld;
+        p.M = (int)(2 * I);
+        p.N = (int)H;
+        p.K = some ? (int)rows : 0;
+        product<kAcross, kAcross>(dtype, p, StoreEnd::Params{d_up, ld_dup, kind, scale, nullptr, 0}, cw, base + at_part, s);
+    }
+    const int launched = launch_status(h, "gated gradient launch");
+    const int released = xgemm_host::release_workspace(h, s);
+    return launched != XGEMM_OK ? launched : released;
+}
+
+// ---------------------------------------------------------------------------
+// log probabilities from a head's weights
+// ---------------------------------------------------------------------------
+
+constexpr int64_t kHeadRows = 16384;   // rows of statistics at a time
+
+bool head_ok(int64_t T, int64_t V, int64_t H, int64_t ldx, int64_t ldw, int dtype)
+{
+    return sixteen(dtype) && T <= kMaxRows && V >= 1 && V <= kMaxSide && H <= kMaxSide && matrix_ok(T, H, ldx) &&
+           matrix_ok(V, H, ldw);
+}
+
+int run_head(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head, int64_t ldw,
+             const int64_t *targets, float *logprob, float *lse, int dtype, hipStream_t s)
+{
+    if (!h || !head_ok(T, V, H, ldx, ldw, dtype))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    if (T == 0)
+        return XGEMM_OK;
+    if ((H > 0 && (!x || !head)) || (logprob && !targets))
+        return XGEMM_ERR_INVALID_ARG;
+    if (!logprob && !lse)
+        return XGEMM_OK;
+    Space ws;
+    Matrix X(x, T, H, ldx, 2, ws), W(head, V, H, ldw, 2, ws);
+    const int64_t K = up_to(H, 8), rows = std::min(T, kHeadRows);
+    const Cut c = cut_of(rows, V, cdiv(K, 64), false, false, h->cu_count);
+    const int64_t tiles = cdiv(V, c.large ? 256 : 128);
+    const size_t at_stat = ws.take((size_t)(tiles * rows) * sizeof(float2)), at_logit = ws.take((size_t)rows * 4);
+    const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+    if (rc != XGEMM_OK)
+        return rc;
+    char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
+    X.place(base, s);
+    W.place(base, s);
+    TileParams p = tile_params(X, W, rows, V, K);
+    for (int64_t t = 0; t < T; t += kHeadRows) {
+        p.M = (int)std::min(kHeadRows, T - t);
+        p.A = X.p + t * X.ld;
+        const StatsEnd::Params e{logprob ? targets + t : nullptr, (float2 *)(base + at_stat), (float *)(base + at_logit)};
+        if (dtype == XGEMM_BF16)
+            launch_product<kBf16, kAlong, kAlong, StatsEnd>(p, e, c, nullptr, s);
+        else
+            launch_product<kFp16, kAlong, kAlong, StatsEnd>(p, e, c, nullptr, s);
+        hipLaunchKernelGGL(head_join, dim3(cdiv(p.M, 16)), dim3(256), 0, s, e.stat, (int)tiles, (int64_t)p.M, e.at,
+                           e.targets, V, lse ? lse + t : nullptr, logprob ? logprob + t : nullptr);
+    }
+    const int launched = launch_status(h, "head launch");
+    const int released = xgemm_host::release_workspace(h, s);
+    return launched != XGEMM_OK ? launched : released;
+}
+
+// Columns of the vocabulary at a time: what holds the slopes of a piece (16 bits
+// each) stays near 256 MB.
+int64_t head_piece(int64_t T, int64_t V)
+{
+    const int64_t some = ((int64_t)1 << 27) / std::max<int64_t>(T, 1);
+    return std::min(up_to(V, 8), std::max<int64_t>(some / 2048 * 2048, 2048));
+}
+
+template <int DT>
+void launch_slopes(TileParams p, const typename SlopeEnd<DT>::Params &at, const Cut &c, int64_t T, hipStream_t s)
+{
+    const char *const A = p.A;
+    typename SlopeEnd<DT>::Params e = at;
+    for (int64_t t = 0; t < T; t += kRowsLaunch) {
+        p.M = (int)std::min(kRowsLaunch, T - t);
+        p.A = A + t * p.lda;
+        e.targets = at.targets ? at.targets + t : nullptr;
+        e.lse = at.lse + t;
+        e.d_logprob = at.d_logprob ? at.d_logprob + t : nullptr;
+        e.d_lse = at.d_lse ? at.d_lse + t : nullptr;
+        e.out = at.out + t * at.ld;   // (two parts only of fewer rows than a launch's)
+        launch_product<DT, kAlong, kAlong, SlopeEnd<DT>>(p, e, c, nullptr, s);
+    }
+}
+
+int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head, int64_t ldw,
+                  const int64_t *targets, const float *lse, const float *d_logprob, const float *d_lse, void *d_x,
+                  int64_t ld_dx, void *d_head, int64_t ld_dw, int dtype, int out, hipStream_t s)
+{
+    if (!h || !head_ok(T, V, H, ldx, ldw, dtype) || (out != XGEMM_OUT_FP32 && out != XGEMM_OUT_SAME) ||
+        (d_x && !matrix_ok(T, H, ld_dx)) || (d_head && !matrix_ok(V, H, ld_dw)))
+        return XGEMM_ERR_INVALID_ARG;
+    h->last_error[0] = '\0';
+    const bool want_x = d_x && T > 0 && H > 0, want_w = d_head && H > 0;
+    if (!want_x && !want_w)
+        return XGEMM_OK;
+    if (T > 0 && (!x || !head || !lse || (d_logprob && !targets)))
+        return XGEMM_ERR_INVALID_ARG;
+    const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
+    Space ws;
+    const size_t at_scale = ws.take(8);
+    const int64_t piece = head_piece(T, V);
+    const int halves = T <= kTwoParts ? 2 : 1;
+    const int64_t rows = T * halves;   // of slopes
+    const size_t at_d = ws.take((size_t)rows * piece * 2);
+    Matrix X(x, T, H, ldx, 2, ws, want_w ? halves : 1), W(head, T > 0 ? V : 0, H, ldw, 2, ws);
+    const int64_t K = up_to(H, 8), pieces = cdiv(V, piece);
+    // d_x over the pieces: in fp32 until the last
+    const bool sums = want_x && pieces > 1 && kind != kFp32;
+    const size_t at_sum = ws.take(sums ? (size_t)T * up_to(H, 4) * 4 : 0);
+    size_t parts = 0;
+    auto cut_x = [&](int64_t n) {
+        Cut c = cut_of(rows, H, cdiv(n, 64), false, true, h->cu_count);
+        c.halves = halves;
+        return c;
+    };
+    auto cut_w = [&](int64_t n) { return cut_of(n, H, cdiv(rows, 64), false, true, h->cu_count); };
+    for (const int64_t n : {std::min(piece, V), V - (pieces - 1) * piece})
+        parts = std::max({parts, part_bytes(cut_x(n), rows), part_bytes(cut_w(n), n)});
+    const size_t at_part = ws.take(parts);
+    const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+    if (rc != XGEMM_OK)
+        return rc;
+    char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
+    X.place(base, s);
+    W.place(base, s);
+    float *const scales = (float *)(base + at_scale);
+    hipLaunchKernelGGL(slope_scale, dim3(1), dim3(256), 0, s, d_logprob, d_lse, T, dtype == XGEMM_FP16 ? 16384.0f : 1.0f,
+                       scales);
+    uint16_t *const d = (uint16_t *)(base + at_d);
+    float *const sum = kind == kFp32 ? (float *)d_x : (float *)(base + at_sum);
+    const int64_t ld_sum = kind == kFp32 ? ld_dx : up_to(H, 4);
+    for (int64_t v = 0; v < V; v += piece) {
+        const int64_t n = std::min(piece, V - v);
+        if (T > 0) {
+            TileParams p = tile_params(X, W, T, n, K);
+            p.B = p.B2 = W.p + v * W.ld;
+            const Cut c = cut_of(T, n, cdiv(K, 64), false, false, h->cu_count);
+            uint16_t *const rest = halves > 1 ? d + T * piece : nullptr;
+            if (dtype == XGEMM_BF16)
+                launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);
+            else
+                launch_slopes<kFp16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);
+        }
+        const float *const scale = scales + 1;
+        TileParams p{};
+        p.A = (const char *)d;
+        p.lda = piece * 2;
+        if (want_x) {
+            const bool last = v + n == V;
+            p.B = p.B2 = W.p + v * W.ld;
+            p.ldb = W.ld;
+            p.M = (int)rows;
+            p.N = (int)H;
+            p.K = (int)n;
+            StoreEnd::Params e{last ? d_x : sum, last ? ld_dx : ld_sum, last ? kind : kFp32, scale, v > 0 ? sum : nullptr, ld_sum};
+            product<kAlong, kAcross>(dtype, p, e, cut_x(n), base + at_part, s);
+        }
+        if (want_w) {
+            p.B = p.B2 = X.p;
+            p.ldb = X.ld;
+            p.M = (int)n;
+            p.N = (int)H;
+            p.K = (int)rows;
+            const StoreEnd::Params e{(char *)d_head + v * ld_dw * (kind == kFp32 ? 4 : 2), ld_dw, kind, scale, nullptr, 0};
+            product<kAcross, kAcross>(dtype, p, e, cut_w(n), base + at_part, s);
+        }
+    }
+    const int launched = launch_status(h, "head gradient launch");
+    const int released = xgemm_host::release_workspace(h, s);
+    return launched != XGEMM_OK ? launched : released;
+}
+
+}  // namespace
+
+extern "C" {
+
+int xgemm_scaled_rows(xgemm_handle_t h, int64_t R, int64_t K, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
+                      float *scales, int dtype, void *stream)
+{
+    return run_scaled_rows(h, R, K, x, ldx, q, ldq, scales, dtype, (hipStream_t)stream);
+}
+
+int xgemm_scaled_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const void *x, int64_t ldx, const float *x_scales,
+                     const int8_t *w, int64_t ldw, const float *w_scales, void *y, int64_t ldy, int x_dtype, int y_dtype,
+                     void *stream)
+{
+    return run_scaled(h, M, N, K, x, ldx, x_scales, w, ldw, w_scales, y, ldy, x_dtype, y_dtype, (hipStream_t)stream);
+}
+
+int xgemm_gated_run(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up,
+                    int64_t ldu, void *y, int64_t ldy, void *pre, int64_t ldp, int act, int dtype, int out, void *stream)
+{
+    return run_gated(h, M, H, I, x, ldx, up, ldu, y, ldy, pre, ldp, act, dtype, out, (hipStream_t)stream);
+}
+
+int xgemm_gated_grad(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up,
+                     int64_t ldu, const void *pre, int64_t ldp, const void *d_y, int64_t ldd, void *d_x, int64_t ld_dx,
+                     void *d_up, int64_t ld_dup, int act, int dtype, int out, void *stream)
+{
+    return run_gated_grad(h, M, H, I, x, ldx, up, ldu, pre, ldp, d_y, ldd, d_x, ld_dx, d_up, ld_dup, act, dtype, out,
+                          (hipStream_t)stream);
+}
+
+int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
+                   int64_t ldw, const int64_t *targets, float *logprob, float *lse, int dtype, void *stream)
+{
+    return run_head(h, T, V, H, x, ldx, head, ldw, targets, logprob, lse, dtype, (hipStream_t)stream);
+}
+
+int xgemm_head_grad(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
+                    int64_t ldw, const int64_t *targets, const float *lse, const float *d_logprob, const float *d_lse,
+                    void *d_x, int64_t ld_dx, void *d_head, int64_t ld_dw, int dtype, int out, void *stream)
+{
+    return run_head_grad(h, T, V, H, x, ldx, head, ldw, targets, lse, d_logprob, d_lse, d_x, ld_dx, d_head, ld_dw, dtype,
+                         out, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,683 @@
+// What becomes of the sums of a tile (fused_tile.hpp): the ends of the 8-bit
+// products, the gated feed-forward block, the log probabilities of a head and
+// their gradients' products.
+//
+// An End takes four neighbouring columns of a row at a time (quad), from the
+// registers of the product or, where k was split over workgroups (kJoins), from
+// the sums of its parts (join_parts, in ascending order).
+#pragma once
+
+#include "fused_tile.hpp"
+
+namespace xfused_dev {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Four values of a row from column `col` of `n`, rounded to the type that
+// `kind` names (kBf16, kFp16 or kFp32).
+constexpr int kFp32 = 2;
+__device__ __forceinline__ void store_quad(void *row, int kind, int col, int n, f32x4 v)
+{
+    if (kind == kFp32) {
+        float *const q = (float *)row + col;
+        if (col + 4 <= n) {
+            store_any<f32x4>(q, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (col + k < n)
+                    q[k] = v[k];
+        }
+        return;
+    }
+    uint16_t h[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        h[k] = kind == kBf16 ? from_float<kBf16>(v[k]) : from_float<kFp16>(v[k]);
+    uint16_t *const q = (uint16_t *)row + col;
+    if (col + 4 <= n) {
+        store_any<uint64_t>(q, (uint64_t)(h[0] | (uint32_t)h[1] << 16) | (uint64_t)(h[2] | (uint32_t)h[3] << 16) << 32);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (col + k < n)
+                q[k] = h[k];
+    }
+}
+__device__ __forceinline__ void *row_at(void *base, int64_t ld, int row, int kind)
+{
+    return (char *)base + (int64_t)row * ld * (kind == kFp32 ? 4 : 2);
+}
+
+// Calls f(row, col, i, j) for the blocks of a wave that hold rows of the result.
+template <int TM, int TN, int FM, int FN, class F>
+__device__ __forceinline__ void each_quad(int M, int N, int m0, int n0, int wm, int wn, int lane, F f)
+{
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int row = m0 + wm * TM + i * 16 + (lane & 15);
+        if (row < M) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+                if (col < N)
+                    f(row, col, i, j);
+            }
+        }
+    }
+}
+
+// Sums of a range of k, as they are: part [ks][M][ld] (4 bytes a value), for a
+// gated tile with the second matrix's columns from ld / 2 on.
+template <int TYPE, bool GATED>
+struct PartEnd {
+    static constexpr bool kGated = GATED;
+    struct Params {
+        char *part;
+        int ld;   // a multiple of 4, of 8 where gated
+    };
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
+                                                  int wm, int wn, int, int ks, int lane)
+    {
+        char *const base = e.part + (int64_t)ks * p.M * e.ld * 4;
+        if constexpr (GATED) {
+            each_quad<TM, TN / 2, FM, FN / 2>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+                char *const q = base + ((int64_t)row * e.ld + col) * 4;
+                *(u32x4 *)q = __builtin_bit_cast(u32x4, acc[i][j]);
+                *(u32x4 *)(q + e.ld / 2 * 4) = __builtin_bit_cast(u32x4, acc[i][j + FN / 2]);
+            });
+        } else {
+            each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+                *(u32x4 *)(base + ((int64_t)row * e.ld + col) * 4) = __builtin_bit_cast(u32x4, acc[i][j]);
+            });
+        }
+    }
+};
+
+// A product as it is: out = sum * scale + add, rounded to out's type.
+struct StoreEnd {
+    static constexpr bool kGated = false, kJoins = true;
+    struct Params {
+        void *out;
+        int64_t ld;
+        int kind;
+        const float *scale;   // a number in memory; null: 1
+        const float *add;     // what earlier parts of k left (leading dimension ld_add); null: nothing
+        int64_t ld_add;
+    };
+    typedef float value_t;
+    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, f32x4 v, f32x4)
+    {
+        if (e.scale) {
+            const float s = *e.scale;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] *= s;
+        }
+        if (e.add) {
+            const float *const q = e.add + (int64_t)row * e.ld_add + col;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < N)
+                    v[k] += q[k];
+        }
+        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, v);
+    }
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
+                                                  int wm, int wn, int, int, int lane)
+    {
+        each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane,
+                                  [&](int row, int col, int i, int j) { quad(e, row, col, p.N, acc[i][j], acc[i][j]); });
+    }
+};
+
+// 8-bit products: out = (sum * scale of the row) * scale of the column.  The sum
+// is exact in 32 bits (|sum| <= 2^14 K < 2^31).
+struct ScaledEnd {
+    static constexpr bool kGated = false, kJoins = true;
+    struct Params {
+        const float *row_scale, *col_scale;
+        void *out;
+        int64_t ld;
+        int kind;
+    };
+    typedef int value_t;
+    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, i32x4 s, i32x4)
+    {
+        const float r = e.row_scale[row];
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = (float)s[k] * r * (col + k < N ? e.col_scale[col + k] : 0.0f);
+        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, v);
+    }
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
+                                                  int wm, int wn, int, int, int lane)
+    {
+        each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane,
+                                  [&](int row, int col, int i, int j) { quad(e, row, col, p.N, acc[i][j], acc[i][j]); });
+    }
+};
+
+// Activations and their slopes.  Far from zero they are a or 0 to the last bit:
+// the argument of the exponentials is held to where that is so, which keeps
+// infinities out of the products (a NaN stays).
+enum { kSilu = 0, kGelu = 1, kGeluTanh = 2 };
+
+__device__ __forceinline__ float hold(float a, float most) { return a > most ? most : a < -most ? -most : a; }
+__device__ __forceinline__ float exp_of(float a) { return __builtin_amdgcn_exp2f(a * kLog2e); }
+
+// the share p of a in act(a) = a p
+__device__ __forceinline__ float share(int act, float a)
+{
+    if (act == kSilu)
+        return 1.0f / (1.0f + exp_of(-a));
+    if (act == kGelu)
+        return 0.5f * erfcf(a * -0.70710678118654752440f);   // (1 + erf would lose the left tail)
+    const float b = hold(a, 16.0f);
+    return 1.0f / (1.0f + exp_of(-1.59576912160573071176f * (b + 0.044715f * b * b * b)));
+}
+__device__ __forceinline__ float act_of(int act, float a) { return a * share(act, a); }
+
+__device__ __forceinline__ void act_slope(int act, float a, float &value, float &slope)
+{
+    const float p = share(act, a);
+    value = a * p;
+    if (act == kSilu) {
+        const float b = hold(a, 200.0f);
+        slope = p * (1.0f + b * (1.0f / (1.0f + exp_of(b))));
+    } else if (act == kGelu) {
+        const float b = hold(a, 40.0f);
+        slope = p + b * (0.39894228040143267794f * exp_of(-0.5f * b * b));
+    } else {
+        const float b = hold(a, 16.0f);
+        const float rest = 1.0f / (1.0f + exp_of(1.59576912160573071176f * (b + 0.044715f * b * b * b)));   // 1 - p
+        slope = p + b * (p * rest) * (1.59576912160573071176f * (1.0f + 0.134145f * b * b));
+    }
+}
+
+// A gated block: out = act(gate) * lift, and both before it (pre) if wanted.
+template <int DT>
+struct GatedEnd {
+    static constexpr bool kGated = true, kJoins = true;
+    struct Params {
+        void *out;
+        int64_t ld;
+        int kind, act;
+        uint16_t *pre;   // null: not wanted
+        int64_t ldp;
+    };
+    typedef float value_t;
+    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, f32x4 g, f32x4 u)
+    {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = act_of(e.act, g[k]) * u[k];
+        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, v);
+        if (e.pre) {
+            uint16_t *const q = e.pre + (int64_t)row * e.ldp;
+            store_quad(q, DT, col, N, g);
+            store_quad(q + N, DT, col, N, u);
+        }
+    }
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
+                                                  int wm, int wn, int, int, int lane)
+    {
+        each_quad<TM, TN / 2, FM, FN / 2>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+            quad(e, row, col, p.N, acc[i][j], acc[i][j + FN / 2]);
+        });
+    }
+};
+
+// Logits of a head: per row and tile the largest and the sum of the exponentials
+// relative to it, and the target's logit.
+struct StatsEnd {
+    static constexpr bool kGated = false, kJoins = false;
+    struct Params {
+        const int64_t *targets;   // null: none wanted
+        float2 *stat;             // [tile of columns][M]
+        float *at;                // [M]
+    };
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
+                                                  int n0, int wm, int wn, int tn, int, int lane)
+    {
+        float2 *const meet_at = (float2 *)smem;   // [BM][WN]
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int r = wm * TM + i * 16 + (lane & 15), row = m0 + r;
+            const int64_t target = e.targets && row < p.M ? e.targets[row] : -1;
+            float most = -INFINITY;
+            bool bad = false;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float v = acc[i][j][k];
+                    if (col + k < p.N) {
+                        if (col + k == target)
+                            e.at[row] = v;
+                        bad |= !(v < INFINITY);
+                        most = fmaxf(most, v);
+                    }
+                }
+            }
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float ref = most > -INFINITY ? most : 0.0f;
+            float sum = bad ? NAN : 0.0f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (col + k < p.N)
+                        sum += exp_of(acc[i][j][k] - ref);
+            }
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (lane < 16)
+                meet_at[r * WN + wn] = make_float2(most, sum);
+        }
+        __syncthreads();
+        for (int r = threadIdx.x; r < BM; r += blockDim.x) {
+            if (m0 + r >= p.M)
+                break;
+            float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WN; ++k)
+                most = fmaxf(most, meet_at[r * WN + k].x);
+#pragma unroll
+            for (int k = 0; k < WN; ++k) {
+                const float2 s = meet_at[r * WN + k];
+                sum += s.x > -INFINITY || !(s.y == s.y) ? s.y * exp_of(s.x - most) : 0.0f;
+            }
+            e.stat[(int64_t)tn * p.M + m0 + r] = make_float2(most, sum);
+        }
+    }
+};
+
+// Slopes between the products of a gradient are rounded to 16 bits, as many as
+// the products' results are: over many rows the roundings of both add up like
+// independent ones.  Few rows, where one slope may decide a whole result, are
+// kept in two parts (the rounded value, and what the rounding left), which cost
+// nothing beside the weights that are read for them.
+template <int DT>
+__device__ __forceinline__ float left_of(float v)
+{
+    const float r = v - to_float<DT>(from_float<DT>(v));
+    return fabsf(r) < INFINITY ? r : 0.0f;   // (of an infinity or a NaN the first part says it all)
+}
+
+// The gradient in a head's logits, d_logprob (hot - p) + d_lse p, as the operand
+// of the products that follow, times a factor that takes the largest |d_logprob| +
+// |d_lse| to 1 (binary16: 2^14, since p / rows would fall below its smallest
+// numbers): with equal d_logprob, as of a mean, the slope of a token that the model
+// gives little is then 1, not a rounded 1 / rows that is off by as much in every row.
+template <int DT>
+struct SlopeEnd {
+    static constexpr bool kGated = false, kJoins = false;
+    struct Params {
+        const int64_t *targets;
+        const float *lse, *d_logprob, *d_lse;   // d_logprob, d_lse: null: zero
+        const float *scale;
+        uint16_t *out, *rest;                   // rest: of two parts the second; null: one part
+        int64_t ld;     // a multiple of 8; columns up to a multiple of 8 are written
+        int64_t first;  // the target of column 0
+        int64_t V;
+    };
+    template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
+                                                  int wm, int wn, int, int, int lane)
+    {
+        const float scale = *e.scale;
+        const int padded = (p.N + 7) / 8 * 8;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int row = m0 + wm * TM + i * 16 + (lane & 15);
+            if (row >= p.M)
+                continue;
+            const int64_t target = e.d_logprob ? e.targets[row] : -1;
+            float dl = target < 0 ? 0.0f : e.d_logprob[row];
+            if (target >= e.V)
+                dl = NAN;
+            const float lse = e.lse[row], dp = (e.d_lse ? e.d_lse[row] : 0.0f) - dl;
+            // (a row of nothing but -inf takes no part, nor does one without factors, whatever its lse)
+            const bool empty = lse == -INFINITY || (dl == 0.0f && dp == 0.0f);
+            const int64_t hot = target - e.first;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+                f32x4 v;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float d = exp_of(acc[i][j][k] - lse) * dp + (hot == col + k ? dl : 0.0f);
+                    v[k] = empty || col + k >= p.N ? 0.0f : d * scale;
+                }
+                if (col < padded) {
+                    store_quad(e.out + (int64_t)row * e.ld, DT, col, padded, v);
+                    if (e.rest) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = left_of<DT>(v[k]);
+                        store_quad(e.rest + (int64_t)row * e.ld, DT, col, padded, v);
+                    }
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// around the products
+// ---------------------------------------------------------------------------
+
+// The parts of sums split over k, and the end of the product: four columns a
+// thread, `quads` of them a row.
+template <class End>
+__global__ void __launch_bounds__(256) join_parts(const char *part, int split, int M, int N, int ld, int64_t quads,
+                                                  typename End::Params e)
+{
+    typedef typename End::value_t value_t;
+    typedef value_t quad_t __attribute__((ext_vector_type(4)));
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(at / quads), col = (int)(at % quads) * 4;
+    if (row >= M)
+        return;
+    quad_t s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (int k = 0; k < split; ++k) {
+        const char *const q = part + (((int64_t)k * M + row) * ld + col) * 4;
+        s[0] += *(const quad_t *)q;
+        if constexpr (End::kGated)
+            s[1] += *(const quad_t *)(q + ld / 2 * 4);
+    }
+    End::quad(e, row, col, N, s[0], s[1]);
+}
+
+// Rows of `bytes` bytes, at any alignment, to rows of `chunks` x 16, zeros after
+// the end.
+__global__ void __launch_bounds__(256) copy_rows(const char *from, int64_t ld, int64_t bytes, int64_t rows, char *to,
+                                                 int64_t chunks)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / chunks, c = at % chunks;
+    if (row < rows)
+        *(u32x4 *)(to + (row * chunks + c) * 16) = load16_end(from + row * ld, c * 16, bytes);
+}
+
+// Per row of K values: scale = max |x| * (1 / 127) (at least 2^-126), q = x / scale
+// rounded to the nearest whole number, ties to even.  A row that holds a NaN or
+// an infinity: scale NaN, q = 0.  One workgroup a row, read twice (the second
+// time from the caches).  Values up to `padded` are written, zeros past K.
+template <int DT>
+__device__ __forceinline__ float value_at(const char *x, int64_t k)
+{
+    if constexpr (DT == kFp32)
+        return ((const float *)x)[k];
+    else
+        return to_float<DT>(((const uint16_t *)x)[k]);
+}
+
+template <int DT>
+__device__ __forceinline__ void eight(const char *x, int64_t k, int64_t K, float (&v)[8])
+{
+    if (k + 8 <= K) {
+        if constexpr (DT == kFp32) {
+            const f32x4 a = load_any<f32x4>(x + k * 4), b = load_any<f32x4>(x + k * 4 + 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = a[j];
+                v[j + 4] = b[j];
+            }
+        } else {
+            const u32x4 a = load_any<u32x4>(x + k * 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = to_float<DT>((uint16_t)(a[j] & 0xffffu));
+                v[2 * j + 1] = to_float<DT>((uint16_t)(a[j] >> 16));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = k + j < K ? value_at<DT>(x, k + j) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ uint32_t most_of(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1)
+        v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    return v;
+}
+
+__device__ __forceinline__ float row_scale(uint32_t most)
+{
+    return most >= 0x7f800000u ? NAN : fmaxf(__builtin_bit_cast(float, most) * (1.0f / 127.0f), 0x1p-126f);
+}
+
+__device__ __forceinline__ uint64_t eight_bytes(const float (&v)[8], float scale)
+{
+    uint64_t q = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float r = scale == scale ? rintf(v[j] / scale) : 0.0f;
+        q |= (uint64_t)(uint8_t)(int8_t)(int)fminf(fmaxf(r, -127.0f), 127.0f) << (8 * j);
+    }
+    return q;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256) scale_rows(const char *x, int64_t ldx, int64_t K, int8_t *q, int64_t ldq,
+                                                  int64_t padded, float *scales)
+{
+    __shared__ uint32_t share_most[4];
+    const int64_t row = blockIdx.x;
+    const char *const r = x + row * ldx * (DT == kFp32 ? 4 : 2);
+    uint32_t most = 0;
+    for (int64_t k = threadIdx.x * 8; k < K; k += 256 * 8) {
+        float v[8];
+        eight<DT>(r, k, K, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            most = max(most, __builtin_bit_cast(uint32_t, v[j]) & 0x7fffffffu);
+    }
+    most = most_of(most);
+    if ((threadIdx.x & 63) == 0)
+        share_most[threadIdx.x >> 6] = most;
+    __syncthreads();
+    most = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
+    const float scale = row_scale(most);
+    if (threadIdx.x == 0)
+        scales[row] = scale;
+    for (int64_t k = threadIdx.x * 8; k < padded; k += 256 * 8) {
+        float v[8];
+        eight<DT>(r, k, K, v);
+        const uint64_t b = eight_bytes(v, scale);
+        int8_t *const to = q + row * ldq + k;
+        if (k + 8 <= padded) {
+            store_any<uint64_t>(to, b);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (k + j < padded)
+                    to[j] = (int8_t)(b >> (8 * j));
+        }
+    }
+}
+
+// A power of two that takes the finite value with bits `most` to 2^14 .. 2^15.
+__device__ __forceinline__ float lift_of(uint32_t most)
+{
+    const int e = (int)(most >> 23) - 127;   // (a subnormal one counts as 2^-127)
+    return most == 0 ? 1.0f : __builtin_ldexpf(1.0f, min(max(14 - e, -126), 126));
+}
+
+// One workgroup: scales[0] takes the largest finite |d_logprob| + |d_lse| to
+// `to`, scales[1] is its inverse.
+__global__ void __launch_bounds__(256) slope_scale(const float *d_logprob, const float *d_lse, int64_t rows, float to,
+                                                   float *scales)
+{
+    __shared__ uint32_t share_most[4];
+    uint32_t most = 0;
+    for (int64_t r = threadIdx.x; r < rows; r += 256) {
+        const float s = (d_logprob ? fabsf(d_logprob[r]) : 0.0f) + (d_lse ? fabsf(d_lse[r]) : 0.0f);
+        const uint32_t b = __builtin_bit_cast(uint32_t, s);
+        most = max(most, b < 0x7f800000u ? b : 0u);
+    }
+    most = most_of(most);
+    if ((threadIdx.x & 63) == 0)
+        share_most[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        most = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
+        // (a smaller factor for what is next to fp32's ends)
+        const float m = fminf(fmaxf(__builtin_bit_cast(float, most), 0x1p-100f), 0x1p100f);
+        scales[0] = most == 0 ? 1.0f : to / m;
+        scales[1] = most == 0 ? 1.0f : m / to;
+    }
+}
+
+__global__ void set_words(uint32_t *w, int n)
+{
+    if ((int)threadIdx.x < n)
+        w[threadIdx.x] = 0;
+}
+
+// The gradient in a gated block's projections, [d lift act'(gate) | d act(gate)],
+// as the operand of the products that follow.  In binary16 times a power of two
+// that takes the largest of them to 2^14: a first launch (MOST) finds it.  Eight columns a
+// thread, the padding after 2 I zeros.
+struct GatedSlopeParams {
+    const uint16_t *pre, *d;
+    int64_t ldp, ldd;
+    uint16_t *out;   // M x ld, ld a multiple of 8 of at least 2 I
+    int64_t rest;    // values from there to the second of two parts; 0: one part
+    int64_t ld;
+    int M, I, act;
+    int chunks;       // of 8 in I columns
+    uint32_t *most;   // bits of the largest (binary16)
+    float *inverse;   // of the power of two
+};
+
+template <int DT>
+__device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v)[8])
+{
+    if (n >= 8) {
+        u32x4 b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            b[j] = from_float<DT>(v[2 * j]) | (uint32_t)from_float<DT>(v[2 * j + 1]) << 16;
+        store_any<u32x4>(to, b);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n)
+                to[j] = from_float<DT>(v[j]);
+    }
+}
+
+template <int DT, bool MOST>
+__global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(at / p.chunks), col = (int)(at % p.chunks) * 8;
+    uint32_t most = 0;
+    if (row < p.M) {
+        float g[8], u[8], d[8], dg[8], du[8];
+        const uint16_t *const pre = p.pre + (int64_t)row * p.ldp;
+        eight<DT>((const char *)pre, col, p.I, g);
+        eight<DT>((const char *)(pre + p.I), col, p.I, u);
+        eight<DT>((const char *)(p.d + (int64_t)row * p.ldd), col, p.I, d);
+        const float s = DT == kFp16 && !MOST ? lift_of(*p.most) : 1.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float value, slope;
+            act_slope(p.act, g[j], value, slope);
+            dg[j] = d[j] * u[j] * slope * s;
+            du[j] = d[j] * value * s;
+        }
+        if constexpr (MOST) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t a = __builtin_bit_cast(uint32_t, dg[j]) & 0x7fffffffu;
+                const uint32_t b = __builtin_bit_cast(uint32_t, du[j]) & 0x7fffffffu;
+                most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
+            }
+        } else {
+            const int n = p.I - col;
+            auto store = [&](uint16_t *out) {
+                store_eight<DT>(out + col, n, dg);
+                store_eight<DT>(out + p.I + col, n, du);
+                if (n <= 8)
+                    for (int c = 2 * p.I; c < p.ld; ++c)
+                        out[c] = 0;
+            };
+            uint16_t *const out = p.out + (int64_t)row * p.ld;
+            store(out);
+            if (p.rest) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    dg[j] = left_of<DT>(dg[j]);
+                    du[j] = left_of<DT>(du[j]);
+                }
+                store(out + p.rest);
+            }
+            if (DT == kFp16 && at == 0)
+                *p.inverse = 1.0f / s;
+        }
+    }
+    if constexpr (MOST) {
+        most = most_of(most);
+        if ((threadIdx.x & 63) == 0 && most)
+            atomicMax(p.most, most);   // (the largest: the same in any order)
+    }
+}
+
+// Log probabilities from the tiles' statistics: 16 rows a workgroup, each by 16
+// threads that take every sixteenth tile.
+__global__ void __launch_bounds__(256) head_join(const float2 *stat, int tiles, int64_t rows, const float *at,
+                                                 const int64_t *targets, int64_t V, float *lse, float *logprob)
+{
+    __shared__ float2 part[16][17];
+    const int r = threadIdx.x & 15, t0 = threadIdx.x >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    float most = -INFINITY, sum = 0.0f;
+    auto add = [&](float m, float s) {
+        const float both = fmaxf(most, m);
+        // (a part of nothing but -inf has no sum; one with a NaN or +inf has a NaN)
+        const float a = most > -INFINITY || !(sum == sum) ? sum * exp_of(most - both) : 0.0f;
+        const float b = m > -INFINITY || !(s == s) ? s * exp_of(m - both) : 0.0f;
+        most = both;
+        sum = a + b;
+    };
+    if (row < rows)
+        for (int t = t0; t < tiles; t += 16) {
+            const float2 s = stat[(int64_t)t * rows + row];
+            add(s.x, s.y);
+        }
+    part[r][t0] = make_float2(most, sum);
+    __syncthreads();
+    if (threadIdx.x >= 16 || row >= rows)
+        return;
+    most = -INFINITY;
+    sum = 0.0f;
+    for (int k = 0; k < 16; ++k)
+        add(part[r][k].x, part[r][k].y);
+    const bool bad = !(sum == sum), empty = most == -INFINITY;
+    const float log_sum = logf(sum);
+    if (lse)
+        lse[row] = bad ? NAN : empty ? -INFINITY : most + log_sum;
+    if (logprob) {
+        const int64_t t = targets[row];
+        logprob[row] = t < 0 ? 0.0f : t >= V || bad ? NAN : empty ? -INFINITY : (at[row] - most) - log_sum;
+    }
+}
+
+}  // namespace xfused_dev

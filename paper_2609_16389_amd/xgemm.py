@@ -24,7 +24,15 @@ _HEADER = os.path.join(os.path.dirname(_PKG), "include", "xgemm.h")
 XGEMM_BF16 = 0
 XGEMM_FP16 = 1
 
-XGEMM_FP32 = 2  # of logits only
+XGEMM_FP32 = 2  # of logits, of rows to be quantised and of 8-bit products' results
+XGEMM_INT8 = 3  # of rows that are quantised already
+
+XGEMM_ACT_SILU = 0
+XGEMM_ACT_GELU = 1
+XGEMM_ACT_GELU_TANH = 2
+
+XGEMM_FUSED_MAX_SIDE = 1 << 22
+XGEMM_SCALED_MAX_K = 131071
 
 XGEMM_OUT_FP32 = 0
 XGEMM_OUT_SAME = 1
@@ -207,6 +215,20 @@ lib.xgemm_logprob_run.argtypes = [_handle_t, _i64, _i64, _p, _i64, _p, _i64, _p,
 lib.xgemm_logprob_run.restype = _i32
 lib.xgemm_logprob_grad.argtypes = [_handle_t, _i64, _i64, _p, _i64, _p, _p, _p, _p, _p, _p, _p, _i64, _i32, _p]
 lib.xgemm_logprob_grad.restype = _i32
+lib.xgemm_scaled_rows.argtypes = [_handle_t, _i64, _i64, _p, _i64, _p, _i64, _p, _i32, _p]
+lib.xgemm_scaled_rows.restype = _i32
+lib.xgemm_scaled_run.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _i64, _i32, _i32, _p]
+lib.xgemm_scaled_run.restype = _i32
+lib.xgemm_gated_run.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _i32, _i32, _p]
+lib.xgemm_gated_run.restype = _i32
+lib.xgemm_gated_grad.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64,
+                                 _i32, _i32, _i32, _p]
+lib.xgemm_gated_grad.restype = _i32
+lib.xgemm_head_run.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _p, _p, _i32, _p]
+lib.xgemm_head_run.restype = _i32
+lib.xgemm_head_grad.argtypes = [_handle_t, _i64, _i64, _i64, _p, _i64, _p, _i64, _p, _p, _p, _p, _p, _i64, _p, _i64, _i32,
+                                _i32, _p]
+lib.xgemm_head_grad.restype = _i32
 lib.xgemm_strerror.argtypes = [_i32]
 lib.xgemm_strerror.restype = ctypes.c_char_p
 lib.xgemm_last_error.argtypes = [_handle_t]
@@ -397,6 +419,34 @@ def xgemm_logprob_grad(h, R, V, logits, ldl, targets, lse, entropy, d_logprob, d
                        stream) -> int:
     return lib.xgemm_logprob_grad(h, R, V, logits, ldl, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits,
                                   ldd, dtype, stream)
+
+
+def xgemm_scaled_rows(h, R, K, x, ldx, q, ldq, scales, dtype, stream) -> int:
+    return lib.xgemm_scaled_rows(h, R, K, x, ldx, q, ldq, scales, dtype, stream)
+
+
+def xgemm_scaled_run(h, M, N, K, x, ldx, x_scales, w, ldw, w_scales, y, ldy, x_dtype, y_dtype, stream) -> int:
+    return lib.xgemm_scaled_run(h, M, N, K, x, ldx, x_scales, w, ldw, w_scales, y, ldy, x_dtype, y_dtype, stream)
+
+
+def xgemm_gated_run(h, M, H, I, x, ldx, up, ldu, y, ldy, pre, ldp, act, dtype, out, stream) -> int:
+    return lib.xgemm_gated_run(h, M, H, I, x, ldx, up, ldu, y, ldy, pre, ldp, act, dtype, out, stream)
+
+
+def xgemm_gated_grad(h, M, H, I, x, ldx, up, ldu, pre, ldp, d_y, ldd, d_x, ld_dx, d_up, ld_dup, act, dtype, out,
+                     stream) -> int:
+    return lib.xgemm_gated_grad(h, M, H, I, x, ldx, up, ldu, pre, ldp, d_y, ldd, d_x, ld_dx, d_up, ld_dup, act, dtype, out,
+                                stream)
+
+
+def xgemm_head_run(h, T, V, H, x, ldx, head, ldw, targets, logprob, lse, dtype, stream) -> int:
+    return lib.xgemm_head_run(h, T, V, H, x, ldx, head, ldw, targets, logprob, lse, dtype, stream)
+
+
+def xgemm_head_grad(h, T, V, H, x, ldx, head, ldw, targets, lse, d_logprob, d_lse, d_x, ld_dx, d_head, ld_dw, dtype, out,
+                    stream) -> int:
+    return lib.xgemm_head_grad(h, T, V, H, x, ldx, head, ldw, targets, lse, d_logprob, d_lse, d_x, ld_dx, d_head, ld_dw,
+                               dtype, out, stream)
 
 
 def xgemm_strerror(status: int) -> str:
@@ -784,6 +834,215 @@ def logprobs_grad(logits, targets, lse, entropy=None, d_logprob=None, d_entropy=
                             _vector("entropy", entropy, (R,)), _vector("d_logprob", d_logprob, (R,)),
                             _vector("d_entropy", d_entropy, (R,)), _vector("d_lse", d_lse, (R,)),
                             out.data_ptr() or None, _ld(out), dtype, _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# products whose ends are fused
+# ---------------------------------------------------------------------------
+
+_REAL = {torch.bfloat16: XGEMM_BF16, torch.float16: XGEMM_FP16, torch.float32: XGEMM_FP32}
+_ACTS = {"silu": XGEMM_ACT_SILU, "gelu": XGEMM_ACT_GELU, "gelu_tanh": XGEMM_ACT_GELU_TANH}
+
+
+def _real_code(name, t) -> int:
+    if t.dtype not in _REAL:
+        raise TypeError("%s must be bfloat16, float16 or float32, got %s" % (name, t.dtype))
+    return _REAL[t.dtype]
+
+
+def _matrix(name, t, shape, dtype=None):
+    """The address of a tensor of this shape and type (None: NULL), and its leading dimension."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != shape or (dtype is not None and t.dtype != dtype):
+        raise ValueError("%s must be a %s%r tensor" % (name, "%s " % dtype if dtype is not None else "", shape))
+    return t.data_ptr() or None, _ld(t)
+
+
+def scaled_rows(x, out=None, stream=None):
+    """8-bit rows with a scale each, through xgemm_scaled_rows: (q, scales) with
+
+        scales[r] = max |x[r]| * (1 / 127)      q[r] = x[r] / scales[r], rounded to whole numbers
+
+    for x (R, K) bfloat16, float16 or float32 with contiguous rows; q: (R, K)
+    int8, scales: (R,) float32, written into the pair ``out`` if given.  Both the
+    activations and, once, the weights of ``gemm_scaled`` are made so.
+    """
+    dtype = _real_code("x", x)
+    if x.dim() != 2:
+        raise ValueError("expected x (R, K)")
+    R, K = x.shape
+    if out is None:
+        # (rows 16 bytes apart are read in place by the products)
+        q = torch.empty((R, (K + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :K]
+        out = (q, torch.empty((R,), dtype=torch.float32, device=x.device))
+    q, scales = out
+    s, h = _place(stream, x, q, scales)
+    pq, ldq = _matrix("q", q, (R, K), torch.int8)
+    rc = xgemm_scaled_rows(h, R, K, x.data_ptr() or None, _ld(x), pq, ldq, _vector("scales", scales, (R,)), dtype,
+                           _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def gemm_scaled(x, w, w_scales, x_scales=None, out=None, stream=None):
+    """Products in 8-bit integers, through xgemm_scaled_run:
+
+        out[m, n] = sum over k of x[m, k] * w[n, k] * x_scales[m] * w_scales[n]
+
+    x: (M, K) int8 CUDA tensor with x_scales (M,) float32, or bfloat16, float16 or
+    float32, which becomes 8-bit rows on the way as by ``scaled_rows``; w: (N, K)
+    int8 and w_scales (N,) float32; out: (M, N) float32, bfloat16 or float16 (the
+    default is x's type, for int8 float32).  Rows are contiguous.
+    """
+    whole = x.dtype == torch.int8
+    x_code = XGEMM_INT8 if whole else _real_code("x", x)
+    if whole != (x_scales is not None):
+        raise ValueError("x_scales are for an int8 x, which needs them")
+    if w.dtype != torch.int8:
+        raise TypeError("w must be int8")
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError("expected x (M, K) and w (N, K)")
+    (M, K), N = x.shape, w.shape[0]
+    if K > XGEMM_SCALED_MAX_K:
+        raise ValueError("K must be at most %d" % XGEMM_SCALED_MAX_K)
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.float32 if whole else x.dtype, device=x.device)
+    code = _real_code("out", out)
+    s, h = _place(stream, x, w, w_scales, x_scales, out)
+    py, ldy = _matrix("out", out, (M, N))
+    rc = xgemm_scaled_run(h, M, N, K, x.data_ptr() or None, _ld(x), _vector("x_scales", x_scales, (M,)),
+                          w.data_ptr() or None, _ld(w), _vector("w_scales", w_scales, (N,)), py, ldy, x_code, code,
+                          _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _gated_sizes(x, up, act):
+    """dtype, M, H, I and the activation's code."""
+    dtype = _dtype_code(x)
+    if up.dtype != x.dtype:
+        raise TypeError("x and up must have the same dtype")
+    if x.dim() != 2 or up.dim() != 2 or up.shape[1] != x.shape[1] or up.shape[0] % 2:
+        raise ValueError("expected x (M, H) and up (2 I, H)")
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(map(repr, _ACTS)), act))
+    return dtype, x.shape[0], x.shape[1], up.shape[0] // 2, _ACTS[act]
+
+
+def gated(x, up, act="silu", out=None, pre=None, stream=None):
+    """The inner values of a gated feed-forward block, through xgemm_gated_run:
+
+        out = act(x @ up[:I].T) * (x @ up[I:].T)
+
+    x: (M, H) and up: (2 I, H) bfloat16/float16 CUDA tensors of one dtype; act:
+    "silu", "gelu" (with erf) or "gelu_tanh"; out: (M, I) of x's dtype (the default)
+    or float32; pre: a (M, 2 I) tensor of x's dtype that takes both products, for
+    ``gated_grad``.  Rows are contiguous.
+    """
+    dtype, M, H, I, code = _gated_sizes(x, up, act)
+    if out is None:
+        out = torch.empty((M, I), dtype=x.dtype, device=x.device)
+    s, h = _place(stream, x, up, out, pre)
+    py, ldy = _matrix("out", out, (M, I))
+    pp, ldp = _matrix("pre", pre, (M, 2 * I), x.dtype)
+    rc = xgemm_gated_run(h, M, H, I, x.data_ptr() or None, _ld(x), up.data_ptr() or None, _ld(up), py, ldy, pp, ldp, code,
+                         dtype, _out_code(out, x.dtype), _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _grads(out, first, second):
+    """The pair of gradients to be written and the code of their type."""
+    if out is None:
+        out = (torch.empty_like(first, memory_format=torch.contiguous_format),
+               torch.empty_like(second, memory_format=torch.contiguous_format))
+    kept = [t for t in out if t is not None]
+    if len(out) != 2 or not kept:
+        raise ValueError("out must be a pair with a tensor in it")
+    if len(kept) == 2 and kept[0].dtype != kept[1].dtype:
+        raise TypeError("both gradients must have the same dtype")
+    return out, _out_code(kept[0], first.dtype)
+
+
+def gated_grad(x, up, pre, d_out, act="silu", out=None, stream=None):
+    """The gradient of ``gated`` in x and up, through xgemm_gated_grad: the pair
+    (d_x, d_up), given pre, as the forward call left it, and d_out (M, I), both of
+    x's dtype.  ``out``: a pair of tensors to write into, both of x's dtype (the
+    default) or both float32; None in a place of the pair: not computed."""
+    dtype, M, H, I, code = _gated_sizes(x, up, act)
+    out, kind = _grads(out, x, up)
+    s, h = _place(stream, x, up, pre, d_out, *out)
+    pp, ldp = _matrix("pre", pre, (M, 2 * I), x.dtype)
+    pd, ldd = _matrix("d_out", d_out, (M, I), x.dtype)
+    px, ldx = _matrix("d_x", out[0], (M, H))
+    pu, ldu = _matrix("d_up", out[1], (2 * I, H))
+    rc = xgemm_gated_grad(h, M, H, I, x.data_ptr() or None, _ld(x), up.data_ptr() or None, _ld(up), pp, ldp, pd, ldd, px,
+                          ldx, pu, ldu, code, dtype, kind, _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def _head_sizes(x, head):
+    dtype = _dtype_code(x)
+    if head.dtype != x.dtype:
+        raise TypeError("x and head must have the same dtype")
+    if x.dim() != 2 or head.dim() != 2 or head.shape[1] != x.shape[1] or head.shape[0] < 1:
+        raise ValueError("expected x (T, H) and head (V, H)")
+    return dtype, x.shape[0], head.shape[0], x.shape[1]
+
+
+def head_logprobs(x, head, targets=None, out=None, stream=None):
+    """Log probabilities under the logits x @ head.T, which are not kept, through
+    xgemm_head_run: a dict of
+
+    * "lse" (T,): log of the sum of the exponentials
+    * "logprob" (T,): log probability of ``targets`` (T,) int64, if given; 0
+      where the target is negative
+
+    both float32.  x: (T, H) and head: (V, H) bfloat16/float16 CUDA tensors of one
+    dtype with contiguous rows.  ``out``: a dict of tensors to write into and
+    return; what it leaves out is not computed.
+    """
+    dtype, T, V, H = _head_sizes(x, head)
+    if out is None:
+        out = {n: torch.empty((T,), dtype=torch.float32, device=x.device)
+               for n in (("lse",) if targets is None else ("lse", "logprob"))}
+    if out.get("logprob") is not None and targets is None:
+        raise ValueError("logprob needs targets")
+    s, h = _place(stream, x, head, targets, *out.values())
+    rc = xgemm_head_run(h, T, V, H, x.data_ptr() or None, _ld(x), head.data_ptr() or None, _ld(head),
+                        _vector("targets", targets, (T,), torch.int64), _vector("logprob", out.get("logprob"), (T,)),
+                        _vector("lse", out.get("lse"), (T,)), dtype, _stream_ptr(s) or None)
+    if rc != XGEMM_OK:
+        raise XgemmError(rc, xgemm_last_error(h))
+    return out
+
+
+def head_logprobs_grad(x, head, targets, lse, d_logprob=None, d_lse=None, out=None, stream=None):
+    """The gradient of ``head_logprobs``' results in x and head, through
+    xgemm_head_grad: the pair (d_x, d_head), given theirs (None: zero) and the
+    forward call's lse (targets only with d_logprob).  All (T,) float32, targets
+    int64.  ``out``: a pair of tensors to write into, both of x's dtype (the
+    default) or both float32; None in a place of the pair: not computed."""
+    dtype, T, V, H = _head_sizes(x, head)
+    if lse is None or (d_logprob is not None and targets is None):
+        raise ValueError("lse is needed, and targets with d_logprob")
+    out, kind = _grads(out, x, head)
+    s, h = _place(stream, x, head, targets, lse, d_logprob, d_lse, *out)
+    px, ldx = _matrix("d_x", out[0], (T, H))
+    pw, ldw = _matrix("d_head", out[1], (V, H))
+    rc = xgemm_head_grad(h, T, V, H, x.data_ptr() or None, _ld(x), head.data_ptr() or None, _ld(head),
+                         _vector("targets", targets, (T,), torch.int64), _vector("lse", lse, (T,)),
+                         _vector("d_logprob", d_logprob, (T,)), _vector("d_lse", d_lse, (T,)), px, ldx, pw, ldw, dtype,
+                         kind, _stream_ptr(s) or None)
     if rc != XGEMM_OK:
         raise XgemmError(rc, xgemm_last_error(h))
     return out

@@ -1,0 +1,225 @@
+"""The gated feed-forward block and its gradient against 64 bits (bounds:
+fused_ref.py)."""
+import math
+
+import pytest
+import torch
+
+import fused_ref
+from paper_2609_16389_amd import xgemm as xg
+
+TORCH = {"bf16": torch.bfloat16, "fp16": torch.float16}
+ACTS = ["silu", "gelu", "gelu_tanh"]
+
+
+def inputs(M, H, I, dtype, seed=0, pad=(0, 0), offset=(0, 0), scale=1.0):
+    dt = TORCH[dtype]
+    return (fused_ref.matrix(M, H, dt, seed, pad[0], offset[0], scale),
+            fused_ref.matrix(2 * I, H, dt, seed + 1, pad[1], offset[1], 1.0 / math.sqrt(max(H, 1))))
+
+
+# one row to a few; H within a chunk, at and past a step; sizes at the ends of
+# tiles; split sums; large tiles
+SHAPES = [(1, 1, 1), (1, 8, 16), (2, 7, 3), (3, 64, 65), (16, 65, 32), (17, 130, 33), (64, 200, 64), (65, 72, 129),
+          (5, 1001, 40), (1, 4096, 100), (130, 520, 270), (40, 2048, 500), (2053, 72, 2052), (2304, 64, 2048)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,H,I", SHAPES)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_shapes(M, H, I, dtype):
+    x, up = inputs(M, H, I, dtype, M + H + I)
+    for act in ACTS:
+        y, bound, pre, pre_bound = fused_ref.gated(x, up, act, TORCH[dtype])
+        saved = torch.empty(M, 2 * I, dtype=x.dtype, device="cuda")
+        fused_ref.check(xg.gated(x, up, act, pre=saved), y, bound, act)
+        fused_ref.check(saved, pre, pre_bound, "pre")
+        y, bound, _, _ = fused_ref.gated(x, up, act, torch.float32)
+        fused_ref.check(xg.gated(x, up, act, out=torch.empty(M, I, device="cuda")), y, bound, act + " fp32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,H,I", [(1, 96, 50), (5, 333, 70), (40, 512, 201), (200, 1030, 130), (2100, 48, 1100)])
+@pytest.mark.parametrize("pad,offset", [((0, 8), (0, 0)), ((3, 0), (0, 0)), ((0, 5), (1, 3)), ((8, 16), (8, 16)), ((1, 1), (7, 8))])
+def test_layouts(M, H, I, pad, offset):
+    for dtype in ("bf16", "fp16"):
+        x, up = inputs(M, H, I, dtype, H, pad, offset)
+        y, bound, pre, pre_bound = fused_ref.gated(x, up, "silu", x.dtype)
+        out, untouched = fused_ref.inside(M, I, x.dtype, pad[0], offset[0])
+        saved, untouched_pre = fused_ref.inside(M, 2 * I, x.dtype, pad[1], offset[1])
+        xg.gated(x, up, out=out, pre=saved)
+        fused_ref.check(out, y, bound, "out")
+        fused_ref.check(saved, pre, pre_bound, "pre")
+        untouched()
+        untouched_pre()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_far_values(act, dtype):
+    """Gates from the far left to the far right, where the activations are 0 or
+    the gate itself, and what is not a number stays so."""
+    dt = TORCH[dtype]
+    gates = torch.tensor([-6e4, -1e3, -100.0, -60.0, -20.0, -9.0, -5.5, -3.0, -0.75, -1e-3, 0.0, 1e-3, 0.5, 4.0, 9.0, 20.0, 100.0,
+                          1e3, 6e4, math.nan], device="cuda").to(dt)
+    n = len(gates)
+    x = torch.ones(3, 1, dtype=dt, device="cuda")
+    up = torch.cat((gates, torch.ones(n, device="cuda").to(dt)))[:, None].contiguous()
+    y, bound, _, _ = fused_ref.gated(x, up, act, torch.float32)
+    fused_ref.check(xg.gated(x, up, act, out=torch.empty(3, n, device="cuda")), y, bound, act)
+    # the gradient: d_up[i] = sum of the rows' slopes
+    pre = torch.cat((gates, torch.ones(n, device="cuda").to(dt))).expand(3, -1).contiguous()
+    d = torch.full((3, n), 0.25, dtype=dt, device="cuda")
+    (_, _), (du, bu) = fused_ref.gated_grad(x, up, pre[:, :], d, act, torch.float32)
+    got = torch.empty(2 * n, 1, device="cuda")
+    xg.gated_grad(x, up, pre, d, act, out=(None, got))
+    keep = torch.arange(2 * n) % n != n - 1          # (the NaN's bound is NaN too)
+    fused_ref.check(got[keep], du[keep], bu[keep], act)
+    assert bool(got[~keep].isnan().all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,H,I", [(1, 1, 1), (2, 7, 3), (3, 64, 65), (17, 130, 33), (65, 72, 129), (5, 1001, 40), (130, 520, 270),
+                                   (333, 100, 60), (2053, 40, 1030), (1024, 4096, 8), (4096, 8, 20), (520, 2048, 2052)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_gradient(M, H, I, dtype):
+    x, up = inputs(M, H, I, dtype, M + H + I)
+    pre = fused_ref.matrix(M, 2 * I, x.dtype, 5)
+    d = fused_ref.matrix(M, I, x.dtype, 6, scale=0.05)
+    for act in ACTS if M < 500 else ACTS[:1]:
+        for out in (x.dtype, torch.float32):
+            (dx, bx), (du, bu) = fused_ref.gated_grad(x, up, pre, d, act, out)
+            got = xg.gated_grad(x, up, pre, d, act, out=(torch.empty(M, H, dtype=out, device="cuda"),
+                                                         torch.empty(2 * I, H, dtype=out, device="cuda")))
+            fused_ref.check(got[0], dx, bx, "%s d_x" % act)
+            fused_ref.check(got[1], du, bu, "%s d_up" % act)
+    both = xg.gated_grad(x, up, pre, d)
+    for at in (0, 1):
+        one = [torch.empty_like(t) for t in both]
+        one[1 - at] = None
+        xg.gated_grad(x, up, pre, d, out=tuple(one))
+        assert torch.equal(one[at], both[at])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,H,I", [(5, 333, 71), (40, 96, 201), (200, 130, 333)])
+@pytest.mark.parametrize("pad,offset", [((3, 5), (1, 3)), ((8, 16), (8, 16)), ((0, 1), (7, 0))])
+def test_gradient_layouts(M, H, I, pad, offset):
+    for dtype in ("bf16", "fp16"):
+        x, up = inputs(M, H, I, dtype, H, pad, offset)
+        pre = fused_ref.matrix(M, 2 * I, x.dtype, 5, pad[0], offset[1])
+        d = fused_ref.matrix(M, I, x.dtype, 6, pad[1], offset[0], 0.05)
+        (dx, bx), (du, bu) = fused_ref.gated_grad(x, up, pre, d, "gelu", x.dtype)
+        out = [fused_ref.inside(M, H, x.dtype, pad[0], offset[0]), fused_ref.inside(2 * I, H, x.dtype, pad[1], offset[1])]
+        xg.gated_grad(x, up, pre, d, "gelu", out=(out[0][0], out[1][0]))
+        fused_ref.check(out[0][0], dx, bx, "d_x")
+        fused_ref.check(out[1][0], du, bu, "d_up")
+        out[0][1]()
+        out[1][1]()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [2.0 ** -24, 2.0 ** -14, 2.0 ** 8])
+def test_gradient_of_any_size_in_binary16(size):
+    """Gradients near binary16's smallest numbers keep their bits up to the results."""
+    x, up = inputs(70, 96, 130, "fp16", 9)
+    pre = fused_ref.matrix(70, 260, x.dtype, 5)
+    d = (torch.randn(70, 130, generator=torch.Generator().manual_seed(1)).sign() * size).to(torch.float16).cuda()
+    (dx, bx), (du, bu) = fused_ref.gated_grad(x, up, pre, d, "silu", torch.float32)
+    got = xg.gated_grad(x, up, pre, d, out=(torch.empty(70, 96, device="cuda"), torch.empty(260, 96, device="cuda")))
+    fused_ref.check(got[0], dx, bx, "d_x")
+    fused_ref.check(got[1], du, bu, "d_up")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS)
+def test_gradient_against_differences(act):
+    """Along a random direction, of the formula's own sum in 64 bits."""
+    M, H, I = 9, 24, 17
+    x, up = inputs(M, H, I, "bf16", 3)
+    d = fused_ref.matrix(M, I, x.dtype, 6)
+    pre = torch.empty(M, 2 * I, dtype=x.dtype, device="cuda")
+    xg.gated(x, up, act, pre=pre)
+    dx, du = xg.gated_grad(x, up, pre, d, act, out=(torch.empty(M, H, device="cuda"), torch.empty(2 * I, H, device="cuda")))
+    g = torch.Generator(device="cuda").manual_seed(4)
+    vx, vu = (torch.randn(t.shape, dtype=torch.float64, device="cuda", generator=g) for t in (x, up))
+
+    def total(t):
+        a = (x.double() + t * vx) @ (up.double() + t * vu).t().contiguous()
+        return float((fused_ref.act(act, a[:, :I])[0] * a[:, I:] * d.double()).sum())
+
+    t = 1e-5
+    slope = (total(t) - total(-t)) / (2 * t)
+    got = float((dx.double() * vx).sum() + (du.double() * vu).sum())
+    # pre and the slopes are rounded to bfloat16: 2^-8 of each term, of either sign
+    size = float((dx.double() * vx).abs().sum() + (du.double() * vu).abs().sum())
+    assert abs(got - slope) <= 4 * 2.0 ** -8 * size
+
+
+@pytest.mark.gpu
+def test_empty():
+    dt = torch.bfloat16
+    new = lambda *s: torch.full(s, 7.0, dtype=dt, device="cuda")  # noqa: E731
+    assert xg.gated(new(0, 8), new(6, 8)).shape == (0, 3)
+    assert xg.gated(new(4, 8), new(0, 8)).shape == (4, 0)
+    pre = new(4, 6)
+    assert bool((xg.gated(new(4, 0), new(6, 0), pre=pre) == 0).all()) and bool((pre == 0).all())
+    dx, du = xg.gated_grad(new(0, 8), new(6, 8), new(0, 6), new(0, 3), out=(new(0, 8), new(6, 8)))
+    assert bool((du == 0).all())
+    dx, du = xg.gated_grad(new(4, 8), new(0, 8), new(4, 0), new(4, 0), out=(new(4, 8), new(0, 8)))
+    assert bool((dx == 0).all())
+    dx, du = xg.gated_grad(new(4, 0), new(6, 0), new(4, 6), new(4, 3))
+    assert dx.shape == (4, 0) and du.shape == (6, 0)
+
+
+def test_refusals():
+    b = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    x, up = b(2, 8), b(6, 8)
+    with pytest.raises(ValueError, match="one GPU"):
+        xg.gated(x, up)
+    for args in ((x, up[:5]), (x, up[:, 1:]), (x[0], up), (x, up, "relu"), (x, up, None)):
+        with pytest.raises(ValueError):
+            xg.gated(*args)
+    for args in ((x.float(), up.float()), (x, up.half()), (x.double(), up)):
+        with pytest.raises(TypeError):
+            xg.gated(*args)
+    for out in ((None, None), (b(2, 8),)):
+        with pytest.raises(ValueError):
+            xg.gated_grad(x, up, b(2, 6), b(2, 3), out=out)
+    with pytest.raises(TypeError):
+        xg.gated_grad(x, up, b(2, 6), b(2, 3), out=(b(2, 8), torch.zeros(6, 8)))
+
+
+def test_status_without_a_gpu():
+    bad = xg.XGEMM_ERR_INVALID_ARG
+    assert xg.xgemm_gated_run(None, 1, 1, 1, None, 1, None, 1, None, 1, None, 0, 0, 0, 0, None) == bad
+    assert xg.xgemm_gated_grad(None, 1, 1, 1, None, 1, None, 1, None, 2, None, 1, None, 1, None, 1, 0, 0, 0, None) == bad
+
+
+@pytest.mark.gpu
+def test_shapes_and_statuses_are_checked():
+    b = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    x, up = b(2, 8), b(6, 8)
+    for kw in ({"out": b(2, 4)}, {"pre": b(2, 5)}, {"pre": b(2, 6).float()}, {"out": b(3, 2).t()}):
+        with pytest.raises(ValueError):
+            xg.gated(x, up, **kw)
+    for args in ((b(2, 5), b(2, 3)), (b(2, 6), b(2, 4)), (b(2, 6).half(), b(2, 3))):
+        with pytest.raises(ValueError):
+            xg.gated_grad(x, up, *args)
+    h, p = xg.handle(0), torch.zeros(4096, device="cuda").data_ptr()
+    ok = [h, 2, 8, 3, p, 8, p, 8, p, 3, p, 6, 0, 0, 1, None]
+    assert xg.xgemm_gated_run(*ok) == xg.XGEMM_OK
+    for at, value in ((1, -1), (2, -1), (3, -1), (3, 2 ** 62), (3, 2 ** 21 + 1), (2, 2 ** 22 + 1), (4, None), (5, 7), (6, None),
+                      (7, 7), (8, None), (9, 2), (11, 5), (12, 3), (12, -1), (13, 2), (14, 2)):
+        args = list(ok)
+        args[at] = value
+        assert xg.xgemm_gated_run(*args) == xg.XGEMM_ERR_INVALID_ARG, (at, value)
+    ok = [h, 2, 8, 3, p, 8, p, 8, p, 6, p, 3, p, 8, p, 8, 0, 0, 1, None]
+    assert xg.xgemm_gated_grad(*ok) == xg.XGEMM_OK
+    for at, value in ((1, -1), (2, -1), (3, -1), (4, None), (5, 7), (6, None), (7, 7), (8, None), (9, 5), (10, None), (11, 2),
+                      (13, 7), (15, 7), (16, 3), (17, 2), (18, -1)):
+        args = list(ok)
+        args[at] = value
+        assert xg.xgemm_gated_grad(*args) == xg.XGEMM_ERR_INVALID_ARG, (at, value)
+    torch.cuda.synchronize()
