@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     const int wm = wave % WM, wn = wave / WM;
     const int m0 = tm * BM, n0 = tn * (End::kGated ? BN / 2 : BN);
     const int k0 = ks * p.chunk * OpA::KS, kend = min(p.K, k0 + p.chunk * OpA::KS);
-    const int nk = kend > k0 ? (kend - k0 + OpA::KS - 1) / OpA::KS : 0;
+    // (at least two steps, so that the code below is one line; what lies past kend is zero)
+    const int nk = max((kend - k0 + OpA::KS - 1) / OpA::KS, 2);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)smem;
     OpA a;
@@ -290,36 +291,101 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         a.next();
         b.next();
     };
-    if (nk > 0)
-        load_step(0);
-    for (int t = 0; t < nk; ++t) {
-        const int stage = t & 1;
-        if (t + 1 < nk) {
-            load_step(stage ^ 1);
-            wait_loads<LD>();
-        } else {
-            wait_loads<0>();
-        }
-        meet();
-        const char *const sa = smem + stage * STAGE, *const sb = sa + OpA::kBytes;
+    auto read_a = [&](int stage, int kk, int i) { return OpA::read(smem + stage * STAGE, wm * TM + i * 16, kk, lane); };
+    auto read_b = [&](int stage, int kk, int j) {
+        return OpB::read(smem + stage * STAGE + OpA::kBytes, wn * TN + j * 16, kk, lane);
+    };
+    // A step of two sub-steps, whose fragments have registers of their own: those
+    // of the next sub-step are read as soon as a row of the current one has issued
+    // its products.  One row of the second sub-step runs before the barrier,
+    // which gives the last read time; after the barrier, which frees this
+    // step's stage, the loads of the step after the next go there, spaced by
+    // products, at a raised priority against the other wave of the SIMD.
+    constexpr int R = 1;
+    constexpr int REST = (FM - R) * FN;               // products after the barrier
+    constexpr int APART = REST / LD > 0 ? REST / LD : 1;
+    constexpr int BR = (FN + FM - R - 1) / (FM - R);   // fragments of B read with each row after it
+    static_assert(FN <= FM && APART * (LD - 1) < REST, "spacing");
+    u32x4 ga[2][FM], gb[2][FN];
+    auto step = [&]<bool LOAD, bool MORE>(int t) {
+        const int stage = t & 1, next = stage ^ 1;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u32x4 fa[FM], fb[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-                fa[i] = OpA::read(sa, wm * TM + i * 16, kk, lane);
+        for (int i = 0; i < FM; ++i) {
 #pragma unroll
             for (int j = 0; j < FN; ++j)
-                fb[j] = OpB::read(sb, wn * TN + j * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    acc[i][j] = mfma<TYPE>(fb[j], fa[i], acc[i][j]);
+                acc[i][j] = mfma<TYPE>(gb[0][j], ga[0][i], acc[i][j]);
+            ga[1][i] = read_a(stage, 1, i);
+            if (i < FN)
+                gb[1][i] = read_b(stage, 1, i);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                acc[i][j] = mfma<TYPE>(gb[1][j], ga[1][i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        // this wave has read all of the stage; its loads of the next step have landed
         wait_lds();
+        if constexpr (MORE)
+            wait_loads<0>();
         meet();
-    }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        u32x4 da, db;
+        if constexpr (LOAD) {
+            da = a.view();
+            db = b.view();
+        }
+        if constexpr (MORE) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                ga[0][i] = read_a(next, 0, i);
+        }
+#pragma unroll
+        for (int i = R; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                acc[i][j] = mfma<TYPE>(gb[1][j], ga[1][i], acc[i][j]);
+                if constexpr (LOAD) {
+                    const int n = (i - R) * FN + j;
+                    if (n % APART == 0 && n / APART < LD) {
+                        const int l = n / APART;
+                        if (l < OpA::kLoads)
+                            a.load(da, stage * STAGE, l);
+                        else
+                            b.load(db, stage * STAGE, l - OpA::kLoads);
+                    }
+                }
+            }
+            if constexpr (MORE) {
+                ga[0][i] = read_a(next, 0, i);
+#pragma unroll
+                for (int j = (i - R) * BR; j < (i - R + 1) * BR && j < FN; ++j)
+                    gb[0][j] = read_b(next, 0, j);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (LOAD) {
+            a.next();
+            b.next();
+        }
+    };
+    load_step(0);
+    load_step(1);
+    wait_loads<LD>();
+    meet();
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+        ga[0][i] = read_a(0, 0, i);
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+        gb[0][j] = read_b(0, 0, j);
+    for (int t = 0; t < nk - 2; ++t)
+        step.template operator()<true, true>(t);
+    step.template operator()<false, true>(nk - 2);
+    step.template operator()<false, false>(nk - 1);
     // lane l holds row l % 16 of each block and columns 4 (l / 16) .. + 3
     End::template finish<BM, BN, TM, TN, FM, FN, WN>(p, e, acc, smem, m0, n0, wm, wn, tn, ks, lane);
 }
