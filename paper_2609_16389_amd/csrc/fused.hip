@@ -2,6 +2,7 @@
 // launch selection and launches.  The C ABI is declared in include/xgemm.h.
 #include "context.hpp"
 #include "fused_ends.hpp"
+#include "fused_rows.hpp"
 #include "fused_tile.hpp"
 
 #include <algorithm>
@@ -151,6 +152,39 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
     launch_tiles<TYPE, LA, LB, End>(p, e, c.large, s);
 }
 
+// Rows that the kernels for few of them take (fused_rows.hpp).
+constexpr int64_t kFewRows = 16;
+
+// Whether rows can be read through LDS: 16-byte chunks, near enough.
+bool whole_chunks(const RowsParams &p)
+{
+    const int64_t x = p.M > 1 ? (int64_t)(uintptr_t)p.x | p.ldx : (int64_t)(uintptr_t)p.x;
+    const int64_t w = (int64_t)((uintptr_t)p.w | (uintptr_t)p.w2) | p.ldw;
+    return (w | x | p.K) % 16 == 0 && p.ldw <= kMaxStep && (p.M == 1 || p.ldx <= kMaxStep);
+}
+
+template <int TYPE, class End>
+void launch_rows(RowsParams p, const typename End::Params &e, int cu_count, hipStream_t s)
+{
+    constexpr bool kGated = End::kGated;
+    if (p.M == 1)
+        p.ldx = 0;
+    if (whole_chunks(p)) {
+        const dim3 grid(std::min<int64_t>(cdiv(p.N, 16), cu_count)), block(64 * kStreamWaves);
+        if (p.M <= 4)
+            hipLaunchKernelGGL((rows_stream<TYPE, End, 1, kGated ? 4 : 6, -1>), grid, block, 0, s, p, e);
+        else
+            hipLaunchKernelGGL((rows_stream<TYPE, End, 4, kGated ? 3 : 4, -1>), grid, block, 0, s, p, e);
+        return;
+    }
+    const bool odd = ((int64_t)((uintptr_t)p.w | (uintptr_t)p.w2 | (uintptr_t)p.x) | p.ldw | p.ldx) & 3;
+    const dim3 grid(cdiv(p.N, 16)), block(64 * 4);
+    if (odd)
+        hipLaunchKernelGGL((rows_product<TYPE, End, 4, true>), grid, block, 0, s, p, e);
+    else
+        hipLaunchKernelGGL((rows_product<TYPE, End, 4, false>), grid, block, 0, s, p, e);
+}
+
 TileParams tile_params(const Matrix &A, const Matrix &B, int64_t M, int64_t N, int64_t K)
 {
     TileParams p{};
@@ -236,6 +270,42 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
     const bool whole = x_dtype == XGEMM_INT8;
     if (!y || !w_scales || (K > 0 && (!x || !w)) || whole != (x_scales != nullptr))
         return XGEMM_ERR_INVALID_ARG;
+    const int kind = y_dtype == XGEMM_FP32 ? kFp32 : y_dtype == XGEMM_FP16 ? kFp16 : kBf16;
+    if (M <= kFewRows && K > 0) {
+        RowsParams p{(const char *)x, (const char *)w, nullptr, ldx, ldw, (int)M, (int)N, (int)K};
+        ScaledEnd::Params e{x_scales, w_scales, y, ldy, kind};
+        // (one row becomes 8-bit within the product)
+        const bool here = ((int64_t)(uintptr_t)w | ldw | K) % 16 == 0 && ldw <= kMaxStep && K <= kQuantBytes;
+        if (!whole && M == 1 && here) {
+            const dim3 grid(std::min<int64_t>(cdiv(N, 16), h->cu_count)), block(64 * kStreamWaves);
+            if (x_dtype == XGEMM_BF16)
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kBf16>), grid, block, 0, s, p, e);
+            else if (x_dtype == XGEMM_FP16)
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp16>), grid, block, 0, s, p, e);
+            else
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp32>), grid, block, 0, s, p, e);
+            return launch_status(h, "scaled product launch");
+        }
+        if (whole) {
+            launch_rows<kInt8, ScaledEnd>(p, e, h->cu_count, s);
+            return launch_status(h, "scaled product launch");
+        }
+        Space ws;
+        const int64_t ld = up_to(K, 16);
+        const size_t at_q = ws.take((size_t)(M * ld)), at_scales = ws.take((size_t)M * 4);
+        const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
+        if (rc != XGEMM_OK)
+            return rc;
+        char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
+        e.row_scale = (const float *)(base + at_scales);
+        p.x = base + at_q;
+        p.ldx = ld;
+        launch_scale_rows(x_dtype, M, K, x, ldx, (int8_t *)(base + at_q), ld, ld, (float *)(base + at_scales), s);
+        launch_rows<kInt8, ScaledEnd>(p, e, h->cu_count, s);
+        const int launched = launch_status(h, "scaled product launch");
+        const int released = xgemm_host::release_workspace(h, s);
+        return launched != XGEMM_OK ? launched : released;
+    }
     Space ws;
     const int64_t padded = up_to(K, 16);
     const size_t at_q = ws.take(whole ? 0 : (size_t)M * padded), at_scales = ws.take(whole ? 0 : (size_t)M * 4);
@@ -257,7 +327,6 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
         x_scales = (const float *)(base + at_scales);
     }
     TileParams p = tile_params(A, B, M, N, padded);
-    const int kind = y_dtype == XGEMM_FP32 ? kFp32 : y_dtype == XGEMM_FP16 ? kFp16 : kBf16;
     for (int64_t m = 0; m < M; m += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, M - m);
         p.A = A.p + m * A.ld;
@@ -302,6 +371,16 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
         return XGEMM_OK;
     if (!y || (H > 0 && (!x || !up)))
         return XGEMM_ERR_INVALID_ARG;
+    const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
+    if (M <= kFewRows && H > 0) {
+        const RowsParams p{(const char *)x, (const char *)up, (const char *)up + I * ldu * 2, ldx * 2, ldu * 2,
+                           (int)M, (int)I, (int)H * 2};
+        if (dtype == XGEMM_BF16)
+            launch_rows<kBf16, GatedEnd<kBf16>>(p, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+        else
+            launch_rows<kFp16, GatedEnd<kFp16>>(p, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+        return launch_status(h, "gated launch");
+    }
     Space ws;
     Matrix A(x, M, H, ldx, 2, ws), B(up, 2 * I, H, ldu, 2, ws);
     const int64_t K = up_to(H, 8);
@@ -317,7 +396,6 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
     B.place(base, s);
     TileParams p = tile_params(A, B, M, I, K);
     p.B2 = B.p + I * B.ld;
-    const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     if (dtype == XGEMM_BF16)
         launch_gated<kBf16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, base + at_part, s);
     else
@@ -374,22 +452,22 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     g.chunks = (int)cdiv(I, 8);
     g.most = word;
     g.inverse = (float *)(word + 1);
-    auto slopes = [&](auto kernel) {
+    auto slopes = [&](auto kernel, int64_t most_blocks) {
         const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 30) / g.chunks);
         for (int64_t m = 0; m < M; m += rows) {
             g.M = (int)std::min(rows, M - m);
             g.pre = (const uint16_t *)pre + m * ldp;
             g.d = (const uint16_t *)d_y + m * ldd;
             g.out = (uint16_t *)(base + at_d) + m * ld;
-            hipLaunchKernelGGL(kernel, dim3(cdiv((int64_t)g.M * g.chunks, 256)), dim3(256), 0, s, g);
+            hipLaunchKernelGGL(kernel, dim3(std::min(cdiv((int64_t)g.M * g.chunks, 256), most_blocks)), dim3(256), 0, s, g);
         }
     };
     if (some && dtype == XGEMM_BF16) {
-        slopes(gated_slope<kBf16, false>);
+        slopes(gated_slope<kBf16, false>, kMaxDim);
     } else if (some) {
         hipLaunchKernelGGL(set_words, dim3(1), dim3(64), 0, s, word, 2);
-        slopes(gated_slope<kFp16, true>);
-        slopes(gated_slope<kFp16, false>);
+        slopes(gated_slope<kFp16, true>, 4 * (int64_t)std::max(h->cu_count, 1));
+        slopes(gated_slope<kFp16, false>, kMaxDim);
     }
     const float *const scale = some && dtype == XGEMM_FP16 ? g.inverse : nullptr;
     TileParams p{};

@@ -586,10 +586,9 @@ __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v
 template <int DT, bool MOST>
 __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(at / p.chunks), col = (int)(at % p.chunks) * 8;
     uint32_t most = 0;
-    if (row < p.M) {
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)p.M * p.chunks; at += (int64_t)gridDim.x * 256) {
+        const int row = (int)(at / p.chunks), col = (int)(at % p.chunks) * 8;
         float g[8], u[8], d[8], dg[8], du[8];
         const uint16_t *const pre = p.pre + (int64_t)row * p.ldp;
         eight<DT>((const char *)pre, col, p.I, g);
@@ -634,9 +633,14 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
         }
     }
     if constexpr (MOST) {
+        // (the largest is the same in any order; atomics on one address take 15 ns each)
+        __shared__ uint32_t share_most[4];
         most = most_of(most);
-        if ((threadIdx.x & 63) == 0 && most)
-            atomicMax(p.most, most);   // (the largest: the same in any order)
+        if ((threadIdx.x & 63) == 0)
+            share_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            atomicMax(p.most, max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
     }
 }
 

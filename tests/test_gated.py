@@ -21,7 +21,8 @@ def inputs(M, H, I, dtype, seed=0, pad=(0, 0), offset=(0, 0), scale=1.0):
 # one row to a few; H within a chunk, at and past a step; sizes at the ends of
 # tiles; split sums; large tiles
 SHAPES = [(1, 1, 1), (1, 8, 16), (2, 7, 3), (3, 64, 65), (16, 65, 32), (17, 130, 33), (64, 200, 64), (65, 72, 129),
-          (5, 1001, 40), (1, 4096, 100), (130, 520, 270), (40, 2048, 500), (2053, 72, 2052), (2304, 64, 2048)]
+          (5, 1001, 40), (1, 4096, 100), (130, 520, 270), (40, 2048, 500), (2053, 72, 2052), (2304, 64, 2048),
+          (1, 64, 4200), (4, 256, 8300), (7, 2056, 4500), (16, 512, 100), (16, 4104, 50)]
 
 
 @pytest.mark.gpu
