@@ -36,6 +36,19 @@ typedef int (*logprob_fn)(void *, int64_t, int64_t, const void *, int64_t, const
 typedef int (*grad_fn)(void *, int64_t, int64_t, const void *, int64_t, const int64_t *, const float *, const float *,
                        const float *, const float *, const float *, void *, int64_t, int, void *);
 
+typedef int (*rows_fn)(void *, int64_t, int64_t, const void *, int64_t, int8_t *, int64_t, float *, int, void *);
+typedef int (*scaled_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const float *, const int8_t *, int64_t,
+                         const float *, void *, int64_t, int, int, void *);
+typedef int (*gated_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const void *, int64_t, void *, int64_t,
+                        void *, int64_t, int, int, int, void *);
+typedef int (*gated_grad_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const void *, int64_t, const void *,
+                             int64_t, const void *, int64_t, void *, int64_t, void *, int64_t, int, int, int, void *);
+typedef int (*head_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const void *, int64_t, const int64_t *,
+                       float *, float *, int, void *);
+typedef int (*head_grad_fn)(void *, int64_t, int64_t, int64_t, const void *, int64_t, const void *, int64_t,
+                            const int64_t *, const float *, const float *, const float *, void *, int64_t, void *, int64_t,
+                            int, int, void *);
+
 gemm_fn f_run, f_noalloc;
 batched_fn f_batched;
 gemv_fn f_gemv;
@@ -43,15 +56,28 @@ quant_fn f_quant;
 experts_fn f_experts;
 logprob_fn f_logprob;
 grad_fn f_grad;
+rows_fn f_rows;
+scaled_fn f_scaled;
+gated_fn f_gated;
+gated_grad_fn f_gated_grad;
+head_fn f_head;
+head_grad_fn f_head_grad;
 PyObject *handles;  // the module's dict: (device index, stream address) -> handle address
 
 PyObject *bind(PyObject *, PyObject *args)
 {
-    unsigned long long run, noalloc, batched, gemv, quant, experts, logprob, grad;
+    unsigned long long run, noalloc, batched, gemv, quant, experts, logprob, grad, rows, scaled, gated, gated_grad, head,
+        head_grad;
     PyObject *d;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKO!", &run, &noalloc, &batched, &gemv, &quant, &experts, &logprob, &grad,
-                          &PyDict_Type, &d))
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKKO!", &run, &noalloc, &batched, &gemv, &quant, &experts, &logprob, &grad,
+                          &rows, &scaled, &gated, &gated_grad, &head, &head_grad, &PyDict_Type, &d))
         return nullptr;
+    f_rows = (rows_fn)rows;
+    f_scaled = (scaled_fn)scaled;
+    f_gated = (gated_fn)gated;
+    f_gated_grad = (gated_grad_fn)gated_grad;
+    f_head = (head_fn)head;
+    f_head_grad = (head_grad_fn)head_grad;
     f_run = (gemm_fn)run;
     f_noalloc = (gemm_fn)noalloc;
     f_batched = (batched_fn)batched;
@@ -365,6 +391,198 @@ PyObject *logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
+// Any of the library's real types, or -1.
+int real_code(const at::Tensor &t) { return logits_code(t); }
+
+// A matrix of this shape on x's device, of a type to be looked at by the caller.
+const at::Tensor *matrix(PyObject *o, const at::Tensor &x, int64_t rows, int64_t cols)
+{
+    const at::Tensor *t = plain(o);
+    return t && t->dim() == 2 && t->device() == x.device() && t->size(0) == rows && t->size(1) == cols && leading(*t, 0) >= 0
+               ? t
+               : nullptr;
+}
+
+PyObject *scaled_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 3 || !handles)
+        Py_RETURN_NONE;
+    const at::Tensor *x = plain(a[0]);
+    if (!x || x->dim() != 2)
+        Py_RETURN_NONE;
+    const int64_t R = x->size(0), K = x->size(1), ldx = leading(*x, 0);
+    const int code = real_code(*x);
+    const at::Tensor *q = matrix(a[1], *x, R, K);
+    void *scales, *stream, *h;
+    if (!q || q->scalar_type() != at::kChar || code < 0 || ldx < 0 || a[2] == Py_None ||
+        !vector_of(a[2], *x, R, 0, at::kFloat, &scales) || !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x);
+    int8_t *pq = (int8_t *)data(*q);
+    const int64_t ldq = leading(*q, 0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_rows(h, R, K, px, ldx, pq, ldq, (float *)scales, code, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+PyObject *gemm_scaled(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 5 || !handles)
+        Py_RETURN_NONE;
+    const at::Tensor *x = plain(a[0]), *w = plain(a[1]), *y = plain(a[4]);
+    if (!x || !w || !y || x->dim() != 2 || w->dim() != 2 || w->device() != x->device())
+        Py_RETURN_NONE;
+    const bool whole = x->scalar_type() == at::kChar;
+    const int64_t M = x->size(0), K = x->size(1), N = w->size(0), ldx = leading(*x, 0), ldw = leading(*w, 0);
+    const int x_code = whole ? 3 : real_code(*x), y_code = real_code(*y);
+    void *ws, *xs, *stream, *h;
+    if (w->scalar_type() != at::kChar || w->size(1) != K || x_code < 0 || y_code < 0 || ldx < 0 || ldw < 0 ||
+        !matrix(a[4], *x, M, N) || whole != (a[3] != Py_None) || a[2] == Py_None || K > 131071 ||
+        !vector_of(a[2], *x, N, 0, at::kFloat, &ws) || !vector_of(a[3], *x, M, 0, at::kFloat, &xs) ||
+        !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x);
+    const int8_t *pw = (const int8_t *)data(*w);
+    void *py = data(*y);
+    const int64_t ldy = leading(*y, 0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_scaled(h, M, N, K, px, ldx, (const float *)xs, pw, ldw, (const float *)ws, py, ldy, x_code, y_code, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// x (M, H), up (2 I, H) and an activation's code.
+bool gated_args(PyObject *const *a, PyObject *act, const at::Tensor **x, const at::Tensor **up, int64_t *code)
+{
+    *x = plain(a[0]);
+    *up = plain(a[1]);
+    return *x && *up && (*x)->dim() == 2 && (*up)->dim() == 2 && code_of(**x) >= 0 && code_of(**up) == code_of(**x) &&
+           (*up)->device() == (*x)->device() && (*up)->size(1) == (*x)->size(1) && (*up)->size(0) % 2 == 0 &&
+           leading(**x, 0) >= 0 && leading(**up, 0) >= 0 && small(act, code) && *code >= 0 && *code <= 2;
+}
+
+PyObject *gated(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    const at::Tensor *x, *up, *pre = nullptr;
+    int64_t act;
+    if (n != 5 || !handles || !gated_args(a, a[2], &x, &up, &act))
+        DECLINE;
+    const int code = code_of(*x);
+    const int64_t M = x->size(0), H = x->size(1), I = up->size(0) / 2;
+    const at::Tensor *y = matrix(a[3], *x, M, I);
+    const int out = y ? out_of(*y, *x) : -1;
+    void *stream, *h;
+    if (out < 0 || (a[4] != Py_None && (!(pre = matrix(a[4], *x, M, 2 * I)) || code_of(*pre) != code)) ||
+        !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x), *pu = data(*up);
+    void *py = data(*y), *pp = pre ? data(*pre) : nullptr;
+    const int64_t ldx = leading(*x, 0), ldu = leading(*up, 0), ldy = leading(*y, 0), ldp = pre ? leading(*pre, 0) : 0;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_gated(h, M, H, I, px, ldx, pu, ldu, py, ldy, pp, ldp, (int)act, code, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// A pair of gradients, either absent (None), of one type; their `out` or -1.
+int grads_of(PyObject *first, PyObject *second, const at::Tensor &x, const at::Tensor &w, const at::Tensor **d_x,
+             const at::Tensor **d_w)
+{
+    *d_x = *d_w = nullptr;
+    if ((first == Py_None && second == Py_None) ||
+        (first != Py_None && !(*d_x = matrix(first, x, x.size(0), x.size(1)))) ||
+        (second != Py_None && !(*d_w = matrix(second, x, w.size(0), w.size(1)))) ||
+        (*d_x && *d_w && (*d_x)->scalar_type() != (*d_w)->scalar_type()))
+        return -1;
+    return out_of(*d_x ? **d_x : **d_w, x);
+}
+
+PyObject *gated_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    const at::Tensor *x, *up, *d_x, *d_up;
+    int64_t act;
+    if (n != 7 || !handles || !gated_args(a, a[4], &x, &up, &act))
+        DECLINE;
+    const int code = code_of(*x), out = grads_of(a[5], a[6], *x, *up, &d_x, &d_up);
+    const int64_t M = x->size(0), H = x->size(1), I = up->size(0) / 2;
+    const at::Tensor *pre = matrix(a[2], *x, M, 2 * I), *d = matrix(a[3], *x, M, I);
+    void *stream, *h;
+    if (out < 0 || !pre || !d || code_of(*pre) != code || code_of(*d) != code || !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x), *pu = data(*up), *pp = data(*pre), *pd = data(*d);
+    void *gx = d_x ? data(*d_x) : nullptr, *gu = d_up ? data(*d_up) : nullptr;
+    const int64_t ldx = leading(*x, 0), ldu = leading(*up, 0), ldp = leading(*pre, 0), ldd = leading(*d, 0),
+                  ldgx = d_x ? leading(*d_x, 0) : 0, ldgu = d_up ? leading(*d_up, 0) : 0;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_gated_grad(h, M, H, I, px, ldx, pu, ldu, pp, ldp, pd, ldd, gx, ldgx, gu, ldgu, (int)act, code, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// x (T, H) and head (V, H).
+bool head_args(PyObject *const *a, const at::Tensor **x, const at::Tensor **w)
+{
+    *x = plain(a[0]);
+    *w = plain(a[1]);
+    return *x && *w && (*x)->dim() == 2 && (*w)->dim() == 2 && code_of(**x) >= 0 && code_of(**w) == code_of(**x) &&
+           (*w)->device() == (*x)->device() && (*w)->size(1) == (*x)->size(1) && (*w)->size(0) >= 1 &&
+           leading(**x, 0) >= 0 && leading(**w, 0) >= 0;
+}
+
+PyObject *head_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    const at::Tensor *x, *w;
+    if (n != 4 || !handles || !PyDict_CheckExact(a[3]) || !head_args(a, &x, &w))
+        DECLINE;
+    const int64_t T = x->size(0), V = w->size(0), H = x->size(1);
+    PyObject *o[2] = {PyDict_GetItemString(a[3], "logprob"), PyDict_GetItemString(a[3], "lse")};
+    void *t, *p[2], *stream, *h;
+    if (PyDict_Size(a[3]) != (o[0] != nullptr) + (o[1] != nullptr) || !vector_of(a[2], *x, T, 0, at::kLong, &t) ||
+        !vector_of(o[0], *x, T, 0, at::kFloat, &p[0]) || !vector_of(o[1], *x, T, 0, at::kFloat, &p[1]) ||
+        (o[0] && o[0] != Py_None && a[2] == Py_None) || !stream_handle(*x, &stream, &h))
+        DECLINE;
+    const int code = code_of(*x);
+    const void *px = data(*x), *pw = data(*w);
+    const int64_t ldx = leading(*x, 0), ldw = leading(*w, 0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_head(h, T, V, H, px, ldx, pw, ldw, (const int64_t *)t, (float *)p[0], (float *)p[1], code, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+PyObject *head_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    const at::Tensor *x, *w, *d_x, *d_w;
+    if (n != 8 || !handles || !head_args(a, &x, &w))
+        DECLINE;
+    const int code = code_of(*x), out = grads_of(a[6], a[7], *x, *w, &d_x, &d_w);
+    const int64_t T = x->size(0), V = w->size(0), H = x->size(1);
+    void *t, *p[3], *stream, *h;
+    if (out < 0 || a[3] == Py_None || (a[4] != Py_None && a[2] == Py_None) || !vector_of(a[2], *x, T, 0, at::kLong, &t))
+        DECLINE;
+    for (int i = 0; i < 3; ++i)   // lse and the two gradients
+        if (!vector_of(a[3 + i], *x, T, 0, at::kFloat, &p[i]))
+            DECLINE;
+    if (!stream_handle(*x, &stream, &h))
+        DECLINE;
+    const void *px = data(*x), *pw = data(*w);
+    void *gx = d_x ? data(*d_x) : nullptr, *gw = d_w ? data(*d_w) : nullptr;
+    const int64_t ldx = leading(*x, 0), ldw = leading(*w, 0), ldgx = d_x ? leading(*d_x, 0) : 0,
+                  ldgw = d_w ? leading(*d_w, 0) : 0;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_head_grad(h, T, V, H, px, ldx, pw, ldw, (const int64_t *)t, (const float *)p[0], (const float *)p[1],
+                     (const float *)p[2], gx, ldgx, gw, ldgw, code, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // xgemm_run / xgemm_run_noalloc on twelve plain integers (addresses may be
 // None); anything else is declined.
 PyObject *twelve(gemm_fn f, PyObject *const *a, Py_ssize_t n)
@@ -419,6 +637,16 @@ PyMethodDef methods[] = {
      "xgemm_logprob_run on (logits, targets, top, dict of outputs)."},
     {"logprobs_grad", (PyCFunction)(void *)guarded<logprobs_grad>, METH_FASTCALL,
      "xgemm_logprob_grad on (logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, out)."},
+    {"scaled_rows", (PyCFunction)(void *)guarded<scaled_rows>, METH_FASTCALL, "xgemm_scaled_rows on (x, q, scales)."},
+    {"gemm_scaled", (PyCFunction)(void *)guarded<gemm_scaled>, METH_FASTCALL,
+     "xgemm_scaled_run on (x, w, w_scales, x_scales, out)."},
+    {"gated", (PyCFunction)(void *)guarded<gated>, METH_FASTCALL, "xgemm_gated_run on (x, up, act's code, out, pre)."},
+    {"gated_grad", (PyCFunction)(void *)guarded<gated_grad>, METH_FASTCALL,
+     "xgemm_gated_grad on (x, up, pre, d_out, act's code, d_x, d_up)."},
+    {"head_logprobs", (PyCFunction)(void *)guarded<head_logprobs>, METH_FASTCALL,
+     "xgemm_head_run on (x, head, targets, dict of outputs)."},
+    {"head_logprobs_grad", (PyCFunction)(void *)guarded<head_logprobs_grad>, METH_FASTCALL,
+     "xgemm_head_grad on (x, head, targets, lse, d_logprob, d_lse, d_x, d_head)."},
     {"run", (PyCFunction)(void *)guarded<run>, METH_FASTCALL, "xgemm_run on its twelve arguments."},
     {"run_noalloc", (PyCFunction)(void *)guarded<run_noalloc>, METH_FASTCALL, "xgemm_run_noalloc likewise."},
     {nullptr, nullptr, 0, nullptr},

@@ -154,6 +154,7 @@ else:
         """Declines every call."""
         bind = run = run_noalloc = gemm = bmm = gemv = staticmethod(lambda *args: None)
         gemv_quant = experts = logprobs = logprobs_grad = run
+        scaled_rows = gemm_scaled = gated = gated_grad = head_logprobs = head_logprobs_grad = run
 
 _i64, _i32, _p = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p
 _handle_t = ctypes.c_void_p
@@ -465,7 +466,9 @@ _handles = {}
 
 _fastcall.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                  (lib.xgemm_run, lib.xgemm_run_noalloc, lib.xgemm_run_strided_batched, lib.xgemv_run,
-                  lib.xgemv_quant_run, lib.xgemm_experts_run, lib.xgemm_logprob_run, lib.xgemm_logprob_grad)), _handles)
+                  lib.xgemv_quant_run, lib.xgemm_experts_run, lib.xgemm_logprob_run, lib.xgemm_logprob_grad,
+                  lib.xgemm_scaled_rows, lib.xgemm_scaled_run, lib.xgemm_gated_run, lib.xgemm_gated_grad,
+                  lib.xgemm_head_run, lib.xgemm_head_grad)), _handles)
 
 
 def _checked(rc, device_index, out):
@@ -871,6 +874,10 @@ def scaled_rows(x, out=None, stream=None):
     int8, scales: (R,) float32, written into the pair ``out`` if given.  Both the
     activations and, once, the weights of ``gemm_scaled`` are made so.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.scaled_rows(x, *out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype = _real_code("x", x)
     if x.dim() != 2:
         raise ValueError("expected x (R, K)")
@@ -899,6 +906,10 @@ def gemm_scaled(x, w, w_scales, x_scales=None, out=None, stream=None):
     int8 and w_scales (N,) float32; out: (M, N) float32, bfloat16 or float16 (the
     default is x's type, for int8 float32).  Rows are contiguous.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.gemm_scaled(x, w, w_scales, x_scales, out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     whole = x.dtype == torch.int8
     x_code = XGEMM_INT8 if whole else _real_code("x", x)
     if whole != (x_scales is not None):
@@ -945,6 +956,10 @@ def gated(x, up, act="silu", out=None, pre=None, stream=None):
     or float32; pre: a (M, 2 I) tensor of x's dtype that takes both products, for
     ``gated_grad``.  Rows are contiguous.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.gated(x, up, _ACTS.get(act), out, pre)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype, M, H, I, code = _gated_sizes(x, up, act)
     if out is None:
         out = torch.empty((M, I), dtype=x.dtype, device=x.device)
@@ -976,6 +991,10 @@ def gated_grad(x, up, pre, d_out, act="silu", out=None, stream=None):
     (d_x, d_up), given pre, as the forward call left it, and d_out (M, I), both of
     x's dtype.  ``out``: a pair of tensors to write into, both of x's dtype (the
     default) or both float32; None in a place of the pair: not computed."""
+    if out is not None and stream is None and len(out) == 2:
+        rc = _fastcall.gated_grad(x, up, pre, d_out, _ACTS.get(act), *out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype, M, H, I, code = _gated_sizes(x, up, act)
     out, kind = _grads(out, x, up)
     s, h = _place(stream, x, up, pre, d_out, *out)
@@ -1011,6 +1030,10 @@ def head_logprobs(x, head, targets=None, out=None, stream=None):
     dtype with contiguous rows.  ``out``: a dict of tensors to write into and
     return; what it leaves out is not computed.
     """
+    if out is not None and stream is None:
+        rc = _fastcall.head_logprobs(x, head, targets, out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype, T, V, H = _head_sizes(x, head)
     if out is None:
         out = {n: torch.empty((T,), dtype=torch.float32, device=x.device)
@@ -1032,6 +1055,10 @@ def head_logprobs_grad(x, head, targets, lse, d_logprob=None, d_lse=None, out=No
     forward call's lse (targets only with d_logprob).  All (T,) float32, targets
     int64.  ``out``: a pair of tensors to write into, both of x's dtype (the
     default) or both float32; None in a place of the pair: not computed."""
+    if out is not None and stream is None and len(out) == 2:
+        rc = _fastcall.head_logprobs_grad(x, head, targets, lse, d_logprob, d_lse, *out)
+        if rc is not None:
+            return _checked(rc, x.device.index, out)
     dtype, T, V, H = _head_sizes(x, head)
     if lse is None or (d_logprob is not None and targets is None):
         raise ValueError("lse is needed, and targets with d_logprob")
