@@ -65,19 +65,36 @@ struct Matrix {
         if (copied)
             at = ws.take((size_t)(rows * times) * up_to(cols, 16));
     }
-    void place(char *ws, hipStream_t s)
+    // The copies of up to two operands, into the workspace.
+    static void place(Matrix &a, Matrix &b, char *ws, hipStream_t s)
     {
-        if (!copied)
-            return;
-        const int64_t chunks = cdiv(cols, 16), some = std::max<int64_t>(1, ((int64_t)1 << 30) / chunks);
-        for (int k = 0; k < times; ++k)
-            for (int64_t r = 0; r < rows; r += some) {
-                const int64_t n = std::min(some, rows - r);
-                hipLaunchKernelGGL(copy_rows, dim3(cdiv(n * chunks, 256)), dim3(256), 0, s, p + r * ld, ld, cols, n,
-                                   ws + at + (k * rows + r) * chunks * 16, chunks);
+        CopyParams p{};
+        int n = 0;
+        for (Matrix *const m : {&a, &b})
+            if (m->copied) {
+                const int64_t chunks = cdiv(m->cols, 16);
+                p.m[n++] = {m->p, ws + m->at, m->ld, m->cols, m->rows, chunks, cdiv(m->rows * chunks, 256), m->times};
+                m->p = ws + m->at;
+                m->ld = chunks * 16;
             }
-        p = ws + at;
-        ld = chunks * 16;
+        // (a launch has at most 2^32 threads: what is larger goes in pieces of rows)
+        constexpr int64_t most = (int64_t)1 << 22;   // blocks
+        if (n == 2 && p.m[0].blocks + p.m[1].blocks <= most) {
+            hipLaunchKernelGGL(copy_rows, dim3(p.m[0].blocks + p.m[1].blocks), dim3(256), 0, s, p);
+            return;
+        }
+        for (int k = 0; k < n; ++k) {
+            const auto whole = p.m[k];
+            const int64_t some = std::max<int64_t>(1, most * 256 / whole.chunks);
+            for (int t = 0; t < whole.times; ++t)
+                for (int64_t r = 0; r < whole.rows; r += some) {
+                    CopyParams one{};
+                    const int64_t rows = std::min(some, whole.rows - r);
+                    one.m[0] = {whole.from + r * whole.ld, whole.to + (t * whole.rows + r) * whole.chunks * 16, whole.ld,
+                                whole.bytes, rows, whole.chunks, cdiv(rows * whole.chunks, 256), 1};
+                    hipLaunchKernelGGL(copy_rows, dim3(one.m[0].blocks), dim3(256), 0, s, one);
+                }
+        }
     }
 };
 
@@ -85,10 +102,13 @@ struct Matrix {
 // products
 // ---------------------------------------------------------------------------
 
-// How a product is cut: tiles of 256 or 128, and ranges of k whose sums are
-// joined by a second launch.
+// How a product is cut: into tiles, and ranges of k whose sums are joined by a
+// second launch.  (Joined by the last workgroup of a tile instead, 3 ranges of 129
+// tiles took 29 us in place of 15 and 7: one workgroup reads them too slowly.)
+enum TileKind { kTile256, kTile128, kTile64 };   // 256 x 256, 128 x 128, 64 x 128
+constexpr int kTileRows[] = {256, 128, 64}, kTileCols[] = {256, 128, 128};
 struct Cut {
-    bool large;
+    TileKind tile;
     int split, chunk;   // steps of a range
     int64_t ld;         // of the parts
     int halves = 1;     // 2: the rows come twice, as two parts of their values, and are joined too
@@ -97,20 +117,46 @@ struct Cut {
 // Rows up to which slopes are kept in two parts (fused_ends.hpp).
 constexpr int64_t kTwoParts = 128;
 
-Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool may_split, int cu_count)
+// The least of the rounds of workgroups that the CUs take times the time of one
+// (microseconds: its beginning and end, and each step, longer where two share a
+// CU), and for a split the parts written and read again.  Fitted to 37 products (8-bit
+// and 16-bit, 37 to 8192 rows), each with all tiles and splits.  Microseconds, 256 /
+// 128 / 64 rows a tile, split where that is faster: 64 x 8192 x 8192 8-bit 24.3 / 20.0 /
+// 16.9; 333 x 5120 x 2048 8-bit 28 / 19.2 / 11.7; 1000 x 8192 x 4096 8-bit 54 / 45.2 / 50.0;
+// 2048 x 14336 x 4096 8-bit 121 / 151 / 172; gated 512 x 4096 x 4096 48 / 45.5 / 40.4;
+// d_x of 2048 x 2048 x 5632 112 (4 ranges; not split 242) / 123 / 128.
+// across: A's rows are its k (a transposed product), which the smallest tile does
+// not take.
+Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool may_split, int cu_count)
 {
+    struct {
+        double ends, step, shared;
+        int per_cu;
+    } constexpr kCost[] = {{6.0, 1.45, 1.45, 1}, {3.0, 0.82, 1.1, 2}, {2.5, 0.43, 0.67, 2}};
     const int64_t cols = gated ? 2 * N : N, cus = std::max(cu_count, 1);
     M = std::min(M, kRowsLaunch);
-    Cut c;
-    c.large = cdiv(M, 256) * cdiv(cols, 256) * 2 >= cus;
-    c.split = 1;
-    const int64_t tiles = c.large ? cdiv(M, 256) * cdiv(cols, 256) : cdiv(M, 128) * cdiv(cols, 128);
-    if (may_split && tiles < cus)
-        c.split = (int)std::max<int64_t>(1, std::min<int64_t>({2 * cus / std::max<int64_t>(tiles, 1), steps / 4, 32}));
-    c.chunk = (int)std::max<int64_t>(cdiv(steps, c.split), 1);
-    c.split = (int)std::max<int64_t>(cdiv(steps, c.chunk), 1);
-    c.ld = gated ? 2 * up_to(N, 4) : up_to(N, 4);
-    return c;
+    steps = std::max<int64_t>(steps, 1);
+    Cut best{};
+    double least = 0;
+    for (const TileKind t : {kTile256, kTile128, kTile64}) {
+        if (t == kTile64 && across)
+            continue;
+        const int64_t tiles = cdiv(M, kTileRows[t]) * cdiv(cols, kTileCols[t]);
+        for (int64_t split = 1; split <= 16; ++split) {
+            const int64_t chunk = cdiv(steps, split);
+            if (split > 1 && (!may_split || chunk < 3 || cdiv(steps, chunk) != split))
+                continue;
+            const int64_t groups = tiles * split, rounds = cdiv(groups, cus * kCost[t].per_cu);
+            const double step = groups > cus ? kCost[t].shared : kCost[t].step;
+            const double join = split > 1 ? 3.0 + (double)split * (double)M * (double)cols * 8.0 / 3.5e6 : 0.0;
+            const double cost = (double)rounds * (kCost[t].ends + step * (double)chunk) + join;
+            if (least == 0 || cost < least) {
+                least = cost;
+                best = Cut{t, (int)split, (int)chunk, gated ? 2 * up_to(N, 4) : up_to(N, 4)};
+            }
+        }
+    }
+    return best;
 }
 
 size_t part_bytes(const Cut &c, int64_t M)
@@ -119,17 +165,18 @@ size_t part_bytes(const Cut &c, int64_t M)
 }
 
 template <int TYPE, int LA, int LB, class End>
-void launch_tiles(TileParams p, const typename End::Params &e, bool large, hipStream_t s)
+void launch_tiles(TileParams p, const typename End::Params &e, TileKind tile, hipStream_t s)
 {
-    const int b = large ? 256 : 128;
-    p.tiles_m = (int)cdiv(p.M, b);
-    p.tiles_n = (int)cdiv(p.N, End::kGated ? b / 2 : b);
+    p.tiles_m = (int)cdiv(p.M, kTileRows[tile]);
+    p.tiles_n = (int)cdiv(End::kGated ? 2 * (int64_t)p.N : p.N, kTileCols[tile]);
     p.group_m = 8;
     p.grid = p.tiles_m * p.tiles_n * p.split;
-    if (large)
-        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 256, 256, 2, 4, End>), dim3(p.grid), dim3(512), 0, s, p, e);
-    else
-        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 128, 128, 2, 2, End>), dim3(p.grid), dim3(256), 0, s, p, e);
+    if (tile == kTile256)
+        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 256, 256, 2, 4, 2, End>), dim3(p.grid), dim3(512), 0, s, p, e);
+    else if (tile == kTile128)
+        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 128, 128, 2, 2, 2, End>), dim3(p.grid), dim3(256), 0, s, p, e);
+    else if constexpr (LA == kAlong)
+        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 64, 128, 1, 4, 3, End>), dim3(p.grid), dim3(256), 0, s, p, e);
 }
 
 // One product of rows [.., .. + p.M) of the result, its sums' parts in `part`.
@@ -141,7 +188,7 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
     if constexpr (End::kJoins) {
         if (c.split * c.halves > 1) {
             typedef PartEnd<TYPE, End::kGated> Part;
-            launch_tiles<TYPE, LA, LB, Part>(p, typename Part::Params{part, (int)c.ld}, c.large, s);
+            launch_tiles<TYPE, LA, LB, Part>(p, typename Part::Params{part, (int)c.ld}, c.tile, s);
             // (the second half's rows follow the first's: a part of their own)
             const int64_t quads = cdiv(p.N, 4), M = p.M / c.halves;
             hipLaunchKernelGGL(join_parts<End>, dim3(cdiv(M * quads, 256)), dim3(256), 0, s, part, c.split * c.halves,
@@ -149,7 +196,7 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
             return;
         }
     }
-    launch_tiles<TYPE, LA, LB, End>(p, e, c.large, s);
+    launch_tiles<TYPE, LA, LB, End>(p, e, c.tile, s);
 }
 
 // Rows that the kernels for few of them take (fused_rows.hpp).
@@ -310,7 +357,7 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
     const int64_t padded = up_to(K, 16);
     const size_t at_q = ws.take(whole ? 0 : (size_t)M * padded), at_scales = ws.take(whole ? 0 : (size_t)M * 4);
     Matrix A(whole ? x : nullptr, whole ? M : 0, K, ldx, 1, ws), B(w, N, K, ldw, 1, ws);
-    const Cut c = cut_of(M, N, cdiv(padded, 128), false, true, h->cu_count);
+    const Cut c = cut_of(M, N, cdiv(padded, 128), false, false, true, h->cu_count);
     const size_t at_part = ws.take(part_bytes(c, M));
     if (ws.bytes > 0) {
         const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
@@ -318,8 +365,7 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
             return rc;
     }
     char *const base = ws.bytes > 0 ? (char *)h->workspace + xgemm_host::kWsPrefix : nullptr;
-    A.place(base, s);
-    B.place(base, s);
+    Matrix::place(A, B, base, s);
     if (!whole) {
         A.p = base + at_q;
         A.ld = padded;
@@ -384,7 +430,7 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
     Space ws;
     Matrix A(x, M, H, ldx, 2, ws), B(up, 2 * I, H, ldu, 2, ws);
     const int64_t K = up_to(H, 8);
-    const Cut c = cut_of(M, I, cdiv(K, 64), true, true, h->cu_count);
+    const Cut c = cut_of(M, I, cdiv(K, 64), true, false, true, h->cu_count);
     const size_t at_part = ws.take(part_bytes(c, M));
     if (ws.bytes > 0) {
         const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
@@ -392,8 +438,7 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
             return rc;
     }
     char *const base = ws.bytes > 0 ? (char *)h->workspace + xgemm_host::kWsPrefix : nullptr;
-    A.place(base, s);
-    B.place(base, s);
+    Matrix::place(A, B, base, s);
     TileParams p = tile_params(A, B, M, I, K);
     p.B2 = B.p + I * B.ld;
     if (dtype == XGEMM_BF16)
@@ -425,23 +470,22 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
         return XGEMM_ERR_INVALID_ARG;
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     Space ws;
-    const size_t at_word = ws.take(8);
+    const size_t at_word = ws.take((1 + kMostBlocks) * 4);   // the slopes' inverse factor, the blocks' largest
     const int64_t ld = up_to(2 * I, 8);
     const int halves = M <= kTwoParts ? 2 : 1;
     const int64_t rows = M * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
     Matrix X(x, want_up && some ? M : 0, H, ldx, 2, ws, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2, ws);
-    Cut cx = cut_of(rows, H, cdiv(ld, 64), false, true, h->cu_count);
+    Cut cx = cut_of(rows, H, cdiv(ld, 64), false, false, true, h->cu_count);
     cx.halves = halves;
-    const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, h->cu_count);
+    const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, true, h->cu_count);
     const size_t at_part = ws.take(std::max(want_x ? part_bytes(cx, rows) : 0, want_up ? part_bytes(cw, 2 * I) : 0));
     const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
     if (rc != XGEMM_OK)
         return rc;
     char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
-    X.place(base, s);
-    W.place(base, s);
-    uint32_t *const word = (uint32_t *)(base + at_word);   // bits of the largest slope, inverse of its power of two
+    Matrix::place(X, W, base, s);
+    float *const inverse = (float *)(base + at_word);
     GatedSlopeParams g;
     g.ldp = ldp;
     g.ldd = ldd;
@@ -450,26 +494,24 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     g.I = (int)I;
     g.act = act;
     g.chunks = (int)cdiv(I, 8);
-    g.most = word;
-    g.inverse = (float *)(word + 1);
-    auto slopes = [&](auto kernel, int64_t most_blocks) {
-        const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 30) / g.chunks);
-        for (int64_t m = 0; m < M; m += rows) {
-            g.M = (int)std::min(rows, M - m);
-            g.pre = (const uint16_t *)pre + m * ldp;
-            g.d = (const uint16_t *)d_y + m * ldd;
-            g.out = (uint16_t *)(base + at_d) + m * ld;
-            hipLaunchKernelGGL(kernel, dim3(std::min(cdiv((int64_t)g.M * g.chunks, 256), most_blocks)), dim3(256), 0, s, g);
+    g.inverse = inverse;
+    g.most = (uint32_t *)(inverse + 1);
+    g.M = (int)M;
+    g.pre = (const uint16_t *)pre;
+    g.d = (const uint16_t *)d_y;
+    g.out = (uint16_t *)(base + at_d);
+    if (some) {
+        const int64_t blocks = cdiv(M * g.chunks, 256), few = std::min<int64_t>(blocks, kMostBlocks);
+        g.blocks = (int)few;
+        const dim3 all(std::min<int64_t>(blocks, (int64_t)1 << 22)), block(256);
+        if (dtype == XGEMM_BF16) {
+            hipLaunchKernelGGL((gated_slope<kBf16, false>), all, block, 0, s, g);
+        } else {
+            hipLaunchKernelGGL((gated_slope<kFp16, true>), dim3(few), block, 0, s, g);
+            hipLaunchKernelGGL((gated_slope<kFp16, false>), all, block, 0, s, g);
         }
-    };
-    if (some && dtype == XGEMM_BF16) {
-        slopes(gated_slope<kBf16, false>, kMaxDim);
-    } else if (some) {
-        hipLaunchKernelGGL(set_words, dim3(1), dim3(64), 0, s, word, 2);
-        slopes(gated_slope<kFp16, true>, 4 * (int64_t)std::max(h->cu_count, 1));
-        slopes(gated_slope<kFp16, false>, kMaxDim);
     }
-    const float *const scale = some && dtype == XGEMM_FP16 ? g.inverse : nullptr;
+    const float *const scale = some && dtype == XGEMM_FP16 ? inverse : nullptr;
     TileParams p{};
     p.A = base + at_d;
     p.lda = ld * 2;
@@ -521,15 +563,14 @@ int run_head(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, int64
     Space ws;
     Matrix X(x, T, H, ldx, 2, ws), W(head, V, H, ldw, 2, ws);
     const int64_t K = up_to(H, 8), rows = std::min(T, kHeadRows);
-    const Cut c = cut_of(rows, V, cdiv(K, 64), false, false, h->cu_count);
-    const int64_t tiles = cdiv(V, c.large ? 256 : 128);
+    const Cut c = cut_of(rows, V, cdiv(K, 64), false, false, false, h->cu_count);
+    const int64_t tiles = cdiv(V, kTileCols[c.tile]);
     const size_t at_stat = ws.take((size_t)(tiles * rows) * sizeof(float2)), at_logit = ws.take((size_t)rows * 4);
     const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
     if (rc != XGEMM_OK)
         return rc;
     char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
-    X.place(base, s);
-    W.place(base, s);
+    Matrix::place(X, W, base, s);
     TileParams p = tile_params(X, W, rows, V, K);
     for (int64_t t = 0; t < T; t += kHeadRows) {
         p.M = (int)std::min(kHeadRows, T - t);
@@ -539,7 +580,7 @@ int run_head(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, int64
             launch_product<kBf16, kAlong, kAlong, StatsEnd>(p, e, c, nullptr, s);
         else
             launch_product<kFp16, kAlong, kAlong, StatsEnd>(p, e, c, nullptr, s);
-        hipLaunchKernelGGL(head_join, dim3(cdiv(p.M, 16)), dim3(256), 0, s, e.stat, (int)tiles, (int64_t)p.M, e.at,
+        hipLaunchKernelGGL(head_join, dim3(cdiv(p.M, kJoinRows)), dim3(256), 0, s, e.stat, (int)tiles, (int64_t)p.M, e.at,
                            e.targets, V, lse ? lse + t : nullptr, logprob ? logprob + t : nullptr);
     }
     const int launched = launch_status(h, "head launch");
@@ -599,11 +640,11 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     const size_t at_sum = ws.take(sums ? (size_t)T * up_to(H, 4) * 4 : 0);
     size_t parts = 0;
     auto cut_x = [&](int64_t n) {
-        Cut c = cut_of(rows, H, cdiv(n, 64), false, true, h->cu_count);
+        Cut c = cut_of(rows, H, cdiv(n, 64), false, false, true, h->cu_count);
         c.halves = halves;
         return c;
     };
-    auto cut_w = [&](int64_t n) { return cut_of(n, H, cdiv(rows, 64), false, true, h->cu_count); };
+    auto cut_w = [&](int64_t n) { return cut_of(n, H, cdiv(rows, 64), false, true, true, h->cu_count); };
     for (const int64_t n : {std::min(piece, V), V - (pieces - 1) * piece})
         parts = std::max({parts, part_bytes(cut_x(n), rows), part_bytes(cut_w(n), n)});
     const size_t at_part = ws.take(parts);
@@ -611,8 +652,7 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     if (rc != XGEMM_OK)
         return rc;
     char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
-    X.place(base, s);
-    W.place(base, s);
+    Matrix::place(X, W, base, s);
     float *const scales = (float *)(base + at_scale);
     hipLaunchKernelGGL(slope_scale, dim3(1), dim3(256), 0, s, d_logprob, d_lse, T, dtype == XGEMM_FP16 ? 16384.0f : 1.0f,
                        scales);
@@ -624,7 +664,7 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
         if (T > 0) {
             TileParams p = tile_params(X, W, T, n, K);
             p.B = p.B2 = W.p + v * W.ld;
-            const Cut c = cut_of(T, n, cdiv(K, 64), false, false, h->cu_count);
+            const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, h->cu_count);
             uint16_t *const rest = halves > 1 ? d + T * piece : nullptr;
             if (dtype == XGEMM_BF16)
                 launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);

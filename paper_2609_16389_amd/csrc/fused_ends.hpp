@@ -170,15 +170,18 @@ enum { kSilu = 0, kGelu = 1, kGeluTanh = 2 };
 __device__ __forceinline__ float hold(float a, float most) { return a > most ? most : a < -most ? -most : a; }
 __device__ __forceinline__ float exp_of(float a) { return __builtin_amdgcn_exp2f(a * kLog2e); }
 
+// 1 / (1 + e), to an ulp or two
+__device__ __forceinline__ float logistic(float e) { return __builtin_amdgcn_rcpf(1.0f + e); }
+
 // the share p of a in act(a) = a p
 __device__ __forceinline__ float share(int act, float a)
 {
     if (act == kSilu)
-        return 1.0f / (1.0f + exp_of(-a));
+        return logistic(exp_of(-a));
     if (act == kGelu)
         return 0.5f * erfcf(a * -0.70710678118654752440f);   // (1 + erf would lose the left tail)
     const float b = hold(a, 16.0f);
-    return 1.0f / (1.0f + exp_of(-1.59576912160573071176f * (b + 0.044715f * b * b * b)));
+    return logistic(exp_of(-1.59576912160573071176f * (b + 0.044715f * b * b * b)));
 }
 __device__ __forceinline__ float act_of(int act, float a) { return a * share(act, a); }
 
@@ -188,13 +191,13 @@ __device__ __forceinline__ void act_slope(int act, float a, float &value, float 
     value = a * p;
     if (act == kSilu) {
         const float b = hold(a, 200.0f);
-        slope = p * (1.0f + b * (1.0f / (1.0f + exp_of(b))));
+        slope = p * (1.0f + b * logistic(exp_of(b)));
     } else if (act == kGelu) {
         const float b = hold(a, 40.0f);
         slope = p + b * (0.39894228040143267794f * exp_of(-0.5f * b * b));
     } else {
         const float b = hold(a, 16.0f);
-        const float rest = 1.0f / (1.0f + exp_of(1.59576912160573071176f * (b + 0.044715f * b * b * b)));   // 1 - p
+        const float rest = logistic(exp_of(1.59576912160573071176f * (b + 0.044715f * b * b * b)));   // 1 - p
         slope = p + b * (p * rest) * (1.59576912160573071176f * (1.0f + 0.134145f * b * b));
     }
 }
@@ -248,38 +251,46 @@ struct StatsEnd {
                                                   int n0, int wm, int wn, int tn, int, int lane)
     {
         float2 *const meet_at = (float2 *)smem;   // [BM][WN]
+        const bool edge = n0 + BN > p.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int r = wm * TM + i * 16 + (lane & 15), row = m0 + r;
-            const int64_t target = e.targets && row < p.M ? e.targets[row] : -1;
-            float most = -INFINITY;
-            bool bad = false;
+            const int r = wm * TM + i * 16 + (lane & 15), row = m0 + r, first = n0 + wn * TN + (lane >> 4) * 4;
+            // the target's place among this lane's columns (j * 16 + k)
+            const int64_t hot = (e.targets && row < p.M ? e.targets[row] : -1) - first;
+            const bool mine = hot >= 0 && hot < TN;
+            if (__any(mine)) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+                for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float v = acc[i][j][k];
-                    if (col + k < p.N) {
-                        if (col + k == target)
-                            e.at[row] = v;
-                        bad |= !(v < INFINITY);
-                        most = fmaxf(most, v);
-                    }
-                }
+                    for (int k = 0; k < 4; ++k)
+                        if (mine && hot == j * 16 + k)
+                            e.at[row] = acc[i][j][k];
             }
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            const float ref = most > -INFINITY ? most : 0.0f;
-            float sum = bad ? NAN : 0.0f;
+            if (edge) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (first + j * 16 + k >= p.N)
+                            acc[i][j][k] = -INFINITY;
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (col + k < p.N)
-                        sum += exp_of(acc[i][j][k] - ref);
-            }
+                    most = fmaxf(most, acc[i][j][k]);
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            // (a NaN or +inf makes the sum NaN; relative to the largest the product with
+            // log2 e may be rounded as the logit itself is)
+            const float ref = most > -INFINITY ? -kLog2e * most : 0.0f;
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][k], kLog2e, ref));
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (lane < 16)
@@ -338,6 +349,7 @@ struct SlopeEnd {
     {
         const float scale = *e.scale;
         const int padded = (p.N + 7) / 8 * 8;
+        const bool edge = n0 + BN > p.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int row = m0 + wm * TM + i * 16 + (lane & 15);
@@ -350,15 +362,27 @@ struct SlopeEnd {
             const float lse = e.lse[row], dp = (e.d_lse ? e.d_lse[row] : 0.0f) - dl;
             // (a row of nothing but -inf takes no part, nor does one without factors, whatever its lse)
             const bool empty = lse == -INFINITY || (dl == 0.0f && dp == 0.0f);
-            const int64_t hot = target - e.first;
+            // the target's place among this lane's columns (j * 16 + k)
+            const int first = n0 + wn * TN + (lane >> 4) * 4;
+            const int64_t hot = target - e.first - first;
+            const bool mine = hot >= 0 && hot < TN && !empty;
+            const float dps = empty ? 0.0f : dp * scale;
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const int col = n0 + wn * TN + j * 16 + (lane >> 4) * 4;
+                const int col = first + j * 16;
                 f32x4 v;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float d = exp_of(acc[i][j][k] - lse) * dp + (hot == col + k ? dl : 0.0f);
-                    v[k] = empty || col + k >= p.N ? 0.0f : d * scale;
+                for (int k = 0; k < 4; ++k)
+                    v[k] = empty ? 0.0f : exp_of(acc[i][j][k] - lse) * dps;
+                if (mine) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] += hot == j * 16 + k ? dl * scale : 0.0f;
+                }
+                if (edge) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = col + k < p.N ? v[k] : 0.0f;
                 }
                 if (col < padded) {
                     store_quad(e.out + (int64_t)row * e.ld, DT, col, padded, v);
@@ -400,14 +424,28 @@ __global__ void __launch_bounds__(256) join_parts(const char *part, int split, i
     End::quad(e, row, col, N, s[0], s[1]);
 }
 
-// Rows of `bytes` bytes, at any alignment, to rows of `chunks` x 16, zeros after
-// the end.
-__global__ void __launch_bounds__(256) copy_rows(const char *from, int64_t ld, int64_t bytes, int64_t rows, char *to,
-                                                 int64_t chunks)
+// Copies of matrices whose rows are not whole 16-byte chunks at such addresses: rows
+// of `bytes` bytes, at any alignment, to rows of `chunks` x 16, zeros after the
+// end, `times` one after another.  Up to two matrices a launch (for a few
+// megabytes a launch takes as long as the copy).
+struct CopyParams {
+    struct {
+        const char *from;
+        char *to;
+        int64_t ld, bytes, rows, chunks, blocks;
+        int times;
+    } m[2];
+};
+__global__ void __launch_bounds__(256) copy_rows(CopyParams p)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / chunks, c = at % chunks;
-    if (row < rows)
-        *(u32x4 *)(to + (row * chunks + c) * 16) = load16_end(from + row * ld, c * 16, bytes);
+    const bool second = blockIdx.x >= p.m[0].blocks;
+    const auto &m = p.m[second];
+    const int64_t at = (blockIdx.x - (second ? p.m[0].blocks : 0)) * 256 + threadIdx.x, row = at / m.chunks, c = at % m.chunks;
+    if (row >= m.rows)
+        return;
+    const u32x4 v = load16_end(m.from + row * m.ld, c * 16, m.bytes);
+    for (int k = 0; k < m.times; ++k)
+        *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
 }
 
 // Per row of K values: scale = max |x| * (1 / 127) (at least 2^-126), q = x / scale
@@ -544,16 +582,10 @@ __global__ void __launch_bounds__(256) slope_scale(const float *d_logprob, const
     }
 }
 
-__global__ void set_words(uint32_t *w, int n)
-{
-    if ((int)threadIdx.x < n)
-        w[threadIdx.x] = 0;
-}
-
 // The gradient in a gated block's projections, [d lift act'(gate) | d act(gate)],
 // as the operand of the products that follow.  In binary16 times a power of two
-// that takes the largest of them to 2^14: a first launch (MOST) finds it.  Eight columns a
-// thread, the padding after 2 I zeros.
+// that takes the largest of them to 2^14: a first launch (MOST) finds each block's.
+// Eight columns a thread, the padding after 2 I zeros.
 struct GatedSlopeParams {
     const uint16_t *pre, *d;
     int64_t ldp, ldd;
@@ -562,9 +594,11 @@ struct GatedSlopeParams {
     int64_t ld;
     int M, I, act;
     int chunks;       // of 8 in I columns
-    uint32_t *most;   // bits of the largest (binary16)
+    uint32_t *most;   // bits of each block's largest (binary16)
+    int blocks;
     float *inverse;   // of the power of two
 };
+constexpr int kMostBlocks = 255;
 
 template <int DT>
 __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v)[8])
@@ -586,7 +620,18 @@ __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v
 template <int DT, bool MOST>
 __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
 {
+    __shared__ uint32_t share_most[4];
     uint32_t most = 0;
+    float s = 1.0f;
+    if constexpr (DT == kFp16 && !MOST) {
+        most = most_of((int)threadIdx.x < p.blocks ? p.most[threadIdx.x] : 0u);
+        if ((threadIdx.x & 63) == 0)
+            share_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        s = lift_of(max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            *p.inverse = 1.0f / s;
+    }
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)p.M * p.chunks; at += (int64_t)gridDim.x * 256) {
         const int row = (int)(at / p.chunks), col = (int)(at % p.chunks) * 8;
         float g[8], u[8], d[8], dg[8], du[8];
@@ -594,7 +639,6 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
         eight<DT>((const char *)pre, col, p.I, g);
         eight<DT>((const char *)(pre + p.I), col, p.I, u);
         eight<DT>((const char *)(p.d + (int64_t)row * p.ldd), col, p.I, d);
-        const float s = DT == kFp16 && !MOST ? lift_of(*p.most) : 1.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float value, slope;
@@ -628,30 +672,29 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
                 }
                 store(out + p.rest);
             }
-            if (DT == kFp16 && at == 0)
-                *p.inverse = 1.0f / s;
         }
     }
     if constexpr (MOST) {
-        // (the largest is the same in any order; atomics on one address take 15 ns each)
-        __shared__ uint32_t share_most[4];
+        // (atomics on one address take 15 ns each: the blocks of the next launch look at
+        // all the places instead)
         most = most_of(most);
         if ((threadIdx.x & 63) == 0)
             share_most[threadIdx.x >> 6] = most;
         __syncthreads();
         if (threadIdx.x == 0)
-            atomicMax(p.most, max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
+            p.most[blockIdx.x] = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
     }
 }
 
-// Log probabilities from the tiles' statistics: 16 rows a workgroup, each by 16
-// threads that take every sixteenth tile.
+// Log probabilities from the tiles' statistics: kJoinRows rows a workgroup, each by
+// 64 threads.  (16 rows and 16 threads took 10 us for 77 rows of 391 tiles.)
+constexpr int kJoinRows = 4, kJoinThreads = 256 / kJoinRows;
 __global__ void __launch_bounds__(256) head_join(const float2 *stat, int tiles, int64_t rows, const float *at,
                                                  const int64_t *targets, int64_t V, float *lse, float *logprob)
 {
-    __shared__ float2 part[16][17];
-    const int r = threadIdx.x & 15, t0 = threadIdx.x >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    __shared__ float2 part[kJoinRows][kJoinThreads + 1];
+    const int r = threadIdx.x % kJoinRows, t0 = threadIdx.x / kJoinRows;
+    const int64_t row = (int64_t)blockIdx.x * kJoinRows + r;
     float most = -INFINITY, sum = 0.0f;
     auto add = [&](float m, float s) {
         const float both = fmaxf(most, m);
@@ -662,18 +705,22 @@ __global__ void __launch_bounds__(256) head_join(const float2 *stat, int tiles, 
         sum = a + b;
     };
     if (row < rows)
-        for (int t = t0; t < tiles; t += 16) {
+        for (int t = t0; t < tiles; t += kJoinThreads) {
             const float2 s = stat[(int64_t)t * rows + row];
             add(s.x, s.y);
         }
     part[r][t0] = make_float2(most, sum);
     __syncthreads();
-    if (threadIdx.x >= 16 || row >= rows)
+    // (in halves, as a tree)
+    for (int n = kJoinThreads / 2; n; n /= 2) {
+        if (t0 < n) {
+            add(part[r][t0 + n].x, part[r][t0 + n].y);
+            part[r][t0] = make_float2(most, sum);
+        }
+        __syncthreads();
+    }
+    if (t0 > 0 || row >= rows)
         return;
-    most = -INFINITY;
-    sum = 0.0f;
-    for (int k = 0; k < 16; ++k)
-        add(part[r][k].x, part[r][k].y);
     const bool bad = !(sum == sum), empty = most == -INFINITY;
     const float log_sum = logf(sum);
     if (lse)

@@ -232,7 +232,7 @@ __device__ __forceinline__ void place(const TileParams &p, int w, int &tm, int &
     tn = r / rows;
 }
 
-template <int TYPE, int LA, int LB, int BM, int BN, int WM, int WN, class End>
+template <int TYPE, int LA, int LB, int BM, int BN, int WM, int WN, int S, class End>
 __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typename End::Params e)
 {
     constexpr int W = WM * WN;
@@ -241,9 +241,10 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     typedef Operand<TYPE, LB, BN, W> OpB;
     typedef typename Sum<TYPE>::type sum_t;
     constexpr int STAGE = OpA::kBytes + OpB::kBytes, LD = OpA::kLoads + OpB::kLoads;
-    static_assert(!End::kGated || (LB == kAlong && TN == 64 && OpB::kRows == 32), "rows of a gated tile");
+    static_assert(!End::kGated || (LB == kAlong && (TN == 64 || TN == 32) && OpB::kRows == 32), "rows of a gated tile");
+    static_assert(S >= 2 && (S - 1) * LD < 64, "loads in flight");
 
-    __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
+    __shared__ __attribute__((aligned(16))) char smem[S * STAGE];
     const int w = blockIdx.x;
     int tm, tn, ks;
     place(p, w, tm, tn, ks);
@@ -251,8 +252,8 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     const int wm = wave % WM, wn = wave / WM;
     const int m0 = tm * BM, n0 = tn * (End::kGated ? BN / 2 : BN);
     const int k0 = ks * p.chunk * OpA::KS, kend = min(p.K, k0 + p.chunk * OpA::KS);
-    // (at least two steps, so that the code below is one line; what lies past kend is zero)
-    const int nk = max((kend - k0 + OpA::KS - 1) / OpA::KS, 2);
+    // (at least S steps, so that the code below is one line; what lies past kend is zero)
+    const int nk = max((kend - k0 + OpA::KS - 1) / OpA::KS, S);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)smem;
     OpA a;
@@ -262,8 +263,8 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     else
         a.start(p.A, p.lda, m0, (int64_t)p.M - m0, k0, kend, lane, wave, lds0);
     if constexpr (End::kGated) {
-        // the tile's rows by 32: gate, lift, gate, lift, so that a wave's 64
-        // columns are 32 of either
+        // the tile's rows by 32: gate, lift, gate, lift, of which a wave takes as
+        // many of either
         const int n = n0 + wave / 2 * 32;
         b.start(wave & 1 ? p.B2 : p.B, p.ldb, n, (int64_t)p.N - n, k0, kend, lane, wave, lds0 + OpA::kBytes);
     } else if constexpr (LB == kAlong) {
@@ -293,7 +294,8 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     };
     auto read_a = [&](int stage, int kk, int i) { return OpA::read(smem + stage * STAGE, wm * TM + i * 16, kk, lane); };
     auto read_b = [&](int stage, int kk, int j) {
-        return OpB::read(smem + stage * STAGE + OpA::kBytes, wn * TN + j * 16, kk, lane);
+        const int row = End::kGated && TN == 32 ? wn / 2 * 64 + wn % 2 * 16 + j * 32 : wn * TN + j * 16;
+        return OpB::read(smem + stage * STAGE + OpA::kBytes, row, kk, lane);
     };
     // A step of two sub-steps, whose fragments have registers of their own: those
     // of the next sub-step are read as soon as a row of the current one has issued
@@ -307,8 +309,10 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     constexpr int BR = (FN + FM - R - 1) / (FM - R);   // fragments of B read with each row after it
     static_assert(FN <= FM && APART * (LD - 1) < REST, "spacing");
     u32x4 ga[2][FM], gb[2][FN];
-    auto step = [&]<bool LOAD, bool MORE>(int t) {
-        const int stage = t & 1, next = stage ^ 1;
+    // LOAD: the step S further on exists; MORE: so does the next.
+    int stage = 0;
+    auto step = [&]<bool LOAD, bool MORE>() {
+        const int next = S == 2 ? stage ^ 1 : stage == S - 1 ? 0 : stage + 1;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -327,7 +331,9 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         __builtin_amdgcn_sched_barrier(0);
         // this wave has read all of the stage; its loads of the next step have landed
         wait_lds();
-        if constexpr (MORE)
+        if constexpr (LOAD)
+            wait_loads<(S - 2) * LD>();
+        else if constexpr (MORE)
             wait_loads<0>();
         meet();
         __builtin_amdgcn_sched_barrier(0);
@@ -371,10 +377,12 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
             a.next();
             b.next();
         }
+        stage = next;
     };
-    load_step(0);
-    load_step(1);
-    wait_loads<LD>();
+#pragma unroll
+    for (int t = 0; t < S; ++t)
+        load_step(t);
+    wait_loads<(S - 1) * LD>();
     meet();
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -382,10 +390,12 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
 #pragma unroll
     for (int j = 0; j < FN; ++j)
         gb[0][j] = read_b(0, 0, j);
-    for (int t = 0; t < nk - 2; ++t)
-        step.template operator()<true, true>(t);
-    step.template operator()<false, true>(nk - 2);
-    step.template operator()<false, false>(nk - 1);
+    for (int t = 0; t < nk - S; ++t)
+        step.template operator()<true, true>();
+#pragma unroll
+    for (int t = 0; t < S - 1; ++t)
+        step.template operator()<false, true>();
+    step.template operator()<false, false>();
     // lane l holds row l % 16 of each block and columns 4 (l / 16) .. + 3
     End::template finish<BM, BN, TM, TN, FM, FN, WN>(p, e, acc, smem, m0, n0, wm, wn, tn, ks, lane);
 }
