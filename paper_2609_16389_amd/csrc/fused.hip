@@ -73,7 +73,7 @@ struct Matrix {
         for (Matrix *const m : {&a, &b})
             if (m->copied) {
                 const int64_t chunks = cdiv(m->cols, 16);
-                p.m[n++] = {m->p, ws + m->at, m->ld, m->cols, m->rows, chunks, cdiv(m->rows * chunks, 256), m->times};
+                p.m[n++] = {m->p, ws + m->at, m->ld, m->cols, m->rows, chunks, cdiv(m->rows, 4), m->times};
                 m->p = ws + m->at;
                 m->ld = chunks * 16;
             }
@@ -85,13 +85,13 @@ struct Matrix {
         }
         for (int k = 0; k < n; ++k) {
             const auto whole = p.m[k];
-            const int64_t some = std::max<int64_t>(1, most * 256 / whole.chunks);
+            constexpr int64_t some = most * 4;
             for (int t = 0; t < whole.times; ++t)
                 for (int64_t r = 0; r < whole.rows; r += some) {
                     CopyParams one{};
                     const int64_t rows = std::min(some, whole.rows - r);
                     one.m[0] = {whole.from + r * whole.ld, whole.to + (t * whole.rows + r) * whole.chunks * 16, whole.ld,
-                                whole.bytes, rows, whole.chunks, cdiv(rows * whole.chunks, 256), 1};
+                                whole.bytes, rows, whole.chunks, cdiv(rows, 4), 1};
                     hipLaunchKernelGGL(copy_rows, dim3(one.m[0].blocks), dim3(256), 0, s, one);
                 }
         }

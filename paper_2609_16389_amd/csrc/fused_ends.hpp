@@ -67,6 +67,51 @@ __device__ __forceinline__ void each_quad(int M, int N, int m0, int n0, int wm, 
     }
 }
 
+// The wave's block of the result from (row0, col0) on, rounded to the 16-bit type
+// that `kind` names, through LDS (the wave's own, TM x TN values), so that a store is
+// 16 bytes a lane of whole rows of the block: 128 bytes of a row where TN is 64.
+// (Straight from the accumulators it is 8 bytes a lane, 32 of 16 rows.)  f(i, j, row,
+// col): the four values of a quad; N: columns that are stored.
+template <int TM, int TN, int FM, int FN, class F>
+__device__ __forceinline__ void store_block(char *sh, uint16_t *out, int64_t ld, int kind, int M, int N, int row0, int col0,
+                                            int lane, F f)
+{
+    constexpr int CH = TN / 8, ROWS = 64 / CH;   // chunks of a row, rows of a store
+    const int r = lane & 15, g = lane >> 4;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const f32x4 v = f(i, j, row0 + i * 16 + r, col0 + j * 16 + g * 4);
+            uint16_t h[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                h[k] = kind == kBf16 ? from_float<kBf16>(v[k]) : from_float<kFp16>(v[k]);
+            const int row = i * 16 + r, c = (j * 2 + (g >> 1)) ^ (row & (CH - 1));
+            *(uint64_t *)(sh + row * TN * 2 + c * 16 + (g & 1) * 8) =
+                (uint64_t)(h[0] | (uint32_t)h[1] << 16) | (uint64_t)(h[2] | (uint32_t)h[3] << 16) << 32;
+        }
+    asm volatile("" ::: "memory");   // (what other lanes have written is read: a wave's LDS accesses stay in order)
+#pragma unroll
+    for (int t = 0; t < TM / ROWS; ++t) {
+        const int row = t * ROWS + lane / CH, c = lane % CH, col = col0 + c * 8;
+        const u32x4 v = *(const u32x4 *)(sh + row * TN * 2 + ((c ^ (row & (CH - 1))) << 4));
+        if (row0 + row < M && col < N) {
+            uint16_t *const to = out + (int64_t)(row0 + row) * ld + col;
+            if (col + 8 <= N) {
+                store_any<u32x4>(to, v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 7; ++k)
+                    if (col + k < N)
+                        to[k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
+            }
+        }
+    }
+    asm volatile("" ::: "memory");
+}
+
 // Sums of a range of k, as they are: part [ks][M][ld] (4 bytes a value), for a
 // gated tile with the second matrix's columns from ld / 2 on.
 template <int TYPE, bool GATED>
@@ -107,7 +152,7 @@ struct StoreEnd {
         int64_t ld_add;
     };
     typedef float value_t;
-    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, f32x4 v, f32x4)
+    static __device__ __forceinline__ f32x4 value(const Params &e, int row, int col, int M, int N, f32x4 v)
     {
         if (e.scale) {
             const float s = *e.scale;
@@ -115,21 +160,32 @@ struct StoreEnd {
             for (int k = 0; k < 4; ++k)
                 v[k] *= s;
         }
-        if (e.add) {
+        if (e.add && row < M) {
             const float *const q = e.add + (int64_t)row * e.ld_add + col;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (col + k < N)
                     v[k] += q[k];
         }
-        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, v);
+        return v;
+    }
+    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, f32x4 v, f32x4)
+    {
+        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, value(e, row, col, row + 1, N, v));
     }
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
-    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
-                                                  int wm, int wn, int, int, int lane)
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
+                                                  int n0, int wm, int wn, int, int, int lane)
     {
-        each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane,
-                                  [&](int row, int col, int i, int j) { quad(e, row, col, p.N, acc[i][j], acc[i][j]); });
+        if (e.kind != kFp32)
+            store_block<TM, TN, FM, FN>(smem + (wm * WN + wn) * TM * TN * 2, (uint16_t *)e.out, e.ld, e.kind, p.M, p.N,
+                                        m0 + wm * TM, n0 + wn * TN, lane, [&](int i, int j, int row, int col) {
+                                            return value(e, row, col, p.M, p.N, acc[i][j]);
+                                        });
+        else
+            each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+                quad(e, row, col, p.N, acc[i][j], acc[i][j]);
+            });
     }
 };
 
@@ -144,21 +200,32 @@ struct ScaledEnd {
         int kind;
     };
     typedef int value_t;
-    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, i32x4 s, i32x4)
+    static __device__ __forceinline__ f32x4 value(const Params &e, int row, int col, int M, int N, i32x4 s)
     {
-        const float r = e.row_scale[row];
+        const float r = row < M ? e.row_scale[row] : 0.0f;
         f32x4 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             v[k] = (float)s[k] * r * (col + k < N ? e.col_scale[col + k] : 0.0f);
-        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, v);
+        return v;
+    }
+    static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, i32x4 s, i32x4)
+    {
+        store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, N, value(e, row, col, row + 1, N, s));
     }
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
-    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
-                                                  int wm, int wn, int, int, int lane)
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
+                                                  int n0, int wm, int wn, int, int, int lane)
     {
-        each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane,
-                                  [&](int row, int col, int i, int j) { quad(e, row, col, p.N, acc[i][j], acc[i][j]); });
+        if (e.kind != kFp32)
+            store_block<TM, TN, FM, FN>(smem + (wm * WN + wn) * TM * TN * 2, (uint16_t *)e.out, e.ld, e.kind, p.M, p.N,
+                                        m0 + wm * TM, n0 + wn * TN, lane, [&](int i, int j, int row, int col) {
+                                            return value(e, row, col, p.M, p.N, acc[i][j]);
+                                        });
+        else
+            each_quad<TM, TN, FM, FN>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+                quad(e, row, col, p.N, acc[i][j], acc[i][j]);
+            });
     }
 };
 
@@ -178,8 +245,24 @@ __device__ __forceinline__ float share(int act, float a)
 {
     if (act == kSilu)
         return logistic(exp_of(-a));
-    if (act == kGelu)
-        return 0.5f * erfcf(a * -0.70710678118654752440f);   // (1 + erf would lose the left tail)
+    if (act == kGelu) {
+        // (1 + erf(a / sqrt 2)) / 2: its left tail is exp(-b^2 / 2) t P(t) with b = |a| and t =
+        // 1 / (1 + b / 4), P of degree 9 fitted to the scaled complementary error function
+        // for the least relative error over b in 0 .. 4000, 1.2e-7 in fp32
+        const float b = fabsf(hold(a, 40.0f)), t = __builtin_amdgcn_rcpf(__builtin_fmaf(b, 0.25f, 1.0f));
+        float v = 0.01981145516037941f;
+        v = __builtin_fmaf(v, t, -0.08100754022598267f);
+        v = __builtin_fmaf(v, t, 0.09583782404661179f);
+        v = __builtin_fmaf(v, t, -0.03195888549089432f);
+        v = __builtin_fmaf(v, t, 0.06384158879518509f);
+        v = __builtin_fmaf(v, t, 0.0589248463511467f);
+        v = __builtin_fmaf(v, t, 0.08161342144012451f);
+        v = __builtin_fmaf(v, t, 0.09346522390842438f);
+        v = __builtin_fmaf(v, t, 0.09973648935556412f);
+        v = __builtin_fmaf(v, t, 0.0997355654835701f);
+        const float tail = exp_of(-0.5f * b * b) * (t * v);
+        return a < 0.0f ? tail : 1.0f - tail;
+    }
     const float b = hold(a, 16.0f);
     return logistic(exp_of(-1.59576912160573071176f * (b + 0.044715f * b * b * b)));
 }
@@ -228,12 +311,32 @@ struct GatedEnd {
         }
     }
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
-    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
-                                                  int wm, int wn, int, int, int lane)
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
+                                                  int n0, int wm, int wn, int, int, int lane)
     {
-        each_quad<TM, TN / 2, FM, FN / 2>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
-            quad(e, row, col, p.N, acc[i][j], acc[i][j + FN / 2]);
-        });
+        constexpr int TH = TN / 2, FH = FN / 2;
+        char *const sh = smem + (wm * WN + wn) * TM * TH * 2;
+        auto store = [&](void *out, int64_t ld, int kind, auto f) {
+            store_block<TM, TH, FM, FH>(sh, (uint16_t *)out, ld, kind, p.M, p.N, m0 + wm * TM, n0 + wn * TH, lane,
+                                        [&](int i, int j, int, int) { return f(i, j); });
+        };
+        auto inner = [&](int i, int j) {
+            f32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = act_of(e.act, acc[i][j][k]) * acc[i][j + FH][k];
+            return v;
+        };
+        if (e.pre) {
+            store(e.pre, e.ldp, DT, [&](int i, int j) { return acc[i][j]; });
+            store(e.pre + p.N, e.ldp, DT, [&](int i, int j) { return acc[i][j + FH]; });
+        }
+        if (e.kind != kFp32)
+            store(e.out, e.ld, e.kind, inner);
+        else
+            each_quad<TM, TH, FM, FH>(p.M, p.N, m0, n0, wm, wn, lane, [&](int row, int col, int i, int j) {
+                store_quad(row_at(e.out, e.ld, row, e.kind), e.kind, col, p.N, inner(i, j));
+            });
     }
 };
 
@@ -344,17 +447,15 @@ struct SlopeEnd {
         int64_t V;
     };
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
-    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *, int m0, int n0,
-                                                  int wm, int wn, int, int, int lane)
+    static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
+                                                  int n0, int wm, int wn, int, int, int lane)
     {
         const float scale = *e.scale;
         const int padded = (p.N + 7) / 8 * 8;
         const bool edge = n0 + BN > p.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int row = m0 + wm * TM + i * 16 + (lane & 15);
-            if (row >= p.M)
-                continue;
+            const int row = min(m0 + wm * TM + i * 16 + (lane & 15), p.M - 1);
             const int64_t target = e.d_logprob ? e.targets[row] : -1;
             float dl = target < 0 ? 0.0f : e.d_logprob[row];
             if (target >= e.V)
@@ -384,17 +485,21 @@ struct SlopeEnd {
                     for (int k = 0; k < 4; ++k)
                         v[k] = col + k < p.N ? v[k] : 0.0f;
                 }
-                if (col < padded) {
-                    store_quad(e.out + (int64_t)row * e.ld, DT, col, padded, v);
-                    if (e.rest) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            v[k] = left_of<DT>(v[k]);
-                        store_quad(e.rest + (int64_t)row * e.ld, DT, col, padded, v);
-                    }
-                }
+                acc[i][j] = v;
             }
         }
+        auto store = [&](uint16_t *out, auto f) {
+            store_block<TM, TN, FM, FN>(smem + (wm * WN + wn) * TM * TN * 2, out, e.ld, DT, p.M, padded, m0 + wm * TM,
+                                        n0 + wn * TN, lane, [&](int i, int j, int, int) { return f(acc[i][j]); });
+        };
+        store(e.out, [](f32x4 v) { return v; });
+        if (e.rest)
+            store(e.rest, [](f32x4 v) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] = left_of<DT>(v[k]);
+                return v;
+            });
     }
 };
 
@@ -424,10 +529,31 @@ __global__ void __launch_bounds__(256) join_parts(const char *part, int split, i
     End::quad(e, row, col, N, s[0], s[1]);
 }
 
+// 16 bytes from p.  ODD: from any byte, as the aligned dwords that hold them,
+// moved into place (a load of 16 bytes a lane between dwords takes the L1 path
+// several times over).
+template <bool ODD>
+__device__ __forceinline__ u32x4 sixteen(const char *p)
+{
+    typedef u32x4 __attribute__((aligned(4))) some;
+    if constexpr (!ODD)
+        return *(const some *)p;
+    const uint32_t by = (uint32_t)(uintptr_t)p & 3;
+    const u32x4 v = *(const some *)(p - by);
+    const uint32_t last = *(const uint32_t *)((uintptr_t)(p + 15) & ~(uintptr_t)3);
+    u32x4 r;
+    r[0] = __builtin_amdgcn_alignbyte(v[1], v[0], by);
+    r[1] = __builtin_amdgcn_alignbyte(v[2], v[1], by);
+    r[2] = __builtin_amdgcn_alignbyte(v[3], v[2], by);
+    r[3] = __builtin_amdgcn_alignbyte(last, v[3], by);
+    return r;
+}
+
 // Copies of matrices whose rows are not whole 16-byte chunks at such addresses: rows
 // of `bytes` bytes, at any alignment, to rows of `chunks` x 16, zeros after the
-// end, `times` one after another.  Up to two matrices a launch (for a few
-// megabytes a launch takes as long as the copy).
+// end, `times` one after another.  Four rows a workgroup, 64 lanes along each.
+// Up to two matrices a launch (for a few megabytes a launch takes as long as
+// the copy).
 struct CopyParams {
     struct {
         const char *from;
@@ -440,12 +566,15 @@ __global__ void __launch_bounds__(256) copy_rows(CopyParams p)
 {
     const bool second = blockIdx.x >= p.m[0].blocks;
     const auto &m = p.m[second];
-    const int64_t at = (blockIdx.x - (second ? p.m[0].blocks : 0)) * 256 + threadIdx.x, row = at / m.chunks, c = at % m.chunks;
+    const int64_t row = (blockIdx.x - (second ? p.m[0].blocks : 0)) * 4 + (threadIdx.x >> 6);
     if (row >= m.rows)
         return;
-    const u32x4 v = load16_end(m.from + row * m.ld, c * 16, m.bytes);
-    for (int k = 0; k < m.times; ++k)
-        *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
+    const char *const from = m.from + row * m.ld;
+    for (int64_t c = threadIdx.x & 63; c < m.chunks; c += 64) {
+        const u32x4 v = c * 16 + 16 <= m.bytes ? sixteen<true>(from + c * 16) : load16_end(from, c * 16, m.bytes);
+        for (int k = 0; k < m.times; ++k)
+            *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
+    }
 }
 
 // Per row of K values: scale = max |x| * (1 / 127) (at least 2^-126), q = x / scale

@@ -15,26 +15,6 @@ namespace xfused_dev {
 
 constexpr int kUnit = 256;          // bytes of k
 
-// 16 bytes from p.  ODD: from any byte, as the aligned dwords that hold them,
-// moved into place (a load of 16 bytes a lane between dwords takes the L1 path
-// several times over).
-template <bool ODD>
-__device__ __forceinline__ u32x4 sixteen(const char *p)
-{
-    typedef u32x4 __attribute__((aligned(4))) some;
-    if constexpr (!ODD)
-        return *(const some *)p;
-    const uint32_t by = (uint32_t)(uintptr_t)p & 3;
-    const u32x4 v = *(const some *)(p - by);
-    const uint32_t last = *(const uint32_t *)((uintptr_t)(p + 15) & ~(uintptr_t)3);
-    u32x4 r;
-    r[0] = __builtin_amdgcn_alignbyte(v[1], v[0], by);
-    r[1] = __builtin_amdgcn_alignbyte(v[2], v[1], by);
-    r[2] = __builtin_amdgcn_alignbyte(v[3], v[2], by);
-    r[3] = __builtin_amdgcn_alignbyte(last, v[3], by);
-    return r;
-}
-
 struct RowsParams {
     const char *x, *w, *w2;   // w2: the second matrix of a gated block
     int64_t ldx, ldw;         // bytes (x to be quantised: values)
