@@ -54,17 +54,26 @@ struct Space {
 struct Matrix {
     const char *p;
     int64_t rows, cols, ld;   // bytes
+    bool ragged;              // in place only the staged tiles read it
     bool copied;
     int times;                // the copy holds the rows so many times, one after another
     size_t at;                // of the copy
 
-    Matrix(const void *data, int64_t r, int64_t c, int64_t leading, int size, Space &ws, int n = 1)
-        : p((const char *)data), rows(r), cols(c * size), ld(r > 1 ? leading * size : up_to(c * size, 16)), times(n), at(0)
+    Matrix(const void *data, int64_t r, int64_t c, int64_t leading, int size, int n = 1)
+        : p((const char *)data), rows(r), cols(c * size), ld(r > 1 ? leading * size : up_to(c * size, 16)), copied(false),
+          times(n), at(0)
     {
-        copied = rows > 0 && cols > 0 && (((uintptr_t)p | ld | cols) % 16 != 0 || ld > kMaxStep || times > 1);
+        ragged = rows > 0 && cols > 0 && (((uintptr_t)p | ld | cols) % 16 != 0 || ld > kMaxStep);
+    }
+    // Room for the copy, where there has to be one.
+    void reserve(bool staged, Space &ws)
+    {
+        copied = (ragged && !staged) || (times > 1 && rows > 0 && cols > 0);
         if (copied)
             at = ws.take((size_t)(rows * times) * up_to(cols, 16));
     }
+    // Microseconds that the copy takes: 2.8 TB/s read and written, the launch.
+    double cost() const { return ragged ? (double)rows * (double)cols * 2.0 / 2.8e6 : 0.0; }
     // The copies of up to two operands, into the workspace.
     static void place(Matrix &a, Matrix &b, char *ws, hipStream_t s)
     {
@@ -109,6 +118,8 @@ enum TileKind { kTile256, kTile128, kTile64 };   // 256 x 256, 128 x 128, 64 x 1
 constexpr int kTileRows[] = {256, 128, 64}, kTileCols[] = {256, 128, 128};
 struct Cut {
     TileKind tile;
+    bool staged;        // its operands may have any address (kTile64)
+    double cost;        // microseconds
     int split, chunk;   // steps of a range
     int64_t ld;         // of the parts
     int halves = 1;     // 2: the rows come twice, as two parts of their values, and are joined too
@@ -127,7 +138,7 @@ constexpr int64_t kTwoParts = 128;
 // d_x of 2048 x 2048 x 5632 112 (4 ranges; not split 242) / 123 / 128.
 // across: A's rows are its k (a transposed product), which the smallest tile does
 // not take.
-Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool may_split, int cu_count)
+Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool may_split, bool staged, int cu_count)
 {
     struct {
         double ends, step, shared;
@@ -139,7 +150,7 @@ Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool ma
     Cut best{};
     double least = 0;
     for (const TileKind t : {kTile256, kTile128, kTile64}) {
-        if (t == kTile64 && across)
+        if ((t == kTile64 && across) || (staged && t != kTile64))
             continue;
         const int64_t tiles = cdiv(M, kTileRows[t]) * cdiv(cols, kTileCols[t]);
         for (int64_t split = 1; split <= 16; ++split) {
@@ -147,16 +158,28 @@ Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool ma
             if (split > 1 && (!may_split || chunk < 3 || cdiv(steps, chunk) != split))
                 continue;
             const int64_t groups = tiles * split, rounds = cdiv(groups, cus * kCost[t].per_cu);
-            const double step = groups > cus ? kCost[t].shared : kCost[t].step;
+            const double step = (groups > cus ? kCost[t].shared : kCost[t].step) * (staged ? 1.5 : 1.0);
             const double join = split > 1 ? 3.0 + (double)split * (double)M * (double)cols * 8.0 / 3.5e6 : 0.0;
             const double cost = (double)rounds * (kCost[t].ends + step * (double)chunk) + join;
             if (least == 0 || cost < least) {
                 least = cost;
-                best = Cut{t, (int)split, (int)chunk, gated ? 2 * up_to(N, 4) : up_to(N, 4)};
+                best = Cut{t, staged, cost, (int)split, (int)chunk, gated ? 2 * up_to(N, 4) : up_to(N, 4)};
             }
         }
     }
     return best;
+}
+
+// The cut of a product that reads a and b: with copies of what is ragged, or
+// through the staged tiles, whichever takes less.
+template <class F>
+Cut cut_with(const Matrix &a, const Matrix &b, F cut)
+{
+    const Cut c = cut(false);
+    if (!a.ragged && !b.ragged)
+        return c;
+    const Cut staged = cut(true);
+    return staged.cost < c.cost + 4.0 + a.cost() + b.cost() ? staged : c;
 }
 
 size_t part_bytes(const Cut &c, int64_t M)
@@ -165,18 +188,23 @@ size_t part_bytes(const Cut &c, int64_t M)
 }
 
 template <int TYPE, int LA, int LB, class End>
-void launch_tiles(TileParams p, const typename End::Params &e, TileKind tile, hipStream_t s)
+void launch_tiles(TileParams p, const typename End::Params &e, TileKind tile, bool staged, hipStream_t s)
 {
     p.tiles_m = (int)cdiv(p.M, kTileRows[tile]);
     p.tiles_n = (int)cdiv(End::kGated ? 2 * (int64_t)p.N : p.N, kTileCols[tile]);
     p.group_m = 8;
     p.grid = p.tiles_m * p.tiles_n * p.split;
+    auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(threads), 0, s, p, e); };
     if (tile == kTile256)
-        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 256, 256, 2, 4, 2, End>), dim3(p.grid), dim3(512), 0, s, p, e);
-    else if (tile == kTile128)
-        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 128, 128, 2, 2, 2, End>), dim3(p.grid), dim3(256), 0, s, p, e);
-    else if constexpr (LA == kAlong)
-        hipLaunchKernelGGL((tile_product<TYPE, LA, LB, 64, 128, 1, 4, 3, End>), dim3(p.grid), dim3(256), 0, s, p, e);
+        return launch(tile_product<TYPE, LA, LB, 256, 256, 2, 4, 2, false, End>, 512);
+    if constexpr (End::kStages && LA == kAlong && LB == kAlong) {
+        if (staged)
+            return launch(tile_product<TYPE, LA, LB, 64, 128, 1, 4, 2, true, End>, 256);
+    }
+    if (tile == kTile128)
+        return launch(tile_product<TYPE, LA, LB, 128, 128, 2, 2, 2, false, End>, 256);
+    if constexpr (LA == kAlong)
+        launch(tile_product<TYPE, LA, LB, 64, 128, 1, 4, 3, false, End>, 256);
 }
 
 // One product of rows [.., .. + p.M) of the result, its sums' parts in `part`.
@@ -188,7 +216,7 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
     if constexpr (End::kJoins) {
         if (c.split * c.halves > 1) {
             typedef PartEnd<TYPE, End::kGated> Part;
-            launch_tiles<TYPE, LA, LB, Part>(p, typename Part::Params{part, (int)c.ld}, c.tile, s);
+            launch_tiles<TYPE, LA, LB, Part>(p, typename Part::Params{part, (int)c.ld}, c.tile, c.staged, s);
             // (the second half's rows follow the first's: a part of their own)
             const int64_t quads = cdiv(p.N, 4), M = p.M / c.halves;
             hipLaunchKernelGGL(join_parts<End>, dim3(cdiv(M * quads, 256)), dim3(256), 0, s, part, c.split * c.halves,
@@ -196,7 +224,7 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
             return;
         }
     }
-    launch_tiles<TYPE, LA, LB, End>(p, e, c.tile, s);
+    launch_tiles<TYPE, LA, LB, End>(p, e, c.tile, c.staged, s);
 }
 
 // Rows that the kernels for few of them take (fused_rows.hpp).
@@ -356,8 +384,12 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
     Space ws;
     const int64_t padded = up_to(K, 16);
     const size_t at_q = ws.take(whole ? 0 : (size_t)M * padded), at_scales = ws.take(whole ? 0 : (size_t)M * 4);
-    Matrix A(whole ? x : nullptr, whole ? M : 0, K, ldx, 1, ws), B(w, N, K, ldw, 1, ws);
-    const Cut c = cut_of(M, N, cdiv(padded, 128), false, false, true, h->cu_count);
+    Matrix A(whole ? x : nullptr, whole ? M : 0, K, ldx, 1), B(w, N, K, ldw, 1);
+    const Cut c = cut_with(A, B, [&](bool staged) {
+        return cut_of(M, N, cdiv(padded, 128), false, false, true, staged, h->cu_count);
+    });
+    A.reserve(c.staged, ws);
+    B.reserve(c.staged, ws);
     const size_t at_part = ws.take(part_bytes(c, M));
     if (ws.bytes > 0) {
         const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
@@ -372,7 +404,7 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
         launch_scale_rows(x_dtype, M, K, x, ldx, (int8_t *)A.p, padded, padded, (float *)(base + at_scales), s);
         x_scales = (const float *)(base + at_scales);
     }
-    TileParams p = tile_params(A, B, M, N, padded);
+    TileParams p = tile_params(A, B, M, N, c.staged ? K : padded);
     for (int64_t m = 0; m < M; m += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, M - m);
         p.A = A.p + m * A.ld;
@@ -428,9 +460,13 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
         return launch_status(h, "gated launch");
     }
     Space ws;
-    Matrix A(x, M, H, ldx, 2, ws), B(up, 2 * I, H, ldu, 2, ws);
-    const int64_t K = up_to(H, 8);
-    const Cut c = cut_of(M, I, cdiv(K, 64), true, false, true, h->cu_count);
+    Matrix A(x, M, H, ldx, 2), B(up, 2 * I, H, ldu, 2);
+    const Cut c = cut_with(A, B, [&](bool staged) {
+        return cut_of(M, I, cdiv(H, 64), true, false, true, staged, h->cu_count);
+    });
+    A.reserve(c.staged, ws);
+    B.reserve(c.staged, ws);
+    const int64_t K = c.staged ? H : up_to(H, 8);
     const size_t at_part = ws.take(part_bytes(c, M));
     if (ws.bytes > 0) {
         const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
@@ -475,10 +511,12 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     const int halves = M <= kTwoParts ? 2 : 1;
     const int64_t rows = M * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
-    Matrix X(x, want_up && some ? M : 0, H, ldx, 2, ws, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2, ws);
-    Cut cx = cut_of(rows, H, cdiv(ld, 64), false, false, true, h->cu_count);
+    Matrix X(x, want_up && some ? M : 0, H, ldx, 2, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2);
+    X.reserve(false, ws);
+    W.reserve(false, ws);
+    Cut cx = cut_of(rows, H, cdiv(ld, 64), false, false, true, false, h->cu_count);
     cx.halves = halves;
-    const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, true, h->cu_count);
+    const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, true, false, h->cu_count);
     const size_t at_part = ws.take(std::max(want_x ? part_bytes(cx, rows) : 0, want_up ? part_bytes(cw, 2 * I) : 0));
     const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
     if (rc != XGEMM_OK)
@@ -496,12 +534,12 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     g.chunks = (int)cdiv(I, 8);
     g.inverse = inverse;
     g.most = (uint32_t *)(inverse + 1);
-    g.M = (int)M;
+    g.units = M * cdiv(g.chunks, 64);
     g.pre = (const uint16_t *)pre;
     g.d = (const uint16_t *)d_y;
     g.out = (uint16_t *)(base + at_d);
     if (some) {
-        const int64_t blocks = cdiv(M * g.chunks, 256), few = std::min<int64_t>(blocks, kMostBlocks);
+        const int64_t blocks = cdiv(g.units, 4), few = std::min<int64_t>(blocks, kMostBlocks);
         g.blocks = (int)few;
         const dim3 all(std::min<int64_t>(blocks, (int64_t)1 << 22)), block(256);
         if (dtype == XGEMM_BF16) {
@@ -561,9 +599,14 @@ int run_head(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, int64
     if (!logprob && !lse)
         return XGEMM_OK;
     Space ws;
-    Matrix X(x, T, H, ldx, 2, ws), W(head, V, H, ldw, 2, ws);
-    const int64_t K = up_to(H, 8), rows = std::min(T, kHeadRows);
-    const Cut c = cut_of(rows, V, cdiv(K, 64), false, false, false, h->cu_count);
+    Matrix X(x, T, H, ldx, 2), W(head, V, H, ldw, 2);
+    const int64_t rows = std::min(T, kHeadRows);
+    const Cut c = cut_with(X, W, [&](bool staged) {
+        return cut_of(rows, V, cdiv(H, 64), false, false, false, staged, h->cu_count);
+    });
+    X.reserve(c.staged, ws);
+    W.reserve(c.staged, ws);
+    const int64_t K = c.staged ? H : up_to(H, 8);
     const int64_t tiles = cdiv(V, kTileCols[c.tile]);
     const size_t at_stat = ws.take((size_t)(tiles * rows) * sizeof(float2)), at_logit = ws.take((size_t)rows * 4);
     const int rc = xgemm_host::acquire_workspace(h, ws.bytes, s);
@@ -633,18 +676,20 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     const int halves = T <= kTwoParts ? 2 : 1;
     const int64_t rows = T * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * piece * 2);
-    Matrix X(x, T, H, ldx, 2, ws, want_w ? halves : 1), W(head, T > 0 ? V : 0, H, ldw, 2, ws);
+    Matrix X(x, T, H, ldx, 2, want_w ? halves : 1), W(head, T > 0 ? V : 0, H, ldw, 2);
+    X.reserve(false, ws);
+    W.reserve(false, ws);
     const int64_t K = up_to(H, 8), pieces = cdiv(V, piece);
     // d_x over the pieces: in fp32 until the last
     const bool sums = want_x && pieces > 1 && kind != kFp32;
     const size_t at_sum = ws.take(sums ? (size_t)T * up_to(H, 4) * 4 : 0);
     size_t parts = 0;
     auto cut_x = [&](int64_t n) {
-        Cut c = cut_of(rows, H, cdiv(n, 64), false, false, true, h->cu_count);
+        Cut c = cut_of(rows, H, cdiv(n, 64), false, false, true, false, h->cu_count);
         c.halves = halves;
         return c;
     };
-    auto cut_w = [&](int64_t n) { return cut_of(n, H, cdiv(rows, 64), false, true, true, h->cu_count); };
+    auto cut_w = [&](int64_t n) { return cut_of(n, H, cdiv(rows, 64), false, true, true, false, h->cu_count); };
     for (const int64_t n : {std::min(piece, V), V - (pieces - 1) * piece})
         parts = std::max({parts, part_bytes(cut_x(n), rows), part_bytes(cut_w(n), n)});
     const size_t at_part = ws.take(parts);
@@ -664,7 +709,7 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
         if (T > 0) {
             TileParams p = tile_params(X, W, T, n, K);
             p.B = p.B2 = W.p + v * W.ld;
-            const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, h->cu_count);
+            const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, false, h->cu_count);
             uint16_t *const rest = halves > 1 ? d + T * piece : nullptr;
             if (dtype == XGEMM_BF16)
                 launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);

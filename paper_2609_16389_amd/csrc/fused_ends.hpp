@@ -116,7 +116,7 @@ __device__ __forceinline__ void store_block(char *sh, uint16_t *out, int64_t ld,
 // gated tile with the second matrix's columns from ld / 2 on.
 template <int TYPE, bool GATED>
 struct PartEnd {
-    static constexpr bool kGated = GATED;
+    static constexpr bool kGated = GATED, kStages = true;   // (of an End that does)
     struct Params {
         char *part;
         int ld;   // a multiple of 4, of 8 where gated
@@ -142,7 +142,7 @@ struct PartEnd {
 
 // A product as it is: out = sum * scale + add, rounded to out's type.
 struct StoreEnd {
-    static constexpr bool kGated = false, kJoins = true;
+    static constexpr bool kGated = false, kJoins = true, kStages = false;
     struct Params {
         void *out;
         int64_t ld;
@@ -192,7 +192,7 @@ struct StoreEnd {
 // 8-bit products: out = (sum * scale of the row) * scale of the column.  The sum
 // is exact in 32 bits (|sum| <= 2^14 K < 2^31).
 struct ScaledEnd {
-    static constexpr bool kGated = false, kJoins = true;
+    static constexpr bool kGated = false, kJoins = true, kStages = true;
     struct Params {
         const float *row_scale, *col_scale;
         void *out;
@@ -288,7 +288,7 @@ __device__ __forceinline__ void act_slope(int act, float a, float &value, float 
 // A gated block: out = act(gate) * lift, and both before it (pre) if wanted.
 template <int DT>
 struct GatedEnd {
-    static constexpr bool kGated = true, kJoins = true;
+    static constexpr bool kGated = true, kJoins = true, kStages = true;
     struct Params {
         void *out;
         int64_t ld;
@@ -343,7 +343,7 @@ struct GatedEnd {
 // Logits of a head: per row and tile the largest and the sum of the exponentials
 // relative to it, and the target's logit.
 struct StatsEnd {
-    static constexpr bool kGated = false, kJoins = false;
+    static constexpr bool kGated = false, kJoins = false, kStages = true;
     struct Params {
         const int64_t *targets;   // null: none wanted
         float2 *stat;             // [tile of columns][M]
@@ -436,7 +436,7 @@ __device__ __forceinline__ float left_of(float v)
 // gives little is then 1, not a rounded 1 / rows that is off by as much in every row.
 template <int DT>
 struct SlopeEnd {
-    static constexpr bool kGated = false, kJoins = false;
+    static constexpr bool kGated = false, kJoins = false, kStages = false;
     struct Params {
         const int64_t *targets;
         const float *lse, *d_logprob, *d_lse;   // d_logprob, d_lse: null: zero
@@ -455,6 +455,7 @@ struct SlopeEnd {
         const bool edge = n0 + BN > p.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);   // (rows one after another: the registers are full)
             const int row = min(m0 + wm * TM + i * 16 + (lane & 15), p.M - 1);
             const int64_t target = e.d_logprob ? e.targets[row] : -1;
             float dl = target < 0 ? 0.0f : e.d_logprob[row];
@@ -496,8 +497,11 @@ struct SlopeEnd {
         if (e.rest)
             store(e.rest, [](f32x4 v) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    v[k] = left_of<DT>(v[k]);
+                for (int k = 0; k < 4; ++k) {
+                    float x = v[k];
+                    asm("" : "+v"(x));   // (rounded again rather than kept from the first part)
+                    v[k] = left_of<DT>(x);
+                }
                 return v;
             });
     }
@@ -527,26 +531,6 @@ __global__ void __launch_bounds__(256) join_parts(const char *part, int split, i
             s[1] += *(const quad_t *)(q + ld / 2 * 4);
     }
     End::quad(e, row, col, N, s[0], s[1]);
-}
-
-// 16 bytes from p.  ODD: from any byte, as the aligned dwords that hold them,
-// moved into place (a load of 16 bytes a lane between dwords takes the L1 path
-// several times over).
-template <bool ODD>
-__device__ __forceinline__ u32x4 sixteen(const char *p)
-{
-    typedef u32x4 __attribute__((aligned(4))) some;
-    if constexpr (!ODD)
-        return *(const some *)p;
-    const uint32_t by = (uint32_t)(uintptr_t)p & 3;
-    const u32x4 v = *(const some *)(p - by);
-    const uint32_t last = *(const uint32_t *)((uintptr_t)(p + 15) & ~(uintptr_t)3);
-    u32x4 r;
-    r[0] = __builtin_amdgcn_alignbyte(v[1], v[0], by);
-    r[1] = __builtin_amdgcn_alignbyte(v[2], v[1], by);
-    r[2] = __builtin_amdgcn_alignbyte(v[3], v[2], by);
-    r[3] = __builtin_amdgcn_alignbyte(last, v[3], by);
-    return r;
 }
 
 // Copies of matrices whose rows are not whole 16-byte chunks at such addresses: rows
@@ -721,13 +705,14 @@ struct GatedSlopeParams {
     uint16_t *out;   // M x ld, ld a multiple of 8 of at least 2 I
     int64_t rest;    // values from there to the second of two parts; 0: one part
     int64_t ld;
-    int M, I, act;
+    int I, act;
     int chunks;       // of 8 in I columns
+    int64_t units;    // rows times 64 chunks
     uint32_t *most;   // bits of each block's largest (binary16)
     int blocks;
     float *inverse;   // of the power of two
 };
-constexpr int kMostBlocks = 255;
+constexpr int kMostBlocks = 1020;
 
 template <int DT>
 __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v)[8])
@@ -753,7 +738,9 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
     uint32_t most = 0;
     float s = 1.0f;
     if constexpr (DT == kFp16 && !MOST) {
-        most = most_of((int)threadIdx.x < p.blocks ? p.most[threadIdx.x] : 0u);
+        for (int b = threadIdx.x; b < p.blocks; b += 256)
+            most = max(most, p.most[b]);
+        most = most_of(most);
         if ((threadIdx.x & 63) == 0)
             share_most[threadIdx.x >> 6] = most;
         __syncthreads();
@@ -761,13 +748,19 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
         if (blockIdx.x == 0 && threadIdx.x == 0)
             *p.inverse = 1.0f / s;
     }
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)p.M * p.chunks; at += (int64_t)gridDim.x * 256) {
-        const int row = (int)(at / p.chunks), col = (int)(at % p.chunks) * 8;
+    // a wave takes 512 columns of a row at a time
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t groups = (p.chunks + 63) / 64;
+    for (int64_t unit = (int64_t)blockIdx.x * 4 + wave; unit < p.units; unit += (int64_t)gridDim.x * 4) {
+        const int64_t row = unit < ((int64_t)1 << 32) ? (uint32_t)unit / groups : unit / groups;
+        const int col = ((int)(unit - row * groups) * 64 + lane) * 8;
+        if (col >= p.I)
+            continue;
         float g[8], u[8], d[8], dg[8], du[8];
-        const uint16_t *const pre = p.pre + (int64_t)row * p.ldp;
+        const uint16_t *const pre = p.pre + row * p.ldp;
         eight<DT>((const char *)pre, col, p.I, g);
         eight<DT>((const char *)(pre + p.I), col, p.I, u);
-        eight<DT>((const char *)(p.d + (int64_t)row * p.ldd), col, p.I, d);
+        eight<DT>((const char *)(p.d + row * p.ldd), col, p.I, d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float value, slope;
@@ -791,7 +784,7 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
                     for (int c = 2 * p.I; c < p.ld; ++c)
                         out[c] = 0;
             };
-            uint16_t *const out = p.out + (int64_t)row * p.ld;
+            uint16_t *const out = p.out + row * p.ld;
             store(out);
             if (p.rest) {
 #pragma unroll

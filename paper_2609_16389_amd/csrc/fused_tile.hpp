@@ -26,6 +26,8 @@
 
 #include "decode_device.hpp"
 
+#include <type_traits>
+
 namespace xfused_dev {
 
 using namespace xdecode_dev;
@@ -215,6 +217,92 @@ struct Operand {
     }
 };
 
+// 16 bytes from p.  ODD: from any byte, as the aligned dwords that hold them,
+// moved into place (a load of 16 bytes a lane between dwords takes the L1 path
+// several times over).
+template <bool ODD>
+__device__ __forceinline__ u32x4 sixteen(const char *p)
+{
+    typedef u32x4 __attribute__((aligned(4))) some;
+    if constexpr (!ODD)
+        return *(const some *)p;
+    const uint32_t by = (uint32_t)(uintptr_t)p & 3;
+    const u32x4 v = *(const some *)(p - by);
+    const uint32_t last = *(const uint32_t *)((uintptr_t)(p + 15) & ~(uintptr_t)3);
+    u32x4 r;
+    r[0] = __builtin_amdgcn_alignbyte(v[1], v[0], by);
+    r[1] = __builtin_amdgcn_alignbyte(v[2], v[1], by);
+    r[2] = __builtin_amdgcn_alignbyte(v[3], v[2], by);
+    r[3] = __builtin_amdgcn_alignbyte(last, v[3], by);
+    return r;
+}
+
+// A kAlong operand with rows at any address and of any length: the same parts of a
+// stage, loaded into registers as aligned dwords, moved into place and written to LDS
+// a step later.  The bytes past the end of k are zeros.  (Operands with rows across
+// k were twice as slow so as with a copy: 44 and 38 us in place of 13 and 15 for the
+// gradients of 333 x 1001 x 2731, and 6 for the copies.)
+template <int TYPE, int R, int W>
+struct StagedOperand : Operand<TYPE, kAlong, R, W> {
+    typedef Operand<TYPE, kAlong, R, W> Base;
+    static constexpr int kLoads = Base::kLoads;
+    const char *row[kLoads];   // this lane's rows
+    int at[kLoads];            // byte of its chunk in it, in the next step
+    int end;                   // bytes of a row up to the end of k
+    u32x4 v[kLoads];
+    uint32_t last[kLoads];
+    bool plain;                // v and last are still to be moved into place
+    char *to;                  // of this lane's loads in stage 0
+
+    __device__ __forceinline__ void start(const char *p, int64_t ld, int64_t first, int64_t rows, int k0, int K, int lane,
+                                          int wave, char *sh)
+    {
+        to = sh + wave * Base::kRows * 128 + lane * 16;
+        // (rows past the last are read as the last, and their sums dropped)
+        end = K * Base::E;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int r = j * 8 + lane / 8;
+            row[j] = p + (first + min((int64_t)r, rows - 1)) * ld;
+            at[j] = k0 * Base::E + (((lane & 7) ^ Base::turn(r)) << 4);
+        }
+    }
+    // The next step's loads, from k (the same for all lanes).
+    __device__ __forceinline__ void fetch(int k)
+    {
+        plain = (k + Base::KS) * Base::E <= end;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            if (plain) {
+                typedef u32x4 __attribute__((aligned(4))) some;
+                const uintptr_t q = (uintptr_t)(row[j] + at[j]);
+                v[j] = *(const some *)(q & ~(uintptr_t)3);
+                last[j] = *(const uint32_t *)((q + 15) & ~(uintptr_t)3);
+            } else {
+                v[j] = u32x4{0, 0, 0, 0};
+                if (at[j] < end)
+                    v[j] = load16_end(row[j], at[j], end);
+                last[j] = 0;
+            }
+            at[j] += 128;
+        }
+    }
+    __device__ __forceinline__ void put(int stage)
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            // (a step further on the address has the same place between dwords)
+            const uint32_t by = plain ? (uint32_t)(uintptr_t)(row[j] + at[j]) & 3 : 0u;
+            u32x4 r;
+            r[0] = __builtin_amdgcn_alignbyte(v[j][1], v[j][0], by);
+            r[1] = __builtin_amdgcn_alignbyte(v[j][2], v[j][1], by);
+            r[2] = __builtin_amdgcn_alignbyte(v[j][3], v[j][2], by);
+            r[3] = __builtin_amdgcn_alignbyte(last[j], v[j][3], by);
+            *(u32x4 *)(to + stage + j * 1024) = r;
+        }
+    }
+};
+
 // Workgroup w of the launch -> its tile and range of k.  The hardware hands
 // workgroups to the XCDs in turn: consecutive tiles are gathered on one, in
 // groups of group_m tile rows, so that what runs there together shares rows of
@@ -232,13 +320,15 @@ __device__ __forceinline__ void place(const TileParams &p, int w, int &tm, int &
     tn = r / rows;
 }
 
-template <int TYPE, int LA, int LB, int BM, int BN, int WM, int WN, int S, class End>
+// STAGED: operands at any address, through registers.
+template <int TYPE, int LA, int LB, int BM, int BN, int WM, int WN, int S, bool STAGED, class End>
 __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typename End::Params e)
 {
     constexpr int W = WM * WN;
     constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    typedef Operand<TYPE, LA, BM, W> OpA;
-    typedef Operand<TYPE, LB, BN, W> OpB;
+    typedef std::conditional_t<STAGED, StagedOperand<TYPE, BM, W>, Operand<TYPE, LA, BM, W>> OpA;
+    typedef std::conditional_t<STAGED, StagedOperand<TYPE, BN, W>, Operand<TYPE, LB, BN, W>> OpB;
+    static_assert(!STAGED || (LA == kAlong && LB == kAlong), "staged operands have k along their rows");
     typedef typename Sum<TYPE>::type sum_t;
     constexpr int STAGE = OpA::kBytes + OpB::kBytes, LD = OpA::kLoads + OpB::kLoads;
     static_assert(!End::kGated || (LB == kAlong && (TN == 64 || TN == 32) && OpB::kRows == 32), "rows of a gated tile");
@@ -255,7 +345,13 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
     // (at least S steps, so that the code below is one line; what lies past kend is zero)
     const int nk = max((kend - k0 + OpA::KS - 1) / OpA::KS, S);
 
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)smem;
+    auto place_of = [&](int off) {
+        if constexpr (STAGED)
+            return smem + off;
+        else
+            return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)smem + off;
+    };
+    const auto lds0 = place_of(0), lds1 = place_of(OpA::kBytes);
     OpA a;
     OpB b;
     if constexpr (LA == kAlong)
@@ -266,12 +362,12 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         // the tile's rows by 32: gate, lift, gate, lift, of which a wave takes as
         // many of either
         const int n = n0 + wave / 2 * 32;
-        b.start(wave & 1 ? p.B2 : p.B, p.ldb, n, (int64_t)p.N - n, k0, kend, lane, wave, lds0 + OpA::kBytes);
+        b.start(wave & 1 ? p.B2 : p.B, p.ldb, n, (int64_t)p.N - n, k0, kend, lane, wave, lds1);
     } else if constexpr (LB == kAlong) {
         b.start(p.B, p.ldb, n0 + wave * OpB::kRows, (int64_t)p.N - n0 - wave * OpB::kRows, k0, kend, lane, wave,
-                lds0 + OpA::kBytes);
+                lds1);
     } else {
-        b.start(p.B, p.ldb, n0, (int64_t)p.N - n0, k0, kend, lane, wave, lds0 + OpA::kBytes);
+        b.start(p.B, p.ldb, n0, (int64_t)p.N - n0, k0, kend, lane, wave, lds1);
     }
 
     sum_t acc[FM][FN];
@@ -281,16 +377,34 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         for (int j = 0; j < FN; ++j)
             acc[i][j] = sum_t{0, 0, 0, 0};
 
+    int kf = k0;   // STAGED: k of the step to be fetched next
+    auto fetch = [&]() {
+        if constexpr (STAGED) {
+            a.fetch(kf);
+            b.fetch(kf);
+            kf += OpA::KS;
+        }
+    };
+    auto put = [&](int stage) {
+        if constexpr (STAGED) {
+            a.put(stage * STAGE);
+            b.put(stage * STAGE);
+        }
+    };
     auto load_step = [&](int stage) {
-        const u32x4 da = a.view(), db = b.view();
+        fetch();
+        put(stage);
+        if constexpr (!STAGED) {
+            const u32x4 da = a.view(), db = b.view();
 #pragma unroll
-        for (int j = 0; j < OpA::kLoads; ++j)
-            a.load(da, stage * STAGE, j);
+            for (int j = 0; j < OpA::kLoads; ++j)
+                a.load(da, stage * STAGE, j);
 #pragma unroll
-        for (int j = 0; j < OpB::kLoads; ++j)
-            b.load(db, stage * STAGE, j);
-        a.next();
-        b.next();
+            for (int j = 0; j < OpB::kLoads; ++j)
+                b.load(db, stage * STAGE, j);
+            a.next();
+            b.next();
+        }
     };
     auto read_a = [&](int stage, int kk, int i) { return OpA::read(smem + stage * STAGE, wm * TM + i * 16, kk, lane); };
     auto read_b = [&](int stage, int kk, int j) {
@@ -331,15 +445,19 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         __builtin_amdgcn_sched_barrier(0);
         // this wave has read all of the stage; its loads of the next step have landed
         wait_lds();
-        if constexpr (LOAD)
+        if constexpr (LOAD && !STAGED)
             wait_loads<(S - 2) * LD>();
-        else if constexpr (MORE)
+        else if constexpr (MORE && !STAGED)
             wait_loads<0>();
         meet();
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
         u32x4 da, db;
-        if constexpr (LOAD) {
+        if constexpr (LOAD && STAGED) {
+            // (fetched a step ago)
+            put(stage);
+            fetch();
+        } else if constexpr (LOAD) {
             da = a.view();
             db = b.view();
         }
@@ -353,7 +471,7 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 acc[i][j] = mfma<TYPE>(gb[1][j], ga[1][i], acc[i][j]);
-                if constexpr (LOAD) {
+                if constexpr (LOAD && !STAGED) {
                     const int n = (i - R) * FN + j;
                     if (n % APART == 0 && n / APART < LD) {
                         const int l = n / APART;
@@ -373,7 +491,7 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
             __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
-        if constexpr (LOAD) {
+        if constexpr (LOAD && !STAGED) {
             a.next();
             b.next();
         }
@@ -382,7 +500,12 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
 #pragma unroll
     for (int t = 0; t < S; ++t)
         load_step(t);
-    wait_loads<(S - 1) * LD>();
+    if constexpr (STAGED) {
+        fetch();
+        wait_lds();
+    } else {
+        wait_loads<(S - 1) * LD>();
+    }
     meet();
 #pragma unroll
     for (int i = 0; i < FM; ++i)

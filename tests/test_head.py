@@ -21,7 +21,7 @@ def inputs(T, V, H, dtype, seed=0, pad=(0, 0), offset=(0, 0)):
 
 
 SHAPES = [(1, 1, 1), (1, 2, 8), (2, 127, 7), (3, 129, 64), (1, 4099, 65), (16, 300, 130), (64, 1000, 200), (77, 5001, 72),
-          (130, 257, 520), (300, 700, 33), (2053, 4100, 72), (1024, 8192, 64)]
+          (130, 257, 520), (300, 700, 33), (2053, 4100, 72), (1024, 8192, 64), (333, 3001, 1001), (20, 2003, 515)]
 
 
 @pytest.mark.gpu
@@ -105,7 +105,7 @@ def test_large_logits(dtype, size):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,V,H", [(1, 1, 1), (2, 127, 7), (3, 129, 64), (77, 5001, 72), (130, 257, 520), (300, 700, 33),
-                                   (1030, 4100, 72), (4100, 2309, 40), (64, 3001, 2048)])
+                                   (1030, 4100, 72), (4100, 2309, 40), (64, 3001, 2048), (333, 3001, 1001)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_gradient(T, V, H, dtype):
     x, w, targets = inputs(T, V, H, dtype, T + V + H)
