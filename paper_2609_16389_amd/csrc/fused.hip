@@ -74,8 +74,10 @@ struct Matrix {
     }
     // Microseconds that the copy takes: 2.8 TB/s read and written, the launch.
     double cost() const { return ragged ? (double)rows * (double)cols * 2.0 / 2.8e6 : 0.0; }
-    // The copies of up to two operands, into the workspace.
-    static void place(Matrix &a, Matrix &b, char *ws, hipStream_t s)
+    // The copies of up to two operands, into the workspace: launched, or, if `later`
+    // is given and they are small, left to another launch, which gets as many blocks
+    // for them as this returns.
+    static int place(Matrix &a, Matrix &b, char *ws, hipStream_t s, CopyParams *later = nullptr)
     {
         CopyParams p{};
         int n = 0;
@@ -88,10 +90,16 @@ struct Matrix {
             }
         // (a launch has at most 2^32 threads: what is larger goes in pieces of rows)
         constexpr int64_t most = (int64_t)1 << 22;   // blocks
-        if (n == 2 && p.m[0].blocks + p.m[1].blocks <= most) {
-            hipLaunchKernelGGL(copy_rows, dim3(p.m[0].blocks + p.m[1].blocks), dim3(256), 0, s, p);
-            return;
+        const int64_t blocks = p.m[0].blocks + p.m[1].blocks;
+        if (blocks <= most) {
+            if (later)
+                *later = p;
+            else if (n > 0)
+                hipLaunchKernelGGL(copy_rows, dim3(blocks), dim3(256), 0, s, p);
+            return (int)blocks;
         }
+        if (later)
+            *later = CopyParams{};
         for (int k = 0; k < n; ++k) {
             const auto whole = p.m[k];
             constexpr int64_t some = most * 4;
@@ -104,12 +112,17 @@ struct Matrix {
                     hipLaunchKernelGGL(copy_rows, dim3(one.m[0].blocks), dim3(256), 0, s, one);
                 }
         }
+        return 0;
     }
 };
 
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
+
+// Distance of rows of slopes: a line more than whole 4 KB, where rows that many
+// apart would share a few of memory's channels.
+int64_t slope_ld(int64_t n) { return up_to(n, 8) + (n * 2 % 4096 == 0 ? 64 : 0); }
 
 // How a product is cut: into tiles, and ranges of k whose sums are joined by a
 // second launch.  (Joined by the last workgroup of a tile instead, 3 ranges of 129
@@ -307,12 +320,16 @@ void launch_scale_rows(int dtype, int64_t R, int64_t K, const void *x, int64_t l
     for (int64_t r = 0; r < R; r += some) {
         const dim3 grid(std::min(some, R - r)), block(256);
         const char *const from = (const char *)x + r * ldx * (dtype == XGEMM_FP32 ? 4 : 2);
+        auto launch = [&](auto held, auto any) {
+            hipLaunchKernelGGL(padded <= kHeld ? held : any, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded,
+                               scales + r);
+        };
         if (dtype == XGEMM_BF16)
-            hipLaunchKernelGGL(scale_rows<kBf16>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+            launch(scale_rows<kBf16, true>, scale_rows<kBf16, false>);
         else if (dtype == XGEMM_FP16)
-            hipLaunchKernelGGL(scale_rows<kFp16>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+            launch(scale_rows<kFp16, true>, scale_rows<kFp16, false>);
         else
-            hipLaunchKernelGGL(scale_rows<kFp32>, grid, block, 0, s, from, ldx, K, q + r * ldq, ldq, padded, scales + r);
+            launch(scale_rows<kFp32, true>, scale_rows<kFp32, false>);
     }
 }
 
@@ -350,7 +367,8 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
         RowsParams p{(const char *)x, (const char *)w, nullptr, ldx, ldw, (int)M, (int)N, (int)K};
         ScaledEnd::Params e{x_scales, w_scales, y, ldy, kind};
         // (one row becomes 8-bit within the product)
-        const bool here = ((int64_t)(uintptr_t)w | ldw | K) % 16 == 0 && ldw <= kMaxStep && K <= kQuantBytes;
+        const bool here = ((int64_t)(uintptr_t)w | ldw | K | (int64_t)(uintptr_t)x) % 16 == 0 && ldw <= kMaxStep &&
+                          K * (x_dtype == XGEMM_FP32 ? 4 : 2) <= kQuantBytes;
         if (!whole && M == 1 && here) {
             const dim3 grid(std::min<int64_t>(cdiv(N, 16), h->cu_count)), block(64 * kStreamWaves);
             if (x_dtype == XGEMM_BF16)
@@ -507,7 +525,7 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     Space ws;
     const size_t at_word = ws.take((1 + kMostBlocks) * 4);   // the slopes' inverse factor, the blocks' largest
-    const int64_t ld = up_to(2 * I, 8);
+    const int64_t ld = slope_ld(2 * I);
     const int halves = M <= kTwoParts ? 2 : 1;
     const int64_t rows = M * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
@@ -522,7 +540,8 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     if (rc != XGEMM_OK)
         return rc;
     char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
-    Matrix::place(X, W, base, s);
+    CopyParams copies;
+    const int copy_blocks = Matrix::place(X, W, base, s, &copies);
     float *const inverse = (float *)(base + at_word);
     GatedSlopeParams g;
     g.ldp = ldp;
@@ -541,12 +560,17 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     if (some) {
         const int64_t blocks = cdiv(g.units, 4), few = std::min<int64_t>(blocks, kMostBlocks);
         g.blocks = (int)few;
-        const dim3 all(std::min<int64_t>(blocks, (int64_t)1 << 22)), block(256);
+        const int64_t all = std::min<int64_t>(blocks, (int64_t)1 << 22);
+        auto launch = [&](auto kernel, int64_t n) {
+            hipLaunchKernelGGL(kernel, dim3(g.copies + n), dim3(256), 0, s, g, copies);
+            g.copies = 0;   // (with the first launch)
+        };
+        g.copies = copy_blocks;
         if (dtype == XGEMM_BF16) {
-            hipLaunchKernelGGL((gated_slope<kBf16, false>), all, block, 0, s, g);
+            launch(gated_slope<kBf16, false>, all);
         } else {
-            hipLaunchKernelGGL((gated_slope<kFp16, true>), dim3(few), block, 0, s, g);
-            hipLaunchKernelGGL((gated_slope<kFp16, false>), all, block, 0, s, g);
+            launch(gated_slope<kFp16, true>, few);
+            launch(gated_slope<kFp16, false>, all);
         }
     }
     const float *const scale = some && dtype == XGEMM_FP16 ? inverse : nullptr;
@@ -672,10 +696,10 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     Space ws;
     const size_t at_scale = ws.take(8);
-    const int64_t piece = head_piece(T, V);
+    const int64_t piece = head_piece(T, V), ld = slope_ld(piece);
     const int halves = T <= kTwoParts ? 2 : 1;
     const int64_t rows = T * halves;   // of slopes
-    const size_t at_d = ws.take((size_t)rows * piece * 2);
+    const size_t at_d = ws.take((size_t)rows * ld * 2);
     Matrix X(x, T, H, ldx, 2, want_w ? halves : 1), W(head, T > 0 ? V : 0, H, ldw, 2);
     X.reserve(false, ws);
     W.reserve(false, ws);
@@ -697,10 +721,11 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     if (rc != XGEMM_OK)
         return rc;
     char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
-    Matrix::place(X, W, base, s);
+    CopyParams copies;
+    const int copy_blocks = Matrix::place(X, W, base, s, &copies);
     float *const scales = (float *)(base + at_scale);
-    hipLaunchKernelGGL(slope_scale, dim3(1), dim3(256), 0, s, d_logprob, d_lse, T, dtype == XGEMM_FP16 ? 16384.0f : 1.0f,
-                       scales);
+    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, d_logprob, d_lse, T,
+                       dtype == XGEMM_FP16 ? 16384.0f : 1.0f, scales);
     uint16_t *const d = (uint16_t *)(base + at_d);
     float *const sum = kind == kFp32 ? (float *)d_x : (float *)(base + at_sum);
     const int64_t ld_sum = kind == kFp32 ? ld_dx : up_to(H, 4);
@@ -710,16 +735,16 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
             TileParams p = tile_params(X, W, T, n, K);
             p.B = p.B2 = W.p + v * W.ld;
             const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, false, h->cu_count);
-            uint16_t *const rest = halves > 1 ? d + T * piece : nullptr;
+            uint16_t *const rest = halves > 1 ? d + T * ld : nullptr;
             if (dtype == XGEMM_BF16)
-                launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);
+                launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, ld, v, V}, c, T, s);
             else
-                launch_slopes<kFp16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, piece, v, V}, c, T, s);
+                launch_slopes<kFp16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, ld, v, V}, c, T, s);
         }
         const float *const scale = scales + 1;
         TileParams p{};
         p.A = (const char *)d;
-        p.lda = piece * 2;
+        p.lda = ld * 2;
         if (want_x) {
             const bool last = v + n == V;
             p.B = p.B2 = W.p + v * W.ld;

@@ -546,11 +546,11 @@ struct CopyParams {
         int times;
     } m[2];
 };
-__global__ void __launch_bounds__(256) copy_rows(CopyParams p)
+__device__ __forceinline__ void copy_block(const CopyParams &p, int64_t block)
 {
-    const bool second = blockIdx.x >= p.m[0].blocks;
+    const bool second = block >= p.m[0].blocks;
     const auto &m = p.m[second];
-    const int64_t row = (blockIdx.x - (second ? p.m[0].blocks : 0)) * 4 + (threadIdx.x >> 6);
+    const int64_t row = (block - (second ? p.m[0].blocks : 0)) * 4 + (threadIdx.x >> 6);
     if (row >= m.rows)
         return;
     const char *const from = m.from + row * m.ld;
@@ -560,6 +560,7 @@ __global__ void __launch_bounds__(256) copy_rows(CopyParams p)
             *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
     }
 }
+__global__ void __launch_bounds__(256) copy_rows(CopyParams p) { copy_block(p, blockIdx.x); }
 
 // Per row of K values: scale = max |x| * (1 / 127) (at least 2^-126), q = x / scale
 // rounded to the nearest whole number, ties to even.  A row that holds a NaN or
@@ -613,31 +614,58 @@ __device__ __forceinline__ float row_scale(uint32_t most)
     return most >= 0x7f800000u ? NAN : fmaxf(__builtin_bit_cast(float, most) * (1.0f / 127.0f), 0x1p-126f);
 }
 
+// Eight values over `scale`, rounded.  v * (1 / scale) is within 2.3e-5 of the
+// quotient in fp32 (three roundings of 127 at most), so that both round alike unless it
+// is as near to the middle between two whole numbers; then the quotient itself is
+// taken (a division costs as much as all the rest).
 __device__ __forceinline__ uint64_t eight_bytes(const float (&v)[8], float scale)
 {
-    uint64_t q = 0;
+    if (!(scale == scale))
+        return 0;
+    const float inverse = 1.0f / scale;
+    float n[8], off = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float r = scale == scale ? rintf(v[j] / scale) : 0.0f;
-        q |= (uint64_t)(uint8_t)(int8_t)(int)fminf(fmaxf(r, -127.0f), 127.0f) << (8 * j);
+        const float r = v[j] * inverse;
+        n[j] = rintf(r);
+        off = fmaxf(off, fabsf(r - n[j]));
     }
-    return q;
+    if (off > 0.5f - 0x1p-15f)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            n[j] = rintf(v[j] / scale);
+    uint32_t q[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        q[j / 4] |= ((uint32_t)(int)fminf(fmaxf(n[j], -127.0f), 127.0f) & 0xffu) << (8 * (j & 3));
+    return q[0] | (uint64_t)q[1] << 32;
 }
 
-template <int DT>
+// HELD: rows of up to kHeld values, which stay in registers between the passes.
+constexpr int kHeld = 256 * 8 * 4;
+template <int DT, bool HELD>
 __global__ void __launch_bounds__(256) scale_rows(const char *x, int64_t ldx, int64_t K, int8_t *q, int64_t ldq,
                                                   int64_t padded, float *scales)
 {
     __shared__ uint32_t share_most[4];
     const int64_t row = blockIdx.x;
     const char *const r = x + row * ldx * (DT == kFp32 ? 4 : 2);
+    float held[4][8];
     uint32_t most = 0;
-    for (int64_t k = threadIdx.x * 8; k < K; k += 256 * 8) {
-        float v[8];
+    auto look = [&](float (&v)[8], int64_t k) {
         eight<DT>(r, k, K, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             most = max(most, __builtin_bit_cast(uint32_t, v[j]) & 0x7fffffffu);
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (threadIdx.x * 8 + i * 2048 < K)
+                look(held[i], threadIdx.x * 8 + i * 2048);
+    } else {
+        for (int64_t k = threadIdx.x * 8; k < K; k += 2048)
+            look(held[0], k);
     }
     most = most_of(most);
     if ((threadIdx.x & 63) == 0)
@@ -647,9 +675,7 @@ __global__ void __launch_bounds__(256) scale_rows(const char *x, int64_t ldx, in
     const float scale = row_scale(most);
     if (threadIdx.x == 0)
         scales[row] = scale;
-    for (int64_t k = threadIdx.x * 8; k < padded; k += 256 * 8) {
-        float v[8];
-        eight<DT>(r, k, K, v);
+    auto write = [&](const float (&v)[8], int64_t k) {
         const uint64_t b = eight_bytes(v, scale);
         int8_t *const to = q + row * ldq + k;
         if (k + 8 <= padded) {
@@ -659,6 +685,24 @@ __global__ void __launch_bounds__(256) scale_rows(const char *x, int64_t ldx, in
             for (int j = 0; j < 7; ++j)
                 if (k + j < padded)
                     to[j] = (int8_t)(b >> (8 * j));
+        }
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t k = threadIdx.x * 8 + i * 2048;
+            if (k < padded) {
+                if (k >= K)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        held[i][j] = 0.0f;
+                write(held[i], k);
+            }
+        }
+    } else {
+        for (int64_t k = threadIdx.x * 8; k < padded; k += 2048) {
+            eight<DT>(r, k, K, held[0]);
+            write(held[0], k);
         }
     }
 }
@@ -670,11 +714,13 @@ __device__ __forceinline__ float lift_of(uint32_t most)
     return most == 0 ? 1.0f : __builtin_ldexpf(1.0f, min(max(14 - e, -126), 126));
 }
 
-// One workgroup: scales[0] takes the largest finite |d_logprob| + |d_lse| to
-// `to`, scales[1] is its inverse.
-__global__ void __launch_bounds__(256) slope_scale(const float *d_logprob, const float *d_lse, int64_t rows, float to,
-                                                   float *scales)
+// The first workgroup: scales[0] takes the largest finite |d_logprob| + |d_lse| to
+// `to`, scales[1] is its inverse.  The others: copies of what the products read.
+__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, const float *d_logprob, const float *d_lse,
+                                                   int64_t rows, float to, float *scales)
 {
+    if (blockIdx.x > 0)
+        return copy_block(copies, blockIdx.x - 1);
     __shared__ uint32_t share_most[4];
     uint32_t most = 0;
     for (int64_t r = threadIdx.x; r < rows; r += 256) {
@@ -709,7 +755,8 @@ struct GatedSlopeParams {
     int chunks;       // of 8 in I columns
     int64_t units;    // rows times 64 chunks
     uint32_t *most;   // bits of each block's largest (binary16)
-    int blocks;
+    int blocks;       // that find them
+    int copies;       // the first blocks copy what the products read
     float *inverse;   // of the power of two
 };
 constexpr int kMostBlocks = 1020;
@@ -732,8 +779,11 @@ __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v
 }
 
 template <int DT, bool MOST>
-__global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
+__global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p, CopyParams copies)
 {
+    if (blockIdx.x < p.copies)
+        return copy_block(copies, blockIdx.x);
+    const int64_t block = blockIdx.x - p.copies, blocks = gridDim.x - p.copies;
     __shared__ uint32_t share_most[4];
     uint32_t most = 0;
     float s = 1.0f;
@@ -745,13 +795,13 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
             share_most[threadIdx.x >> 6] = most;
         __syncthreads();
         s = lift_of(max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
-        if (blockIdx.x == 0 && threadIdx.x == 0)
+        if (block == 0 && threadIdx.x == 0)
             *p.inverse = 1.0f / s;
     }
     // a wave takes 512 columns of a row at a time
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t groups = (p.chunks + 63) / 64;
-    for (int64_t unit = (int64_t)blockIdx.x * 4 + wave; unit < p.units; unit += (int64_t)gridDim.x * 4) {
+    for (int64_t unit = block * 4 + wave; unit < p.units; unit += blocks * 4) {
         const int64_t row = unit < ((int64_t)1 << 32) ? (uint32_t)unit / groups : unit / groups;
         const int col = ((int)(unit - row * groups) * 64 + lane) * 8;
         if (col >= p.I)
@@ -781,7 +831,7 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
                 store_eight<DT>(out + col, n, dg);
                 store_eight<DT>(out + p.I + col, n, du);
                 if (n <= 8)
-                    for (int c = 2 * p.I; c < p.ld; ++c)
+                    for (int c = 2 * p.I; c < (2 * p.I + 7) / 8 * 8; ++c)
                         out[c] = 0;
             };
             uint16_t *const out = p.out + row * p.ld;
@@ -804,7 +854,7 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p)
             share_most[threadIdx.x >> 6] = most;
         __syncthreads();
         if (threadIdx.x == 0)
-            p.most[blockIdx.x] = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
+            p.most[block] = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
     }
 }
 

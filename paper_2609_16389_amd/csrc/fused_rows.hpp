@@ -11,6 +11,8 @@
 
 #include "fused_ends.hpp"
 
+#include <utility>
+
 namespace xfused_dev {
 
 constexpr int kUnit = 256;          // bytes of k
@@ -114,8 +116,9 @@ __global__ void __launch_bounds__(64 * W) rows_product(RowsParams p, typename En
 // their queues run on over them: memory never waits for a join.
 //
 // XI: loads of x's part of a unit, 1 for up to 4 rows and 4 for up to 16.  QUANT: x is
-// one row of values of that type (kBf16, kFp16, kFp32), of which each workgroup
-// makes the 8-bit row for itself, in LDS (K up to kQuantBytes); else -1.
+// one row of values of that type (kBf16, kFp16, kFp32; at 16-byte addresses, up to
+// kQuantBytes), of which each workgroup makes the 8-bit row for itself, in LDS,
+// while its first weights are on their way; else -1.
 constexpr int kStreamWaves = 4;
 constexpr int kQuantBytes = 16384;
 
@@ -124,10 +127,10 @@ __global__ void __launch_bounds__(64 * kStreamWaves) rows_stream(RowsParams p, t
 {
     constexpr int W = kStreamWaves, NM = End::kGated ? 2 : 1, NX = QUANT >= 0 ? 0 : XI;
     constexpr int LD = 4 * NM + NX, STAGE = LD * 1024;
-    static_assert((S - 1) * LD < 64, "loads in flight");
+    static_assert(S * LD < 64, "loads in flight");
     typedef typename Sum<TYPE>::type sum_t;
     constexpr int kSums = W * NM * 1024;   // twice
-    __shared__ __attribute__((aligned(16))) char smem[W * S * STAGE + 2 * kSums + (QUANT >= 0 ? kQuantBytes : 0)];
+    __shared__ __attribute__((aligned(16))) char smem[W * S * STAGE + 2 * kSums + (QUANT >= 0 ? 2 * kQuantBytes : 0)];
     __shared__ uint32_t sh_most[W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -174,13 +177,46 @@ __global__ void __launch_bounds__(64 * kStreamWaves) rows_stream(RowsParams p, t
         }
     };
 
+    constexpr int E = QUANT == kFp32 ? 4 : 2;
+    const int first = min(S, total);   // units on their way at the beginning
+    // until no more than n units' loads are on their way
+    auto wait_units = [](int n) {
+        [n]<int... I>(std::integer_sequence<int, I...>) {
+            ((n == I ? wait_loads<I * LD>() : (void)0), ...);
+        }(std::make_integer_sequence<int, S + 1>());
+    };
+    if constexpr (QUANT >= 0) {
+        // x as it is, 1 KB a load, the waves in turn
+        const u32x4 d = descriptor(p.x, (int64_t)p.K * E);
+        const uint32_t raw_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)(qx + kQuantBytes);
+        for (int at = wave * 1024; at < p.K * E; at += W * 1024)
+            load_lds(d, at + lane * 16, __builtin_amdgcn_readfirstlane(raw_at + at));
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+        if (s < total)
+            load(s);
     float row_scale_of_x = 0.0f;
     if constexpr (QUANT >= 0) {
-        // (before the weights' loads, which would have to land first)
+        // (x has landed once no more than the units' loads are left)
+        wait_units(first);
+        meet();
+        const char *const raw = qx + kQuantBytes;
+        // (K is a multiple of 16)
+        auto here = [&](int k, float (&v)[8]) {
+            const u32x4 *const q = (const u32x4 *)(raw + k * E);
+            const u32x4 zero = {0, 0, 0, 0}, lo = k < p.K ? q[0] : zero, hi = k < p.K && E == 4 ? q[1] : zero;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if constexpr (QUANT == kFp32)
+                    v[j] = __builtin_bit_cast(float, j < 4 ? lo[j] : hi[j - 4]);
+                else
+                    v[j] = to_float<QUANT>((uint16_t)(lo[j / 2] >> (16 * (j & 1))));
+        };
         uint32_t most = 0;
         for (int k = threadIdx.x * 8; k < p.K; k += 64 * W * 8) {
             float v[8];
-            eight<QUANT>(p.x, k, p.K, v);
+            here(k, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 most = max(most, __builtin_bit_cast(uint32_t, v[j]) & 0x7fffffffu);
@@ -194,16 +230,12 @@ __global__ void __launch_bounds__(64 * kStreamWaves) rows_stream(RowsParams p, t
         row_scale_of_x = row_scale(most);
         for (int k = threadIdx.x * 8; k < units * kUnit; k += 64 * W * 8) {
             float v[8];
-            eight<QUANT>(p.x, k, p.K, v);
+            here(k, v);
             *(uint64_t *)(qx + k) = eight_bytes(v, row_scale_of_x);
         }
         wait_lds();
         meet();
     }
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-        if (s < total)
-            load(s);
 
     int step = 0, stage = 0;
     for (int block = blockIdx.x, turn = 0; block < blocks; block += gridDim.x, ++turn) {
@@ -212,11 +244,7 @@ __global__ void __launch_bounds__(64 * kStreamWaves) rows_stream(RowsParams p, t
         for (int m = 0; m < NM; ++m)
             acc[m] = sum_t{0, 0, 0, 0};
         for (int i = 0; i < each; ++i, ++step) {
-            // (near the end the units behind this one are waited for too)
-            if (total - step >= S)
-                wait_loads<(S - 1) * LD>();
-            else
-                wait_loads<0>();
+            wait_units(min(total - step, S) - 1);
             asm volatile("" ::: "memory");
             const char *const q = queue + stage * STAGE;
             u32x4 wf[NM][4], xf[4];
