@@ -189,7 +189,7 @@ template <class F>
 Cut cut_with(const Matrix &a, const Matrix &b, F cut)
 {
     const Cut c = cut(false);
-    if (!a.ragged && !b.ragged)
+    if ((!a.ragged && !b.ragged) || b.cols < 16)   // (the staged tiles read 16 bytes of a row at a time)
         return c;
     const Cut staged = cut(true);
     return staged.cost < c.cost + 4.0 + a.cost() + b.cost() ? staged : c;

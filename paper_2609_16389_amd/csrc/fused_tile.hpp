@@ -217,6 +217,18 @@ struct Operand {
     }
 };
 
+// The aligned dwords around an address (in device memory, which a pointer made of a
+// masked address would not show).
+__device__ __forceinline__ u32x4 dwords_at(uintptr_t q)
+{
+    typedef u32x4 __attribute__((aligned(4))) some;
+    return *(const __attribute__((address_space(1))) some *)(q & ~(uintptr_t)3);
+}
+__device__ __forceinline__ uint32_t dword_at(uintptr_t q)
+{
+    return *(const __attribute__((address_space(1))) uint32_t *)(q & ~(uintptr_t)3);
+}
+
 // 16 bytes from p.  ODD: from any byte, as the aligned dwords that hold them,
 // moved into place (a load of 16 bytes a lane between dwords takes the L1 path
 // several times over).
@@ -227,8 +239,8 @@ __device__ __forceinline__ u32x4 sixteen(const char *p)
     if constexpr (!ODD)
         return *(const some *)p;
     const uint32_t by = (uint32_t)(uintptr_t)p & 3;
-    const u32x4 v = *(const some *)(p - by);
-    const uint32_t last = *(const uint32_t *)((uintptr_t)(p + 15) & ~(uintptr_t)3);
+    const u32x4 v = dwords_at((uintptr_t)p);
+    const uint32_t last = dword_at((uintptr_t)p + 15);
     u32x4 r;
     r[0] = __builtin_amdgcn_alignbyte(v[1], v[0], by);
     r[1] = __builtin_amdgcn_alignbyte(v[2], v[1], by);
@@ -251,7 +263,6 @@ struct StagedOperand : Operand<TYPE, kAlong, R, W> {
     int end;                   // bytes of a row up to the end of k
     u32x4 v[kLoads];
     uint32_t last[kLoads];
-    bool plain;                // v and last are still to be moved into place
     char *to;                  // of this lane's loads in stage 0
 
     __device__ __forceinline__ void start(const char *p, int64_t ld, int64_t first, int64_t rows, int k0, int K, int lane,
@@ -267,37 +278,40 @@ struct StagedOperand : Operand<TYPE, kAlong, R, W> {
             at[j] = k0 * Base::E + (((lane & 7) ^ Base::turn(r)) << 4);
         }
     }
-    // The next step's loads, from k (the same for all lanes).
-    __device__ __forceinline__ void fetch(int k)
+    // Past the next step.
+    __device__ __forceinline__ void skip()
     {
-        plain = (k + Base::KS) * Base::E <= end;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            if (plain) {
-                typedef u32x4 __attribute__((aligned(4))) some;
-                const uintptr_t q = (uintptr_t)(row[j] + at[j]);
-                v[j] = *(const some *)(q & ~(uintptr_t)3);
-                last[j] = *(const uint32_t *)((q + 15) & ~(uintptr_t)3);
-            } else {
-                v[j] = u32x4{0, 0, 0, 0};
-                if (at[j] < end)
-                    v[j] = load16_end(row[j], at[j], end);
-                last[j] = 0;
-            }
+        for (int j = 0; j < kLoads; ++j)
             at[j] += 128;
-        }
     }
-    __device__ __forceinline__ void put(int stage)
+    // The next step's loads.  A chunk that goes past the end is read as the row's last 16
+    // bytes (it has as many), and moved down when it is put in place.
+    __device__ __forceinline__ void fetch()
     {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            // (a step further on the address has the same place between dwords)
-            const uint32_t by = plain ? (uint32_t)(uintptr_t)(row[j] + at[j]) & 3 : 0u;
+            const uintptr_t q = (uintptr_t)(row[j] + min(at[j], end - 16));
+            v[j] = dwords_at(q);
+            last[j] = dword_at(q + 15);
+        }
+        skip();
+    }
+    // What was fetched last, from k (the same for all lanes).
+    __device__ __forceinline__ void put(int stage, int k)
+    {
+        const bool whole = (k + Base::KS) * Base::E <= end;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int c = at[j] - 128, from = min(c, end - 16);
+            const uint32_t by = (uint32_t)(uintptr_t)(row[j] + from) & 3;
             u32x4 r;
             r[0] = __builtin_amdgcn_alignbyte(v[j][1], v[j][0], by);
             r[1] = __builtin_amdgcn_alignbyte(v[j][2], v[j][1], by);
             r[2] = __builtin_amdgcn_alignbyte(v[j][3], v[j][2], by);
             r[3] = __builtin_amdgcn_alignbyte(last[j], v[j][3], by);
+            if (!whole)
+                r = shift_down(r, min(c - from, 16));
             *(u32x4 *)(to + stage + j * 1024) = r;
         }
     }
@@ -377,23 +391,21 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         for (int j = 0; j < FN; ++j)
             acc[i][j] = sum_t{0, 0, 0, 0};
 
-    int kf = k0;   // STAGED: k of the step to be fetched next
+    int kf = k0;   // STAGED: k of the step to be put into LDS next
     auto fetch = [&]() {
         if constexpr (STAGED) {
-            a.fetch(kf);
-            b.fetch(kf);
-            kf += OpA::KS;
+            a.fetch();
+            b.fetch();
         }
     };
     auto put = [&](int stage) {
         if constexpr (STAGED) {
-            a.put(stage * STAGE);
-            b.put(stage * STAGE);
+            a.put(stage * STAGE, kf);
+            b.put(stage * STAGE, kf);
+            kf += OpA::KS;
         }
     };
     auto load_step = [&](int stage) {
-        fetch();
-        put(stage);
         if constexpr (!STAGED) {
             const u32x4 da = a.view(), db = b.view();
 #pragma unroll
@@ -497,13 +509,25 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         }
         stage = next;
     };
-#pragma unroll
-    for (int t = 0; t < S; ++t)
-        load_step(t);
     if constexpr (STAGED) {
+        static_assert(S == 2, "steps on their way at the beginning");
+        OpA a0 = a;
+        OpB b0 = b;
+        a0.fetch();
+        b0.fetch();
+        a.skip();
+        b.skip();
+        fetch();
+        a0.put(0, kf);
+        b0.put(0, kf);
+        kf += OpA::KS;
+        put(1);
         fetch();
         wait_lds();
     } else {
+#pragma unroll
+        for (int t = 0; t < S; ++t)
+            load_step(t);
         wait_loads<(S - 1) * LD>();
     }
     meet();
