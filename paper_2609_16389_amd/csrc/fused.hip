@@ -170,7 +170,10 @@ Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool ma
             const int64_t chunk = cdiv(steps, split);
             if (split > 1 && (!may_split || chunk < 3 || cdiv(steps, chunk) != split))
                 continue;
-            const int64_t groups = tiles * split, rounds = cdiv(groups, cus * kCost[t].per_cu);
+            const int64_t groups = tiles * split;
+            if (t != kTile256 && groups > (int64_t)1 << 22)   // (a launch has at most 2^32 threads)
+                break;
+            const int64_t rounds = cdiv(groups, cus * kCost[t].per_cu);
             const double step = (groups > cus ? kCost[t].shared : kCost[t].step) * (staged ? 1.5 : 1.0);
             const double join = split > 1 ? 3.0 + (double)split * (double)M * (double)cols * 8.0 / 3.5e6 : 0.0;
             const double cost = (double)rounds * (kCost[t].ends + step * (double)chunk) + join;
@@ -240,15 +243,22 @@ void launch_product(TileParams p, const typename End::Params &e, const Cut &c, c
     launch_tiles<TYPE, LA, LB, End>(p, e, c.tile, c.staged, s);
 }
 
-// Rows that the kernels for few of them take (fused_rows.hpp).
-constexpr int64_t kFewRows = 16;
-
 // Whether rows can be read through LDS: 16-byte chunks, near enough.
 bool whole_chunks(const RowsParams &p)
 {
     const int64_t x = p.M > 1 ? (int64_t)(uintptr_t)p.x | p.ldx : (int64_t)(uintptr_t)p.x;
     const int64_t w = (int64_t)((uintptr_t)p.w | (uintptr_t)p.w2) | p.ldw;
     return (w | x | p.K) % 16 == 0 && p.ldw <= kMaxStep && (p.M == 1 || p.ldx <= kMaxStep);
+}
+
+// Whether the kernels for few rows take a product: through LDS up to 16; rows at any
+// address up to 4, while the weights are few.  (Microseconds of one row, 12 rows of
+// weights at odd addresses, in these kernels / in tiles: 8-bit 5003 x 2047 9.0, 11.6 /
+// 10.7, 11.0; gated 2731 x 1001 9.0 / 10.0; gated 5003 x 2047 25.2, 31.1 / 19.4, 20.5.)
+template <int TYPE, class End>
+bool few_rows(const RowsParams &p)
+{
+    return whole_chunks(p) ? p.M <= 16 : p.M <= 4 && (int64_t)p.N * p.K * (End::kGated ? 2 : 1) <= (int64_t)1 << 24;
 }
 
 template <int TYPE, class End>
@@ -363,24 +373,29 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
     if (!y || !w_scales || (K > 0 && (!x || !w)) || whole != (x_scales != nullptr))
         return XGEMM_ERR_INVALID_ARG;
     const int kind = y_dtype == XGEMM_FP32 ? kFp32 : y_dtype == XGEMM_FP16 ? kFp16 : kBf16;
-    if (M <= kFewRows && K > 0) {
-        RowsParams p{(const char *)x, (const char *)w, nullptr, ldx, ldw, (int)M, (int)N, (int)K};
+    RowsParams few{(const char *)x, (const char *)w, nullptr, ldx, ldw, (int)M, (int)N, (int)K};
+    if (!whole) {
+        few.x = nullptr;   // (its 8-bit rows will lie in the workspace)
+        few.ldx = up_to(K, 16);
+    }
+    if (K > 0 && few_rows<kInt8, ScaledEnd>(few)) {
         ScaledEnd::Params e{x_scales, w_scales, y, ldy, kind};
         // (one row becomes 8-bit within the product)
         const bool here = ((int64_t)(uintptr_t)w | ldw | K | (int64_t)(uintptr_t)x) % 16 == 0 && ldw <= kMaxStep &&
                           K * (x_dtype == XGEMM_FP32 ? 4 : 2) <= kQuantBytes;
         if (!whole && M == 1 && here) {
+            few.x = (const char *)x;
             const dim3 grid(std::min<int64_t>(cdiv(N, 16), h->cu_count)), block(64 * kStreamWaves);
             if (x_dtype == XGEMM_BF16)
-                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kBf16>), grid, block, 0, s, p, e);
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kBf16>), grid, block, 0, s, few, e);
             else if (x_dtype == XGEMM_FP16)
-                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp16>), grid, block, 0, s, p, e);
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp16>), grid, block, 0, s, few, e);
             else
-                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp32>), grid, block, 0, s, p, e);
+                hipLaunchKernelGGL((rows_stream<kInt8, ScaledEnd, 1, 6, kFp32>), grid, block, 0, s, few, e);
             return launch_status(h, "scaled product launch");
         }
         if (whole) {
-            launch_rows<kInt8, ScaledEnd>(p, e, h->cu_count, s);
+            launch_rows<kInt8, ScaledEnd>(few, e, h->cu_count, s);
             return launch_status(h, "scaled product launch");
         }
         Space ws;
@@ -391,10 +406,9 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
             return rc;
         char *const base = (char *)h->workspace + xgemm_host::kWsPrefix;
         e.row_scale = (const float *)(base + at_scales);
-        p.x = base + at_q;
-        p.ldx = ld;
+        few.x = base + at_q;
         launch_scale_rows(x_dtype, M, K, x, ldx, (int8_t *)(base + at_q), ld, ld, (float *)(base + at_scales), s);
-        launch_rows<kInt8, ScaledEnd>(p, e, h->cu_count, s);
+        launch_rows<kInt8, ScaledEnd>(few, e, h->cu_count, s);
         const int launched = launch_status(h, "scaled product launch");
         const int released = xgemm_host::release_workspace(h, s);
         return launched != XGEMM_OK ? launched : released;
@@ -468,13 +482,13 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
     if (!y || (H > 0 && (!x || !up)))
         return XGEMM_ERR_INVALID_ARG;
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
-    if (M <= kFewRows && H > 0) {
-        const RowsParams p{(const char *)x, (const char *)up, (const char *)up + I * ldu * 2, ldx * 2, ldu * 2,
-                           (int)M, (int)I, (int)H * 2};
+    const RowsParams few{(const char *)x, (const char *)up, (const char *)up + I * ldu * 2, ldx * 2, ldu * 2,
+                         (int)M, (int)I, (int)H * 2};
+    if (H > 0 && few_rows<kBf16, GatedEnd<kBf16>>(few)) {
         if (dtype == XGEMM_BF16)
-            launch_rows<kBf16, GatedEnd<kBf16>>(p, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+            launch_rows<kBf16, GatedEnd<kBf16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
         else
-            launch_rows<kFp16, GatedEnd<kFp16>>(p, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+            launch_rows<kFp16, GatedEnd<kFp16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
         return launch_status(h, "gated launch");
     }
     Space ws;
