@@ -251,68 +251,76 @@ __device__ __forceinline__ u32x4 sixteen(const char *p)
 
 // A kAlong operand with rows at any address and of any length: the same parts of a
 // stage, loaded into registers as aligned dwords, moved into place and written to LDS
-// a step later.  The bytes past the end of k are zeros.  (Operands with rows across
-// k were twice as slow so as with a copy: 44 and 38 us in place of 13 and 15 for the
-// gradients of 333 x 1001 x 2731, and 6 for the copies.)
+// a step later.  The bytes past the end of k are zeros.  Eight neighbouring lanes have
+// a row's eight chunks, so that the dword a chunk ends in is the first of the next
+// lane's; only the eighth loads it (with a load of their own for all lanes a step of
+// 333 x 1001 x 2731 took a third longer: the L1 path, which a load
+// between lines takes twice, is the bound).  (Operands with rows across k were twice
+// as slow so as with a copy: 44 and 38 us in place of 13 and 15 for the gradients of 333 x
+// 1001 x 2731, and 6 for the copies.)
 template <int TYPE, int R, int W>
 struct StagedOperand : Operand<TYPE, kAlong, R, W> {
     typedef Operand<TYPE, kAlong, R, W> Base;
     static constexpr int kLoads = Base::kLoads;
     const char *row[kLoads];   // this lane's rows
-    int at[kLoads];            // byte of its chunk in it, in the next step
+    int at;                    // byte of its chunk in them, in the next step
     int end;                   // bytes of a row up to the end of k
     u32x4 v[kLoads];
     uint32_t last[kLoads];
-    char *to;                  // of this lane's loads in stage 0
+    char *to[2];               // of this lane's loads of even and odd number, in stage 0
+    bool eighth;
 
     __device__ __forceinline__ void start(const char *p, int64_t ld, int64_t first, int64_t rows, int k0, int K, int lane,
                                           int wave, char *sh)
     {
-        to = sh + wave * Base::kRows * 128 + lane * 16;
         // (rows past the last are read as the last, and their sums dropped)
         end = K * Base::E;
+        at = k0 * Base::E + (lane & 7) * 16;
+        eighth = (lane & 7) == 7;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int r = j * 8 + lane / 8;
             row[j] = p + (first + min((int64_t)r, rows - 1)) * ld;
-            at[j] = k0 * Base::E + (((lane & 7) ^ Base::turn(r)) << 4);
+            if (j < 2)
+                to[j] = sh + (wave * Base::kRows + r) * 128 + (((lane & 7) ^ Base::turn(r)) << 4);
         }
     }
     // Past the next step.
-    __device__ __forceinline__ void skip()
+    __device__ __forceinline__ void skip() { at += 128; }
+    // The loads of the next step, from k (the same for all lanes).  A chunk that goes
+    // past the end is read as the row's last 16 bytes (it has as many), and moved
+    // down when it is put in place.
+    __device__ __forceinline__ void fetch(int k)
     {
+        const bool whole = (k + Base::KS) * Base::E <= end;
+        const int from = min(at, end - 16);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-            at[j] += 128;
-    }
-    // The next step's loads.  A chunk that goes past the end is read as the row's last 16
-    // bytes (it has as many), and moved down when it is put in place.
-    __device__ __forceinline__ void fetch()
-    {
+            v[j] = dwords_at((uintptr_t)(row[j] + from));
+        if (!whole || eighth)
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const uintptr_t q = (uintptr_t)(row[j] + min(at[j], end - 16));
-            v[j] = dwords_at(q);
-            last[j] = dword_at(q + 15);
-        }
+            for (int j = 0; j < kLoads; ++j)
+                last[j] = dword_at((uintptr_t)(row[j] + from) + 15);
         skip();
     }
-    // What was fetched last, from k (the same for all lanes).
+    // What was fetched last, from k.
     __device__ __forceinline__ void put(int stage, int k)
     {
         const bool whole = (k + Base::KS) * Base::E <= end;
+        const int c = at - 128, from = min(c, end - 16);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int c = at[j] - 128, from = min(c, end - 16);
             const uint32_t by = (uint32_t)(uintptr_t)(row[j] + from) & 3;
+            const uint32_t beside = (uint32_t)__builtin_amdgcn_mov_dpp((int)v[j][0], 0x101, 0xF, 0xF, true);   // of lane + 1
+            const uint32_t after = whole && !eighth ? beside : last[j];
             u32x4 r;
             r[0] = __builtin_amdgcn_alignbyte(v[j][1], v[j][0], by);
             r[1] = __builtin_amdgcn_alignbyte(v[j][2], v[j][1], by);
             r[2] = __builtin_amdgcn_alignbyte(v[j][3], v[j][2], by);
-            r[3] = __builtin_amdgcn_alignbyte(last[j], v[j][3], by);
+            r[3] = __builtin_amdgcn_alignbyte(after, v[j][3], by);
             if (!whole)
                 r = shift_down(r, min(c - from, 16));
-            *(u32x4 *)(to + stage + j * 1024) = r;
+            *(u32x4 *)(to[j & 1] + stage + j / 2 * 2048) = r;
         }
     }
 };
@@ -392,10 +400,10 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
             acc[i][j] = sum_t{0, 0, 0, 0};
 
     int kf = k0;   // STAGED: k of the step to be put into LDS next
-    auto fetch = [&]() {
+    auto fetch = [&](int ahead) {
         if constexpr (STAGED) {
-            a.fetch();
-            b.fetch();
+            a.fetch(kf + OpA::KS * ahead);
+            b.fetch(kf + OpA::KS * ahead);
         }
     };
     auto put = [&](int stage) {
@@ -468,7 +476,7 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         if constexpr (LOAD && STAGED) {
             // (fetched a step ago)
             put(stage);
-            fetch();
+            fetch(0);
         } else if constexpr (LOAD) {
             da = a.view();
             db = b.view();
@@ -513,16 +521,16 @@ __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typen
         static_assert(S == 2, "steps on their way at the beginning");
         OpA a0 = a;
         OpB b0 = b;
-        a0.fetch();
-        b0.fetch();
+        a0.fetch(kf);
+        b0.fetch(kf);
         a.skip();
         b.skip();
-        fetch();
+        fetch(1);
         a0.put(0, kf);
         b0.put(0, kf);
         kf += OpA::KS;
         put(1);
-        fetch();
+        fetch(0);
         wait_lds();
     } else {
 #pragma unroll
