@@ -738,7 +738,7 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     CopyParams copies;
     const int copy_blocks = Matrix::place(X, W, base, s, &copies);
     float *const scales = (float *)(base + at_scale);
-    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, d_logprob, d_lse, T,
+    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, targets, d_logprob, d_lse, T,
                        dtype == XGEMM_FP16 ? 16384.0f : 1.0f, scales);
     uint16_t *const d = (uint16_t *)(base + at_d);
     float *const sum = kind == kFp32 ? (float *)d_x : (float *)(base + at_sum);

@@ -714,17 +714,18 @@ __device__ __forceinline__ float lift_of(uint32_t most)
     return most == 0 ? 1.0f : __builtin_ldexpf(1.0f, min(max(14 - e, -126), 126));
 }
 
-// The first workgroup: scales[0] takes the largest finite |d_logprob| + |d_lse| to
-// `to`, scales[1] is its inverse.  The others: copies of what the products read.
-__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, const float *d_logprob, const float *d_lse,
-                                                   int64_t rows, float to, float *scales)
+// The first workgroup: scales[0] takes the largest finite |d_logprob| + |d_lse| (of
+// d_logprob where there is a target) to `to`, scales[1] is its inverse.  The others:
+// copies of what the products read.
+__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, const int64_t *targets, const float *d_logprob,
+                                                   const float *d_lse, int64_t rows, float to, float *scales)
 {
     if (blockIdx.x > 0)
         return copy_block(copies, blockIdx.x - 1);
     __shared__ uint32_t share_most[4];
     uint32_t most = 0;
     for (int64_t r = threadIdx.x; r < rows; r += 256) {
-        const float s = (d_logprob ? fabsf(d_logprob[r]) : 0.0f) + (d_lse ? fabsf(d_lse[r]) : 0.0f);
+        const float s = (d_logprob && targets[r] >= 0 ? fabsf(d_logprob[r]) : 0.0f) + (d_lse ? fabsf(d_lse[r]) : 0.0f);
         const uint32_t b = __builtin_bit_cast(uint32_t, s);
         most = max(most, b < 0x7f800000u ? b : 0u);
     }

@@ -173,6 +173,23 @@ def test_gradient_of_any_size_in_binary16(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("T", [20, 300])
+def test_rows_without_a_target_leave_no_trace(T, dtype):
+    """Whatever their d_logprob holds."""
+    x, w, targets = inputs(T, 700, 40, dtype, 6)
+    targets[:: 3] = -100
+    lse = xg.head_logprobs(x, w)["lse"]
+    clean = torch.full((T,), -1.0 / T, device="cuda")
+    d = clean.clone()
+    d[0], d[3], d[6], d[9] = 1e30, -INF, math.nan, 1e-30
+    ref = xg.head_logprobs_grad(x, w, targets, lse, clean)
+    got = xg.head_logprobs_grad(x, w, targets, lse, d)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    assert bool((got[0][:: 3] == 0).all())
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences():
     T, V, H = 11, 60, 24
     x, w, targets = inputs(T, V, H, "bf16", 3)
