@@ -166,7 +166,7 @@ Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool ma
         if ((t == kTile64 && across) || (staged && t != kTile64))
             continue;
         const int64_t tiles = cdiv(M, kTileRows[t]) * cdiv(cols, kTileCols[t]);
-        for (int64_t split = 1; split <= 16; ++split) {
+        for (int64_t split = 1; split <= 32; ++split) {
             const int64_t chunk = cdiv(steps, split);
             if (split > 1 && (!may_split || chunk < 3 || cdiv(steps, chunk) != split))
                 continue;

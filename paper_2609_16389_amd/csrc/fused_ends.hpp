@@ -877,10 +877,18 @@ __global__ void __launch_bounds__(256) head_join(const float2 *stat, int tiles, 
         most = both;
         sum = a + b;
     };
+    // (eight loads at a time: the tiles are few, and their latency is the time)
     if (row < rows)
-        for (int t = t0; t < tiles; t += kJoinThreads) {
-            const float2 s = stat[(int64_t)t * rows + row];
-            add(s.x, s.y);
+        for (int t = t0; t < tiles; t += 8 * kJoinThreads) {
+            float2 s[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int at_t = t + k * kJoinThreads;
+                s[k] = at_t < tiles ? stat[(int64_t)at_t * rows + row] : make_float2(-INFINITY, 0.0f);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                add(s[k].x, s[k].y);
         }
     part[r][t0] = make_float2(most, sum);
     __syncthreads();
