@@ -785,7 +785,9 @@ int xgemm_scaled_run(xgemm_handle_t h, int64_t M, int64_t N, int64_t K, const vo
  *   act        XGEMM_ACT_SILU: a / (1 + exp(-a)); XGEMM_ACT_GELU: a (1 + erf(a /
  *              sqrt(2))) / 2; XGEMM_ACT_GELU_TANH: a (1 + tanh(sqrt(2 / pi) (a +
  *              0.044715 a^3))) / 2
- * y is computed from gate and lift in fp32, before their rounding to pre.
+ * y is computed from gate and lift in fp32, before their rounding to pre.  Up to 16
+ * rows need no workspace where x and up are read in place; more use the workspace
+ * for copies, and for partial sums where there are few tiles.
  */
 enum xgemm_act {
     XGEMM_ACT_SILU = 0,
@@ -845,7 +847,7 @@ int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void
  *   d_x, d_head        T x H and V x H values of the type that `out` names,
  *                      both; NULL: not wanted
  * The logits are computed again in pieces of the vocabulary.  d is rounded to
- * dtype between the products, relative to the largest |d_logprob| + |d_lse|, whose
+ * dtype between the products, relative to the largest |d_logprob| or |d_lse|, whose
  * size does not matter: whatever `out` is, d_x and d_head have an error of half a
  * step of dtype in each term.  (Up to 128 rows d is kept in two parts, with twice the
  * bits.)  p holds lse's own

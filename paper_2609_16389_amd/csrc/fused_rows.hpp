@@ -115,6 +115,10 @@ __global__ void __launch_bounds__(64 * W) rows_product(RowsParams p, typename En
 // take 64 of 16 rows).  Workgroups stay for several blocks of 16 columns, and
 // their queues run on over them: memory never waits for a join.
 //
+// What bounds it: HBM (gated 1 x 4096 x 14336: 235 MB in 37 us, 6.4 TB/s; fragments
+// loaded straight into registers took 49), for small weights the launch and one
+// latency (8-bit 4096 x 4096 5.2 us, of which a third is the row's own 8-bit values).
+//
 // XI: loads of x's part of a unit, 1 for up to 4 rows and 4 for up to 16.  QUANT: x is
 // one row of values of that type (kBf16, kFp16, kFp32; at 16-byte addresses, up to
 // kQuantBytes), of which each workgroup makes the 8-bit row for itself, in LDS,

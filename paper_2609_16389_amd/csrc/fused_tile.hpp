@@ -253,9 +253,11 @@ __device__ __forceinline__ u32x4 sixteen(const char *p)
 // stage, loaded into registers as aligned dwords, moved into place and written to LDS
 // a step later.  The bytes past the end of k are zeros.  Eight neighbouring lanes have
 // a row's eight chunks, so that the dword a chunk ends in is the first of the next
-// lane's; only the eighth loads it (with a load of their own for all lanes a step of
-// 333 x 1001 x 2731 took a third longer: the L1 path, which a load
-// between lines takes twice, is the bound).  (Operands with rows across k were twice
+// lane's; only the eighth loads it.  A step takes 0.90 us for a workgroup alone on its CU
+// (0.94 with that dword loaded by every lane, 1.05 from aligned 16-byte loads with
+// the chunks put together from two lanes' dwords, as long with two steps under way;
+// 0.5 for whole chunks), which is less than copies and those up to some 10 MB: 8-bit 37 x
+// 5003 x 2047 7.3 us, with copies 5.3 and 8.  (Operands with rows across k were twice
 // as slow so as with a copy: 44 and 38 us in place of 13 and 15 for the gradients of 333 x
 // 1001 x 2731, and 6 for the copies.)
 template <int TYPE, int R, int W>
@@ -342,6 +344,17 @@ __device__ __forceinline__ void place(const TileParams &p, int w, int &tm, int &
     tn = r / rows;
 }
 
+// What bounds it, for tiles of 256 x 256 on random values: LDS and the matrix units
+// together (192 KB read and 64 KB written for 2048 cycles of products on each SIMD in a
+// step) and the power limit.  A step takes 1.40 us with k along both rows and 1.5 to
+// 1.6 with rows across k (K from 1024 to 8192, all CUs at work), as an 8-bit one does,
+// and a tile 5 to 13 us more for its beginning, its end and its stores, which
+// nothing else on the CU hides.  4096 x 28672 x 4096 with the gated end 752 us (1280
+// TFLOP/s; the library's product alone 752), 4096 x 131072 x 4096 with the
+// statistics 3120 us (1410), 4096 x 14336 x 4096 8-bit 229 us (2100 TOP/s).  Tiles of 128
+// x 128 take 0.82 us a step alone on a CU and 1.1 shared, of 64 x 128 0.43 and 0.67.
+// (Measured and left: groups of 2 to 16 tile rows within 3%, 4 and 8 best.)
+//
 // STAGED: operands at any address, through registers.
 template <int TYPE, int LA, int LB, int BM, int BN, int WM, int WN, int S, bool STAGED, class End>
 __global__ void __launch_bounds__(WM * WN * 64) tile_product(TileParams p, typename End::Params e)
