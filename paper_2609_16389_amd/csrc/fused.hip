@@ -151,12 +151,13 @@ constexpr int64_t kTwoParts = 128;
 // d_x of 2048 x 2048 x 5632 112 (4 ranges; not split 242) / 123 / 128.
 // across: A's rows are its k (a transposed product), which the smallest tile does
 // not take.
+struct TileCost {
+    double ends, step, shared;
+    int per_cu;
+};
+constexpr TileCost kCost[] = {{6.0, 1.45, 1.45, 1}, {3.0, 0.82, 1.1, 2}, {2.5, 0.43, 0.67, 2}};
 Cut cut_of(int64_t M, int64_t N, int64_t steps, bool gated, bool across, bool may_split, bool staged, int cu_count)
 {
-    struct {
-        double ends, step, shared;
-        int per_cu;
-    } constexpr kCost[] = {{6.0, 1.45, 1.45, 1}, {3.0, 0.82, 1.1, 2}, {2.5, 0.43, 0.67, 2}};
     const int64_t cols = gated ? 2 * N : N, cus = std::max(cu_count, 1);
     M = std::min(M, kRowsLaunch);
     steps = std::max<int64_t>(steps, 1);
@@ -196,6 +197,27 @@ Cut cut_with(const Matrix &a, const Matrix &b, F cut)
         return c;
     const Cut staged = cut(true);
     return staged.cost < c.cost + 4.0 + a.cost() + b.cost() ? staged : c;
+}
+
+// Where the last round of large tiles would leave CUs idle: the columns of the whole
+// rounds (`body`), and the cut of those after them, which are a launch of their own.
+// (8-bit 4096 x 5120 x 4096, one round and a quarter: 93 us in place of 115; 4096 x
+// 14336 x 4096, three and a half: 250 in place of 264, with x's 8-bit rows; gated 2048 x
+// 2048 x 5632, one and three eighths: 96 in place of 108.)
+struct Band {
+    int64_t body;   // all columns: no band
+    Cut rest;
+};
+Band band_of(const Cut &c, int64_t M, int64_t N, int64_t steps, bool gated, int cu_count)
+{
+    const int64_t cus = std::max(cu_count, 1), width = gated ? 128 : 256, rows = cdiv(M, 256);
+    const int64_t whole = c.tile == kTile256 && c.split == 1 && M <= kRowsLaunch ? rows * cdiv(N, width) / cus : 0;
+    const int64_t body = whole * cus / rows * width;
+    if (body <= 0 || body >= N)
+        return Band{N, c};
+    const Cut rest = cut_of(M, N - body, steps, gated, false, false, false, cu_count);
+    const double cost = (double)whole * (kCost[kTile256].ends + kCost[kTile256].step * (double)c.chunk) + rest.cost + 3.0;
+    return cost < 0.97 * c.cost ? Band{body, rest} : Band{N, c};
 }
 
 size_t part_bytes(const Cut &c, int64_t M)
@@ -437,11 +459,20 @@ int run_scaled(xgemm_ctx *h, int64_t M, int64_t N, int64_t K, const void *x, int
         x_scales = (const float *)(base + at_scales);
     }
     TileParams p = tile_params(A, B, M, N, c.staged ? K : padded);
+    const Band band = band_of(c, M, N, cdiv(padded, 128), false, h->cu_count);
     for (int64_t m = 0; m < M; m += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, M - m);
         p.A = A.p + m * A.ld;
-        const ScaledEnd::Params e{x_scales + m, w_scales, (char *)y + m * ldy * (kind == kFp32 ? 4 : 2), ldy, kind};
+        ScaledEnd::Params e{x_scales + m, w_scales, (char *)y + m * ldy * (kind == kFp32 ? 4 : 2), ldy, kind};
+        p.N = (int)band.body;
         launch_product<kInt8, kAlong, kAlong, ScaledEnd>(p, e, c, base + at_part, s);
+        if (band.body < N) {   // (all rows are one launch)
+            p.B += band.body * B.ld;
+            p.N = (int)(N - band.body);
+            e.col_scale += band.body;
+            e.out = (char *)e.out + band.body * (kind == kFp32 ? 4 : 2);
+            launch_product<kInt8, kAlong, kAlong, ScaledEnd>(p, e, band.rest, nullptr, s);
+        }
     }
     const int launched = launch_status(h, "scaled product launch");
     const int released = ws.bytes > 0 ? xgemm_host::release_workspace(h, s) : XGEMM_OK;
@@ -456,15 +487,25 @@ bool act_ok(int act) { return act == XGEMM_ACT_SILU || act == XGEMM_ACT_GELU || 
 
 template <int DT>
 void launch_gated(TileParams p, int64_t M, void *out, int64_t ld, int kind, int act, uint16_t *pre, int64_t ldp,
-                  const Cut &c, char *part, hipStream_t s)
+                  const Cut &c, const Band &band, char *part, hipStream_t s)
 {
     const char *const A = p.A;
+    const int64_t I = p.N;
     for (int64_t m = 0; m < M; m += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, M - m);
         p.A = A + m * p.lda;
-        const typename GatedEnd<DT>::Params e{(char *)out + m * ld * (kind == kFp32 ? 4 : 2), ld, kind, act,
-                                              pre ? pre + m * ldp : nullptr, ldp};
+        typename GatedEnd<DT>::Params e{(char *)out + m * ld * (kind == kFp32 ? 4 : 2), ld, kind, act,
+                                        pre ? pre + m * ldp : nullptr, ldp, I};
+        p.N = (int)band.body;
         launch_product<DT, kAlong, kAlong, GatedEnd<DT>>(p, e, c, part, s);
+        if (band.body < I) {   // (all rows are one launch)
+            p.B += band.body * p.ldb;
+            p.B2 += band.body * p.ldb;
+            p.N = (int)(I - band.body);
+            e.out = (char *)e.out + band.body * (kind == kFp32 ? 4 : 2);
+            e.pre = pre ? e.pre + band.body : nullptr;
+            launch_product<DT, kAlong, kAlong, GatedEnd<DT>>(p, e, band.rest, nullptr, s);
+        }
     }
 }
 
@@ -486,9 +527,9 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
                          (int)M, (int)I, (int)H * 2};
     if (H > 0 && few_rows<kBf16, GatedEnd<kBf16>>(few)) {
         if (dtype == XGEMM_BF16)
-            launch_rows<kBf16, GatedEnd<kBf16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+            launch_rows<kBf16, GatedEnd<kBf16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp, I}, h->cu_count, s);
         else
-            launch_rows<kFp16, GatedEnd<kFp16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp}, h->cu_count, s);
+            launch_rows<kFp16, GatedEnd<kFp16>>(few, {y, ldy, kind, act, (uint16_t *)pre, ldp, I}, h->cu_count, s);
         return launch_status(h, "gated launch");
     }
     Space ws;
@@ -509,10 +550,11 @@ int run_gated(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x, int6
     Matrix::place(A, B, base, s);
     TileParams p = tile_params(A, B, M, I, K);
     p.B2 = B.p + I * B.ld;
+    const Band band = band_of(c, M, I, cdiv(H, 64), true, h->cu_count);
     if (dtype == XGEMM_BF16)
-        launch_gated<kBf16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, base + at_part, s);
+        launch_gated<kBf16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, band, base + at_part, s);
     else
-        launch_gated<kFp16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, base + at_part, s);
+        launch_gated<kFp16>(p, M, y, ldy, kind, act, (uint16_t *)pre, ldp, c, band, base + at_part, s);
     const int launched = launch_status(h, "gated launch");
     const int released = ws.bytes > 0 ? xgemm_host::release_workspace(h, s) : XGEMM_OK;
     return launched != XGEMM_OK ? launched : released;

@@ -296,6 +296,7 @@ struct GatedEnd {
         int kind, act;
         uint16_t *pre;   // null: not wanted
         int64_t ldp;
+        int64_t lift;    // columns of pre from the gate to the lift
     };
     typedef float value_t;
     static __device__ __forceinline__ void quad(const Params &e, int row, int col, int N, f32x4 g, f32x4 u)
@@ -308,7 +309,7 @@ struct GatedEnd {
         if (e.pre) {
             uint16_t *const q = e.pre + (int64_t)row * e.ldp;
             store_quad(q, DT, col, N, g);
-            store_quad(q + N, DT, col, N, u);
+            store_quad(q + e.lift, DT, col, N, u);
         }
     }
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
@@ -330,7 +331,7 @@ struct GatedEnd {
         };
         if (e.pre) {
             store(e.pre, e.ldp, DT, [&](int i, int j) { return acc[i][j]; });
-            store(e.pre + p.N, e.ldp, DT, [&](int i, int j) { return acc[i][j + FH]; });
+            store(e.pre + e.lift, e.ldp, DT, [&](int i, int j) { return acc[i][j + FH]; });
         }
         if (e.kind != kFp32)
             store(e.out, e.ld, e.kind, inner);

@@ -23,7 +23,7 @@ def inputs(M, H, I, dtype, seed=0, pad=(0, 0), offset=(0, 0), scale=1.0):
 SHAPES = [(1, 1, 1), (1, 8, 16), (2, 7, 3), (3, 64, 65), (16, 65, 32), (17, 130, 33), (64, 200, 64), (65, 72, 129),
           (5, 1001, 40), (1, 4096, 100), (130, 520, 270), (40, 2048, 500), (2053, 72, 2052), (2304, 64, 2048),
           (1, 64, 4200), (4, 256, 8300), (7, 2056, 4500), (16, 512, 100), (16, 4104, 50),
-          (333, 1001, 701), (37, 2047, 515), (1, 2047, 77), (9, 1001, 130)]
+          (333, 1001, 701), (37, 2047, 515), (1, 2047, 77), (9, 1001, 130), (4096, 512, 2505), (2100, 1000, 4601)]
 
 
 @pytest.mark.gpu

@@ -33,7 +33,7 @@ def check(a, w, ws, xs, out, what=""):
 SHAPES = [(1, 1, 1), (1, 5, 16), (2, 3, 17), (3, 129, 127), (1, 64, 128), (16, 256, 129), (17, 33, 255), (64, 65, 1000),
           (65, 300, 64), (100, 127, 2048), (129, 257, 400), (1, 700, 4096), (8, 96, 5001), (300, 500, 4100), (2053, 4100, 272),
           (2304, 4096, 128), (1, 8200, 512), (4, 4200, 2048), (5, 4200, 2064), (16, 100, 8192), (1, 40, 16400), (1, 33, 16384),
-          (3, 12345, 272), (37, 1003, 2047), (333, 700, 1001)]
+          (3, 12345, 272), (37, 1003, 2047), (333, 700, 1001), (4096, 5001, 1024), (2100, 9100, 512)]
 
 
 @pytest.mark.gpu
