@@ -39,6 +39,7 @@ def test_gradients(tokens, dtype):
     nll = lse - logits.gather(1, targets.clamp(min=0)[:, None])[:, 0]
     exact = (nll + 1e-4 * lse ** 2)[kept].mean()
     exact.backward()
+    exact = exact.detach()
     # Everything passed on is rounded to 16 bits: x, inner, hidden, pre, the slopes, their products.  Each
     # rounding moves what follows by at most half a step of it: eight of them on the longest path, of
     # quantities that the path's factors make no larger than the result's own scale; the logits (up to 10
