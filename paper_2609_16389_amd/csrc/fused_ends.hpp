@@ -387,15 +387,26 @@ struct StatsEnd {
                     most = fmaxf(most, acc[i][j][k]);
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            // (a NaN or +inf makes the sum NaN; relative to the largest the product with
-            // log2 e may be rounded as the logit itself is)
-            const float ref = most > -INFINITY ? -kLog2e * most : 0.0f;
+            // Relative to the largest.  Times log2 e it is rounded as a logit is, and what that
+            // left (`off`) is taken out of the sum again; far from zero that would be more than
+            // an exponent, and the difference is taken first.  (A NaN or +inf makes the sum NaN.)
+            const float ref = most > -INFINITY ? most : 0.0f;
             float sum = 0.0f;
+            if (__any(fabsf(ref) > 0x1p20f)) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
+                for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][k], kLog2e, ref));
+                    for (int k = 0; k < 4; ++k)
+                        sum += exp_of(acc[i][j][k] - ref);
+            } else {
+                const float times = -kLog2e * ref, off = __builtin_fmaf(ref, kLog2e, times);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][k], kLog2e, times));
+                sum *= __builtin_amdgcn_exp2f(-off);
+            }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (lane < 16)
