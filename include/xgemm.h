@@ -852,10 +852,11 @@ int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void
  * step of dtype in each term.  (Up to 128 rows d is kept in two parts, with twice the
  * bits.)  p holds lse's own
  * rounding, a relative |lse| 2^-24.  A row whose lse is -inf, or whose d_logprob (or
- * target's part in it) and d_lse are zero, has d = 0.  Uses the
+ * target's part in it) and d_lse are zero, has d = 0 and takes no part in d_head,
+ * whatever its x and lse hold.  Uses the
  * workspace: some 256 MB for d (2 bytes a logit; 4096 bytes a row if that is
- * more), and 4 bytes for each value of d_x where it is not fp32 and there are several
- * pieces.
+ * more), a copy of x for d_head, and 4 bytes for each value of d_x where it is not fp32
+ * and there are several pieces.
  */
 int xgemm_head_grad(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
                     int64_t ldw, const int64_t *targets, const float *lse, const float *d_logprob, const float *d_lse,

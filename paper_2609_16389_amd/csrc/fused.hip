@@ -49,18 +49,19 @@ struct Matrix {
     bool ragged;              // in place only the staged tiles read it
     bool copied;
     int times;                // the copy holds the rows so many times, one after another
+    const HeadRows *part;     // a copy anyhow, in which rows that take no part in this are zeros; null: all do
     size_t at;                // of the copy
 
-    Matrix(const void *data, int64_t r, int64_t c, int64_t leading, int size, int n = 1)
+    Matrix(const void *data, int64_t r, int64_t c, int64_t leading, int size, int n = 1, const HeadRows *of = nullptr)
         : p((const char *)data), rows(r), cols(c * size), ld(r > 1 ? leading * size : up_to(c * size, 16)), copied(false),
-          times(n), at(0)
+          times(n), part(of), at(0)
     {
         ragged = rows > 0 && cols > 0 && (((uintptr_t)p | ld | cols) % 16 != 0 || ld > kMaxStep);
     }
     // Room for the copy, where there has to be one.
     void reserve(bool staged, Space &ws)
     {
-        copied = (ragged && !staged) || (times > 1 && rows > 0 && cols > 0);
+        copied = (ragged && !staged) || ((times > 1 || part) && rows > 0 && cols > 0);
         if (copied)
             at = ws.take((size_t)(rows * times) * up_to(cols, 16));
     }
@@ -76,7 +77,9 @@ struct Matrix {
         for (Matrix *const m : {&a, &b})
             if (m->copied) {
                 const int64_t chunks = cdiv(m->cols, 16);
-                p.m[n++] = {m->p, ws + m->at, m->ld, m->cols, m->rows, chunks, cdiv(m->rows, 4), m->times};
+                p.m[n++] = {m->p, ws + m->at, m->ld, m->cols, m->rows, chunks, cdiv(m->rows, 4), m->times, m->part != nullptr};
+                if (m->part)
+                    p.of = *m->part;
                 m->p = ws + m->at;
                 m->ld = chunks * 16;
             }
@@ -100,7 +103,8 @@ struct Matrix {
                     CopyParams one{};
                     const int64_t rows = std::min(some, whole.rows - r);
                     one.m[0] = {whole.from + r * whole.ld, whole.to + (t * whole.rows + r) * whole.chunks * 16, whole.ld,
-                                whole.bytes, rows, whole.chunks, cdiv(rows, 4), 1};
+                                whole.bytes, rows, whole.chunks, cdiv(rows, 4), 1, whole.part};
+                    one.of = p.of.from(r);
                     hipLaunchKernelGGL(copy_rows, dim3(one.m[0].blocks), dim3(256), 0, s, one);
                 }
         }
@@ -618,10 +622,7 @@ void launch_slopes(TileParams p, const typename SlopeEnd<DT>::Params &at, const 
     for (int64_t t = 0; t < T; t += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, T - t);
         p.A = A + t * p.lda;
-        e.targets = at.targets ? at.targets + t : nullptr;
-        e.lse = at.lse + t;
-        e.d_logprob = at.d_logprob ? at.d_logprob + t : nullptr;
-        e.d_lse = at.d_lse ? at.d_lse + t : nullptr;
+        e.of = at.of.from(t);
         e.out = at.out + t * at.ld;   // (two parts only of fewer rows than a launch's)
         launch_product<DT, kAlong, kAlong, SlopeEnd<DT>>(p, e, c, nullptr, s);
     }
@@ -647,7 +648,10 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     const int halves = T <= kTwoParts ? 2 : 1;
     const int64_t rows = T * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
-    Matrix X(x, T, H, ldx, 2, want_w ? halves : 1), W(head, T > 0 ? V : 0, H, ldw, 2);
+    // (d_head multiplies x by slopes of 0 where a row takes no part: such a row's x, which may hold
+    // anything, is left out)
+    const HeadRows of{targets, lse, d_logprob, d_lse, V};
+    Matrix X(x, T, H, ldx, 2, want_w ? halves : 1, want_w ? &of : nullptr), W(head, T > 0 ? V : 0, H, ldw, 2);
     X.reserve(false, ws);
     W.reserve(false, ws);
     const int64_t K = up_to(H, 8), pieces = cdiv(V, piece);
@@ -671,7 +675,7 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     CopyParams copies;
     const int copy_blocks = Matrix::place(X, W, base, s, &copies);
     float *const scales = (float *)(base + at_scale);
-    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, targets, d_logprob, d_lse, T,
+    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, of, T,
                        dtype == XGEMM_FP16 ? 16384.0f : 1.0f, scales);
     uint16_t *const d = (uint16_t *)(base + at_d);
     float *const sum = kind == kFp32 ? (float *)d_x : (float *)(base + at_sum);
@@ -684,9 +688,9 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
             const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, false, h->cu_count);
             uint16_t *const rest = halves > 1 ? d + T * ld : nullptr;
             if (dtype == XGEMM_BF16)
-                launch_slopes<kBf16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, ld, v, V}, c, T, s);
+                launch_slopes<kBf16>(p, {of, scales, d, rest, ld, v}, c, T, s);
             else
-                launch_slopes<kFp16>(p, {targets, lse, d_logprob, d_lse, scales, d, rest, ld, v, V}, c, T, s);
+                launch_slopes<kFp16>(p, {of, scales, d, rest, ld, v}, c, T, s);
         }
         const float *const scale = scales + 1;
         TileParams p{};

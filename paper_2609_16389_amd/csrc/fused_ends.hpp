@@ -442,6 +442,32 @@ __device__ __forceinline__ float left_of(float v)
     return fabsf(r) < INFINITY ? r : 0.0f;   // (of an infinity or a NaN the first part says it all)
 }
 
+// What the gradient of a head's log probabilities takes of each row.
+struct HeadRows {
+    const int64_t *targets;
+    const float *lse, *d_logprob, *d_lse;   // d_logprob, d_lse: null: zero
+    int64_t V;
+
+    // Those from row r on.
+    HeadRows from(int64_t r) const
+    {
+        return {targets ? targets + r : nullptr, lse ? lse + r : nullptr, d_logprob ? d_logprob + r : nullptr,
+                d_lse ? d_lse + r : nullptr, V};
+    }
+    // The factors of the target's place and of p (minus d_logprob plus d_lse), and
+    // whether the row takes part: one of nothing but -inf does not, nor does one without
+    // factors, whatever its lse.
+    __device__ __forceinline__ bool factors(int64_t row, int64_t &target, float &dl, float &dp) const
+    {
+        target = d_logprob ? targets[row] : -1;
+        dl = target < 0 ? 0.0f : d_logprob[row];
+        if (target >= V)
+            dl = NAN;
+        dp = (d_lse ? d_lse[row] : 0.0f) - dl;
+        return !(lse[row] == -INFINITY || (dl == 0.0f && dp == 0.0f));
+    }
+};
+
 // The gradient in a head's logits, d_logprob (hot - p) + d_lse p, as the operand
 // of the products that follow, times a factor that takes the largest |d_logprob| or
 // |d_lse| to 1 (binary16: 2^14, since p / rows would fall below its smallest numbers;
@@ -452,13 +478,11 @@ template <int DT>
 struct SlopeEnd {
     static constexpr bool kGated = false, kJoins = false, kStages = false;
     struct Params {
-        const int64_t *targets;
-        const float *lse, *d_logprob, *d_lse;   // d_logprob, d_lse: null: zero
+        HeadRows of;
         const float *scale;
         uint16_t *out, *rest;                   // rest: of two parts the second; null: one part
         int64_t ld;     // a multiple of 8; columns up to a multiple of 8 are written
         int64_t first;  // the target of column 0
-        int64_t V;
     };
     template <int BM, int BN, int TM, int TN, int FM, int FN, int WN, class Acc>
     static __device__ __forceinline__ void finish(const TileParams &p, const Params &e, Acc &acc, char *smem, int m0,
@@ -471,13 +495,10 @@ struct SlopeEnd {
         for (int i = 0; i < FM; ++i) {
             __builtin_amdgcn_sched_barrier(0);   // (rows one after another: the registers are full)
             const int row = min(m0 + wm * TM + i * 16 + (lane & 15), p.M - 1);
-            const int64_t target = e.d_logprob ? e.targets[row] : -1;
-            float dl = target < 0 ? 0.0f : e.d_logprob[row];
-            if (target >= e.V)
-                dl = NAN;
-            const float lse = e.lse[row], dp = (e.d_lse ? e.d_lse[row] : 0.0f) - dl;
-            // (a row of nothing but -inf takes no part, nor does one without factors, whatever its lse)
-            const bool empty = lse == -INFINITY || (dl == 0.0f && dp == 0.0f);
+            int64_t target;
+            float dl, dp;
+            const bool empty = !e.of.factors(row, target, dl, dp);
+            const float lse = e.of.lse[row];
             // the target's place among this lane's columns (j * 16 + k)
             const int first = n0 + wn * TN + (lane >> 4) * 4;
             const int64_t hot = target - e.first - first;
@@ -551,14 +572,16 @@ __global__ void __launch_bounds__(256) join_parts(const char *part, int split, i
 // of `bytes` bytes, at any alignment, to rows of `chunks` x 16, zeros after the
 // end, `times` one after another.  Four rows a workgroup, 64 lanes along each.
 // Up to two matrices a launch (for a few megabytes a launch takes as long as
-// the copy).
+// the copy).  `part`: rows that take none in a head's gradient are zeros.
 struct CopyParams {
     struct {
         const char *from;
         char *to;
         int64_t ld, bytes, rows, chunks, blocks;
         int times;
+        bool part;
     } m[2];
+    HeadRows of;
 };
 __device__ __forceinline__ void copy_block(const CopyParams &p, int64_t block)
 {
@@ -568,8 +591,13 @@ __device__ __forceinline__ void copy_block(const CopyParams &p, int64_t block)
     if (row >= m.rows)
         return;
     const char *const from = m.from + row * m.ld;
+    int64_t target;
+    float dl, dp;
+    const bool none = m.part && !p.of.factors(row, target, dl, dp);
     for (int64_t c = threadIdx.x & 63; c < m.chunks; c += 64) {
-        const u32x4 v = c * 16 + 16 <= m.bytes ? sixteen<true>(from + c * 16) : load16_end(from, c * 16, m.bytes);
+        const u32x4 v = none                    ? u32x4{0, 0, 0, 0}
+                        : c * 16 + 16 <= m.bytes ? sixteen<true>(from + c * 16)
+                                                 : load16_end(from, c * 16, m.bytes);
         for (int k = 0; k < m.times; ++k)
             *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
     }
@@ -733,8 +761,7 @@ __device__ __forceinline__ float lift_of(uint32_t most)
 // The first workgroup: scales[0] takes the largest finite |d_logprob| (where there
 // is a target) or |d_lse| to `to`, scales[1] is its inverse.  The others: copies of
 // what the products read.
-__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, const int64_t *targets, const float *d_logprob,
-                                                   const float *d_lse, int64_t rows, float to, float *scales)
+__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, HeadRows of, int64_t rows, float to, float *scales)
 {
     if (blockIdx.x > 0)
         return copy_block(copies, blockIdx.x - 1);
@@ -742,8 +769,8 @@ __global__ void __launch_bounds__(256) slope_scale(CopyParams copies, const int6
     uint32_t most = 0;
 #pragma unroll 8
     for (int64_t r = threadIdx.x; r < rows; r += 256) {
-        const uint32_t a = d_logprob && targets[r] >= 0 ? __builtin_bit_cast(uint32_t, d_logprob[r]) & 0x7fffffffu : 0u;
-        const uint32_t b = d_lse ? __builtin_bit_cast(uint32_t, d_lse[r]) & 0x7fffffffu : 0u;
+        const uint32_t a = of.d_logprob && of.targets[r] >= 0 ? __builtin_bit_cast(uint32_t, of.d_logprob[r]) & 0x7fffffffu : 0u;
+        const uint32_t b = of.d_lse ? __builtin_bit_cast(uint32_t, of.d_lse[r]) & 0x7fffffffu : 0u;
         most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
     }
     most = most_of(most);
