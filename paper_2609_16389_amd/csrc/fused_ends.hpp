@@ -779,8 +779,8 @@ __global__ void __launch_bounds__(256) slope_scale(CopyParams copies, HeadRows o
     __syncthreads();
     if (threadIdx.x == 0) {
         most = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
-        // (a smaller factor for what is next to fp32's ends)
-        const float m = fminf(fmaxf(__builtin_bit_cast(float, most), 0x1p-100f), 0x1p100f);
+        // (a smaller factor for what is next to fp32's ends, where it or its inverse would be no normal number)
+        const float m = fminf(fmaxf(__builtin_bit_cast(float, most), to * 0x1p-126f), to * 0x1p126f);
         scales[0] = most == 0 ? 1.0f : to / m;
         scales[1] = most == 0 ? 1.0f : m / to;
     }
