@@ -806,11 +806,15 @@ int xgemm_gated_run(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const voi
  *   d_y, ldd       M x I values of dtype
  *   d_x, d_up      M x H and 2 I x H values of the type that `out` names, both;
  *                  NULL: not wanted (x is read for d_up only, up for d_x only)
- * d_gate and d_lift are rounded to dtype between the products (with XGEMM_FP16
- * times a power of two, so that their size does not matter): whatever `out` is,
- * d_x and d_up have an error of half a step of dtype in each term.  (Up to 128 rows
- * they are kept in two parts, and the error is that of fp32.)  Uses 4 I bytes of
- * workspace for each row, 8 I up to 128 rows.
+ * d_gate and d_lift are rounded to dtype between the products: whatever `out` is, d_x
+ * and d_up have an error of half a step of dtype (2^-8 with XGEMM_BF16, 2^-11 with
+ * XGEMM_FP16) in each term, up to 128 rows, where they are kept in two parts, of that
+ * squared.  With XGEMM_FP16 they are kept times a power of two for each row, so that
+ * their size does not matter, nor that of one row beside another: add 2^-28 of the
+ * row's largest to each of them, and in d_up, a sum over the rows, 2^-33 of the
+ * largest of all rows in each term.  Uses the workspace: 4 I bytes for each row, 8 I
+ * up to 128 rows, a copy of x (two up to 128 rows) with XGEMM_FP16 or up to 128 rows,
+ * copies of what is not read in place, and partial sums where there are few tiles.
  */
 int xgemm_gated_grad(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const void *x, int64_t ldx, const void *up,
                      int64_t ldu, const void *pre, int64_t ldp, const void *d_y, int64_t ldd, void *d_x, int64_t ld_dx,
@@ -849,8 +853,11 @@ int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void
  * The logits are computed again in pieces of the vocabulary.  d is rounded to
  * dtype between the products, relative to the largest |d_logprob| or |d_lse|, whose
  * size does not matter: whatever `out` is, d_x and d_head have an error of half a
- * step of dtype in each term.  (Up to 128 rows d is kept in two parts, with twice the
- * bits.)  p holds lse's own
+ * step of dtype (2^-8 with XGEMM_BF16, 2^-11 with XGEMM_FP16) in each term, up to 128
+ * rows, where d is kept in two parts, of that squared.  With XGEMM_FP16 rows of small
+ * factors are kept times a power of two each: add 2^-28 of the row's largest factor
+ * to each slope, and in d_head, a sum over the rows, 2^-33 of the largest factor of
+ * all rows in each term.  p holds lse's own
  * rounding, a relative |lse| 2^-24.  A row whose lse is -inf, or whose d_logprob (or
  * target's part in it) and d_lse are zero, has d = 0 and takes no part in d_head,
  * whatever its x and lse hold.  Uses the

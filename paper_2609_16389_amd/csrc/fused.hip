@@ -224,21 +224,22 @@ TileParams tile_params(const Matrix &A, const Matrix &B, int64_t M, int64_t N, i
 // out = a product of 16-bit operands (rows of A and out in launches of
 // kRowsLaunch).
 template <int LA, int LB>
-void product(int dtype, TileParams p, StoreEnd::Params e, const Cut &c, char *part, hipStream_t s)
+void product(int dtype, TileParams p, StoreParams e, const Cut &c, char *part, hipStream_t s)
 {
     const int64_t M = p.M;
     const char *const A = p.A;
     void *const out = e.out;
-    const float *const add = e.add;
+    const float *const add = e.add, *const raise = e.raise;
     for (int64_t m = 0; m < M; m += kRowsLaunch) {
         p.M = (int)std::min(kRowsLaunch, M - m);
         p.A = A + m * (LA == kAlong ? p.lda : 2);
         e.out = (char *)out + m * e.ld * (e.kind == kFp32 ? 4 : 2);
         e.add = add ? add + m * e.ld_add : nullptr;
+        e.raise = raise ? raise + m : nullptr;
         if (dtype == XGEMM_BF16)
             launch_product<kBf16, LA, LB, StoreEnd>(p, e, c, part, s);
-        else
-            launch_product<kFp16, LA, LB, StoreEnd>(p, e, c, part, s);
+        else   // (rows of slopes are raised)
+            launch_product<kFp16, LA, LB, StoreEndOf<LA == kAlong>>(p, e, c, part, s);
     }
 }
 
@@ -483,14 +484,20 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
         return XGEMM_ERR_INVALID_ARG;
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     Space ws;
+    const bool raised = dtype == XGEMM_FP16 && some;
     const size_t at_word = ws.take((1 + kMostBlocks) * 4);   // the slopes' inverse factor, the blocks' largest
+    const int64_t units = M * cdiv(cdiv(I, 8), 64);
+    const size_t at_unit = ws.take(raised ? (size_t)units * 4 : 0), at_raise = ws.take(raised ? (size_t)M * 4 : 0);
     const int64_t ld = slope_ld(2 * I);
     const int halves = M <= kTwoParts ? 2 : 1;
     const int64_t rows = M * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
-    Matrix X(x, want_up && some ? M : 0, H, ldx, 2, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2);
+    // (binary16: a copy of x anyhow, lowered as the slopes are raised)
+    Matrix X(x, want_up && some && !raised ? M : 0, H, ldx, 2, halves), W(up, want_x && some ? 2 * I : 0, H, ldu, 2);
     X.reserve(false, ws);
     W.reserve(false, ws);
+    const int64_t x_chunks = cdiv(H, 8);
+    const size_t at_x = ws.take(raised && want_up ? (size_t)(rows * x_chunks) * 16 : 0);
     Cut cx = cut_of(rows, H, cdiv(ld, 64), false, false, true, false, h->cu_count);
     cx.halves = halves;
     const Cut cw = cut_of(2 * I, H, cdiv(rows, 64), false, true, true, false, h->cu_count);
@@ -512,7 +519,11 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
     g.chunks = (int)cdiv(I, 8);
     g.inverse = inverse;
     g.most = (uint32_t *)(inverse + 1);
-    g.units = M * cdiv(g.chunks, 64);
+    g.unit_most = (uint32_t *)(base + at_unit);
+    g.raise = (float *)(base + at_raise);
+    g.x = RaisedCopy{(const char *)x, base + at_x, ldx * 2, H * 2, want_up ? M : 0, x_chunks, halves};
+    g.rows = M;
+    g.units = units;
     g.pre = (const uint16_t *)pre;
     g.d = (const uint16_t *)d_y;
     g.out = (uint16_t *)(base + at_d);
@@ -529,10 +540,13 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
             launch(gated_slope<kBf16, false>, all);
         } else {
             launch(gated_slope<kFp16, true>, few);
-            launch(gated_slope<kFp16, false>, all);
+            g.copies = (int)std::min<int64_t>(cdiv(g.x.rows, 4), (int64_t)1 << 22);
+            // (each block begins with the blocks' largest and its row's: 4096 x 14336 with 14 blocks a CU 140 us,
+            // with one for each four units 180)
+            launch(gated_slope<kFp16, false>, std::min<int64_t>(all, 14 * (int64_t)std::max(h->cu_count, 1)));
         }
     }
-    const float *const scale = some && dtype == XGEMM_FP16 ? inverse : nullptr;
+    const float *const scale = raised ? inverse : nullptr, *const raise = raised ? g.raise : nullptr;
     TileParams p{};
     p.A = base + at_d;
     p.lda = ld * 2;
@@ -542,15 +556,15 @@ int run_gated_grad(xgemm_ctx *h, int64_t M, int64_t H, int64_t I, const void *x,
         p.M = (int)rows;
         p.N = (int)H;
         p.K = some ? (int)(2 * I) : 0;
-        product<kAlong, kAcross>(dtype, p, StoreEnd::Params{d_x, ld_dx, kind, scale, nullptr, 0}, cx, base + at_part, s);
+        product<kAlong, kAcross>(dtype, p, StoreParams{d_x, ld_dx, kind, scale, nullptr, 0, raise}, cx, base + at_part, s);
     }
     if (want_up) {
-        p.B = p.B2 = X.p;
-        p.ldb = X.ld;
+        p.B = p.B2 = raised ? g.x.to : X.p;
+        p.ldb = raised ? x_chunks * 16 : X.ld;
         p.M = (int)(2 * I);
         p.N = (int)H;
         p.K = some ? (int)rows : 0;
-        product<kAcross, kAcross>(dtype, p, StoreEnd::Params{d_up, ld_dup, kind, scale, nullptr, 0}, cw, base + at_part, s);
+        product<kAcross, kAcross>(dtype, p, StoreParams{d_up, ld_dup, kind, scale, nullptr, 0, nullptr}, cw, base + at_part, s);
     }
     const int launched = launch_status(h, "gated gradient launch");
     const int released = xgemm_host::release_workspace(h, s);
@@ -623,6 +637,7 @@ void launch_slopes(TileParams p, const typename SlopeEnd<DT>::Params &at, const 
         p.M = (int)std::min(kRowsLaunch, T - t);
         p.A = A + t * p.lda;
         e.of = at.of.from(t);
+        e.raise = at.raise ? at.raise + t : nullptr;
         e.out = at.out + t * at.ld;   // (two parts only of fewer rows than a launch's)
         launch_product<DT, kAlong, kAlong, SlopeEnd<DT>>(p, e, c, nullptr, s);
     }
@@ -643,17 +658,21 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
         return XGEMM_ERR_INVALID_ARG;
     const int kind = out == XGEMM_OUT_FP32 ? kFp32 : dtype == XGEMM_BF16 ? kBf16 : kFp16;
     Space ws;
-    const size_t at_scale = ws.take(8);
+    const bool raised = dtype == XGEMM_FP16 && T > 0;
+    const size_t at_scale = ws.take(8), at_raise = ws.take(raised ? (size_t)T * 4 : 0);
     const int64_t piece = head_piece(T, V), ld = slope_ld(piece);
     const int halves = T <= kTwoParts ? 2 : 1;
     const int64_t rows = T * halves;   // of slopes
     const size_t at_d = ws.take((size_t)rows * ld * 2);
     // (d_head multiplies x by slopes of 0 where a row takes no part: such a row's x, which may hold
-    // anything, is left out)
+    // anything, is left out.  binary16: in a copy that the logits are not made of)
     const HeadRows of{targets, lse, d_logprob, d_lse, V};
-    Matrix X(x, T, H, ldx, 2, want_w ? halves : 1, want_w ? &of : nullptr), W(head, T > 0 ? V : 0, H, ldw, 2);
+    const bool same = want_w && !raised;
+    Matrix X(x, T, H, ldx, 2, same ? halves : 1, same ? &of : nullptr), W(head, T > 0 ? V : 0, H, ldw, 2);
     X.reserve(false, ws);
     W.reserve(false, ws);
+    const int64_t x_chunks = cdiv(H, 8);
+    const size_t at_x = ws.take(raised && want_w ? (size_t)(rows * x_chunks) * 16 : 0);
     const int64_t K = up_to(H, 8), pieces = cdiv(V, piece);
     // d_x over the pieces: in fp32 until the last
     const bool sums = want_x && pieces > 1 && kind != kFp32;
@@ -675,8 +694,11 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
     CopyParams copies;
     const int copy_blocks = Matrix::place(X, W, base, s, &copies);
     float *const scales = (float *)(base + at_scale);
-    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks), dim3(256), 0, s, copies, of, T,
-                       dtype == XGEMM_FP16 ? 16384.0f : 1.0f, scales);
+    float *const raise = raised ? (float *)(base + at_raise) : nullptr;
+    const int raise_blocks = raised ? (int)std::min<int64_t>(cdiv(T, 4), 1024) : 0;
+    hipLaunchKernelGGL(slope_scale, dim3(1 + copy_blocks + raise_blocks), dim3(256), 0, s, copies, copy_blocks,
+                       RaisedCopy{(const char *)x, raised && want_w ? base + at_x : nullptr, ldx * 2, H * 2, T, x_chunks, halves}, of,
+                       T, dtype == XGEMM_FP16 ? 16384.0f : 1.0f, scales, raise);
     uint16_t *const d = (uint16_t *)(base + at_d);
     float *const sum = kind == kFp32 ? (float *)d_x : (float *)(base + at_sum);
     const int64_t ld_sum = kind == kFp32 ? ld_dx : up_to(H, 4);
@@ -688,9 +710,9 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
             const Cut c = cut_of(T, n, cdiv(K, 64), false, false, false, false, h->cu_count);
             uint16_t *const rest = halves > 1 ? d + T * ld : nullptr;
             if (dtype == XGEMM_BF16)
-                launch_slopes<kBf16>(p, {of, scales, d, rest, ld, v}, c, T, s);
+                launch_slopes<kBf16>(p, {of, scales, raise, d, rest, ld, v}, c, T, s);
             else
-                launch_slopes<kFp16>(p, {of, scales, d, rest, ld, v}, c, T, s);
+                launch_slopes<kFp16>(p, {of, scales, raise, d, rest, ld, v}, c, T, s);
         }
         const float *const scale = scales + 1;
         TileParams p{};
@@ -703,16 +725,17 @@ int run_head_grad(xgemm_ctx *h, int64_t T, int64_t V, int64_t H, const void *x, 
             p.M = (int)rows;
             p.N = (int)H;
             p.K = (int)n;
-            StoreEnd::Params e{last ? d_x : sum, last ? ld_dx : ld_sum, last ? kind : kFp32, scale, v > 0 ? sum : nullptr, ld_sum};
+            const StoreParams e{last ? d_x : sum, last ? ld_dx : ld_sum, last ? kind : kFp32, scale, v > 0 ? sum : nullptr, ld_sum,
+                                raise};
             product<kAlong, kAcross>(dtype, p, e, cut_x(n), base + at_part, s);
         }
         if (want_w) {
-            p.B = p.B2 = X.p;
-            p.ldb = X.ld;
+            p.B = p.B2 = raised ? base + at_x : X.p;
+            p.ldb = raised ? x_chunks * 16 : X.ld;
             p.M = (int)n;
             p.N = (int)H;
             p.K = (int)rows;
-            const StoreEnd::Params e{(char *)d_head + v * ld_dw * (kind == kFp32 ? 4 : 2), ld_dw, kind, scale, nullptr, 0};
+            const StoreParams e{(char *)d_head + v * ld_dw * (kind == kFp32 ? 4 : 2), ld_dw, kind, scale, nullptr, 0, nullptr};
             product<kAcross, kAcross>(dtype, p, e, cut_w(n), base + at_part, s);
         }
     }

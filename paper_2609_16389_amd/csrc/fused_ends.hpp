@@ -141,17 +141,72 @@ struct PartEnd {
     }
 };
 
-// A product as it is: out = sum * scale + add, rounded to out's type.
-struct StoreEnd {
+// Slopes of a gradient in binary16 have one factor that takes the largest of the matrix
+// to 2^14, and a row whose largest is more than 2^kRoom below that would lose bits and
+// then vanish.  Its slopes are raised by a power of two to where a row 2^kRoom below
+// has them: its row of d_x, which no other row takes part in, is divided by that again,
+// and in the weights' gradient, a sum over the rows, it meets a row of x that has been
+// divided by it.  So slopes are off by at most 2^-28 of their row's largest beside half a
+// step, whatever the sizes of the rows; what x loses is at most 2^-33 of the largest
+// slope of all, in terms that small beside it.  (More room leaves less to the small
+// slopes of a row, less of it takes bits from x in more rows.)
+constexpr int kRoom = 10, kMostRaise = 100;
+
+// The exponent, from the bits of the largest magnitudes of the row and of all.
+__device__ __forceinline__ int raise_of(uint32_t row, uint32_t most)
+{
+    return row == 0 ? 0 : min(max((int)(most >> 23) - (int)(row >> 23) - kRoom, 0), kMostRaise);
+}
+__device__ __forceinline__ float power_of_two(int n) { return __builtin_bit_cast(float, (uint32_t)(127 + n) << 23); }
+// 1 over a power of two, exactly.
+__device__ __forceinline__ float over(float power)
+{
+    return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, power));
+}
+
+// Rows of binary16 values, 16 bytes of them at a time, as copies whose rows are whole
+// chunks.
+struct RaisedCopy {
+    const char *from;
+    char *to;                        // null: no copies
+    int64_t ld, bytes, rows, chunks;
+    int times;                       // the copies stand one after another
+};
+// One row, over 2^n (n < 0: zeros), by a wave.
+__device__ __forceinline__ void copy_lowered(const RaisedCopy &m, int64_t row, int n, int lane)
+{
+    const char *const from = m.from + row * m.ld;
+    const float by = power_of_two(-max(n, 0));
+#pragma unroll 2
+    for (int64_t c = lane; c < m.chunks; c += 64) {
+        u32x4 v = {0, 0, 0, 0};
+        if (n >= 0)
+            v = c * 16 + 16 <= m.bytes ? sixteen<true>(from + c * 16) : load16_end(from, c * 16, m.bytes);
+        if (n > 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[j] = from_float<kFp16>(to_float<kFp16>((uint16_t)(v[j] & 0xffffu)) * by) |
+                       (uint32_t)from_float<kFp16>(to_float<kFp16>((uint16_t)(v[j] >> 16)) * by) << 16;
+        for (int k = 0; k < m.times; ++k)
+            *(u32x4 *)(m.to + ((k * m.rows + row) * m.chunks + c) * 16) = v;
+    }
+}
+
+// A product as it is: out = sum * scale + add, rounded to out's type.  RAISED: rows
+// are sums of raised slopes (see there), and each is divided by its power of two.
+struct StoreParams {
+    void *out;
+    int64_t ld;
+    int kind;
+    const float *scale;   // a number in memory; null: 1
+    const float *add;     // what earlier parts of k left (leading dimension ld_add); null: nothing
+    int64_t ld_add;
+    const float *raise;   // null: 1
+};
+template <bool RAISED>
+struct StoreEndOf {
     static constexpr bool kGated = false, kJoins = true, kStages = false;
-    struct Params {
-        void *out;
-        int64_t ld;
-        int kind;
-        const float *scale;   // a number in memory; null: 1
-        const float *add;     // what earlier parts of k left (leading dimension ld_add); null: nothing
-        int64_t ld_add;
-    };
+    typedef StoreParams Params;
     typedef float value_t;
     static __device__ __forceinline__ f32x4 value(const Params &e, int row, int col, int M, int N, f32x4 v)
     {
@@ -160,6 +215,14 @@ struct StoreEnd {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 v[k] *= s;
+        }
+        if constexpr (RAISED) {
+            if (e.raise && row < M) {
+                const float r = over(e.raise[row]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] *= r;
+            }
         }
         if (e.add && row < M) {
             const float *const q = e.add + (int64_t)row * e.ld_add + col;
@@ -189,6 +252,7 @@ struct StoreEnd {
             });
     }
 };
+typedef StoreEndOf<false> StoreEnd;
 
 // 8-bit products: out = (sum * scale of the row) * scale of the column.  The sum
 // is exact in 32 bits (|sum| <= 2^14 K < 2^31).
@@ -466,6 +530,13 @@ struct HeadRows {
         dp = (d_lse ? d_lse[row] : 0.0f) - dl;
         return !(lse[row] == -INFINITY || (dl == 0.0f && dp == 0.0f));
     }
+    // Bits of the largest of the finite factors.
+    __device__ __forceinline__ uint32_t size(int64_t row) const
+    {
+        const uint32_t a = d_logprob && targets[row] >= 0 ? __builtin_bit_cast(uint32_t, d_logprob[row]) & 0x7fffffffu : 0u;
+        const uint32_t b = d_lse ? __builtin_bit_cast(uint32_t, d_lse[row]) & 0x7fffffffu : 0u;
+        return max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u);
+    }
 };
 
 // The gradient in a head's logits, d_logprob (hot - p) + d_lse p, as the operand
@@ -480,6 +551,7 @@ struct SlopeEnd {
     struct Params {
         HeadRows of;
         const float *scale;
+        const float *raise;                     // binary16: of each row
         uint16_t *out, *rest;                   // rest: of two parts the second; null: one part
         int64_t ld;     // a multiple of 8; columns up to a multiple of 8 are written
         int64_t first;  // the target of column 0
@@ -503,7 +575,11 @@ struct SlopeEnd {
             const int first = n0 + wn * TN + (lane >> 4) * 4;
             const int64_t hot = target - e.first - first;
             const bool mine = hot >= 0 && hot < TN && !empty;
-            const float dps = empty ? 0.0f : dp * scale;
+            float dps = empty ? 0.0f : dp * scale, dls = dl * scale;
+            if constexpr (DT == kFp16) {
+                dps *= e.raise[row];
+                dls *= e.raise[row];
+            }
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const int col = first + j * 16;
@@ -514,7 +590,7 @@ struct SlopeEnd {
                 if (mine) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        v[k] += hot == j * 16 + k ? dl * scale : 0.0f;
+                        v[k] += hot == j * 16 + k ? dls : 0.0f;
                 }
                 if (edge) {
 #pragma unroll
@@ -759,36 +835,53 @@ __device__ __forceinline__ float lift_of(uint32_t most)
 }
 
 // The first workgroup: scales[0] takes the largest finite |d_logprob| (where there
-// is a target) or |d_lse| to `to`, scales[1] is its inverse.  The others: copies of
-// what the products read.
-__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, HeadRows of, int64_t rows, float to, float *scales)
+// is a target) or |d_lse| to `to`, scales[1] is its inverse.  The next `copy_blocks`:
+// copies of what the products read.  Those after them (binary16), a wave a row: the
+// powers of two by which rows are raised, and the copies of x that the weights' gradient
+// multiplies, zeros where a row takes no part.  Each finds the largest for itself, while
+// the first does: a launch of their own took 5 us.
+__global__ void __launch_bounds__(256) slope_scale(CopyParams copies, int copy_blocks, RaisedCopy x, HeadRows of, int64_t rows,
+                                                   float to, float *scales, float *raise)
 {
-    if (blockIdx.x > 0)
+    if (blockIdx.x > 0 && blockIdx.x <= copy_blocks)
         return copy_block(copies, blockIdx.x - 1);
     __shared__ uint32_t share_most[4];
     uint32_t most = 0;
 #pragma unroll 8
-    for (int64_t r = threadIdx.x; r < rows; r += 256) {
-        const uint32_t a = of.d_logprob && of.targets[r] >= 0 ? __builtin_bit_cast(uint32_t, of.d_logprob[r]) & 0x7fffffffu : 0u;
-        const uint32_t b = of.d_lse ? __builtin_bit_cast(uint32_t, of.d_lse[r]) & 0x7fffffffu : 0u;
-        most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
-    }
+    for (int64_t r = threadIdx.x; r < rows; r += 256)
+        most = max(most, of.size(r));
     most = most_of(most);
     if ((threadIdx.x & 63) == 0)
         share_most[threadIdx.x >> 6] = most;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        most = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
-        // (a smaller factor for what is next to fp32's ends, where it or its inverse would be no normal number)
-        const float m = fminf(fmaxf(__builtin_bit_cast(float, most), to * 0x1p-126f), to * 0x1p126f);
-        scales[0] = most == 0 ? 1.0f : to / m;
-        scales[1] = most == 0 ? 1.0f : m / to;
+    most = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) {
+            // (a smaller factor for what is next to fp32's ends, where it or its inverse would be no normal number)
+            const float m = fminf(fmaxf(__builtin_bit_cast(float, most), to * 0x1p-126f), to * 0x1p126f);
+            scales[0] = most == 0 ? 1.0f : to / m;
+            scales[1] = most == 0 ? 1.0f : m / to;
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int64_t before = 1 + (int64_t)copy_blocks;
+    for (int64_t row = (blockIdx.x - before) * 4 + (threadIdx.x >> 6); row < rows; row += (gridDim.x - before) * 4) {
+        int64_t target;
+        float dl, dp;
+        const bool part = of.factors(row, target, dl, dp);
+        const int n = raise_of(of.size(row), most);
+        if (lane == 0)
+            raise[row] = power_of_two(n);
+        if (x.to)
+            copy_lowered(x, row, part ? n : -1, lane);
     }
 }
 
 // The gradient in a gated block's projections, [d lift act'(gate) | d act(gate)],
 // as the operand of the products that follow.  In binary16 times a power of two
-// that takes the largest of them to 2^14: a first launch (MOST) finds each block's.
+// that takes the largest of them to 2^14, rows of small ones raised: a first launch (MOST)
+// finds the largest of each block and unit.
 // Eight columns a thread, the padding after 2 I zeros.  HBM is the bound: 4096 x 14336
 // bfloat16 101 us, 5.8 TB/s; for a megabyte or two the launch and a chain of latencies.
 struct GatedSlopeParams {
@@ -799,11 +892,14 @@ struct GatedSlopeParams {
     int64_t ld;
     int I, act;
     int chunks;       // of 8 in I columns
-    int64_t units;    // rows times 64 chunks
+    int64_t rows, units;   // rows times 64 chunks
     uint32_t *most;   // bits of each block's largest (binary16)
     int blocks;       // that find them
+    uint32_t *unit_most;   // and of each unit's
     int copies;       // the first blocks copy what the products read
     float *inverse;   // of the power of two
+    float *raise;     // of each row
+    RaisedCopy x;     // binary16, by the last launch
 };
 constexpr int kMostBlocks = 1020;
 
@@ -827,51 +923,96 @@ __device__ __forceinline__ void store_eight(uint16_t *to, int n, const float (&v
 template <int DT, bool MOST>
 __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p, CopyParams copies)
 {
-    if (blockIdx.x < p.copies)
+    constexpr bool kRaised = DT == kFp16 && !MOST;
+    const bool copying = blockIdx.x < p.copies;
+    if (!kRaised && copying)
         return copy_block(copies, blockIdx.x);
-    const int64_t block = blockIdx.x - p.copies, blocks = gridDim.x - p.copies;
-    __shared__ uint32_t share_most[4];
-    uint32_t most = 0;
-    float s = 1.0f;
-    if constexpr (DT == kFp16 && !MOST) {
-        for (int b = threadIdx.x; b < p.blocks; b += 256)
-            most = max(most, p.most[b]);
-        most = most_of(most);
-        if ((threadIdx.x & 63) == 0)
-            share_most[threadIdx.x >> 6] = most;
-        __syncthreads();
-        s = lift_of(max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
-        if (block == 0 && threadIdx.x == 0)
-            *p.inverse = 1.0f / s;
-    }
     // a wave takes 512 columns of a row at a time
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t groups = (p.chunks + 63) / 64;
-    for (int64_t unit = block * 4 + wave; unit < p.units; unit += blocks * 4) {
-        const int64_t row = unit < ((int64_t)1 << 32) ? (uint32_t)unit / groups : unit / groups;
-        const int col = ((int)(unit - row * groups) * 64 + lane) * 8;
-        if (col >= p.I)
-            continue;
+    const int64_t block = blockIdx.x - p.copies, blocks = gridDim.x - p.copies;
+    // (where rows are raised a wave's units are neighbours, of a row or two)
+    const int64_t each = kRaised ? (p.units + blocks * 4 - 1) / (blocks * 4) : 1;
+    auto row_of = [&](int64_t unit) -> int64_t { return unit < ((int64_t)1 << 32) ? (uint32_t)unit / groups : unit / groups; };
+    // the largest of a row, from its units'
+    auto row_most = [&](int64_t row) {
+        uint32_t v = 0;
+        for (uint32_t g = lane; g < groups; g += 64)
+            v = max(v, p.unit_most[row * groups + g]);
+        return (uint32_t)__builtin_amdgcn_readfirstlane(most_of(v));
+    };
+    __shared__ uint32_t share_most[4];
+    uint32_t most = 0, row_size = 0;   // row_size: of the first row
+    float s = 1.0f;
+    if constexpr (kRaised) {
+        for (int b = threadIdx.x; b < p.blocks; b += 256)
+            most = max(most, p.most[b]);
+        const int64_t row = copying ? (int64_t)blockIdx.x * 4 + wave : row_of((block * 4 + wave) * each);
+        if (row < (copying ? p.x.rows : p.rows))
+            row_size = row_most(row);
+        most = most_of(most);
+        if (lane == 0)
+            share_most[wave] = most;
+        __syncthreads();
+        most = __builtin_amdgcn_readfirstlane(max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3])));
+        s = lift_of(most);
+        if (blockIdx.x == p.copies && threadIdx.x == 0)
+            *p.inverse = 1.0f / s;
+        if (copying) {
+            for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < p.x.rows; row += (int64_t)p.copies * 4) {
+                copy_lowered(p.x, row, raise_of(row_size, most), lane);
+                if (row + (int64_t)p.copies * 4 < p.x.rows)
+                    row_size = row_most(row + (int64_t)p.copies * 4);
+            }
+            return;
+        }
+    }
+    const int64_t first = (block * 4 + wave) * each;
+    for (int64_t unit = first; unit < (kRaised ? min(first + each, p.units) : p.units); unit += kRaised ? 1 : blocks * 4) {
+        const int64_t row = row_of(unit);
+        const int group = (int)(unit - row * groups), col = (group * 64 + lane) * 8;
+        float raise = 1.0f;
+        if constexpr (kRaised) {
+            if (group == 0 && unit > first)
+                row_size = row_most(row);
+            raise = power_of_two(raise_of(row_size, most));
+            if (group == 0 && lane == 0)
+                p.raise[row] = raise;
+        }
+        const bool inside = col < p.I;
         float g[8], u[8], d[8], dg[8], du[8];
         const uint16_t *const pre = p.pre + row * p.ldp;
-        eight<DT>((const char *)pre, col, p.I, g);
-        eight<DT>((const char *)(pre + p.I), col, p.I, u);
-        eight<DT>((const char *)(p.d + row * p.ldd), col, p.I, d);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float value, slope;
-            act_slope(p.act, g[j], value, slope);
-            dg[j] = d[j] * u[j] * slope * s;
-            du[j] = d[j] * value * s;
-        }
-        if constexpr (MOST) {
+        if (inside) {
+            eight<DT>((const char *)pre, col, p.I, g);
+            eight<DT>((const char *)(pre + p.I), col, p.I, u);
+            eight<DT>((const char *)(p.d + row * p.ldd), col, p.I, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t a = __builtin_bit_cast(uint32_t, dg[j]) & 0x7fffffffu;
-                const uint32_t b = __builtin_bit_cast(uint32_t, du[j]) & 0x7fffffffu;
-                most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
+                float value, slope;
+                act_slope(p.act, g[j], value, slope);
+                dg[j] = d[j] * u[j] * slope * s;
+                du[j] = d[j] * value * s;
+                if constexpr (kRaised) {
+                    dg[j] *= raise;
+                    du[j] *= raise;
+                }
             }
-        } else {
+        }
+        if constexpr (MOST) {
+            uint32_t here = 0;
+            if (inside) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t a = __builtin_bit_cast(uint32_t, dg[j]) & 0x7fffffffu;
+                    const uint32_t b = __builtin_bit_cast(uint32_t, du[j]) & 0x7fffffffu;
+                    here = max(here, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
+                }
+            }
+            here = most_of(here);
+            if (lane == 0)
+                p.unit_most[unit] = here;
+            most = max(most, here);
+        } else if (inside) {
             const int n = p.I - col;
             auto store = [&](uint16_t *out) {
                 store_eight<DT>(out + col, n, dg);
@@ -895,9 +1036,8 @@ __global__ void __launch_bounds__(256) gated_slope(GatedSlopeParams p, CopyParam
     if constexpr (MOST) {
         // (atomics on one address take 15 ns each: the blocks of the next launch look at
         // all the places instead)
-        most = most_of(most);
-        if ((threadIdx.x & 63) == 0)
-            share_most[threadIdx.x >> 6] = most;
+        if (lane == 0)
+            share_most[wave] = most;
         __syncthreads();
         if (threadIdx.x == 0)
             p.most[block] = max(max(share_most[0], share_most[1]), max(share_most[2], share_most[3]));
