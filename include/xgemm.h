@@ -729,8 +729,14 @@ int xgemm_logprob_grad(xgemm_handle_t h, int64_t R, int64_t V, const void *logit
  *
  * Alignment: matrices that go into a product (x, w, up, head) are read in place
  * where they begin on 16 bytes and rows and their distance are multiples of 16
- * bytes; others are copied into the handle's workspace first, at every call.
- * Everything else may have any alignment that its type has.
+ * bytes.  Of others the forward products read some in place as well, and copy some
+ * into the handle's workspace, at every call, whichever takes less time; gradients
+ * copy them.  Everything else may have any alignment that its type has.
+ *
+ * Workspace: copies take the size of what is copied, rows rounded up to 16 bytes;
+ * partial sums, where k is split
+ * because there are few tiles, up to 32 times 4 bytes for each value of a product
+ * (of 65536 rows at most).
  */
 #define XGEMM_FUSED_MAX_SIDE (1 << 22)
 
@@ -833,7 +839,7 @@ int xgemm_gated_grad(xgemm_handle_t h, int64_t M, int64_t H, int64_t I, const vo
  *   logprob, lse  T floats each; NULL: not wanted
  * Logits are fp32 sums.  A row with a logit of NaN or +inf has lse and logprob
  * NaN; one of nothing but -inf has -inf.  Uses the workspace: 8 bytes for each 128
- * or 256 logits of at most 16384 rows.
+ * or 256 logits of at most 16384 rows, and copies.
  */
 int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
                    int64_t ldw, const int64_t *targets, float *logprob, float *lse, int dtype, void *stream);
@@ -861,9 +867,10 @@ int xgemm_head_run(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void
  * rounding, a relative |lse| 2^-24.  A row whose lse is -inf, or whose d_logprob (or
  * target's part in it) and d_lse are zero, has d = 0 and takes no part in d_head,
  * whatever its x and lse hold.  Uses the
- * workspace: some 256 MB for d (2 bytes a logit; 4096 bytes a row if that is
- * more), a copy of x for d_head, and 4 bytes for each value of d_x where it is not fp32
- * and there are several pieces.
+ * workspace: up to some 256 MB for d (2 bytes a logit of a piece; 4096 bytes a row if
+ * that is more), twice that up to 128 rows; for d_head a copy of x (two up to 128
+ * rows); copies of what is not read in place; 4 bytes for each value of d_x where it
+ * is not fp32 and there are several pieces; partial sums.
  */
 int xgemm_head_grad(xgemm_handle_t h, int64_t T, int64_t V, int64_t H, const void *x, int64_t ldx, const void *head,
                     int64_t ldw, const int64_t *targets, const float *lse, const float *d_logprob, const float *d_lse,

@@ -45,6 +45,10 @@ constexpr int64_t kTwoParts = 128;
 // 16.9; 333 x 5120 x 2048 8-bit 28 / 19.2 / 11.7; 1000 x 8192 x 4096 8-bit 54 / 45.2 / 50.0;
 // 2048 x 14336 x 4096 8-bit 121 / 151 / 172; gated 512 x 4096 x 4096 48 / 45.5 / 40.4;
 // d_x of 2048 x 2048 x 5632 112 (4 ranges; not split 242) / 123 / 128.
+// What it leaves out: what an end stores, and rows across k, which take 1.5 to 1.6 us a
+// step of the largest tile (the three products of a head's gradient, 333 x 32001 x 1001:
+// 29 / 47 / 29 us by this, 41 / 46 / 49 measured); and of the staged tile three fit on a CU
+// (48 KB of LDS, 108 registers) where two are counted.
 // across: A's rows are its k (a transposed product), which the smallest tile does
 // not take.  Staged products have only that tile: of too many rows and columns
 // they have no cut, and its cost is infinite.
