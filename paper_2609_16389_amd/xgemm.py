@@ -1053,7 +1053,8 @@ def head_logprobs_grad(x, head, targets, lse, d_logprob=None, d_lse=None, out=No
     """The gradient of ``head_logprobs``' results in x and head, through
     xgemm_head_grad: the pair (d_x, d_head), given theirs (None: zero) and the
     forward call's lse (targets only with d_logprob).  All (T,) float32, targets
-    int64.  ``out``: a pair of tensors to write into, both of x's dtype (the
+    int64.  A row without factors (a negative target or a d_logprob of 0, and no
+    d_lse) takes no part, whatever its x and lse hold.  ``out``: a pair of tensors to write into, both of x's dtype (the
     default) or both float32; None in a place of the pair: not computed."""
     if out is not None and stream is None and len(out) == 2:
         rc = _fastcall.head_logprobs_grad(x, head, targets, lse, d_logprob, d_lse, *out)
