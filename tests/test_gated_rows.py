@@ -42,7 +42,7 @@ def bounds_of_rows(x, up, pre, d, act, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,H,I", [(2, 8, 5), (9, 40, 1030), (128, 43, 70), (129, 48, 130), (333, 100, 701), (2053, 40, 520)])
+@pytest.mark.parametrize("M,H,I", [(2, 8, 5), (9, 40, 1030), (128, 43, 70), (129, 48, 130), (333, 100, 701), (2053, 40, 520), (66001, 16, 20)])
 @pytest.mark.parametrize("low", [-8, -20, -32])
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 def test_rows_of_different_size_in_binary16(M, H, I, low, act):

@@ -70,7 +70,7 @@ def bounds_of_rows(x, w, targets, lse, d, z, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,V,H", [(2, 60, 8), (50, 900, 48), (128, 301, 43), (129, 900, 48), (300, 700, 33), (700, 4100, 72)])
+@pytest.mark.parametrize("T,V,H", [(2, 60, 8), (50, 900, 48), (128, 301, 43), (129, 900, 48), (300, 700, 33), (700, 4100, 72), (66001, 120, 16)])
 @pytest.mark.parametrize("low", [-8, -20, -45, -90])
 def test_rows_of_different_size_in_binary16(T, V, H, low):
     """Each row of d_x keeps its bits, however small its factors beside another's."""
